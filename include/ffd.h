@@ -21,6 +21,12 @@
  *                               refinement + attention spread over every CU, merge.
  *   ffd_dense_decode_attention  exact dense decode attention over the bf16 cache (the dense
  *                               comparator of Sec. 4.2), same split-and-merge scheme.
+ *   ffd_write_kv8, ffd_read_kv8  an 8-bit cache of keys and values: new tokens quantized into it at
+ *                               device-side positions, and read back in bf16.
+ *   ffd_kv8_decode_attention    exact dense decode attention over the 8-bit cache.
+ *   ffd_shared_prefix_decode_attention  exact dense decode attention of a batch whose sequences begin
+ *                               with the same tokens: that prefix, kept once, is read once for all of
+ *                               them, then each sequence's own cache; bf16 or 8-bit.
  *
  * Conventions for every entry point
  *  - Tensor arguments are DEVICE pointers to contiguous row-major buffers owned by the caller.
@@ -249,6 +255,79 @@ int ffd_dense_decode_attention(const void* q, const void* k, const void* v, cons
                                int B, int Hq, int Hkv, int Lcap, int D, int num_splits,
                                float softmax_scale, void* out, float* lse,
                                void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A cache of keys and values as the entry points below take it, for B sequences:
+ *   8 bits   k, v int8 [B, Hkv, Lcap, D] codes n and k_absmax, v_absmax bf16 [B, Hkv, Lcap]. A token's vector x of one
+ *            KV head is kept as M = max_d |x_d| and n_d = rint(127 x_d / M) in [-127, 127], half to even, exact for
+ *            every finite bf16 x; it stands for n M / 127. M = 0 has n = 0. A token with an infinity or a NaN
+ *            keeps M = NaN, n = 0: it reads back as NaN in every dim, and attention that sees it gives NaN.
+ *   bf16     k, v bf16 [B, Hkv, Lcap, D], k_absmax and v_absmax NULL (ffd_shared_prefix_decode_attention only).
+ * One absmax pointer NULL and the other not is FFD_ERR_INVALID_ARGUMENT.
+ */
+typedef struct ffd_kv {
+    void* k;
+    void* k_absmax;
+    void* v;
+    void* v_absmax;
+} ffd_kv;
+
+/*
+ * Quantizes new tokens into an 8-bit cache: token t < counts[b] of sequence b goes to position start[b] + t. Tokens
+ * whose position lies outside [0, Lcap) are not written, and nothing else of the cache is touched. Lengths are the
+ * caller's to advance (the layers of a model share them). One token per sequence (T = 1) is the decode step's form;
+ * everything happens on the device, so it can be captured in a HIP graph.
+ *   k_new, v_new   bf16 [B, T, Hkv, D], the dims of a vector contiguous; k_strides, v_strides are HOST arrays of
+ *                  three strides in elements (sequence, token, head), each >= 0 and a multiple of 8, or NULL for a
+ *                  contiguous tensor.
+ *   start          int32 [B] (device);  counts  int32 [B] (device) or NULL for T everywhere; values above T mean T,
+ *                  negative ones 0.
+ */
+int ffd_write_kv8(const void* k_new, const void* v_new, const int64_t* k_strides, const int64_t* v_strides,
+                  const ffd_kv* cache, const int32_t* start, const int32_t* counts, int B, int T, int Hkv, int Lcap,
+                  int D, hipStream_t stream);
+
+/*
+ * Reads tokens [t_begin, t_end) of an 8-bit cache back: k, v bf16 [B, Hkv, t_end - t_begin, D], n M / 127 correctly
+ * rounded. seq_lens: int32 [B] (device) or NULL; with it the rows of tokens at or behind seq_lens[b] are zeros (and
+ * the cache there is not read). 0 <= t_begin <= t_end <= Lcap.
+ */
+int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v, int B, int Hkv, int Lcap, int D,
+                 int t_begin, int t_end, hipStream_t stream);
+
+/*
+ * Exact dense decode attention over an 8-bit cache: ffd_dense_decode_attention with k = n M / 127 and v likewise,
+ * neither rounded to bf16. Arguments, splits and workspace (ffd_dense_workspace_bytes) are those of that call; the
+ * cache holds B sequences. B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
+ */
+int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
+                             int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Exact dense decode attention of a batch over a shared prefix and each sequence's own tokens: sequence b attends
+ * over the first prefix_lens[b] tokens of the prefix and then tokens [0, seq_lens[b]) of its own cache, with one
+ * softmax over both. The prefix is read once for the batch, up to its longest use.
+ *   prefix        cache of one sequence, [Hkv, Pcap, ..], bf16 or 8 bits; Pcap a multiple of 64
+ *   prefix_lens   int32 [B] (device), clamped to [0, Pcap]; 0 for a sequence that does not begin with the prefix
+ *   own           cache of B sequences, [B, Hkv, Lcap, ..], bf16 or 8 bits (apart from the prefix's form)
+ *   seq_lens      int32 [B] (device): each sequence's own tokens, clamped to [0, Lcap]
+ *   num_splits    runs of the prefix per tile of query rows, and runs of blocks of the own caches as for
+ *                 ffd_dense_decode_attention (1..FFD_MAX_SPLITS), or 0 for automatic
+ *   out, lse      as ffd_dense_decode_attention; a sequence with no token at all gets out = 0, lse = -inf
+ *   workspace     ffd_shared_prefix_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that
+ *                 overlap in time need separate workspaces.
+ * B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
+ */
+int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
+                                       const ffd_kv* own, const int32_t* seq_lens, int B, int Hq, int Hkv, int Lcap,
+                                       int D, int num_splits, float softmax_scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ffd_shared_prefix_decode_attention: (D + 2) * 4 bytes for each query row (their number per KV head
+ * rounded up to the kernel's row tiles) and run of the prefix, on a 256-byte boundary, then
+ * ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits). 0 on invalid or unsupported input. */
+size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits);
 
 /* The split count S for this num_splits (0 = automatic), which sizes the workspace: num_splits itself, or
  * automatically the largest with (S + 1) * B * Hkv at most one per compute unit of the current device

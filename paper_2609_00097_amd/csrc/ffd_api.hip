@@ -400,6 +400,85 @@ int decode_checks(const void* q, const void* k_codes, const void* k_absmax, cons
     return FFD_OK;
 }
 
+// Pointers of a cache argument: all there and aligned; *bits is 8 or 16. An 8-bit one is required where only8.
+int check_kv(const ffd_kv* c, bool only8, int* bits) {
+    if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return FFD_ERR_INVALID_ARGUMENT;
+    if (!c->k_absmax != !c->v_absmax || (only8 && !c->k_absmax)) return FFD_ERR_INVALID_ARGUMENT;
+    if (c->k_absmax && (!aligned16(c->k_absmax) || !aligned16(c->v_absmax))) return FFD_ERR_INVALID_ARGUMENT;
+    *bits = c->k_absmax ? 8 : 16;
+    return FFD_OK;
+}
+
+KvSource source_of(const ffd_kv& c) {
+    return KvSource{static_cast<const uint8_t*>(c.k), static_cast<const uint8_t*>(c.v),
+                    static_cast<const uint16_t*>(c.k_absmax), static_cast<const uint16_t*>(c.v_absmax)};
+}
+
+// Partial states of a dense attention over whole caches, at the start of its workspace.
+struct OwnPartials {
+    Partials p;
+    int2* table;                      // or null: S rows per head
+    dim3 grid;
+};
+OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {
+    const bool balanced = B <= kDenseBalanceMaxSeqs;
+    OwnPartials o;
+    o.p = carve(workspace, (size_t)B * Hq * (balanced ? S + 1 : S));
+    o.table = balanced ? reinterpret_cast<int2*>(static_cast<uint8_t*>(workspace) +
+                                                 round_up(partials_bytes((size_t)B * Hq * (S + 1)), kAlign))
+                       : nullptr;
+    o.grid = balanced ? dim3((unsigned)((S + 1) * B * Hkv)) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B);
+    return o;
+}
+
+void launch_dense(const OwnPartials& o, const uint16_t* q, const void* k, const void* v, const int32_t* seq_lens, int B,
+                  int Hq, int Hkv, int Lcap, int S, float scale, hipStream_t stream) {
+    const int G = Hq / Hkv;
+    DenseArgs a{q, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), seq_lens, o.p.m, o.p.l, o.p.acc,
+                o.table, B, Hq, Hkv, Lcap, G, S, scale};
+    if (G <= 4) hipLaunchKernelGGL(dense_decode_kernel<1>, o.grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(dense_decode_kernel<2>, o.grid, dim3(kThreads), 0, stream, a);
+}
+
+void launch_kv8(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const int32_t* seq_lens, int B, int Hq, int Hkv,
+                int Lcap, int S, float scale, hipStream_t stream) {
+    Kv8Args a{q, source_of(kv), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, Hq / Hkv, S, scale};
+    hipLaunchKernelGGL(kv8_decode_kernel, o.grid, dim3(kThreads), 0, stream, a);
+}
+
+// Tiles of 16 CT query rows and runs of the prefix attention.
+struct PrefixPlan {
+    int ct, tiles, S;
+    size_t rows;                      // partial rows in all
+};
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
+    const long long rows = (long long)B * (Hq / Hkv);
+    PrefixPlan p;
+    p.ct = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.tiles = (int)((rows + 16 * p.ct - 1) / (16 * p.ct));
+    long long s = num_splits;
+    if (s == 0) {
+        s = (p.ct == 4 ? 1LL : 2LL) * device_cus() / ((long long)Hkv * p.tiles);
+        s = std::min(s, (long long)(Pcap + kPrefixRound - 1) / kPrefixRound);
+        s = std::max(1LL, std::min(s, (long long)FFD_MAX_SPLITS));
+    }
+    p.S = (int)s;
+    p.rows = (size_t)Hkv * p.tiles * p.S * 16 * p.ct;
+    return p;
+}
+
+template <bool I8>
+void launch_prefix(int ct, dim3 grid, hipStream_t stream, const PrefixArgs& a) {
+    if (ct == 1) hipLaunchKernelGGL((prefix_kernel<1, I8>), grid, dim3(kThreads), 0, stream, a);
+    else if (ct == 2) hipLaunchKernelGGL((prefix_kernel<2, I8>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prefix_kernel<4, I8>), grid, dim3(kThreads), 0, stream, a);
+}
+
+int check_pcap(int Pcap) {
+    if (Pcap < FFD_BLOCK || Pcap % FFD_BLOCK) return FFD_ERR_INVALID_ARGUMENT;
+    return Pcap > (1 << 30) ? FFD_ERR_UNSUPPORTED : FFD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -656,23 +735,120 @@ int ffd_dense_decode_attention(const void* q, const void* k, const void* v, cons
     if (!k || !aligned16(k)) return FFD_ERR_INVALID_ARGUMENT;
     if (workspace_bytes < ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits))
         return FFD_ERR_WORKSPACE_TOO_SMALL;
-    const int G = Hq / Hkv;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
-    const bool balanced = B <= kDenseBalanceMaxSeqs;
-    const Partials P = carve(workspace, (size_t)B * Hq * (balanced ? S + 1 : S));
-    int2* table = balanced ? reinterpret_cast<int2*>(static_cast<uint8_t*>(workspace) +
-                                                     round_up(partials_bytes((size_t)B * Hq * (S + 1)), kAlign))
-                           : nullptr;
-    DenseArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
-                static_cast<const uint16_t*>(v), seq_lens, P.m, P.l, P.acc, table, B, Hq, Hkv, Lcap, G, S, scale};
-    const dim3 grid = balanced ? dim3((unsigned)((S + 1) * B * Hkv)) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B);
-    if (G <= 4)
-        hipLaunchKernelGGL(dense_decode_kernel<1>, grid, dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL(dense_decode_kernel<2>, grid, dim3(kThreads), 0, stream, a);
+    const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
+    launch_dense(o, static_cast<const uint16_t*>(q), k, v, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     st = launch_status();
     if (st != FFD_OK) return st;
-    launch_merge(B * Hq, stream, P.m, P.l, P.acc, S, table, balanced ? G : 1, static_cast<uint16_t*>(out), lse);
+    launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
+    return launch_status();
+}
+
+int ffd_write_kv8(const void* k_new, const void* v_new, const int64_t* k_strides, const int64_t* v_strides,
+                  const ffd_kv* cache, const int32_t* start, const int32_t* counts, int B, int T, int Hkv, int Lcap,
+                  int D, hipStream_t stream) {
+    int st = check_shapes(B, Hkv, Hkv, Lcap, D);
+    if (st != FFD_OK) return st;
+    if (T < 0) return FFD_ERR_INVALID_ARGUMENT;
+    const int64_t contiguous[3] = {(int64_t)T * Hkv * D, (int64_t)Hkv * D, D};
+    if (!k_strides) k_strides = contiguous;
+    if (!v_strides) v_strides = contiguous;
+    for (int i = 0; i < 3; ++i)
+        if (k_strides[i] < 0 || k_strides[i] % 8 || v_strides[i] < 0 || v_strides[i] % 8) return FFD_ERR_INVALID_ARGUMENT;
+    if (B == 0 || T == 0) return FFD_OK;
+    int bits;
+    st = check_kv(cache, true, &bits);
+    if (st != FFD_OK) return st;
+    if (!k_new || !v_new || !start || !aligned16(k_new) || !aligned16(v_new)) return FFD_ERR_INVALID_ARGUMENT;
+    if ((reinterpret_cast<uintptr_t>(start) & 3u) || (reinterpret_cast<uintptr_t>(counts) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
+    WriteKv8Args a{static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new),
+                   static_cast<int8_t*>(cache->k), static_cast<uint16_t*>(cache->k_absmax),
+                   static_cast<int8_t*>(cache->v), static_cast<uint16_t*>(cache->v_absmax), start, counts,
+                   {k_strides[0], k_strides[1], k_strides[2]}, {v_strides[0], v_strides[1], v_strides[2]}, T, Hkv, Lcap, 0};
+    while (a.tok_shift < 5 && 1 << a.tok_shift < T) ++a.tok_shift;
+    const int tokens = 1 << a.tok_shift, heads = 32 / tokens;
+    const dim3 grid((unsigned)((T + (long long)tokens - 1) / tokens), (unsigned)((Hkv + heads - 1) / heads), (unsigned)B);
+    hipLaunchKernelGGL(write_kv8_kernel, grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v, int B, int Hkv, int Lcap, int D,
+                 int t_begin, int t_end, hipStream_t stream) {
+    int st = check_shapes(B, Hkv, Hkv, Lcap, D);
+    if (st != FFD_OK) return st;
+    if (t_begin < 0 || t_end < t_begin || t_end > Lcap) return FFD_ERR_INVALID_ARGUMENT;
+    if (B == 0 || t_end == t_begin) return FFD_OK;
+    int bits;
+    st = check_kv(cache, true, &bits);
+    if (st != FFD_OK) return st;
+    if (!k || !v || !aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
+    ReadKv8Args a{static_cast<const int8_t*>(cache->k), static_cast<const uint16_t*>(cache->k_absmax),
+                  static_cast<const int8_t*>(cache->v), static_cast<const uint16_t*>(cache->v_absmax),
+                  static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), seq_lens, Hkv, Lcap, t_begin, t_end};
+    const dim3 grid((unsigned)((t_end - t_begin + kReadTokens - 1) / kReadTokens), (unsigned)Hkv, (unsigned)B);
+    hipLaunchKernelGGL(read_kv8_kernel, grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
+                             int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    CallScope scope;
+    int S = 0, bits;
+    int st = attention_common_checks(q, cache ? cache->v : nullptr, seq_lens, B, Hq, Hkv, Lcap, D, num_splits,
+                                     softmax_scale, out, lse, workspace, workspace_bytes, true, &S);
+    if (st != FFD_OK || B == 0) return st;
+    if ((long long)B * Hkv > (1LL << 20)) return FFD_ERR_UNSUPPORTED;
+    if ((st = check_kv(cache, true, &bits)) != FFD_OK) return st;
+    if (workspace_bytes < ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
+    const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
+    launch_kv8(o, static_cast<const uint16_t*>(q), *cache, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    if ((st = launch_status()) != FFD_OK) return st;
+    launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
+    return launch_status();
+}
+
+size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits) {
+    const size_t own = ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits);
+    if (own == 0 || B == 0 || check_pcap(Pcap) != FFD_OK || (long long)B * Hkv > (1LL << 20)) return 0;
+    return round_up(partials_bytes(prefix_plan(B, Hq, Hkv, Pcap, num_splits).rows), kAlign) + own;
+}
+
+int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
+                                       const ffd_kv* own, const int32_t* seq_lens, int B, int Hq, int Hkv, int Lcap,
+                                       int D, int num_splits, float softmax_scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    CallScope scope;
+    int S = 0, prefix_bits, own_bits;
+    int st = attention_common_checks(q, own ? own->v : nullptr, seq_lens, B, Hq, Hkv, Lcap, D, num_splits,
+                                     softmax_scale, out, lse, workspace, workspace_bytes, true, &S);
+    if (st != FFD_OK) return st;
+    if ((st = check_pcap(Pcap)) != FFD_OK || B == 0) return st;
+    if ((long long)B * Hkv > (1LL << 20)) return FFD_ERR_UNSUPPORTED;
+    if ((st = check_kv(prefix, false, &prefix_bits)) != FFD_OK || (st = check_kv(own, false, &own_bits)) != FFD_OK) return st;
+    if (!prefix_lens || (reinterpret_cast<uintptr_t>(prefix_lens) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < ffd_shared_prefix_workspace_bytes(B, Hq, Hkv, Pcap, Lcap, D, num_splits))
+        return FFD_ERR_WORKSPACE_TOO_SMALL;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
+    const int G = Hq / Hkv;
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits);
+    const Partials P = carve(workspace, plan.rows);
+    const OwnPartials o = own_partials(static_cast<uint8_t*>(workspace) + round_up(partials_bytes(plan.rows), kAlign), B, Hq, Hkv, S);
+    const uint16_t* qp = static_cast<const uint16_t*>(q);
+    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
+    const dim3 grid((unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles));
+    if (prefix_bits == 8) launch_prefix<true>(plan.ct, grid, stream, a);
+    else launch_prefix<false>(plan.ct, grid, stream, a);
+    if ((st = launch_status()) != FFD_OK) return st;
+    if (own_bits == 8) launch_kv8(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    else launch_dense(o, qp, own->k, own->v, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    if ((st = launch_status()) != FFD_OK) return st;
+    const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, static_cast<uint16_t*>(out), lse,
+                            Hq, Hkv, G, plan.tiles, 16 * plan.ct, plan.S, S};
+    const dim3 merge_grid((unsigned)(B * Hq), kMergeSlices);
+    if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, merge_grid, dim3(64), 0, stream, m);
+    else hipLaunchKernelGGL(shared_merge_kernel<4>, merge_grid, dim3(256), 0, stream, m);
     return launch_status();
 }
 

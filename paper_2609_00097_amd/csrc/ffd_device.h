@@ -27,6 +27,20 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
+// Two floats as bf16, the first in the low half, round to nearest even (one conversion instruction).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    const v2f f = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2bf));
+}
+
+// Larger of two pairs of 16-bit integers (bf16 magnitudes order as integers, NaN above infinity).
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+    typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2u16, a), __builtin_bit_cast(v2u16, b)));
+}
+
 // Reductions over the 16 lanes of one MFMA row group (lanes 16g..16g+15), every lane receiving
 // the result: DPP quad permutes (xor 1, xor 2) then row rotations by 4 and 8.
 template <int CTRL>

@@ -146,6 +146,76 @@ struct DenseArgs {
     float scale;
 };
 
+// An 8-bit cache (per KV head rows of 128 codes, one absmax a row) being written and read back.
+struct WriteKv8Args {
+    const uint16_t* k_new;      // bf16 [B, T, Hkv, 128], element strides ks, vs of sequence, token, head
+    const uint16_t* v_new;
+    int8_t* k_codes;            // [B, Hkv, Lcap, 128]
+    uint16_t* k_absmax;         // bf16 [B, Hkv, Lcap]
+    int8_t* v_codes;
+    uint16_t* v_absmax;
+    const int32_t* start;       // [B]
+    const int32_t* counts;      // [B] or null: T
+    int64_t ks[3], vs[3];
+    int T, Hkv, Lcap, tok_shift;
+};
+struct ReadKv8Args {
+    const int8_t* k_codes;
+    const uint16_t* k_absmax;
+    const int8_t* v_codes;
+    const uint16_t* v_absmax;
+    uint16_t* k;                // bf16 [B, Hkv, t_end - t_begin, 128]
+    uint16_t* v;
+    const int32_t* seq_lens;    // [B] or null: Lcap
+    int Hkv, Lcap, t_begin, t_end;
+};
+constexpr int kReadTokens = 64;                // tokens per workgroup of the read
+
+// Attention over one cache, bf16 (absmax null) or 8-bit, see ffd_attend.hip.
+struct KvSource {
+    const uint8_t* k;           // [.., cap, 128] bf16 or int8
+    const uint8_t* v;
+    const uint16_t* k_absmax;   // bf16 [.., cap] or null
+    const uint16_t* v_absmax;
+};
+
+// Dense decode over an 8-bit cache: the workgroups, rows and table of DenseArgs.
+struct Kv8Args {
+    const uint16_t* q;          // bf16 [B, Hq, 128]
+    KvSource kv;                // [B, Hkv, Lcap, ..]
+    const int32_t* seq_lens;
+    float* part_m;
+    float* part_l;
+    float* part_acc;
+    int2* table;
+    int B, Hq, Hkv, Lcap, G, S;
+    float scale;
+};
+
+// Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in tiles of
+// 16 CT, each tile's prefix in S runs. Partial row ((kvh * tiles + tile) * S + run) * 16 CT + row in tile.
+constexpr int kPrefixRound = 128;              // tokens that a workgroup of it takes at a time
+struct PrefixArgs {
+    const uint16_t* q;          // bf16 [B, Hq, 128]
+    KvSource kv;                // [Hkv, Pcap, ..]
+    const int32_t* prefix_lens; // [B]
+    float* part_m;
+    float* part_l;
+    float* part_acc;
+    int B, Hq, Hkv, Pcap, G, S, tiles;
+    float scale;
+};
+
+// Partial rows of the shared prefix and of the sequences' own caches, for the merge of both.
+struct SharedMergeArgs {
+    const float *prefix_m, *prefix_l, *prefix_acc;
+    const float *own_m, *own_l, *own_acc;
+    const int2* table;          // own rows as in lse_merge_kernel
+    uint16_t* out;
+    float* lse;
+    int Hq, Hkv, G, tiles, tile_rows, S_prefix, S_own;
+};
+
 struct QuantArgs {
     const uint16_t* k;          // bf16 [B, Hkv, Lcap, 128]
     uint32_t* codes;
@@ -187,6 +257,12 @@ constexpr int kTopkSelectThreads = 1024;
 template <int NT> __global__ void dense_decode_kernel(DenseArgs a);
 template <int BITS> __global__ void quantize_keys_kernel(QuantArgs a);
 template <int BITS> __global__ void append_kv_kernel(AppendArgs a);
+__global__ void write_kv8_kernel(WriteKv8Args a);
+__global__ void read_kv8_kernel(ReadKv8Args a);
+__global__ void kv8_decode_kernel(Kv8Args a);
+// CT: tiles of 16 query rows per workgroup; I8: an 8-bit prefix.
+template <int CT, bool I8> __global__ void prefix_kernel(PrefixArgs a);
+template <int NW> __global__ void shared_merge_kernel(SharedMergeArgs a);
 constexpr int kMergeSlices = 4;                // workgroups per head of the merge, 32 dims each
 // NW waves per workgroup: 4, or 1 from kMergeOneWaveHeads heads on (their waves fill the chip alone).
 constexpr int kMergeOneWaveHeads = 256;

@@ -83,33 +83,11 @@ __device__ __forceinline__ float rows_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-}  // namespace
-
-// Grid (B * Hq, kMergeSlices).
+// Joins the states of the workgroup's threads and writes head blockIdx.x's dims of slice blockIdx.y.
 template <int NW>
-__global__ __launch_bounds__(64 * NW) void lse_merge_kernel(const float* __restrict__ part_m,
-                                                             const float* __restrict__ part_l,
-                                                             const float* __restrict__ part_acc, int S,
-                                                             const int2* __restrict__ table, int G,
-                                                             uint16_t* __restrict__ out, float* __restrict__ lse) {
-    constexpr int kRowLanes = 8 * NW;               // rows in parallel
-    alignas(16) __shared__ float part[NW][8][8];    // each wave's state per d4
-    const int tid = threadIdx.x, d4 = tid & 7, r = tid >> 3, wave = tid >> 6, lane = tid & 63;
-    const size_t x = blockIdx.x / G;                        // blockIdx.x = b * Hq + h
-    size_t first = x * S;
-    if (table) {
-        const int2 fl = table[x];
-        first = fl.x;
-        S = fl.y - fl.x + 1;
-    }
-    const size_t row0 = first * G + blockIdx.x % G;
-    const float* acc = part_acc + blockIdx.y * kSliceDims + 4 * d4;
-    State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    if (S > 2 * kRowLanes) {                                // uniform
-        for (int s0 = 0; s0 < S; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, part_m, part_l, acc, row0, G, S, s0 + r);
-    } else if (S > 0) {
-        fold_rows<2, kRowLanes>(st, part_m, part_l, acc, row0, G, S, r);
-    }
+__device__ __forceinline__ void finish(State st, float (&part)[NW][8][8], uint16_t* __restrict__ out,
+                                       float* __restrict__ lse) {
+    const int tid = threadIdx.x, d4 = tid & 7, wave = tid >> 6, lane = tid & 63;
     const float M = rows_max(st.m);
     const float c = rescale(st.m, M);
     const float l = rows_sum(st.l * c);
@@ -149,7 +127,71 @@ __global__ __launch_bounds__(64 * NW) void lse_merge_kernel(const float* __restr
     if (lse && blockIdx.y == 0 && d4 == 0) lse[blockIdx.x] = any ? Mx + logf(lx) : -INFINITY;
 }
 
+}  // namespace
+
+// Grid (B * Hq, kMergeSlices).
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void lse_merge_kernel(const float* __restrict__ part_m,
+                                                             const float* __restrict__ part_l,
+                                                             const float* __restrict__ part_acc, int S,
+                                                             const int2* __restrict__ table, int G,
+                                                             uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int kRowLanes = 8 * NW;               // rows in parallel
+    alignas(16) __shared__ float part[NW][8][8];    // each wave's state per d4
+    const int tid = threadIdx.x, d4 = tid & 7, r = tid >> 3;
+    const size_t x = blockIdx.x / G;                        // blockIdx.x = b * Hq + h
+    size_t first = x * S;
+    if (table) {
+        const int2 fl = table[x];
+        first = fl.x;
+        S = fl.y - fl.x + 1;
+    }
+    const size_t row0 = first * G + blockIdx.x % G;
+    const float* acc = part_acc + blockIdx.y * kSliceDims + 4 * d4;
+    State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    if (S > 2 * kRowLanes) {                                // uniform
+        for (int s0 = 0; s0 < S; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, part_m, part_l, acc, row0, G, S, s0 + r);
+    } else if (S > 0) {
+        fold_rows<2, kRowLanes>(st, part_m, part_l, acc, row0, G, S, r);
+    }
+    finish<NW>(st, part, out, lse);
+}
+
 template __global__ void lse_merge_kernel<1>(const float*, const float*, const float*, int, const int2*, int, uint16_t*, float*);
 template __global__ void lse_merge_kernel<4>(const float*, const float*, const float*, int, const int2*, int, uint16_t*, float*);
+
+
+// The same over the rows of two attentions: the head's S_prefix rows of the shared prefix, tile_rows apart, and the
+// own cache's.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void shared_merge_kernel(SharedMergeArgs a) {
+    constexpr int kRowLanes = 8 * NW;
+    alignas(16) __shared__ float part[NW][8][8];
+    const int tid = threadIdx.x, d4 = tid & 7, r = tid >> 3;
+    const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, kvh = h / a.G;
+    const int q_row = b * a.G + h % a.G;
+    const size_t x = (size_t)b * a.Hkv + kvh;
+    const size_t prefix0 = (size_t)(kvh * a.tiles + q_row / a.tile_rows) * a.S_prefix * a.tile_rows + q_row % a.tile_rows;
+    size_t first = x * a.S_own;
+    int S = a.S_own;
+    if (a.table) {
+        const int2 fl = a.table[x];
+        first = fl.x;
+        S = fl.y - fl.x + 1;
+    }
+    // without a table a head's rows lie side by side, with one those of a group's heads
+    const size_t own0 = a.table ? first * a.G + h % a.G : (size_t)blockIdx.x * a.S_own;
+    const size_t stride = a.table ? a.G : 1;
+    const int dims = blockIdx.y * kSliceDims + 4 * d4;
+    State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    for (int s0 = 0; s0 < a.S_prefix; s0 += 2 * kRowLanes)
+        fold_rows<2, kRowLanes>(st, a.prefix_m, a.prefix_l, a.prefix_acc + dims, prefix0, a.tile_rows, a.S_prefix, s0 + r);
+    for (int s0 = 0; s0 < S; s0 += 2 * kRowLanes)
+        fold_rows<2, kRowLanes>(st, a.own_m, a.own_l, a.own_acc + dims, own0, stride, S, s0 + r);
+    finish<NW>(st, part, a.out, a.lse);
+}
+
+template __global__ void shared_merge_kernel<1>(SharedMergeArgs);
+template __global__ void shared_merge_kernel<4>(SharedMergeArgs);
 
 }  // namespace ffd

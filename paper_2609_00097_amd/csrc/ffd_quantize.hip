@@ -36,8 +36,6 @@ namespace ffd {
 
 namespace {
 
-typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
-
 // A token's absmax and 254 Lv / M as hi + lo (zero for M = 0).
 struct TokenScale {
     float m, hi, lo;
@@ -50,10 +48,6 @@ struct QuantSlice {
     uint32_t code[BITS / 2];
     uint32_t res[4];
 };
-
-__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2u16, a), __builtin_bit_cast(v2u16, b)));
-}
 
 // Largest |k| bit patterns of the slice, even and odd dims in the two halves.
 __device__ __forceinline__ uint32_t slice_absmax(const uint4 (&raw)[2]) {

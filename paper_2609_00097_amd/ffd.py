@@ -24,7 +24,8 @@ STATUS = {0: "FFD_OK", 1: "FFD_ERR_INVALID_ARGUMENT", 2: "FFD_ERR_UNSUPPORTED",
 NOALLOC_SCRATCH_BYTES = 16 << 20     # FFD_NOALLOC_SCRATCH_BYTES
 
 EXPORTS = ("ffd_quantize_keys", "ffd_append_kv", "ffd_decode_attention", "ffd_decode_attention_ex",
-           "ffd_decode_attention_noalloc", "ffd_dense_decode_attention",
+           "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_write_kv8", "ffd_read_kv8",
+           "ffd_kv8_decode_attention", "ffd_shared_prefix_decode_attention", "ffd_shared_prefix_workspace_bytes",
            "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits",
            "ffd_workspace_bytes", "ffd_dense_workspace_bytes", "ffd_status_string")
 
@@ -55,6 +56,11 @@ class DecodeExtras(ctypes.Structure):
     _fields_ = [("stage_events", P), ("m_tilde", P), ("pseudo_max", I), ("top_k", I), ("kernels", I)]
 
 
+class KvCache(ctypes.Structure):
+    """``ffd_kv``: a cache's keys, their absmaxes, its values and theirs (absmaxes None: bf16)."""
+    _fields_ = [("k", P), ("k_absmax", P), ("v", P), ("v_absmax", P)]
+
+
 def lib() -> ctypes.CDLL:
     """Load libffd.so (once) and declare its signatures."""
     global _lib
@@ -74,6 +80,13 @@ def lib() -> ctypes.CDLL:
     so.ffd_decode_attention_noalloc.argtypes = [P, P, P, P, P, P, I, I, I, I, I, I, I, F, I, I, I, F,
                                                 P, P, P, P]
     so.ffd_dense_decode_attention.argtypes = [P, P, P, P, I, I, I, I, I, I, F, P, P, P, SZ, P]
+    KV, STRIDES = ctypes.POINTER(KvCache), ctypes.POINTER(ctypes.c_int64)
+    so.ffd_write_kv8.argtypes = [P, P, STRIDES, STRIDES, KV, P, P, I, I, I, I, I, P]
+    so.ffd_read_kv8.argtypes = [KV, P, P, P, I, I, I, I, I, I, P]
+    so.ffd_kv8_decode_attention.argtypes = [P, KV, P, I, I, I, I, I, I, F, P, P, P, SZ, P]
+    so.ffd_shared_prefix_decode_attention.argtypes = [P, KV, P, I, KV, P, I, I, I, I, I, I, F, P, P, P, SZ, P]
+    so.ffd_shared_prefix_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
+    so.ffd_shared_prefix_workspace_bytes.restype = SZ
     so.ffd_resolve_splits.argtypes = [I, I, I, I]
     so.ffd_fused_splits.argtypes = [I, I, I, I]
     so.ffd_select_kernels.argtypes = [I, I, I, I]
@@ -84,7 +97,8 @@ def lib() -> ctypes.CDLL:
     so.ffd_status_string.argtypes = [I]
     so.ffd_status_string.restype = ctypes.c_char_p
     for name in ("ffd_quantize_keys", "ffd_append_kv", "ffd_decode_attention", "ffd_decode_attention_ex",
-                 "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_resolve_splits",
+                 "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_write_kv8", "ffd_read_kv8",
+                 "ffd_kv8_decode_attention", "ffd_shared_prefix_decode_attention", "ffd_resolve_splits",
                  "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits"):
         getattr(so, name).restype = I
     _lib = so
@@ -345,6 +359,191 @@ def dense_decode_attention(q, k, v, seq_lens, *, num_splits: int = 0, softmax_sc
         _ptr(q), _ptr(k), _ptr(v), _ptr(seq_lens), B, Hq, Hkv, Lcap, D, num_splits,
         float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream(q)))
+    return out, lse
+
+
+# ---- 8-bit caches and shared prefixes -----------------------------------------------------------------
+# An 8-bit cache is (k_codes, k_absmax, v_codes, v_absmax): codes int8 [B, Hkv, Lcap, 128], absmaxes bf16
+# [B, Hkv, Lcap]; a bf16 cache (k, v). The calls below run on the device of their tensors, whatever device is
+# current, and require all of them there.
+
+def kv8_shapes(B: int, Hkv: int, Lcap: int):
+    """Shapes of (k_codes, k_absmax, v_codes, v_absmax) of an 8-bit cache of capacity Lcap."""
+    return ((B, Hkv, Lcap, HEAD_DIM), (B, Hkv, Lcap)) * 2
+
+
+def empty_kv8(B: int, Hkv: int, Lcap: int, device="cuda"):
+    """An 8-bit cache with uninitialised contents: (k_codes, k_absmax, v_codes, v_absmax)."""
+    return tuple(torch.empty(s, dtype=torch.int8 if len(s) == 4 else torch.bfloat16, device=device)
+                 for s in kv8_shapes(B, Hkv, Lcap))
+
+
+def _need_on(device, t, name, dtype, shape):
+    _need(t, name, dtype, shape)
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, got {t.device}")
+
+
+def _launch(fn, device, *args):
+    """The library call on this device: its launches go to the current one."""
+    if torch._C._cuda_getDevice() == device:
+        st = getattr(lib(), fn)(*args)
+    else:
+        with torch.cuda.device(device):
+            st = getattr(lib(), fn)(*args)
+    _check(fn, st)
+
+
+def _cache_dims(cache, name, bf16=False):
+    """(B, Hkv, Lcap) of a cache, from its keys."""
+    if not isinstance(cache, (tuple, list)) or len(cache) not in ((2, 4) if bf16 else (4,)):
+        raise ValueError(f"{name} must be (k_codes, k_absmax, v_codes, v_absmax)" + (" or (k, v)" if bf16 else ""))
+    if not isinstance(cache[0], torch.Tensor) or cache[0].dim() != 4:
+        raise ValueError(f"{name}'s keys must be [B, Hkv, Lcap, {HEAD_DIM}]")
+    return tuple(cache[0].shape[:3])
+
+
+def _kv_cache(cache, name, device, B, Hkv, Lcap):
+    """``ffd_kv`` of a cache whose tensors are as they have to be."""
+    rows = (B, Hkv, Lcap, HEAD_DIM)
+    if len(cache) == 2:
+        k, v = cache
+        _need_on(device, k, f"{name} k", torch.bfloat16, rows)
+        _need_on(device, v, f"{name} v", torch.bfloat16, rows)
+        return KvCache(k.data_ptr(), None, v.data_ptr(), None)
+    k, k_absmax, v, v_absmax = cache
+    _need_on(device, k, f"{name} k_codes", torch.int8, rows)
+    _need_on(device, k_absmax, f"{name} k_absmax", torch.bfloat16, rows[:3])
+    _need_on(device, v, f"{name} v_codes", torch.int8, rows)
+    _need_on(device, v_absmax, f"{name} v_absmax", torch.bfloat16, rows[:3])
+    return KvCache(k.data_ptr(), k_absmax.data_ptr(), v.data_ptr(), v_absmax.data_ptr())
+
+
+def _strided(t, name, device, shape):
+    """``t`` as [B, T, Hkv, 128]: its three strides in elements. Only the dims of a vector need to be contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != torch.bfloat16 or t.get_device() != device:
+        raise ValueError(f"{name} must be torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    strides = [0 if n == 1 else s for n, s in zip(t.shape[:-1], t.stride()[:-1])]     # one of them is never used
+    if len(strides) == 2:
+        strides.insert(1, 0)
+    return (ctypes.c_int64 * 3)(*strides)
+
+
+def write_kv8(k_new, v_new, cache, start, *, counts=None):
+    """Quantize new tokens into the 8-bit ``cache``: token t < ``counts[b]`` of sequence b goes to position
+    ``start[b] + t`` (device-side; positions outside the capacity are not written, nor is anything else of the cache).
+    ``k_new``/``v_new``: bf16 ``[B, T, Hkv, 128]``, or ``[B, Hkv, 128]`` for one token each, with any strides (slices
+    of a projection's output are taken as they are) that are multiples of 8 elements. ``start``, ``counts``: int32
+    ``[B]``; without ``counts`` all T. Lengths are the caller's to advance."""
+    B, Hkv, Lcap = _cache_dims(cache, "cache")
+    device = cache[0].get_device()
+    kv = _kv_cache(cache, "cache", device, B, Hkv, Lcap)
+    one = isinstance(k_new, torch.Tensor) and k_new.dim() == 3
+    T = 1 if one or not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 else k_new.shape[1]
+    shape = (B, Hkv, HEAD_DIM) if one else (B, T, Hkv, HEAD_DIM)
+    k_strides, v_strides = _strided(k_new, "k_new", device, shape), _strided(v_new, "v_new", device, shape)
+    _need_on(device, start, "start", torch.int32, (B,))
+    if counts is not None:
+        _need_on(device, counts, "counts", torch.int32, (B,))
+    _launch("ffd_write_kv8", device, _ptr(k_new), _ptr(v_new), k_strides, v_strides, ctypes.byref(kv), _ptr(start),
+            _ptr(counts), B, T, Hkv, Lcap, HEAD_DIM, _stream(start))
+
+
+def read_kv8(cache, t_begin: int = 0, t_end: int | None = None, *, seq_lens=None, out=None):
+    """Tokens ``[t_begin, t_end)`` of an 8-bit cache as bf16 ``(k, v)``, each ``[B, Hkv, t_end - t_begin, 128]``;
+    with ``seq_lens`` (int32 ``[B]``) the rows of tokens at or behind a sequence's length are zeros."""
+    B, Hkv, Lcap = _cache_dims(cache, "cache")
+    device = cache[0].get_device()
+    kv = _kv_cache(cache, "cache", device, B, Hkv, Lcap)
+    t_end = Lcap if t_end is None else t_end
+    if not 0 <= t_begin <= t_end <= Lcap:
+        raise ValueError(f"need 0 <= t_begin <= t_end <= {Lcap}, got {t_begin}, {t_end}")
+    shape = (B, Hkv, t_end - t_begin, HEAD_DIM)
+    if seq_lens is not None:
+        _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache[0].device) for _ in range(2))
+    k, v = out
+    _need_on(device, k, "out k", torch.bfloat16, shape)
+    _need_on(device, v, "out v", torch.bfloat16, shape)
+    _launch("ffd_read_kv8", device, ctypes.byref(kv), _ptr(seq_lens), _ptr(k), _ptr(v), B, Hkv, Lcap, HEAD_DIM,
+            t_begin, t_end, _stream(cache[0]))
+    return k, v
+
+
+def _dense_arguments(q, cache, name, seq_lens, return_lse, out, lse, bf16):
+    """Checks shared by the attentions below; (device, B, Hq, Hkv, Lcap, cache, out, lse)."""
+    B, Hkv, Lcap = _cache_dims(cache, name, bf16)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError(f"q must be [B, Hq, {HEAD_DIM}]")
+    Hq, device = q.shape[1], q.get_device()
+    _need(q, "q", torch.bfloat16, (B, Hq, HEAD_DIM))
+    kv = _kv_cache(cache, name, device, B, Hkv, Lcap)
+    _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need_on(device, out, "out", torch.bfloat16, (B, Hq, HEAD_DIM))
+    if lse is not None:
+        _need_on(device, lse, "lse", torch.float32, (B, Hq))
+    elif return_lse:
+        lse = q.new_empty((B, Hq), dtype=torch.float32)
+    return device, B, Hq, Hkv, Lcap, kv, out, lse
+
+
+def _need_workspace(workspace, device):
+    if (not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or workspace.get_device() != device
+            or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{device}")
+    return workspace.numel() * workspace.element_size()
+
+
+def kv8_decode_attention(q, cache, seq_lens, *, num_splits: int = 0, softmax_scale: float = 0.0,
+                         return_lse: bool = True, workspace=None, out=None, lse=None):
+    """Exact dense decode attention over an 8-bit cache: ``dense_decode_attention`` on the values that it stands
+    for. Returns ``(out, lse)``. ``workspace``: ``new_workspace(..., dense=True)``'s."""
+    device, B, Hq, Hkv, Lcap, kv, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, False)
+    if workspace is None:
+        workspace = new_workspace(B, Hq, Hkv, Lcap, num_splits, q.device, dense=True)
+    _launch("ffd_kv8_decode_attention", device, _ptr(q), ctypes.byref(kv), _ptr(seq_lens), B, Hq, Hkv, Lcap, HEAD_DIM,
+            num_splits, float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+            _need_workspace(workspace, device), _stream(q))
+    return out, lse
+
+
+def shared_prefix_workspace_bytes(B: int, Hq: int, Hkv: int, Pcap: int, Lcap: int, num_splits: int = 0) -> int:
+    """Bytes for ``shared_prefix_decode_attention`` with a prefix of capacity Pcap and caches of capacity Lcap."""
+    return lib().ffd_shared_prefix_workspace_bytes(B, Hq, Hkv, Pcap, Lcap, HEAD_DIM, num_splits)
+
+
+def new_shared_prefix_workspace(B: int, Hq: int, Hkv: int, Pcap: int, Lcap: int, num_splits: int = 0, device="cuda"):
+    """A workspace for ``shared_prefix_decode_attention`` (one per stream)."""
+    return torch.empty(max(shared_prefix_workspace_bytes(B, Hq, Hkv, Pcap, Lcap, num_splits), 16), dtype=torch.uint8,
+                       device=device)
+
+
+def shared_prefix_decode_attention(q, prefix, prefix_lens, cache, seq_lens, *, num_splits: int = 0,
+                                   softmax_scale: float = 0.0, return_lse: bool = True, workspace=None, out=None,
+                                   lse=None):
+    """Exact dense decode attention of a batch whose sequences begin with the same tokens: sequence b attends over the
+    first ``prefix_lens[b]`` tokens of ``prefix`` and the ``seq_lens[b]`` tokens of its own ``cache``. The prefix is a
+    cache of one sequence (B = 1) and is read once for the whole batch. ``prefix`` and ``cache`` are each ``(k, v)``
+    in bf16 or an 8-bit cache; the lengths int32 ``[B]``. Returns ``(out, lse)``."""
+    device, B, Hq, Hkv, Lcap, own, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, True)
+    Pcap = _cache_dims(prefix, "prefix", True)[2]
+    shared = _kv_cache(prefix, "prefix", device, 1, Hkv, Pcap)
+    _need_on(device, prefix_lens, "prefix_lens", torch.int32, (B,))
+    if workspace is None:
+        workspace = new_shared_prefix_workspace(B, Hq, Hkv, Pcap, Lcap, num_splits, q.device)
+    _launch("ffd_shared_prefix_decode_attention", device, _ptr(q), ctypes.byref(shared), _ptr(prefix_lens), Pcap,
+            ctypes.byref(own), _ptr(seq_lens), B, Hq, Hkv, Lcap, HEAD_DIM, num_splits, float(softmax_scale), _ptr(out),
+            _ptr(lse), _ptr(workspace), _need_workspace(workspace, device), _stream(q))
     return out, lse
 
 

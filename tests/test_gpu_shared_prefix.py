@@ -1,0 +1,259 @@
+"""Decode attention over a shared prefix and each sequence's own tokens against a plain 64-bit form."""
+import math
+
+import pytest
+import torch
+
+from tests.kv8_reference import D, P_BF16, attention, check_attention, random_cache, values
+
+pytestmark = pytest.mark.gpu
+
+
+def _gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def _normal(gen, *shape):
+    return torch.randn(*shape, generator=gen, device="cuda", dtype=torch.bfloat16)
+
+
+def _int32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _cap(lens):
+    return max(64, -(-max(lens) // 64) * 64)
+
+
+def _spoil(cache, lens):
+    """NaN behind each sequence's tokens (the codes of an 8-bit cache at their limit)."""
+    for t in cache:
+        for b, n in enumerate(lens):
+            t[b, :, max(n, 0):] = 127 if t.dtype == torch.int8 else math.nan
+
+
+def _reference(q, prefix, prefix_lens, cache, lens, scale=None):
+    return attention(q, [(*values(prefix), prefix_lens), (*values(cache), lens)], scale)
+
+
+# query rows of a KV head (B * G) around the kernel's tiles of 16, 32 and 64 rows
+@pytest.mark.parametrize("B,Hq,Hkv", [(1, 1, 1), (1, 16, 2), (4, 8, 2), (17, 2, 2), (8, 8, 2), (33, 1, 1), (16, 4, 1), (13, 10, 2)])
+@pytest.mark.parametrize("prefix_bits,own_bits", [(16, 16), (8, 8), (8, 16), (16, 8)])
+def test_full_prefix(B, Hq, Hkv, prefix_bits, own_bits):
+    from paper_2609_00097_amd import ffd
+    if Hq // Hkv not in (1, 2, 4, 8):
+        Hq = 8 * Hkv
+    gen = _gen(B * Hq)
+    P, lens = 300, [(37 * b + 1) % 130 for b in range(B)]
+    q = _normal(gen, B, Hq, D)
+    prefix, cache = random_cache(gen, 1, Hkv, _cap([P]), prefix_bits), random_cache(gen, B, Hkv, _cap(lens), own_bits)
+    _spoil(prefix, [P])
+    _spoil(cache, lens)
+    print(f"case shared B={B} Hq={Hq} Hkv={Hkv} bits {prefix_bits} {own_bits}", flush=True)
+    got = ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens))
+    torch.cuda.synchronize()
+    check_attention(got, _reference(q, prefix, [P] * B, cache, lens), P + 130, P_BF16)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("prefix_lens,lens", [
+    ([0, 1, 31, 32, 33, 127, 128, 129], [0, 0, 1, 64, 65, 3, 0, 0]),
+    ([0] * 5, [0, 5, 0, 64, 1]),                                      # nobody uses it
+    ([1000, 0, 4000, -7, 99999], [0, 0, 0, 10, -1]),                  # clamped to the capacity
+    ([64], [0]),
+    ([0, 0], [0, 0]),
+])
+def test_parts_of_the_prefix(bits, prefix_lens, lens):
+    from paper_2609_00097_amd import ffd
+    gen = _gen(len(lens) + bits)
+    B, Hq, Hkv, Pcap = len(lens), 16, 2, 4032
+    q = _normal(gen, B, Hq, D)
+    prefix, cache = random_cache(gen, 1, Hkv, Pcap, bits), random_cache(gen, B, Hkv, 128, bits)
+    clamped = [min(max(n, 0), Pcap) for n in prefix_lens]
+    own = [min(max(n, 0), 128) for n in lens]
+    _spoil(prefix, [max(clamped)])
+    _spoil(cache, own)
+    print(f"case shared parts {prefix_lens} {lens} bits {bits}", flush=True)
+    got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+    torch.cuda.synchronize()
+    check_attention(got, _reference(q, prefix, clamped, cache, own), Pcap + 128, P_BF16)
+
+
+def test_infinities_and_nan_reach_only_the_rows_that_see_them():
+    """Keys and values of prefix tokens that some sequences use and others do not, within one tile of tokens and in
+    tiles of their own."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(5)
+    prefix_lens, lens = [40, 44, 60, 200, 300], [3, 0, 10, 0, 1]
+    q = _normal(gen, 5, 4, D)
+    prefix, cache = random_cache(gen, 1, 1, 320, 16), random_cache(gen, 5, 1, 64, 16)
+    clean = _reference(q, prefix, prefix_lens, cache, lens)
+    prefix[1][0, 0, 42, 9] = math.inf
+    prefix[1][0, 0, 50, 17] = math.nan
+    prefix[0][0, 0, 250, 3] = math.nan
+    prefix[1][0, 0, 299, 100] = -math.inf
+    out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+    torch.cuda.synchronize()
+    want = torch.zeros(5, 4, D, dtype=torch.bool)
+    want[1:, :, 9] = want[2:, :, 17] = True
+    want[4] = True
+    assert torch.equal(~out.isfinite().cpu(), want)
+    assert bool((out[1:4, :, 9] == math.inf).all()) and out[2:, :, 17].isnan().all()
+    o, ref = out.cpu().clone(), clean[0]
+    o[want] = ref[want].bfloat16()
+    check_attention((o[:4], lse[:4]), tuple(t[:4] for t in clean), 310, P_BF16)
+
+
+def test_splits_scale_and_given_outputs():
+    from paper_2609_00097_amd import ffd
+    gen = _gen(7)
+    B, Hq, Hkv, P, lens = 6, 8, 2, 2500, [700, 0, 1, 64, 333, 10]
+    q, prefix, cache = _normal(gen, B, Hq, D), random_cache(gen, 1, Hkv, _cap([P])), random_cache(gen, B, Hkv, 704, 16)
+    ref = _reference(q, prefix, [P] * B, cache, lens, 0.15)
+    for splits in (1, 2, 9, 40, 0):                       # 40: more runs than the prefix has rounds
+        out, lse = torch.full_like(q, 7.0), torch.full((B, Hq), 7.0, device="cuda")
+        ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, _cap([P]), 704, splits)
+        ws.fill_(255)                                     # NaN wherever the call reads what it has not written
+        got = ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens), num_splits=splits,
+                                                 softmax_scale=0.15, workspace=ws, out=out, lse=lse)
+        torch.cuda.synchronize()
+        assert got[0] is out and got[1] is lse
+        check_attention(got, ref, P + 700, P_BF16)
+    assert ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens), return_lse=False)[1] is None
+    with pytest.raises(ffd.FfdError, match="WORKSPACE"):
+        ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens), workspace=ws[:4096])
+    with pytest.raises(ValueError, match="prefix"):
+        ffd.shared_prefix_decode_attention(q, cache, _int32([P] * B), cache, _int32(lens))
+    with pytest.raises(ValueError, match="prefix_lens"):
+        ffd.shared_prefix_decode_attention(q, prefix, _int32([P]), cache, _int32(lens))
+    with pytest.raises(ValueError, match="cache v"):
+        ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), (cache[0], cache[1][:, :, :64]), _int32(lens))
+
+
+def test_many_sequences():
+    """300 sequences (the own caches beyond the balanced mode) in several row tiles, the last one in part."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(9)
+    B, Hq, Hkv, P = 301, 4, 1, 1500
+    lens, prefix_lens = [(53 * b) % 200 for b in range(B)], [P if b % 3 else (7 * b) % P for b in range(B)]
+    q = _normal(gen, B, Hq, D)
+    for bits in (16, 8):
+        prefix, cache = random_cache(gen, 1, Hkv, _cap([P]), bits), random_cache(gen, B, Hkv, 256, bits)
+        got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+        torch.cuda.synchronize()
+        check_attention(got, _reference(q, prefix, prefix_lens, cache, lens), P + 200, P_BF16)
+
+
+def test_equals_dense_attention_over_the_whole():
+    """The same tokens as one bf16 cache per sequence through dense_decode_attention: the two round differently, each by
+    a half step of bf16 and, here, of the probabilities."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(15)
+    B, Hq, Hkv, P, n = 3, 8, 2, 640, 192
+    q, (pk, pv), (k, v) = _normal(gen, B, Hq, D), random_cache(gen, 1, Hkv, P, 16), random_cache(gen, B, Hkv, n, 16)
+    whole = [torch.cat([a.expand(B, -1, -1, -1), b], 2) for a, b in ((pk, k), (pv, v))]
+    dense = ffd.dense_decode_attention(q, *whole, _int32([P + n] * B))
+    got = ffd.shared_prefix_decode_attention(q, (pk, pv), _int32([P] * B), (k, v), _int32([n] * B))
+    torch.cuda.synchronize()
+    ref = attention(q, [(whole[0].double(), whole[1].double(), [P + n] * B)])
+    check_attention(dense, ref, P + n, P_BF16)
+    check_attention(got, ref, P + n, P_BF16)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_prefix_behind_32_bit_offsets(bits):
+    """Rows of the prefix beyond 4 GiB: everything zero but tokens near the end, whose weights are known."""
+    from paper_2609_00097_amd import ffd
+    P = (1 << (24 if bits == 16 else 25)) + 192
+    dtype, one = (torch.bfloat16, 1.0) if bits == 16 else (torch.int8, 127)
+    k, v = (torch.zeros(1, 1, P, D, dtype=dtype, device="cuda") for _ in range(2))
+    q = torch.zeros(2, 1, D, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 2.0
+    for i, t in enumerate((P - 1, P - 70, P - 130)):
+        k[0, 0, t, 0], v[0, 0, t, i] = one, one
+    prefix = (k, v)
+    if bits == 8:
+        m = torch.ones(1, 1, P, dtype=torch.bfloat16, device="cuda")
+        prefix = (k, m, v, m)
+    cache = random_cache(_gen(1), 2, 1, 64, 16)
+    out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32([P, P - 1]), cache, _int32([0, 0]), softmax_scale=10.0)
+    torch.cuda.synchronize()
+    for b in range(2):
+        total = math.exp(20.0) * (3 - b) + (P - b - (3 - b))
+        want = math.exp(20.0) / total
+        assert abs(lse[b, 0].item() - math.log(total)) < 1e-3
+        for i in range(3):
+            w = want if i >= b else 0.0
+            assert abs(out[b, 0, i].item() - w) <= (2.0 ** -7 + 4e-3) * w
+
+
+def _capture(fn):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        fn()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fn()
+    torch.cuda.synchronize()
+    return g
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_served_batch(bits):
+    """As a serving program uses them together: a prompt is written once, a captured step (write or copy the new
+    token, advance, attend over prompt and own tokens) is replayed between eager work on the same workspace, and one
+    sequence starts anew without the prompt. Every step equals the eager call and the 64-bit form."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(29)
+    B, Hq, Hkv, P, L = 5, 16, 2, 700, 64
+    prompt_k, prompt_v = _normal(gen, 1, P, Hkv, D), _normal(gen, 1, P, Hkv, D)
+    if bits == 8:
+        prefix, cache = ffd.empty_kv8(1, Hkv, _cap([P])), ffd.empty_kv8(B, Hkv, L)
+        for chunk in range(0, P, 256):                   # a chunked prefill, which reads back what it attends over
+            ffd.write_kv8(prompt_k[:, chunk:chunk + 256], prompt_v[:, chunk:chunk + 256], prefix, _int32([chunk]))
+        read = ffd.read_kv8(prefix, 0, P)
+        assert torch.equal(read[0], values(prefix)[0][:, :, :P].bfloat16())
+    else:
+        prefix = tuple(torch.zeros(1, Hkv, _cap([P]), D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        cache = tuple(torch.zeros(B, Hkv, L, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        prefix[0][:, :, :P], prefix[1][:, :, :P] = prompt_k.transpose(1, 2), prompt_v.transpose(1, 2)
+    prefix_lens, lens = _int32([P, P, 350, P, 0]), _int32([0, 3, 0, 17, 0])
+    for t in cache:
+        t.zero_()
+    k_new, v_new, q = (_normal(gen, B, n, D) for n in (Hkv, Hkv, Hq))
+    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, _cap([P]), L)
+    out, lse = torch.empty_like(q), torch.empty(B, Hq, device="cuda")
+
+    def write():
+        if bits == 8:
+            ffd.write_kv8(k_new, v_new, cache, lens)
+        else:
+            at = lens.long().view(B, 1, 1, 1).expand(B, Hkv, 1, D)
+            cache[0].scatter_(2, at, k_new.unsqueeze(2))
+            cache[1].scatter_(2, at, v_new.unsqueeze(2))
+
+    def step():
+        write()
+        lens.add_(1)
+        ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens, workspace=ws, out=out, lse=lse)
+
+    first = lens.clone()
+    g = _capture(step)
+    lens.copy_(first)
+    for i in range(4):
+        for t, n in ((k_new, Hkv), (v_new, Hkv), (q, Hq)):
+            t.copy_(_normal(gen, B, n, D))
+        if i == 2:                                       # another request takes sequence 1's place
+            prefix_lens[1] = 0
+            lens[1] = 0
+        out.fill_(math.nan)
+        g.replay()
+        eager = ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens)
+        ffd.shared_prefix_decode_attention(q.flip(0), prefix, prefix_lens, cache, lens, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1]), f"replay {i}"
+        ref = _reference(q, prefix, prefix_lens.tolist(), cache, lens.tolist())
+        check_attention((out, lse), ref, P + L, P_BF16)
