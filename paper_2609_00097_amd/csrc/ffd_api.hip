@@ -446,32 +446,37 @@ void launch_kv8(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const
     hipLaunchKernelGGL(kv8_decode_kernel, o.grid, dim3(kThreads), 0, stream, a);
 }
 
-// Tiles of 16 CT query rows and runs of the prefix attention.
+// Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head (a prefix is then
+// read once), at most 256; as many runs as give each CU one workgroup (two of the small ones that fit there).
 struct PrefixPlan {
-    int ct, tiles, S;
+    int tile_rows, tiles, S;
     size_t rows;                      // partial rows in all
 };
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
     const long long rows = (long long)B * (Hq / Hkv);
     PrefixPlan p;
-    p.ct = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.tiles = (int)((rows + 16 * p.ct - 1) / (16 * p.ct));
+    p.tile_rows = 16;
+    while (p.tile_rows < rows && p.tile_rows < 256) p.tile_rows *= 2;
+    p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
     long long s = num_splits;
     if (s == 0) {
-        s = (p.ct == 4 ? 1LL : 2LL) * device_cus() / ((long long)Hkv * p.tiles);
-        s = std::min(s, (long long)(Pcap + kPrefixRound - 1) / kPrefixRound);
+        s = (p.tile_rows <= 32 ? 2LL : 1LL) * device_cus() / ((long long)Hkv * p.tiles);
+        s = std::min(s, (long long)(Pcap + 127) / 128);
         s = std::max(1LL, std::min(s, (long long)FFD_MAX_SPLITS));
     }
     p.S = (int)s;
-    p.rows = (size_t)Hkv * p.tiles * p.S * 16 * p.ct;
+    p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
     return p;
 }
 
 template <bool I8>
-void launch_prefix(int ct, dim3 grid, hipStream_t stream, const PrefixArgs& a) {
-    if (ct == 1) hipLaunchKernelGGL((prefix_kernel<1, I8>), grid, dim3(kThreads), 0, stream, a);
-    else if (ct == 2) hipLaunchKernelGGL((prefix_kernel<2, I8>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((prefix_kernel<4, I8>), grid, dim3(kThreads), 0, stream, a);
+void launch_prefix(int tile_rows, dim3 grid, hipStream_t stream, const PrefixArgs& a) {
+    const dim3 small(kThreads), large(kPrefixTileThreads);
+    if (tile_rows == 16) hipLaunchKernelGGL((prefix_kernel<1, I8>), grid, small, 0, stream, a);
+    else if (tile_rows == 32) hipLaunchKernelGGL((prefix_kernel<2, I8>), grid, small, 0, stream, a);
+    else if (tile_rows == 64) hipLaunchKernelGGL((prefix_tile_kernel<2, I8>), grid, large, 0, stream, a);
+    else if (tile_rows == 128) hipLaunchKernelGGL((prefix_tile_kernel<4, I8>), grid, large, 0, stream, a);
+    else hipLaunchKernelGGL((prefix_tile_kernel<8, I8>), grid, large, 0, stream, a);
 }
 
 int check_pcap(int Pcap) {
@@ -838,14 +843,14 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     const uint16_t* qp = static_cast<const uint16_t*>(q);
     const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
     const dim3 grid((unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles));
-    if (prefix_bits == 8) launch_prefix<true>(plan.ct, grid, stream, a);
-    else launch_prefix<false>(plan.ct, grid, stream, a);
+    if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, grid, stream, a);
+    else launch_prefix<false>(plan.tile_rows, grid, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
     if (own_bits == 8) launch_kv8(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     else launch_dense(o, qp, own->k, own->v, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     if ((st = launch_status()) != FFD_OK) return st;
     const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, static_cast<uint16_t*>(out), lse,
-                            Hq, Hkv, G, plan.tiles, 16 * plan.ct, plan.S, S};
+                            Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};
     const dim3 merge_grid((unsigned)(B * Hq), kMergeSlices);
     if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, merge_grid, dim3(64), 0, stream, m);
     else hipLaunchKernelGGL(shared_merge_kernel<4>, merge_grid, dim3(256), 0, stream, m);

@@ -29,7 +29,6 @@ namespace {
 
 constexpr int kTile = 32;                      // tokens a wave takes at a time
 constexpr int kRound = kTile * kWaves;         // and a workgroup
-static_assert(kRound == kPrefixRound, "the host counts runs in rounds");
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -231,6 +230,7 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
     if (t0 >= end) return;
     KeyTile<I8> kt;
     ValueTile<I8> vt;
+    wait_loads();
     kt.load(kv, t0, rows - 1 - t0, n, g);
     vt.load(kv, t0, rows - 1 - t0, n, g);
     while (true) {
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
 // The batch over its shared prefix. Workgroups of one run and KV head but different row tiles read the same
 // tokens: they are eight apart, so on one XCD (consecutive workgroups go to the eight XCDs in turn) and at one time.
 template <int CT, bool I8>
-__global__ __launch_bounds__(kThreads, CT == 4 ? 1 : 2) void prefix_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a) {
     __shared__ JoinLds<CT> lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
@@ -509,9 +509,7 @@ __global__ __launch_bounds__(kThreads, CT == 4 ? 1 : 2) void prefix_kernel(Prefi
 
 template __global__ void prefix_kernel<1, false>(PrefixArgs);
 template __global__ void prefix_kernel<2, false>(PrefixArgs);
-template __global__ void prefix_kernel<4, false>(PrefixArgs);
 template __global__ void prefix_kernel<1, true>(PrefixArgs);
 template __global__ void prefix_kernel<2, true>(PrefixArgs);
-template __global__ void prefix_kernel<4, true>(PrefixArgs);
 
 }  // namespace ffd

@@ -192,9 +192,9 @@ struct Kv8Args {
     float scale;
 };
 
-// Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in tiles of
-// 16 CT, each tile's prefix in S runs. Partial row ((kvh * tiles + tile) * S + run) * 16 CT + row in tile.
-constexpr int kPrefixRound = 128;              // tokens that a workgroup of it takes at a time
+// Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in tiles of R rows,
+// each tile's prefix in S runs. Partial row ((kvh * tiles + tile) * S + run) * R + row in tile. R is 16 CT of
+// prefix_kernel (up to 32 rows) or 32 RW of prefix_tile_kernel.
 struct PrefixArgs {
     const uint16_t* q;          // bf16 [B, Hq, 128]
     KvSource kv;                // [Hkv, Pcap, ..]
@@ -260,8 +260,11 @@ template <int BITS> __global__ void append_kv_kernel(AppendArgs a);
 __global__ void write_kv8_kernel(WriteKv8Args a);
 __global__ void read_kv8_kernel(ReadKv8Args a);
 __global__ void kv8_decode_kernel(Kv8Args a);
-// CT: tiles of 16 query rows per workgroup; I8: an 8-bit prefix.
+// CT (1, 2): tiles of 16 query rows per workgroup; I8: an 8-bit prefix.
 template <int CT, bool I8> __global__ void prefix_kernel(PrefixArgs a);
+constexpr int kPrefixTileThreads = 512;
+// RW (2, 4, 8): groups of 32 query rows per workgroup.
+template <int RW, bool I8> __global__ void prefix_tile_kernel(PrefixArgs a);
 template <int NW> __global__ void shared_merge_kernel(SharedMergeArgs a);
 constexpr int kMergeSlices = 4;                // workgroups per head of the merge, 32 dims each
 // NW waves per workgroup: 4, or 1 from kMergeOneWaveHeads heads on (their waves fill the chip alone).

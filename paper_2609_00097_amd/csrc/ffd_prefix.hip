@@ -1,0 +1,473 @@
+// A batch's attention over its shared prefix for gfx950, for more than 32 query rows per KV head (ffd_attend.hip has
+// the mathematics and serves fewer): tokens staged in LDS once for all rows of a workgroup.
+//
+// Bound. A prefix token costs 512 bytes (8 bits: 260) and 512 operations per query row: up to about 128 rows
+// HBM's, beyond them the matrix cores'. Next to these, a score costs about eight VALU slots (scale and subtract,
+// exponential, maximum, sum, conversion), as much time as its matrix instructions.
+//
+// Mapping. Eight waves: RW row groups of 32 query rows by 8 / RW token groups. Scores are computed transposed by
+// v_mfma_f32_32x32x16_bf16, S^T = K Q^T: lane (n, h) = (lane & 31, lane >> 5) holds, of query row n, tokens
+// 8 a + 4 h + i (a, i = 0 .. 3) of a 32-token tile, which are just the contraction indices it has to hold of P^T in
+// O^T = V^T P^T: the probabilities never leave their registers, and maximum, sum and rescaling are per lane. V^T
+// comes out of LDS by transposing reads (a 16-lane group gets, of four rows of 16 values, four of one column each).
+// Rows of 256 bytes lie in LDS as 16-byte chunks in an order that depends on the row (xor), so that the lanes of a
+// read, which all read the same columns of different rows, spread over the banks.
+//
+// 8-bit codes become bf16 integers on their way into LDS; M / 127 of a key multiplies its score, that of a value its
+// probability. The maximum that the exponents are taken against follows the running one only when that has grown by
+// 2^8, so that the accumulators are rarely rescaled.
+//
+// Phases. A tile has a matrix phase (the values' product of the tile before, then this one's scores) and a vector
+// phase (softmax; staging), each closed by a barrier. The two teams of four waves, one wave of each on every SIMD, are
+// one phase apart, so that one's matrix instructions and LDS reads run beside the other's vector instructions. In
+// phase number 2 u, team 0 has the matrix phase of tile u and team 1 the vector phase of tile u - 1; in 2 u + 1 team 0
+// the vector phase of u, team 1 the matrix phase of u. The keys of tile u are read in phases 2 u and 2 u + 1, its
+// values in 2 u + 2 and 2 u + 3. Each team stages half of the rows in its vector phases: team 1 the keys of tile u + 1
+// and the values of u in phase 2 u, team 0 the same in 2 u + 1, which is after the last read of tiles u - 1 and u - 2,
+// whose places they take, and before their first use. The loads for them are issued one vector phase earlier.
+#include <cfloat>
+
+#include "ffd_device.h"
+#include "ffd_kernels.h"
+
+namespace ffd {
+
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+
+constexpr int kPThreads = kPrefixTileThreads;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;                  // growth of the maximum, in powers of two, that rescales
+
+template <int RW>
+struct PrefixShape {
+    static constexpr int kTokenGroups = 8 / RW;
+    static constexpr int kSub = RW == 2 ? 1 : 2;                        // 32-token tiles of a wave
+    static constexpr int kTokens = 32 * kSub * kTokenGroups;            // tokens of a tile of the workgroup
+    static constexpr int kRows = 32 * RW;
+    static constexpr int kBytes = kTokens * 2 * kD;                     // of a tile's keys, or values, in LDS
+    static constexpr int kLoads = kTokens / 32;                         // 16-byte chunks per thread of half of them
+};
+constexpr int kTeam = kPThreads / 2;           // threads that stage one half of a tile
+constexpr int kJoinPad = kD + 4;
+
+template <int RW>
+struct PrefixLds {
+    using Sh = PrefixShape<RW>;
+    union {
+        struct {
+            alignas(16) uint8_t keys[2][Sh::kBytes];
+            alignas(16) uint8_t values[2][Sh::kBytes];
+        };
+        float join[Sh::kTokenGroups > 1 ? Sh::kRows : 1][kJoinPad];
+    };
+    alignas(16) float km[4][Sh::kTokens];                               // 8 bits: M / 127 of keys and values
+    alignas(16) float vm[4][Sh::kTokens];
+    int nonfinite[4];                          // last tile with this index mod 4 that has an infinity or NaN as value
+    float m[8][32], l[8][32];
+};
+
+// Chunk order of the two kinds of rows.
+__device__ __forceinline__ int key_chunk(int row, int c) { return c ^ (row & 15); }
+__device__ __forceinline__ int value_chunk(int row, int c) { return c ^ (((row & 3) << 2) | ((row >> 2) & 3)); }
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float halves_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+template <int BYTE>
+__device__ __forceinline__ float byte_value(uint32_t w) { return (float)(int8_t)(w >> (8 * BYTE)); }
+__device__ __forceinline__ uint2 expand4(uint32_t w) {          // four codes as bf16 (exact: their floats end in zeros)
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(byte_value<1>(w)), __float_as_uint(byte_value<0>(w)), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(byte_value<3>(w)), __float_as_uint(byte_value<2>(w)), 0x07060302u));
+}
+
+// Half of a tile on its way from memory to LDS, in the registers of a team: rows [team kTokens / 2, ..) of the tile.
+// `last` is the last row of the tile that any query sees; rows behind it repeat it.
+template <int RW, bool I8> struct Staged;
+template <int RW> struct Staged<RW, false> {
+    using Sh = PrefixShape<RW>;
+    v4u k[Sh::kLoads], v[Sh::kLoads];
+    static __device__ __forceinline__ int row_of(int j, int team, int id) { return team * (Sh::kTokens / 2) + (id >> 4) + j * (kTeam / 16); }
+    static __device__ __forceinline__ void load(v4u (&x)[Sh::kLoads], const uint8_t* from, int t0, int last, int team, int id) {
+        const uint8_t* base = from + (size_t)t0 * (2 * kD);
+#pragma unroll
+        for (int j = 0; j < Sh::kLoads; ++j)
+            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, team, id), last) * (2 * kD) + 16 * (id & 15));
+    }
+    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int team, int id) { load(k, kv.k, t0, last, team, id); }
+    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int team, int id) { load(v, kv.v, t0, last, team, id); }
+    __device__ __forceinline__ void store_keys(PrefixLds<RW>& lds, int u, int, int team, int id) const {
+#pragma unroll
+        for (int j = 0; j < Sh::kLoads; ++j) {
+            const int row = row_of(j, team, id);
+            *reinterpret_cast<v4u*>(&lds.keys[u & 1][row * (2 * kD) + 16 * key_chunk(row, id & 15)]) = k[j];
+        }
+    }
+    __device__ __forceinline__ void store_values(PrefixLds<RW>& lds, int u, int team, int id) const {
+#pragma unroll
+        for (int j = 0; j < Sh::kLoads; ++j) {
+            const int row = row_of(j, team, id);
+            v4u x = v[j];
+            const uint32_t big = pk_max_u16(pk_max_u16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max_u16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+            if (max(big & 0xffffu, big >> 16) >= 0x7f80u) {
+                lds.nonfinite[u & 3] = u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t lo = (x[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu, hi = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
+                    x[i] &= lo | hi;
+                }
+            }
+            *reinterpret_cast<v4u*>(&lds.values[u & 1][row * (2 * kD) + 16 * value_chunk(row, id & 15)]) = x;
+        }
+    }
+};
+template <int RW> struct Staged<RW, true> {
+    using Sh = PrefixShape<RW>;
+    static constexpr int kLoads = Sh::kLoads / 2;
+    static constexpr int kScales = Sh::kTokens / 2;
+    static_assert(2 * kScales <= kTeam, "one absmax per thread");
+    v4u k[kLoads], v[kLoads];
+    uint32_t m;                                 // absmax of a key (threads below kScales) or value (the next kScales)
+    static __device__ __forceinline__ int row_of(int j, int team, int id) { return team * (Sh::kTokens / 2) + (id >> 3) + j * (kTeam / 8); }
+    static __device__ __forceinline__ void load(v4u (&x)[kLoads], const uint8_t* from, int t0, int last, int team, int id) {
+        const uint8_t* base = from + (size_t)t0 * kD;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, team, id), last) * kD + 16 * (id & 7));
+    }
+    static __device__ __forceinline__ void expand(uint8_t* tile, int row, int c, bool keys, const v4u& w) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint2 a = expand4(w[2 * x]), b = expand4(w[2 * x + 1]);
+            const int at = keys ? key_chunk(row, c + x) : value_chunk(row, c + x);
+            *reinterpret_cast<v4u*>(tile + row * (2 * kD) + 16 * at) = v4u{a.x, a.y, b.x, b.y};
+        }
+    }
+    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int team, int id) {
+        load(k, kv.k, t0, last, team, id);
+        m = 0;                                  // the values' absmaxes come with the keys: they are needed with the scores
+        if (id < 2 * kScales)
+            m = (id < kScales ? kv.k_absmax : kv.v_absmax)[(size_t)t0 + min(team * kScales + (id & (kScales - 1)), last)];
+    }
+    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int team, int id) { load(v, kv.v, t0, last, team, id); }
+    __device__ __forceinline__ void store_keys(PrefixLds<RW>& lds, int u, int last, int team, int id) const {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) expand(lds.keys[u & 1], row_of(j, team, id), 2 * (id & 7), true, k[j]);
+        if (id < 2 * kScales) {
+            const int t = team * kScales + (id & (kScales - 1));
+            const float x = t <= last ? bf16_to_f32((uint16_t)m) * (1.f / 127.f) : 0.f;
+            const bool finite = fabsf(x) < INFINITY;
+            if (id < kScales) {
+                lds.km[u & 3][t] = x;
+            } else {
+                lds.vm[u & 3][t] = finite ? x : 0.f;
+                if (!finite) lds.nonfinite[u & 3] = u;
+            }
+        }
+    }
+    __device__ __forceinline__ void store_values(PrefixLds<RW>& lds, int u, int team, int id) const {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) expand(lds.values[u & 1], row_of(j, team, id), 2 * (id & 7), false, v[j]);
+    }
+};
+
+// Infinities and NaN among the values of tokens [begin, end), which are zeros in LDS (zero times infinity would reach
+// rows that do not see the token): added to the rows that see them. An absmax that is NaN makes a whole row NaN.
+template <bool I8>
+__device__ __forceinline__ void add_nonfinite(v16f (&o)[4], const KvSource& kv, int begin, int end, int lim, int h) {
+#pragma unroll 1
+    for (int t = begin; t < end; ++t) {
+        const uint16_t* row = I8 ? kv.v_absmax + t : reinterpret_cast<const uint16_t*>(kv.v) + (size_t)t * kD + 4 * h;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = bf16_to_f32(row[I8 ? 0 : 32 * d + 8 * (i >> 2) + (i & 3)]);
+                o[d][i] += !(fabsf(x) < INFINITY) && t < lim ? x : 0.f;
+            }
+    }
+}
+
+}  // namespace
+
+template <int RW, bool I8>
+__global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a) {
+    using Sh = PrefixShape<RW>;
+    __shared__ PrefixLds<RW> lds;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int n = lane & 31, h = lane >> 5;
+    const int rg = wave % RW, tg = wave / RW;
+    const int tile = (int)(blockIdx.x >> 3) % a.tiles;
+    const int pair = (int)(blockIdx.x >> 3) / a.tiles * 8 + (int)(blockIdx.x & 7);
+    if (pair >= a.Hkv * a.S) return;
+    const int kvh = pair / a.S, run = pair % a.S;
+    const int rows = a.B * a.G;
+
+    // longest use of the prefix among the workgroup's rows, and this wave's longest and shortest
+    const int r = tile * Sh::kRows + 32 * rg + n;
+    const bool live = r < rows;
+    const int lim = live ? min(max(a.prefix_lens[r / a.G], 0), a.Pcap) : 0;
+    int longest = lim, shortest = live ? lim : INT32_MAX;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) {
+        longest = max(longest, __shfl_xor(longest, x));
+        shortest = min(shortest, __shfl_xor(shortest, x));
+    }
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    shortest = __builtin_amdgcn_readfirstlane(shortest);
+    if (lane == 0) reinterpret_cast<int*>(lds.m[wave])[0] = longest;
+    if (tid < 4) lds.nonfinite[tid] = -1;
+    v8bf q[8];
+    const uint16_t* qrow = a.q + ((size_t)(r / a.G) * a.Hq + kvh * a.G + r % a.G) * kD;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = *reinterpret_cast<const uint4*>(qrow + 16 * s + 8 * h);
+        q[s] = __builtin_bit_cast(v8bf, w);
+    }
+    wait_loads();
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) all = max(all, reinterpret_cast<const int*>(lds.m[w])[0]);
+    all = __builtin_amdgcn_readfirstlane(all);
+    const int units = (all + Sh::kTokens - 1) / Sh::kTokens;
+    const int first = (int)((long long)units * run / a.S), last = (int)((long long)units * (run + 1) / a.S);
+
+    const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
+    const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
+                      I8 ? a.kv.v_absmax + row0 : nullptr};
+    const float zscale = a.scale * kLog2e;
+    v16f o[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    // this lane's places in a tile: its key row's chunk for step 0, and its piece of a transposing read of dims 0 .. 31
+    const int wave_row = tg * 32 * Sh::kSub;
+    const uint32_t k_at = (wave_row + n) * (2 * kD) + 16 * key_chunk(n, h);
+    const int i16 = lane & 15;
+    const int v_row = 4 * h + (i16 >> 2), v_c = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+    const uint32_t v_at = (wave_row + v_row) * (2 * kD) + 16 * value_chunk(v_row, v_c) + 8 * (i16 & 1);
+
+    const int team = wave >> 2, id = tid & (kTeam - 1);
+    Staged<RW, I8> st;
+    // Stores this team's half of the keys of tile u and the values of tile u - 1, and asks for those after them.
+    // Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for one tile's
+    // registers would fall on the next one's loads.
+    auto last_row = [&](int u) { return all - 1 - u * Sh::kTokens; };
+    auto stage = [&](int u) {
+        st.store_keys(lds, u, last_row(min(u, last - 1)), team, id);
+        st.store_values(lds, u - 1, team, id);
+        const int k = min(u + 1, last - 1), v = min(u, last - 1);
+        st.load_keys(kv, k * Sh::kTokens, last_row(k), team, id);
+        st.load_values(kv, v * Sh::kTokens, last_row(v), team, id);
+    };
+    if (first < last) {
+        const int second = min(first + 1, last - 1);
+        st.load_keys(kv, first * Sh::kTokens, last_row(first), team, id);
+        st.store_keys(lds, first, last_row(first), team, id);
+        st.load_keys(kv, second * Sh::kTokens, last_row(second), team, id);
+        st.load_values(kv, first * Sh::kTokens, last_row(first), team, id);
+        __syncthreads();
+        if (team == 1) {
+            stage(first + 1);
+            __syncthreads();
+        }
+        v16f s[Sh::kSub];
+        v8bf p[2 * Sh::kSub];
+        for (int u = first; u <= last; ++u) {
+            const int w0 = u * Sh::kTokens + wave_row;      // this wave's first token
+            if (u > first && w0 - Sh::kTokens < longest) {  // uniform
+                const uint8_t* values = lds.values[(u - 1) & 1];
+#pragma unroll
+                for (int y = 0; y < 2 * Sh::kSub; ++y)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        v4s v[2];
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+                            v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
+                                values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
+                        const v8s f = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
+                    }
+                if (lds.nonfinite[(u - 1) & 3] == u - 1)
+                    add_nonfinite<I8>(o, kv, w0 - Sh::kTokens, min(w0 - Sh::kTokens + 32 * Sh::kSub, all), lim, h);
+            }
+            if (u < last && w0 < longest) {
+                // the next four key operands are on their way from LDS while four are used
+                const uint8_t* keys = lds.keys[u & 1];
+                v8bf kf[2][4];
+#pragma unroll
+                for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
+                    if (j < 2 * Sh::kSub) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (j > 0) {
+                        const int x = (j - 1) >> 1, k = (j - 1) & 1;
+                        if (k == 0) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
+                    }
+                }
+            }
+            __syncthreads();
+            if (u < last) {
+                if (w0 < longest) {                         // uniform
+                    if constexpr (I8) {
+#pragma unroll
+                        for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                const float4 k4 = *reinterpret_cast<const float4*>(&lds.km[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
+                                s[x][4 * b] *= k4.x;
+                                s[x][4 * b + 1] *= k4.y;
+                                s[x][4 * b + 2] *= k4.z;
+                                s[x][4 * b + 3] *= k4.w;
+                            }
+                    }
+                    if (w0 + 32 * Sh::kSub > shortest) {    // uniform
+                        const int rel = lim - w0 - 4 * h;   // tokens 32 x + 8 b + i below it are seen
+#pragma unroll
+                        for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[x][i] = 32 * x + 8 * (i >> 2) + (i & 3) < rel ? s[x][i] : -INFINITY;
+                    }
+                    float mx = s[0][0];
+#pragma unroll
+                    for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+                    mx = halves_max(mx) * zscale;
+                    const bool up = w0 < lim && (m == -INFINITY || !(mx <= m + kSlack));    // NaN: up
+                    if (__ballot(up) != 0) {                // uniform
+                        const float mn = up ? fmaxf(fmaxf(m, mx), -FLT_MAX) : m;            // finite once a token is seen
+                        const float corr = mn == m ? 1.f : exp2_hw(m - mn);
+                        m = mn;
+                        l *= corr;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[d] *= corr;
+                    }
+                    const float m0 = m == -INFINITY ? 0.f : m;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int x = 0; x < Sh::kSub; ++x) {
+                        float e[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            e[i] = exp2_hw(fmaf(s[x][i], zscale, -m0));
+                            sum += e[i];
+                        }
+                        if constexpr (I8) {
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                const float4 v4 = *reinterpret_cast<const float4*>(&lds.vm[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
+                                e[4 * b] *= v4.x;
+                                e[4 * b + 1] *= v4.y;
+                                e[4 * b + 2] *= v4.z;
+                                e[4 * b + 3] *= v4.w;
+                            }
+                        }
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+                            p[2 * x + y] = __builtin_bit_cast(v8bf, make_uint4(pack_bf16(e[8 * y], e[8 * y + 1]), pack_bf16(e[8 * y + 2], e[8 * y + 3]),
+                                                                               pack_bf16(e[8 * y + 4], e[8 * y + 5]), pack_bf16(e[8 * y + 6], e[8 * y + 7])));
+                    }
+                    l += sum;
+                }
+                stage(u + 1 + team);
+            }
+            __syncthreads();
+        }
+        if (team == 0) __syncthreads();
+    }
+
+    // token groups joined in LDS, then one partial row per query row
+    l = halves_sum(l);
+    const size_t out0 = ((size_t)(kvh * a.tiles + tile) * a.S + run) * Sh::kRows;
+    if constexpr (Sh::kTokenGroups > 1) {
+        if (h == 0) {
+            lds.m[wave][n] = m;
+            lds.l[wave][n] = l;
+        }
+        __syncthreads();
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int x = 0; x < Sh::kTokenGroups; ++x) M = fmaxf(M, lds.m[x * RW + rg][n]);
+#pragma unroll
+        for (int x = 0; x < Sh::kTokenGroups; ++x) {
+            const float mx = lds.m[x * RW + rg][n];
+            if (mx != -INFINITY) L = fmaf(exp2_hw(mx - M), lds.l[x * RW + rg][n], L);
+        }
+        const float f = m == -INFINITY ? 0.f : exp2_hw(m - M);
+#pragma unroll
+        for (int x = Sh::kTokenGroups - 1; x >= 0; --x) {
+            if (tg == x) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        float4* at = reinterpret_cast<float4*>(&lds.join[32 * rg + n][32 * d + 8 * b + 4 * h]);
+                        float4 y = make_float4(o[d][4 * b] * f, o[d][4 * b + 1] * f, o[d][4 * b + 2] * f, o[d][4 * b + 3] * f);
+                        if (x < Sh::kTokenGroups - 1) {
+                            const float4 z = *at;
+                            y = make_float4(y.x + z.x, y.y + z.y, y.z + z.z, y.w + z.w);
+                        }
+                        *at = y;
+                    }
+            }
+            __syncthreads();
+        }
+        const int count = min(Sh::kRows, rows - tile * Sh::kRows);
+        for (int i = tid; i < count * (kD / 4); i += kPThreads)
+            *reinterpret_cast<float4*>(a.part_acc + (out0 + (i >> 5)) * kD + 4 * (i & 31)) =
+                *reinterpret_cast<const float4*>(&lds.join[i >> 5][4 * (i & 31)]);
+        if (tg == 0 && h == 0 && live) {
+            a.part_m[out0 + 32 * rg + n] = M * 0.69314718055994531f;
+            a.part_l[out0 + 32 * rg + n] = L;
+        }
+    } else {
+        if (live) {
+            const size_t row = out0 + 32 * rg + n;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    *reinterpret_cast<float4*>(a.part_acc + row * kD + 32 * d + 8 * b + 4 * h) =
+                        make_float4(o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]);
+            if (h == 0) {
+                a.part_m[row] = m * 0.69314718055994531f;
+                a.part_l[row] = l;
+            }
+        }
+    }
+}
+
+template __global__ void prefix_tile_kernel<2, false>(PrefixArgs);
+template __global__ void prefix_tile_kernel<4, false>(PrefixArgs);
+template __global__ void prefix_tile_kernel<8, false>(PrefixArgs);
+template __global__ void prefix_tile_kernel<2, true>(PrefixArgs);
+template __global__ void prefix_tile_kernel<4, true>(PrefixArgs);
+template __global__ void prefix_tile_kernel<8, true>(PrefixArgs);
+
+}  // namespace ffd

@@ -79,14 +79,17 @@ def test_parts_of_the_prefix(bits, prefix_lens, lens):
     check_attention(got, _reference(q, prefix, clamped, cache, own), Pcap + 128, P_BF16)
 
 
-def test_infinities_and_nan_reach_only_the_rows_that_see_them():
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("copies", [1, 9])
+def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies):
     """Keys and values of prefix tokens that some sequences use and others do not, within one tile of tokens and in
-    tiles of their own."""
+    tiles of their own; from 5 to 360 query rows."""
     from paper_2609_00097_amd import ffd
     gen = _gen(5)
-    prefix_lens, lens = [40, 44, 60, 200, 300], [3, 0, 10, 0, 1]
-    q = _normal(gen, 5, 4, D)
-    prefix, cache = random_cache(gen, 1, 1, 320, 16), random_cache(gen, 5, 1, 64, 16)
+    prefix_lens, lens = [40, 44, 60, 200, 300] * copies, [3, 0, 10, 0, 1] * copies
+    B = len(lens)
+    q = _normal(gen, B, G, D)
+    prefix, cache = random_cache(gen, 1, 1, 320, 16), random_cache(gen, B, 1, 64, 16)
     clean = _reference(q, prefix, prefix_lens, cache, lens)
     prefix[1][0, 0, 42, 9] = math.inf
     prefix[1][0, 0, 50, 17] = math.nan
@@ -94,14 +97,34 @@ def test_infinities_and_nan_reach_only_the_rows_that_see_them():
     prefix[1][0, 0, 299, 100] = -math.inf
     out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
     torch.cuda.synchronize()
-    want = torch.zeros(5, 4, D, dtype=torch.bool)
-    want[1:, :, 9] = want[2:, :, 17] = True
-    want[4] = True
+    used = torch.tensor(prefix_lens)
+    want = torch.zeros(B, G, D, dtype=torch.bool)
+    want[used > 42, :, 9] = True
+    want[used > 50, :, 17] = True
+    want[used > 299] = True
     assert torch.equal(~out.isfinite().cpu(), want)
-    assert bool((out[1:4, :, 9] == math.inf).all()) and out[2:, :, 17].isnan().all()
-    o, ref = out.cpu().clone(), clean[0]
-    o[want] = ref[want].bfloat16()
-    check_attention((o[:4], lse[:4]), tuple(t[:4] for t in clean), 310, P_BF16)
+    mid = (used > 42) & (used <= 299)
+    assert bool((out.cpu()[mid][:, :, 9] == math.inf).all()) and out.cpu()[used > 50][:, :, 17].isnan().all()
+    o, fine = out.cpu().clone(), used <= 299
+    o[want] = clean[0][want].bfloat16()
+    check_attention((o[fine], lse.cpu()[fine]), tuple(t[fine] for t in clean), 310, P_BF16)
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G):
+    from paper_2609_00097_amd import ffd
+    gen = _gen(6)
+    prefix_lens, lens = [40, 44, 60, 200, 300] * 5, [3, 0, 10, 0, 1] * 5
+    q = _normal(gen, 25, G, D)
+    prefix, cache = random_cache(gen, 1, 1, 320), random_cache(gen, 25, 1, 64)
+    clean = _reference(q, prefix, prefix_lens, cache, lens)
+    prefix[3][0, 0, 42] = math.nan                        # a value
+    prefix[1][0, 0, 250] = math.nan                       # a key
+    out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+    torch.cuda.synchronize()
+    fine = torch.tensor(prefix_lens) <= 42
+    assert out.cpu()[~fine].isnan().all()
+    check_attention((out.cpu()[fine], lse.cpu()[fine]), tuple(t[fine] for t in clean), 310, P_BF16)
 
 
 def test_splits_scale_and_given_outputs():
