@@ -230,7 +230,9 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
     if (t0 >= end) return;
     KeyTile<I8> kt;
     ValueTile<I8> vt;
-    wait_loads();
+    // The queries are waited for here (vmcnt(0)): first used inside the loop, they would be waited for there, together
+    // with the loads that the loop has just issued.
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     kt.load(kv, t0, rows - 1 - t0, n, g);
     vt.load(kv, t0, rows - 1 - t0, n, g);
     while (true) {
@@ -389,15 +391,11 @@ __device__ __forceinline__ void joined_ml(const JoinLds<CT>& lds, int row, float
     m = M * 0.69314718055994531f;
 }
 
-// Query row `row` (or zeros) as the second operand of S^T.
+// A query row as the second operand of S^T. (Rows that no query has repeat one; nothing reads their results.)
 template <bool I8>
-__device__ __forceinline__ void load_query(v8bf (&q)[4], const uint16_t* row, bool live, int g) {
+__device__ __forceinline__ void load_query(v8bf (&q)[4], const uint16_t* row, int g) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live) w = *reinterpret_cast<const uint4*>(row + key_dim<I8>(s, g));
-        q[s] = __builtin_bit_cast(v8bf, w);
-    }
+    for (int s = 0; s < 4; ++s) q[s] = __builtin_bit_cast(v8bf, *reinterpret_cast<const uint4*>(row + key_dim<I8>(s, g)));
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -411,9 +409,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
     const bool balanced = a.table != nullptr;
-    int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, jb = 0, je = 0;
+    int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, L = 0, jb = 0, je = 0;
     if (balanced) {
-        if (!balanced_share(a, blockIdx.x, lane, b, kvh, jb, je)) return;
+        if (!balanced_share(a, blockIdx.x, lane, b, kvh, L, jb, je)) return;
         b = __builtin_amdgcn_readfirstlane(b);
         kvh = __builtin_amdgcn_readfirstlane(kvh);
         jb = __builtin_amdgcn_readfirstlane(jb);
@@ -421,8 +419,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
     }
     const int G = a.G, hq0 = kvh * G;
     const size_t bh = (size_t)b * a.Hkv + kvh;
-    const int L = min(max(a.seq_lens[b], 0), a.Lcap);
     if (!balanced) {
+        L = min(max(a.seq_lens[b], 0), a.Lcap);
         const int nblk = (L + kBlock - 1) / kBlock, bps = (nblk + a.S - 1) / a.S;
         jb = min(s * bps, nblk);
         je = min(jb + bps, nblk);
@@ -430,7 +428,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
     const size_t row0 = bh * (size_t)a.Lcap;
     const KvSource kv{a.kv.k + row0 * kD, a.kv.v + row0 * kD, a.kv.k_absmax + row0, a.kv.v_absmax + row0};
     v8bf q[1][4];
-    load_query<true>(q[0], a.q + ((size_t)b * a.Hq + hq0 + (n & 7)) * kD, (n & 7) < G, g);
+    load_query<true>(q[0], a.q + ((size_t)b * a.Hq + hq0 + min(n & 7, G - 1)) * kD, g);
     RowState<1> st;
     st.clear();
     const int lim[1] = {L};
@@ -463,16 +461,21 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a) {
     if (pair >= a.Hkv * a.S) return;
     const int kvh = pair / a.S, run = pair % a.S;
     const int rows = a.B * a.G;
+    const int gs = __builtin_ctz(a.G);
     v8bf q[CT][4];
-    int lim[CT], longest = 0, shortest = INT32_MAX;
+    int len[CT], lim[CT], longest = 0, shortest = INT32_MAX;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {                      // queries and lengths, asked for together
+        const int r = (tile * CT + c) * 16 + n, b = min(r >> gs, a.B - 1);
+        load_query<I8>(q[c], a.q + ((size_t)b * a.Hq + kvh * a.G + (r & (a.G - 1))) * kD, g);
+        len[c] = a.prefix_lens[b];
+    }
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int r = (tile * CT + c) * 16 + n, b = r / a.G;
-        const bool live = r < rows;
-        lim[c] = live ? min(max(a.prefix_lens[b], 0), a.Pcap) : INT32_MAX;
+        const bool live = (tile * CT + c) * 16 + n < rows;
+        lim[c] = live ? min(max(len[c], 0), a.Pcap) : INT32_MAX;
         longest = max(longest, live ? lim[c] : 0);
         shortest = min(shortest, lim[c]);
-        load_query<I8>(q[c], a.q + ((size_t)b * a.Hq + kvh * a.G + r % a.G) * kD, live, g);
     }
 #pragma unroll
     for (int x = 8; x; x >>= 1) {
@@ -481,9 +484,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a) {
     }
     longest = __builtin_amdgcn_readfirstlane(longest);
     shortest = __builtin_amdgcn_readfirstlane(shortest);
-    const int units = (longest + kRound - 1) / kRound;
-    const int begin = (int)((long long)units * run / a.S) * kRound;
-    const int end = min((int)((long long)units * (run + 1) / a.S) * kRound, longest);
+    // equal runs of whole rounds, the first ones one longer
+    const int units = (longest + kRound - 1) / kRound, each = units / a.S, more = units - each * a.S;
+    const int begin = (each * run + min(run, more)) * kRound;
+    const int end = min(begin + (each + (run < more)) * kRound, longest);
     const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
     const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
                       I8 ? a.kv.v_absmax + row0 : nullptr};

@@ -46,9 +46,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void dense_decode_kernel
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
     const bool balanced = a.table != nullptr;
-    int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, jb = 0, je = 0;
+    int s = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, L = 0, jb = 0, je = 0;
     if (balanced) {
-        if (!balanced_share(a, blockIdx.x, lane, b, kvh, jb, je)) return;
+        if (!balanced_share(a, blockIdx.x, lane, b, kvh, L, jb, je)) return;
         b = __builtin_amdgcn_readfirstlane(b);
         kvh = __builtin_amdgcn_readfirstlane(kvh);
         jb = __builtin_amdgcn_readfirstlane(jb);
@@ -56,9 +56,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void dense_decode_kernel
     }
     const int G = a.G, hq0 = kvh * G;
     const size_t bh = (size_t)b * a.Hkv + kvh;
-    const int L = min(max(a.seq_lens[b], 0), a.Lcap);
-    const int nblk = (L + kBlock - 1) / kBlock;
     if (!balanced) {
+        L = min(max(a.seq_lens[b], 0), a.Lcap);
+        const int nblk = (L + kBlock - 1) / kBlock;
         const int bps = (nblk + a.S - 1) / a.S;
         jb = min(s * bps, nblk);
         je = min(jb + bps, nblk);

@@ -108,10 +108,6 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Waits for this wave's memory loads. Before a loop whose body issues loads: registers loaded before it (and not yet
-// used) would otherwise be waited for inside, together with the loads just issued there.
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }     // vmcnt(0) alone
-
 // Exclusive prefix sum over the workgroup (thread order) of x; *total receives the sum. One
 // barrier: consecutive calls must alternate between the two halves of wsum[2][kWaves] (a wave
 // reaching call k + 2 has passed call k + 1's barrier, so every wave has read call k's half).

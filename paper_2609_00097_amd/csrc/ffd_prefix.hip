@@ -51,6 +51,7 @@ struct PrefixShape {
     static constexpr int kRows = 32 * RW;
     static constexpr int kBytes = kTokens * 2 * kD;                     // of a tile's keys, or values, in LDS
     static constexpr int kLoads = kTokens / 32;                         // 16-byte chunks per thread of half of them
+    static constexpr bool kPhased = RW > 2;
 };
 constexpr int kTeam = kPThreads / 2;           // threads that stage one half of a tile
 constexpr int kJoinPad = kD + 4;
@@ -214,10 +215,20 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const int kvh = pair / a.S, run = pair % a.S;
     const int rows = a.B * a.G;
 
-    // longest use of the prefix among the workgroup's rows, and this wave's longest and shortest
-    const int r = tile * Sh::kRows + 32 * rg + n;
+    // queries and lengths, asked for together
+    const int r = tile * Sh::kRows + 32 * rg + n, gs = __builtin_ctz(a.G), b = min(r >> gs, a.B - 1);
     const bool live = r < rows;
-    const int lim = live ? min(max(a.prefix_lens[r / a.G], 0), a.Pcap) : 0;
+    v4u qw[8];
+    const uint16_t* qrow = a.q + ((size_t)b * a.Hq + kvh * a.G + (r & (a.G - 1))) * kD + 8 * h;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qw[s] = *reinterpret_cast<const v4u*>(qrow + 16 * s);
+    const int len = a.prefix_lens[b];
+    if (tid < 4) lds.nonfinite[tid] = -1;
+    v8bf q[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(v8bf, live ? qw[s] : v4u{0, 0, 0, 0});
+    // longest use of the prefix among the workgroup's rows, and this wave's longest and shortest
+    const int lim = live ? min(max(len, 0), a.Pcap) : 0;
     int longest = lim, shortest = live ? lim : INT32_MAX;
 #pragma unroll
     for (int x = 16; x; x >>= 1) {
@@ -227,23 +238,14 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     longest = __builtin_amdgcn_readfirstlane(longest);
     shortest = __builtin_amdgcn_readfirstlane(shortest);
     if (lane == 0) reinterpret_cast<int*>(lds.m[wave])[0] = longest;
-    if (tid < 4) lds.nonfinite[tid] = -1;
-    v8bf q[8];
-    const uint16_t* qrow = a.q + ((size_t)(r / a.G) * a.Hq + kvh * a.G + r % a.G) * kD;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live) w = *reinterpret_cast<const uint4*>(qrow + 16 * s + 8 * h);
-        q[s] = __builtin_bit_cast(v8bf, w);
-    }
-    wait_loads();
     __syncthreads();
     int all = 0;
 #pragma unroll
     for (int w = 0; w < 8; ++w) all = max(all, reinterpret_cast<const int*>(lds.m[w])[0]);
     all = __builtin_amdgcn_readfirstlane(all);
-    const int units = (all + Sh::kTokens - 1) / Sh::kTokens;
-    const int first = (int)((long long)units * run / a.S), last = (int)((long long)units * (run + 1) / a.S);
+    // equal runs of whole tiles, the first ones one longer
+    const int units = (all + Sh::kTokens - 1) / Sh::kTokens, each = units / a.S, more = units - each * a.S;
+    const int first = each * run + min(run, more), last = first + each + (run < more);
 
     const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
     const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
@@ -263,143 +265,171 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const int v_row = 4 * h + (i16 >> 2), v_c = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
     const uint32_t v_at = (wave_row + v_row) * (2 * kD) + 16 * value_chunk(v_row, v_c) + 8 * (i16 & 1);
 
+    v16f s[Sh::kSub];
+    v8bf p[2 * Sh::kSub];
+    auto first_token = [&](int u) { return u * Sh::kTokens + wave_row; };
+
+    // s = K Q^T of tile u; the next four key operands are on their way from LDS while four are used.
+    auto scores = [&](int u) {
+        if (first_token(u) >= longest) return;          // uniform, here and below
+        const uint8_t* keys = lds.keys[u & 1];
+        v8bf kf[2][4];
+#pragma unroll
+        for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
+            if (j < 2 * Sh::kSub) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (j > 0) {
+                const int x = (j - 1) >> 1, k = (j - 1) & 1;
+                if (k == 0) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
+            }
+        }
+    };
+
+    // p = the probabilities of tile u against the maximum m, which follows the running one; their sum into l.
+    auto softmax = [&](int u) {
+        const int w0 = first_token(u);
+        if (w0 >= longest) return;
+        if constexpr (I8) {
+#pragma unroll
+            for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const v4f k4 = *reinterpret_cast<const v4f*>(&lds.km[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[x][4 * b + i] *= k4[i];
+                }
+        }
+        if (w0 + 32 * Sh::kSub > shortest) {
+            const int rel = lim - w0 - 4 * h;           // tokens 32 x + 8 b + i below it are seen
+#pragma unroll
+            for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[x][i] = 32 * x + 8 * (i >> 2) + (i & 3) < rel ? s[x][i] : -INFINITY;
+        }
+        float mx[4];                                    // four chains, as for the sum below
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = s[0][i];
+#pragma unroll
+        for (int x = 0; x < Sh::kSub; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[x][i]);
+        const float top = halves_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * zscale;
+        const bool up = w0 < lim && (m == -INFINITY || !(top <= m + kSlack));           // NaN: up
+        if (__ballot(up) != 0) {
+            const float mn = up ? fmaxf(fmaxf(m, top), -FLT_MAX) : m;                   // finite once a token is seen
+            const float corr = mn == m ? 1.f : exp2_hw(m - mn);
+            m = mn;
+            l *= corr;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[d] *= corr;
+        }
+        const float m0 = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < Sh::kSub; ++x) {
+            float e[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                e[i] = exp2_hw(fmaf(s[x][i], zscale, -m0));
+                sum[i & 3] += e[i];
+            }
+            if constexpr (I8) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const v4f v4 = *reinterpret_cast<const v4f*>(&lds.vm[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[4 * b + i] *= v4[i];
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{pack_bf16(e[8 * y], e[8 * y + 1]), pack_bf16(e[8 * y + 2], e[8 * y + 3]),
+                                                            pack_bf16(e[8 * y + 4], e[8 * y + 5]), pack_bf16(e[8 * y + 6], e[8 * y + 7])});
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+
+    // o += V^T P^T of tile u.
+    auto products = [&](int u) {
+        const int w0 = first_token(u);
+        if (w0 >= longest) return;
+        const uint8_t* values = lds.values[u & 1];
+#pragma unroll
+        for (int y = 0; y < 2 * Sh::kSub; ++y)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                v4s v[2];
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
+                        values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
+                const v8s f = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
+            }
+        if (lds.nonfinite[u & 3] == u) add_nonfinite<I8>(o, kv, w0, min(w0 + 32 * Sh::kSub, all), lim, h);
+    };
+
+    // Staging. Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for
+    // one tile's registers would fall on the next one's loads.
     const int team = wave >> 2, id = tid & (kTeam - 1);
     Staged<RW, I8> st;
-    // Stores this team's half of the keys of tile u and the values of tile u - 1, and asks for those after them.
-    // Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for one tile's
-    // registers would fall on the next one's loads.
     auto last_row = [&](int u) { return all - 1 - u * Sh::kTokens; };
-    auto stage = [&](int u) {
-        st.store_keys(lds, u, last_row(min(u, last - 1)), team, id);
-        st.store_values(lds, u - 1, team, id);
-        const int k = min(u + 1, last - 1), v = min(u, last - 1);
-        st.load_keys(kv, k * Sh::kTokens, last_row(k), team, id);
-        st.load_values(kv, v * Sh::kTokens, last_row(v), team, id);
-    };
+    auto load_keys = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_keys(kv, u * Sh::kTokens, last_row(u), team, id); };
+    auto load_values = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_values(kv, u * Sh::kTokens, last_row(u), team, id); };
     if (first < last) {
-        const int second = min(first + 1, last - 1);
-        st.load_keys(kv, first * Sh::kTokens, last_row(first), team, id);
-        st.store_keys(lds, first, last_row(first), team, id);
-        st.load_keys(kv, second * Sh::kTokens, last_row(second), team, id);
-        st.load_values(kv, first * Sh::kTokens, last_row(first), team, id);
-        __syncthreads();
-        if (team == 1) {
-            stage(first + 1);
+        Staged<RW, I8> head;
+        load_keys(head, first);
+        load_values(st, first);
+        load_keys(st, first + 1);
+        head.store_keys(lds, first, last_row(first), team, id);
+        if constexpr (Sh::kPhased) {
+            // this team's half of the keys of tile u and the values of u - 1 to LDS; those after them are asked for
+            auto stage = [&](int u) {
+                st.store_keys(lds, u, last_row(min(u, last - 1)), team, id);
+                st.store_values(lds, u - 1, team, id);
+                load_keys(st, u + 1);
+                load_values(st, u);
+            };
             __syncthreads();
-        }
-        v16f s[Sh::kSub];
-        v8bf p[2 * Sh::kSub];
-        for (int u = first; u <= last; ++u) {
-            const int w0 = u * Sh::kTokens + wave_row;      // this wave's first token
-            if (u > first && w0 - Sh::kTokens < longest) {  // uniform
-                const uint8_t* values = lds.values[(u - 1) & 1];
-#pragma unroll
-                for (int y = 0; y < 2 * Sh::kSub; ++y)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        v4s v[2];
-#pragma unroll
-                        for (int z = 0; z < 2; ++z)
-                            v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
-                                values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
-                        const v8s f = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
-                    }
-                if (lds.nonfinite[(u - 1) & 3] == u - 1)
-                    add_nonfinite<I8>(o, kv, w0 - Sh::kTokens, min(w0 - Sh::kTokens + 32 * Sh::kSub, all), lim, h);
+            if (team == 1) {
+                stage(first + 1);
+                __syncthreads();
             }
-            if (u < last && w0 < longest) {
-                // the next four key operands are on their way from LDS while four are used
-                const uint8_t* keys = lds.keys[u & 1];
-                v8bf kf[2][4];
-#pragma unroll
-                for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
-                    if (j < 2 * Sh::kSub) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (j > 0) {
-                        const int x = (j - 1) >> 1, k = (j - 1) & 1;
-                        if (k == 0) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
-                    }
+            for (int u = first; u <= last; ++u) {
+                if (u > first) products(u - 1);
+                if (u < last) scores(u);
+                __syncthreads();
+                if (u < last) {
+                    softmax(u);
+                    stage(u + 1 + team);
                 }
+                __syncthreads();
             }
+            if (team == 0) __syncthreads();
+        } else {
+            st.store_values(lds, first, team, id);
+            load_values(st, first + 1);
             __syncthreads();
-            if (u < last) {
-                if (w0 < longest) {                         // uniform
-                    if constexpr (I8) {
-#pragma unroll
-                        for (int x = 0; x < Sh::kSub; ++x)
-#pragma unroll
-                            for (int b = 0; b < 4; ++b) {
-                                const float4 k4 = *reinterpret_cast<const float4*>(&lds.km[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
-                                s[x][4 * b] *= k4.x;
-                                s[x][4 * b + 1] *= k4.y;
-                                s[x][4 * b + 2] *= k4.z;
-                                s[x][4 * b + 3] *= k4.w;
-                            }
-                    }
-                    if (w0 + 32 * Sh::kSub > shortest) {    // uniform
-                        const int rel = lim - w0 - 4 * h;   // tokens 32 x + 8 b + i below it are seen
-#pragma unroll
-                        for (int x = 0; x < Sh::kSub; ++x)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) s[x][i] = 32 * x + 8 * (i >> 2) + (i & 3) < rel ? s[x][i] : -INFINITY;
-                    }
-                    float mx = s[0][0];
-#pragma unroll
-                    for (int x = 0; x < Sh::kSub; ++x)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
-                    mx = halves_max(mx) * zscale;
-                    const bool up = w0 < lim && (m == -INFINITY || !(mx <= m + kSlack));    // NaN: up
-                    if (__ballot(up) != 0) {                // uniform
-                        const float mn = up ? fmaxf(fmaxf(m, mx), -FLT_MAX) : m;            // finite once a token is seen
-                        const float corr = mn == m ? 1.f : exp2_hw(m - mn);
-                        m = mn;
-                        l *= corr;
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) o[d] *= corr;
-                    }
-                    const float m0 = m == -INFINITY ? 0.f : m;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int x = 0; x < Sh::kSub; ++x) {
-                        float e[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            e[i] = exp2_hw(fmaf(s[x][i], zscale, -m0));
-                            sum += e[i];
-                        }
-                        if constexpr (I8) {
-#pragma unroll
-                            for (int b = 0; b < 4; ++b) {
-                                const float4 v4 = *reinterpret_cast<const float4*>(&lds.vm[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
-                                e[4 * b] *= v4.x;
-                                e[4 * b + 1] *= v4.y;
-                                e[4 * b + 2] *= v4.z;
-                                e[4 * b + 3] *= v4.w;
-                            }
-                        }
-#pragma unroll
-                        for (int y = 0; y < 2; ++y)
-                            p[2 * x + y] = __builtin_bit_cast(v8bf, make_uint4(pack_bf16(e[8 * y], e[8 * y + 1]), pack_bf16(e[8 * y + 2], e[8 * y + 3]),
-                                                                               pack_bf16(e[8 * y + 4], e[8 * y + 5]), pack_bf16(e[8 * y + 6], e[8 * y + 7])));
-                    }
-                    l += sum;
-                }
-                stage(u + 1 + team);
+            for (int u = first; u < last; ++u) {
+                scores(u);
+                softmax(u);
+                products(u);
+                st.store_keys(lds, u + 1, last_row(min(u + 1, last - 1)), team, id);
+                st.store_values(lds, u + 1, team, id);
+                load_keys(st, u + 2);
+                load_values(st, u + 2);
+                __syncthreads();
             }
-            __syncthreads();
         }
-        if (team == 0) __syncthreads();
     }
 
     // token groups joined in LDS, then one partial row per query row

@@ -378,20 +378,26 @@ def empty_kv8(B: int, Hkv: int, Lcap: int, device="cuda"):
                  for s in kv8_shapes(B, Hkv, Lcap))
 
 
-def _need_on(device, t, name, dtype, shape):
+def _need_on(device, t, name, dtype, shape, part=""):
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == device >= 0
+            and t.is_contiguous()):
+        return                                           # the usual tensor, cheaply; see _need
+    name += part
     _need(t, name, dtype, shape)
     if t.get_device() != device:
         raise ValueError(f"{name} must be on cuda:{device}, got {t.device}")
 
 
-def _launch(fn, device, *args):
-    """The library call on this device: its launches go to the current one."""
+def _launch(name, fn, device, *args):
+    """The library call ``fn`` on this device (its launches go to the current one) and on its current stream."""
+    stream = _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
     if torch._C._cuda_getDevice() == device:
-        st = getattr(lib(), fn)(*args)
+        st = fn(*args, stream)
     else:
         with torch.cuda.device(device):
-            st = getattr(lib(), fn)(*args)
-    _check(fn, st)
+            st = fn(*args, stream)
+    if st != 0:
+        _check(name, st)
 
 
 def _cache_dims(cache, name, bf16=False):
@@ -403,36 +409,40 @@ def _cache_dims(cache, name, bf16=False):
     return tuple(cache[0].shape[:3])
 
 
-def _kv_cache(cache, name, device, B, Hkv, Lcap):
-    """``ffd_kv`` of a cache whose tensors are as they have to be."""
-    rows = (B, Hkv, Lcap, HEAD_DIM)
+def _kv_cache(cache, name, device, rows):
+    """``ffd_kv`` of a cache whose tensors are as they have to be; rows = [B, Hkv, Lcap, 128]."""
     if len(cache) == 2:
         k, v = cache
-        _need_on(device, k, f"{name} k", torch.bfloat16, rows)
-        _need_on(device, v, f"{name} v", torch.bfloat16, rows)
+        _need_on(device, k, name, torch.bfloat16, rows, " k")
+        _need_on(device, v, name, torch.bfloat16, rows, " v")
         return KvCache(k.data_ptr(), None, v.data_ptr(), None)
     k, k_absmax, v, v_absmax = cache
-    _need_on(device, k, f"{name} k_codes", torch.int8, rows)
-    _need_on(device, k_absmax, f"{name} k_absmax", torch.bfloat16, rows[:3])
-    _need_on(device, v, f"{name} v_codes", torch.int8, rows)
-    _need_on(device, v_absmax, f"{name} v_absmax", torch.bfloat16, rows[:3])
+    vectors = rows[:3]
+    _need_on(device, k, name, torch.int8, rows, " k_codes")
+    _need_on(device, k_absmax, name, torch.bfloat16, vectors, " k_absmax")
+    _need_on(device, v, name, torch.int8, rows, " v_codes")
+    _need_on(device, v_absmax, name, torch.bfloat16, vectors, " v_absmax")
     return KvCache(k.data_ptr(), k_absmax.data_ptr(), v.data_ptr(), v_absmax.data_ptr())
 
 
+_Strides = ctypes.c_int64 * 3
+
+
 def _strided(t, name, device, shape):
-    """``t`` as [B, T, Hkv, 128]: its three strides in elements. Only the dims of a vector need to be contiguous."""
+    """The three strides, in elements, of ``t`` as [B, T, Hkv, 128]. Only the dims of a vector need to be contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != torch.bfloat16 or t.get_device() != device:
         raise ValueError(f"{name} must be torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-    if t.stride(-1) != 1:
+    strides = t.stride()
+    if strides[-1] != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    strides = [0 if n == 1 else s for n, s in zip(t.shape[:-1], t.stride()[:-1])]     # one of them is never used
-    if len(strides) == 2:
-        strides.insert(1, 0)
-    return (ctypes.c_int64 * 3)(*strides)
+    # the stride of a dimension of one is never used, and may be anything
+    if len(shape) == 3:
+        return _Strides(strides[0] if shape[0] > 1 else 0, 0, strides[1] if shape[1] > 1 else 0)
+    return _Strides(strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0, strides[2] if shape[2] > 1 else 0)
 
 
 def write_kv8(k_new, v_new, cache, start, *, counts=None):
@@ -443,16 +453,16 @@ def write_kv8(k_new, v_new, cache, start, *, counts=None):
     ``[B]``; without ``counts`` all T. Lengths are the caller's to advance."""
     B, Hkv, Lcap = _cache_dims(cache, "cache")
     device = cache[0].get_device()
-    kv = _kv_cache(cache, "cache", device, B, Hkv, Lcap)
-    one = isinstance(k_new, torch.Tensor) and k_new.dim() == 3
-    T = 1 if one or not isinstance(k_new, torch.Tensor) or k_new.dim() != 4 else k_new.shape[1]
-    shape = (B, Hkv, HEAD_DIM) if one else (B, T, Hkv, HEAD_DIM)
+    kv = _kv_cache(cache, "cache", device, (B, Hkv, Lcap, HEAD_DIM))
+    dims = k_new.dim() if isinstance(k_new, torch.Tensor) else 0
+    T = k_new.shape[1] if dims == 4 else 1
+    shape = (B, Hkv, HEAD_DIM) if dims == 3 else (B, T, Hkv, HEAD_DIM)
     k_strides, v_strides = _strided(k_new, "k_new", device, shape), _strided(v_new, "v_new", device, shape)
     _need_on(device, start, "start", torch.int32, (B,))
     if counts is not None:
         _need_on(device, counts, "counts", torch.int32, (B,))
-    _launch("ffd_write_kv8", device, _ptr(k_new), _ptr(v_new), k_strides, v_strides, ctypes.byref(kv), _ptr(start),
-            _ptr(counts), B, T, Hkv, Lcap, HEAD_DIM, _stream(start))
+    _launch("ffd_write_kv8", lib().ffd_write_kv8, device, k_new.data_ptr(), v_new.data_ptr(), k_strides, v_strides,
+            ctypes.byref(kv), start.data_ptr(), _ptr(counts), B, T, Hkv, Lcap, HEAD_DIM)
 
 
 def read_kv8(cache, t_begin: int = 0, t_end: int | None = None, *, seq_lens=None, out=None):
@@ -460,7 +470,7 @@ def read_kv8(cache, t_begin: int = 0, t_end: int | None = None, *, seq_lens=None
     with ``seq_lens`` (int32 ``[B]``) the rows of tokens at or behind a sequence's length are zeros."""
     B, Hkv, Lcap = _cache_dims(cache, "cache")
     device = cache[0].get_device()
-    kv = _kv_cache(cache, "cache", device, B, Hkv, Lcap)
+    kv = _kv_cache(cache, "cache", device, (B, Hkv, Lcap, HEAD_DIM))
     t_end = Lcap if t_end is None else t_end
     if not 0 <= t_begin <= t_end <= Lcap:
         raise ValueError(f"need 0 <= t_begin <= t_end <= {Lcap}, got {t_begin}, {t_end}")
@@ -468,12 +478,13 @@ def read_kv8(cache, t_begin: int = 0, t_end: int | None = None, *, seq_lens=None
     if seq_lens is not None:
         _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
     if out is None:
-        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache[0].device) for _ in range(2))
-    k, v = out
-    _need_on(device, k, "out k", torch.bfloat16, shape)
-    _need_on(device, v, "out v", torch.bfloat16, shape)
-    _launch("ffd_read_kv8", device, ctypes.byref(kv), _ptr(seq_lens), _ptr(k), _ptr(v), B, Hkv, Lcap, HEAD_DIM,
-            t_begin, t_end, _stream(cache[0]))
+        k, v = cache[1].new_empty(shape), cache[1].new_empty(shape)
+    else:
+        k, v = out
+        _need_on(device, k, "out k", torch.bfloat16, shape)
+        _need_on(device, v, "out v", torch.bfloat16, shape)
+    _launch("ffd_read_kv8", lib().ffd_read_kv8, device, ctypes.byref(kv), _ptr(seq_lens), k.data_ptr(), v.data_ptr(), B,
+            Hkv, Lcap, HEAD_DIM, t_begin, t_end)
     return k, v
 
 
@@ -483,8 +494,8 @@ def _dense_arguments(q, cache, name, seq_lens, return_lse, out, lse, bf16):
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError(f"q must be [B, Hq, {HEAD_DIM}]")
     Hq, device = q.shape[1], q.get_device()
-    _need(q, "q", torch.bfloat16, (B, Hq, HEAD_DIM))
-    kv = _kv_cache(cache, name, device, B, Hkv, Lcap)
+    _need_on(device, q, "q", torch.bfloat16, (B, Hq, HEAD_DIM))
+    kv = _kv_cache(cache, name, device, (B, Hkv, Lcap, HEAD_DIM))
     _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
     if out is None:
         out = torch.empty_like(q)
@@ -498,10 +509,10 @@ def _dense_arguments(q, cache, name, seq_lens, return_lse, out, lse, bf16):
 
 
 def _need_workspace(workspace, device):
-    if (not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or workspace.get_device() != device
-            or not workspace.is_contiguous()):
+    """The workspace's bytes."""
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on cuda:{device}")
-    return workspace.numel() * workspace.element_size()
+    return workspace.nbytes
 
 
 def kv8_decode_attention(q, cache, seq_lens, *, num_splits: int = 0, softmax_scale: float = 0.0,
@@ -511,9 +522,9 @@ def kv8_decode_attention(q, cache, seq_lens, *, num_splits: int = 0, softmax_sca
     device, B, Hq, Hkv, Lcap, kv, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, False)
     if workspace is None:
         workspace = new_workspace(B, Hq, Hkv, Lcap, num_splits, q.device, dense=True)
-    _launch("ffd_kv8_decode_attention", device, _ptr(q), ctypes.byref(kv), _ptr(seq_lens), B, Hq, Hkv, Lcap, HEAD_DIM,
-            num_splits, float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
-            _need_workspace(workspace, device), _stream(q))
+    _launch("ffd_kv8_decode_attention", lib().ffd_kv8_decode_attention, device, q.data_ptr(), ctypes.byref(kv),
+            seq_lens.data_ptr(), B, Hq, Hkv, Lcap, HEAD_DIM, num_splits, softmax_scale, out.data_ptr(), _ptr(lse),
+            workspace.data_ptr(), _need_workspace(workspace, device))
     return out, lse
 
 
@@ -537,13 +548,14 @@ def shared_prefix_decode_attention(q, prefix, prefix_lens, cache, seq_lens, *, n
     in bf16 or an 8-bit cache; the lengths int32 ``[B]``. Returns ``(out, lse)``."""
     device, B, Hq, Hkv, Lcap, own, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, True)
     Pcap = _cache_dims(prefix, "prefix", True)[2]
-    shared = _kv_cache(prefix, "prefix", device, 1, Hkv, Pcap)
+    shared = _kv_cache(prefix, "prefix", device, (1, Hkv, Pcap, HEAD_DIM))
     _need_on(device, prefix_lens, "prefix_lens", torch.int32, (B,))
     if workspace is None:
         workspace = new_shared_prefix_workspace(B, Hq, Hkv, Pcap, Lcap, num_splits, q.device)
-    _launch("ffd_shared_prefix_decode_attention", device, _ptr(q), ctypes.byref(shared), _ptr(prefix_lens), Pcap,
-            ctypes.byref(own), _ptr(seq_lens), B, Hq, Hkv, Lcap, HEAD_DIM, num_splits, float(softmax_scale), _ptr(out),
-            _ptr(lse), _ptr(workspace), _need_workspace(workspace, device), _stream(q))
+    _launch("ffd_shared_prefix_decode_attention", lib().ffd_shared_prefix_decode_attention, device, q.data_ptr(),
+            ctypes.byref(shared), prefix_lens.data_ptr(), Pcap, ctypes.byref(own), seq_lens.data_ptr(), B, Hq, Hkv, Lcap,
+            HEAD_DIM, num_splits, softmax_scale, out.data_ptr(), _ptr(lse), workspace.data_ptr(),
+            _need_workspace(workspace, device))
     return out, lse
 
 
