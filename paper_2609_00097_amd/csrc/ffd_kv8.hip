@@ -78,36 +78,40 @@ __global__ __launch_bounds__(kThreads) void write_kv8_kernel(WriteKv8Args a) {
 }
 
 // A workgroup reads back kReadTokens tokens of one (sequence, KV head), keys and values, 16 lanes a token: 8 codes
-// in, 16 bytes out each, so that every access of a wave is whole rows.
+// in, 16 bytes out each, so that every access of a wave is whole rows. All of a thread's loads are asked for first;
+// tokens behind the last one repeat it and are not stored.
 __global__ __launch_bounds__(kThreads) void read_kv8_kernel(ReadKv8Args a) {
-    const int l16 = threadIdx.x & 15;
+    constexpr int kSteps = kReadTokens / 16;
+    const int l16 = threadIdx.x & 15, n = a.t_end - a.t_begin;
     const size_t bh = (size_t)blockIdx.z * a.Hkv + blockIdx.y;
     const int len = a.seq_lens ? min(max(a.seq_lens[blockIdx.z], 0), a.Lcap) : a.Lcap;
-    const int n = a.t_end - a.t_begin;
+    const int i0 = blockIdx.x * kReadTokens + (threadIdx.x >> 4);
+    uint2 c[2][kSteps];
+    uint16_t m[2][kSteps];
 #pragma unroll
-    for (int u = 0; u < kReadTokens / 16; ++u) {
-        const int i = blockIdx.x * kReadTokens + 16 * u + (threadIdx.x >> 4);
-        if (i >= n) return;
-        const int t = a.t_begin + i;
+    for (int u = 0; u < kSteps; ++u) {
+        const size_t row = bh * a.Lcap + a.t_begin + min(i0 + 16 * u, n - 1);
+        c[0][u] = reinterpret_cast<const uint2*>(a.k_codes)[row * 16 + l16];
+        c[1][u] = reinterpret_cast<const uint2*>(a.v_codes)[row * 16 + l16];
+        m[0][u] = a.k_absmax[row];
+        m[1][u] = a.v_absmax[row];
+    }
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        const int i = i0 + 16 * u;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const int8_t* codes = which ? a.v_codes : a.k_codes;
-            const uint16_t* absmax = which ? a.v_absmax : a.k_absmax;
-            uint16_t* dst = which ? a.v : a.k;
-            uint32_t o[4] = {0, 0, 0, 0};
-            if (t < len) {
-                const size_t row = bh * a.Lcap + t;
-                const uint2 c = reinterpret_cast<const uint2*>(codes)[row * 16 + l16];
-                const float m = bf16_to_f32(absmax[row]);
-                const uint32_t w[2] = {c.x, c.y};
+            const uint32_t w[2] = {c[which][u].x, c[which][u].y};
+            const float M = bf16_to_f32(m[which][u]);
+            uint32_t o[4];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float x0 = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3))) * (1.f / 127.f) * m;
-                    const float x1 = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3) + 8)) * (1.f / 127.f) * m;
-                    o[e >> 1] = pack_bf16(x0, x1);
-                }
+            for (int e = 0; e < 8; e += 2) {
+                const float x0 = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3))) * (1.f / 127.f) * M;
+                const float x1 = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3) + 8)) * (1.f / 127.f) * M;
+                o[e >> 1] = a.t_begin + i < len ? pack_bf16(x0, x1) : 0u;
             }
-            reinterpret_cast<uint4*>(dst)[(bh * n + i) * 16 + l16] = make_uint4(o[0], o[1], o[2], o[3]);
+            uint16_t* dst = which ? a.v : a.k;
+            if (i < n) reinterpret_cast<uint4*>(dst)[(bh * n + i) * 16 + l16] = make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
 }
