@@ -431,19 +431,11 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {
     return o;
 }
 
-void launch_dense(const OwnPartials& o, const uint16_t* q, const void* k, const void* v, const int32_t* seq_lens, int B,
-                  int Hq, int Hkv, int Lcap, int S, float scale, hipStream_t stream) {
-    const int G = Hq / Hkv;
-    DenseArgs a{q, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), seq_lens, o.p.m, o.p.l, o.p.acc,
-                o.table, B, Hq, Hkv, Lcap, G, S, scale};
-    if (G <= 4) hipLaunchKernelGGL(dense_decode_kernel<1>, o.grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL(dense_decode_kernel<2>, o.grid, dim3(kThreads), 0, stream, a);
-}
-
-void launch_kv8(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const int32_t* seq_lens, int B, int Hq, int Hkv,
+void launch_own(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const int32_t* seq_lens, int B, int Hq, int Hkv,
                 int Lcap, int S, float scale, hipStream_t stream) {
-    Kv8Args a{q, source_of(kv), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, Hq / Hkv, S, scale};
-    hipLaunchKernelGGL(kv8_decode_kernel, o.grid, dim3(kThreads), 0, stream, a);
+    OwnArgs a{q, source_of(kv), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, Hq / Hkv, S, scale};
+    if (kv.k_absmax) hipLaunchKernelGGL(own_decode_kernel<true>, o.grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(own_decode_kernel<false>, o.grid, dim3(kThreads), 0, stream, a);
 }
 
 // Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head (a prefix is then
@@ -742,10 +734,14 @@ int ffd_dense_decode_attention(const void* q, const void* k, const void* v, cons
         return FFD_ERR_WORKSPACE_TOO_SMALL;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
-    launch_dense(o, static_cast<const uint16_t*>(q), k, v, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    const int G = Hq / Hkv;
+    DenseArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), seq_lens,
+                o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, S, scale};
+    if (G <= 4) hipLaunchKernelGGL(dense_decode_kernel<1>, o.grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(dense_decode_kernel<2>, o.grid, dim3(kThreads), 0, stream, a);
     st = launch_status();
     if (st != FFD_OK) return st;
-    launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
+    launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? G : 1, static_cast<uint16_t*>(out), lse);
     return launch_status();
 }
 
@@ -808,7 +804,7 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
     if (workspace_bytes < ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
-    launch_kv8(o, static_cast<const uint16_t*>(q), *cache, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    launch_own(o, static_cast<const uint16_t*>(q), *cache, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     if ((st = launch_status()) != FFD_OK) return st;
     launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
     return launch_status();
@@ -846,8 +842,7 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, grid, stream, a);
     else launch_prefix<false>(plan.tile_rows, grid, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
-    if (own_bits == 8) launch_kv8(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
-    else launch_dense(o, qp, own->k, own->v, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    launch_own(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     if ((st = launch_status()) != FFD_OK) return st;
     const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, static_cast<uint16_t*>(out), lse,
                             Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};

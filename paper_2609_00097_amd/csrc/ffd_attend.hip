@@ -1,4 +1,4 @@
-// Attention of many query rows over one cache for gfx950: decode over an 8-bit cache (kv8_decode_kernel) and the
+// Attention of many query rows over one cache for gfx950: decode over an 8-bit cache (own_decode_kernel) and the
 // attention of a whole batch over its shared prefix (prefix_kernel, bf16 or 8-bit).
 //
 // Mathematics. z_t = scale q . k_t, out = sum_t e^(z_t - m) v_t / sum_t e^(z_t - m) with the running maximum m of an
@@ -402,9 +402,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 }  // namespace
 
-// Decode over an 8-bit cache: a workgroup per run of blocks of a (sequence, KV head), as in dense_decode_kernel. The
+// Decode over an 8-bit (I8) or bf16 cache: a workgroup per run of blocks of a (sequence, KV head), as in dense_decode_kernel. The
 // group's G <= 8 queries are rows 0 .. G - 1 and, for the low halves of the probabilities, 8 .. 8 + G - 1.
-__global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
+template <bool I8>
+__global__ __launch_bounds__(kThreads, 2) void own_decode_kernel(OwnArgs a) {
     __shared__ JoinLds<1> lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
@@ -425,14 +426,15 @@ __global__ __launch_bounds__(kThreads, 2) void kv8_decode_kernel(Kv8Args a) {
         jb = min(s * bps, nblk);
         je = min(jb + bps, nblk);
     }
-    const size_t row0 = bh * (size_t)a.Lcap;
-    const KvSource kv{a.kv.k + row0 * kD, a.kv.v + row0 * kD, a.kv.k_absmax + row0, a.kv.v_absmax + row0};
+    const size_t row0 = bh * (size_t)a.Lcap, bytes = I8 ? kD : 2 * kD;
+    const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
+                      I8 ? a.kv.v_absmax + row0 : nullptr};
     v8bf q[1][4];
-    load_query<true>(q[0], a.q + ((size_t)b * a.Hq + hq0 + min(n & 7, G - 1)) * kD, g);
+    load_query<I8>(q[0], a.q + ((size_t)b * a.Hq + hq0 + min(n & 7, G - 1)) * kD, g);
     RowState<1> st;
     st.clear();
     const int lim[1] = {L};
-    attend<1, true, true>(st, q, kv, kBlock * jb, min(kBlock * je, L), L, lim, L, a.scale * kLog2e / 127.f, wave, n, g);
+    attend<1, I8, true>(st, q, kv, kBlock * jb, min(kBlock * je, L), L, lim, L, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
     join_waves<1>(lds, st, wave, n, g);
     const size_t out0 = balanced ? (size_t)blockIdx.x * G : ((size_t)b * a.Hq + hq0) * a.S + s;
     const size_t stride = balanced ? 1 : a.S;
@@ -511,6 +513,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a) {
     }
 }
 
+template __global__ void own_decode_kernel<false>(OwnArgs);
+template __global__ void own_decode_kernel<true>(OwnArgs);
 template __global__ void prefix_kernel<1, false>(PrefixArgs);
 template __global__ void prefix_kernel<2, false>(PrefixArgs);
 template __global__ void prefix_kernel<1, true>(PrefixArgs);

@@ -1,5 +1,5 @@
 // Workgroups of a ragged batch in proportion to its sequences' blocks, for the decode kernels over whole caches
-// (DenseArgs, Kv8Args).
+// (DenseArgs, OwnArgs).
 #pragma once
 
 #include "ffd_device.h"

@@ -179,8 +179,8 @@ struct KvSource {
     const uint16_t* v_absmax;
 };
 
-// Dense decode over an 8-bit cache: the workgroups, rows and table of DenseArgs.
-struct Kv8Args {
+// Dense decode over each sequence's own cache, bf16 or 8-bit: the workgroups, rows and table of DenseArgs.
+struct OwnArgs {
     const uint16_t* q;          // bf16 [B, Hq, 128]
     KvSource kv;                // [B, Hkv, Lcap, ..]
     const int32_t* seq_lens;
@@ -259,7 +259,7 @@ template <int BITS> __global__ void quantize_keys_kernel(QuantArgs a);
 template <int BITS> __global__ void append_kv_kernel(AppendArgs a);
 __global__ void write_kv8_kernel(WriteKv8Args a);
 __global__ void read_kv8_kernel(ReadKv8Args a);
-__global__ void kv8_decode_kernel(Kv8Args a);
+template <bool I8> __global__ void own_decode_kernel(OwnArgs a);
 // CT (1, 2): tiles of 16 query rows per workgroup; I8: an 8-bit prefix.
 template <int CT, bool I8> __global__ void prefix_kernel(PrefixArgs a);
 constexpr int kPrefixTileThreads = 512;

@@ -74,7 +74,8 @@ struct PrefixLds {
 
 // Chunk order of the two kinds of rows.
 __device__ __forceinline__ int key_chunk(int row, int c) { return c ^ (row & 15); }
-__device__ __forceinline__ int value_chunk(int row, int c) { return c ^ (((row & 3) << 2) | ((row >> 2) & 3)); }
+template <bool I8>                             // 8 bits: a store takes every second chunk of two rows, which then complement
+__device__ __forceinline__ int value_chunk(int row, int c) { return c ^ (((row & 3) << 2) | ((row >> 2) & 3)) ^ (I8 ? row & 1 : 0); }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float halves_max(float x) {
@@ -129,7 +130,7 @@ template <int RW> struct Staged<RW, false> {
                     x[i] &= lo | hi;
                 }
             }
-            *reinterpret_cast<v4u*>(&lds.values[u & 1][row * (2 * kD) + 16 * value_chunk(row, id & 15)]) = x;
+            *reinterpret_cast<v4u*>(&lds.values[u & 1][row * (2 * kD) + 16 * value_chunk<false>(row, id & 15)]) = x;
         }
     }
 };
@@ -151,7 +152,7 @@ template <int RW> struct Staged<RW, true> {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const uint2 a = expand4(w[2 * x]), b = expand4(w[2 * x + 1]);
-            const int at = keys ? key_chunk(row, c + x) : value_chunk(row, c + x);
+            const int at = keys ? key_chunk(row, c + x) : value_chunk<true>(row, c + x);
             *reinterpret_cast<v4u*>(tile + row * (2 * kD) + 16 * at) = v4u{a.x, a.y, b.x, b.y};
         }
     }
@@ -263,16 +264,41 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const uint32_t k_at = (wave_row + n) * (2 * kD) + 16 * key_chunk(n, h);
     const int i16 = lane & 15;
     const int v_row = 4 * h + (i16 >> 2), v_c = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-    const uint32_t v_at = (wave_row + v_row) * (2 * kD) + 16 * value_chunk(v_row, v_c) + 8 * (i16 & 1);
+    const uint32_t v_at = (wave_row + v_row) * (2 * kD) + 16 * value_chunk<I8>(v_row, v_c) + 8 * (i16 & 1);
 
     v16f s[Sh::kSub];
     v8bf p[2 * Sh::kSub];
     auto first_token = [&](int u) { return u * Sh::kTokens + wave_row; };
 
+    // Reads of LDS that can be under way before their use. Without phases (one tile of 32 tokens, registers to spare) a
+    // tile's scales and first value operands are asked for with its keys: read where they are used, each is another
+    // latency of LDS in the wave's chain (16 sequences on 128K in 8 bits: 80 us of kernel).
+    v4f km[Sh::kSub][4], vm[Sh::kSub][4];
+    v8s head_values[4];
+    int flag = 0;
+    auto read_scales = [&](v4f (&x)[Sh::kSub][4], const float* from) {
+#pragma unroll
+        for (int y = 0; y < Sh::kSub; ++y)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) x[y][b] = *reinterpret_cast<const v4f*>(from + wave_row + 32 * y + 8 * b + 4 * h);
+    };
+    auto value_operand = [&](const uint8_t* values, int y, int d) {
+        v4s v[2];
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+            v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
+                values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
+        return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
     // s = K Q^T of tile u; the next four key operands are on their way from LDS while four are used.
     auto scores = [&](int u) {
         if (first_token(u) >= longest) return;          // uniform, here and below
         const uint8_t* keys = lds.keys[u & 1];
+        if constexpr (!Sh::kPhased) {
+            if constexpr (I8) read_scales(km, lds.km[u & 3]);
+            flag = lds.nonfinite[u & 3];
+        }
         v8bf kf[2][4];
 #pragma unroll
         for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
@@ -292,6 +318,11 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
             }
         }
+        if constexpr (!Sh::kPhased) {
+            if constexpr (I8) read_scales(vm, lds.vm[u & 3]);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) head_values[d] = value_operand(lds.values[u & 1], 0, d);
+        }
     };
 
     // p = the probabilities of tile u against the maximum m, which follows the running one; their sum into l.
@@ -299,14 +330,11 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         const int w0 = first_token(u);
         if (w0 >= longest) return;
         if constexpr (I8) {
+            if constexpr (Sh::kPhased) read_scales(km, lds.km[u & 3]);
 #pragma unroll
             for (int x = 0; x < Sh::kSub; ++x)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const v4f k4 = *reinterpret_cast<const v4f*>(&lds.km[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[x][4 * b + i] *= k4[i];
-                }
+                for (int i = 0; i < 16; ++i) s[x][i] *= km[x][i >> 2][i & 3];
         }
         if (w0 + 32 * Sh::kSub > shortest) {
             const int rel = lim - w0 - 4 * h;           // tokens 32 x + 8 b + i below it are seen
@@ -334,6 +362,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         }
         const float m0 = m == -INFINITY ? 0.f : m;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (I8 && Sh::kPhased) read_scales(vm, lds.vm[u & 3]);
 #pragma unroll
         for (int x = 0; x < Sh::kSub; ++x) {
             float e[16];
@@ -344,11 +373,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             }
             if constexpr (I8) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const v4f v4 = *reinterpret_cast<const v4f*>(&lds.vm[u & 3][wave_row + 32 * x + 8 * b + 4 * h]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[4 * b + i] *= v4[i];
-                }
+                for (int i = 0; i < 16; ++i) e[i] *= vm[x][i >> 2][i & 3];
             }
 #pragma unroll
             for (int y = 0; y < 2; ++y)
@@ -367,15 +392,11 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         for (int y = 0; y < 2 * Sh::kSub; ++y)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                v4s v[2];
-#pragma unroll
-                for (int z = 0; z < 2; ++z)
-                    v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
-                        values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
-                const v8s f = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                const v8s f = y == 0 && !Sh::kPhased ? head_values[d] : value_operand(values, y, d);
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
             }
-        if (lds.nonfinite[u & 3] == u) add_nonfinite<I8>(o, kv, w0, min(w0 + 32 * Sh::kSub, all), lim, h);
+        if constexpr (Sh::kPhased) flag = lds.nonfinite[u & 3];
+        if (__builtin_amdgcn_readfirstlane(flag) == u) add_nonfinite<I8>(o, kv, w0, min(w0 + 32 * Sh::kSub, all), lim, h);
     };
 
     // Staging. Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for
