@@ -442,7 +442,9 @@ void launch_own(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const
 // read once), at most 256; as many runs as give each CU one workgroup (two of the small ones that fit there).
 struct PrefixPlan {
     int tile_rows, tiles, S;
+    bool sorted;                      // the order of sequences and the tiles' workgroups follow the lengths
     size_t rows;                      // partial rows in all
+    size_t table_off, places_off, own_off;      // in the workspace, behind the partial rows
 };
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
     const long long rows = (long long)B * (Hq / Hkv);
@@ -457,7 +459,11 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
         s = std::max(1LL, std::min(s, (long long)FFD_MAX_SPLITS));
     }
     p.S = (int)s;
+    p.sorted = p.tiles > 1 && B <= kPrefixSortSeqs;
     p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
+    p.table_off = round_up(partials_bytes(p.rows), kAlign);
+    p.places_off = p.table_off + round_up(p.sorted ? p.tiles * sizeof(PrefixTable) : 0, kAlign);
+    p.own_off = p.places_off + round_up(p.sorted ? B * sizeof(int) : 0, kAlign);
     return p;
 }
 
@@ -813,7 +819,7 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits) {
     const size_t own = ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits);
     if (own == 0 || B == 0 || check_pcap(Pcap) != FFD_OK || (long long)B * Hkv > (1LL << 20)) return 0;
-    return round_up(partials_bytes(prefix_plan(B, Hq, Hkv, Pcap, num_splits).rows), kAlign) + own;
+    return prefix_plan(B, Hq, Hkv, Pcap, num_splits).own_off + own;
 }
 
 int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
@@ -835,16 +841,19 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     const int G = Hq / Hkv;
     const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits);
     const Partials P = carve(workspace, plan.rows);
-    const OwnPartials o = own_partials(static_cast<uint8_t*>(workspace) + round_up(partials_bytes(plan.rows), kAlign), B, Hq, Hkv, S);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    PrefixTable* table = plan.sorted ? reinterpret_cast<PrefixTable*>(ws + plan.table_off) : nullptr;
+    int* places = plan.sorted ? reinterpret_cast<int*>(ws + plan.places_off) : nullptr;
+    const OwnPartials o = own_partials(ws + plan.own_off, B, Hq, Hkv, S);
     const uint16_t* qp = static_cast<const uint16_t*>(q);
-    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
+    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, table, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
     const dim3 grid((unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles));
     if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, grid, stream, a);
     else launch_prefix<false>(plan.tile_rows, grid, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
     launch_own(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     if ((st = launch_status()) != FFD_OK) return st;
-    const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, static_cast<uint16_t*>(out), lse,
+    const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, table, places, static_cast<uint16_t*>(out), lse,
                             Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};
     const dim3 merge_grid((unsigned)(B * Hq), kMergeSlices);
     if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, merge_grid, dim3(64), 0, stream, m);

@@ -497,7 +497,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a) {
     st.clear();
     attend<CT, I8, false>(st, q, kv, begin, end, longest, lim, shortest, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
     join_waves<CT>(lds, st, wave, n, g);
-    const size_t out0 = ((size_t)(kvh * a.tiles + tile) * a.S + run) * (16 * CT);
+    const size_t out0 = ((size_t)(kvh * a.S + run) * a.tiles + tile) * (16 * CT);
     const int live = min(16 * CT, rows - tile * 16 * CT);
     for (int i = tid; i < live * (kD / 4); i += kThreads) {
         const int r = i >> 5, d4 = i & 31;

@@ -192,9 +192,15 @@ struct OwnArgs {
     float scale;
 };
 
-// Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in tiles of R rows,
-// each tile's prefix in S runs. Partial row ((kvh * tiles + tile) * S + run) * R + row in tile. R is 16 CT of
-// prefix_kernel (up to 32 rows) or 32 RW of prefix_tile_kernel.
+// Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in `tiles` tiles of R
+// rows (16 CT of prefix_kernel, up to 32 rows; 32 RW of prefix_tile_kernel), S * tiles workgroups per KV head, workgroup
+// w of them writing R partial rows from (kvh * S * tiles + w) * R on. Without a table tile t has S equal runs, those of
+// workgroups t, t + tiles, ..; with one (prefix_tile_kernel<8>) the sequences' order and the tiles' workgroups follow
+// the lengths.
+constexpr int kPrefixSortSeqs = 256;           // most sequences that are sorted
+struct PrefixTable {
+    int first, stride, count;                  // workgroups of a tile
+};
 struct PrefixArgs {
     const uint16_t* q;          // bf16 [B, Hq, 128]
     KvSource kv;                // [Hkv, Pcap, ..]
@@ -202,6 +208,8 @@ struct PrefixArgs {
     float* part_m;
     float* part_l;
     float* part_acc;
+    PrefixTable* table;         // [tiles] or null
+    int* places;                // [B] with a table: each sequence's place among the query rows
     int B, Hq, Hkv, Pcap, G, S, tiles;
     float scale;
 };
@@ -211,6 +219,8 @@ struct SharedMergeArgs {
     const float *prefix_m, *prefix_l, *prefix_acc;
     const float *own_m, *own_l, *own_acc;
     const int2* table;          // own rows as in lse_merge_kernel
+    const PrefixTable* prefix_table;    // of PrefixArgs, or null
+    const int* places;
     uint16_t* out;
     float* lse;
     int Hq, Hkv, G, tiles, tile_rows, S_prefix, S_own;

@@ -161,17 +161,20 @@ template __global__ void lse_merge_kernel<1>(const float*, const float*, const f
 template __global__ void lse_merge_kernel<4>(const float*, const float*, const float*, int, const int2*, int, uint16_t*, float*);
 
 
-// The same over the rows of two attentions: the head's S_prefix rows of the shared prefix, tile_rows apart, and the
-// own cache's.
+// The same over the rows of two attentions: the head's rows of the shared prefix, one of each workgroup of its tile, and
+// the own cache's.
 template <int NW>
 __global__ __launch_bounds__(64 * NW) void shared_merge_kernel(SharedMergeArgs a) {
     constexpr int kRowLanes = 8 * NW;
     alignas(16) __shared__ float part[NW][8][8];
     const int tid = threadIdx.x, d4 = tid & 7, r = tid >> 3;
     const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, kvh = h / a.G;
-    const int q_row = b * a.G + h % a.G;
     const size_t x = (size_t)b * a.Hkv + kvh;
-    const size_t prefix0 = (size_t)(kvh * a.tiles + q_row / a.tile_rows) * a.S_prefix * a.tile_rows + q_row % a.tile_rows;
+    const int q_row = (a.prefix_table ? a.places[b] : b) * a.G + h % a.G, tile = q_row / a.tile_rows;
+    PrefixTable p{tile, a.tiles, a.S_prefix};
+    if (a.prefix_table) p = a.prefix_table[tile];
+    const size_t prefix0 = ((size_t)kvh * a.S_prefix * a.tiles + p.first) * a.tile_rows + q_row % a.tile_rows;
+    const size_t prefix_stride = (size_t)p.stride * a.tile_rows;
     size_t first = x * a.S_own;
     int S = a.S_own;
     if (a.table) {
@@ -184,8 +187,8 @@ __global__ __launch_bounds__(64 * NW) void shared_merge_kernel(SharedMergeArgs a
     const size_t stride = a.table ? a.G : 1;
     const int dims = blockIdx.y * kSliceDims + 4 * d4;
     State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    for (int s0 = 0; s0 < a.S_prefix; s0 += 2 * kRowLanes)
-        fold_rows<2, kRowLanes>(st, a.prefix_m, a.prefix_l, a.prefix_acc + dims, prefix0, a.tile_rows, a.S_prefix, s0 + r);
+    for (int s0 = 0; s0 < p.count; s0 += 2 * kRowLanes)
+        fold_rows<2, kRowLanes>(st, a.prefix_m, a.prefix_l, a.prefix_acc + dims, prefix0, prefix_stride, p.count, s0 + r);
     for (int s0 = 0; s0 < S; s0 += 2 * kRowLanes)
         fold_rows<2, kRowLanes>(st, a.own_m, a.own_l, a.own_acc + dims, own0, stride, S, s0 + r);
     finish<NW>(st, part, a.out, a.lse);

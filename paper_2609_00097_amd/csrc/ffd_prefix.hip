@@ -201,6 +201,64 @@ __device__ __forceinline__ void add_nonfinite(v16f (&o)[4], const KvSource& kv, 
     }
 }
 
+// Sequences that use different parts of the prefix, in order of their lengths: then the waves of a tile end together
+// and a tile is as long as its own sequences need. The tiles get workgroups by their lengths. Computed by every
+// workgroup alone; `writes`: this one leaves places and table for the merge. False, and nothing changed, where all
+// lengths are equal; else lds.vm holds the order, tile is this workgroup's (-1: none) and mine its tile's workgroups.
+template <int RW>
+__device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW>& lds, bool writes, int w, int& tile, PrefixTable& mine) {
+    static_assert(sizeof(lds.km) >= kPrefixSortSeqs * sizeof(int) && sizeof(lds.vm) >= kPrefixSortSeqs * sizeof(int));
+    const int tid = threadIdx.x;
+    int* lens = reinterpret_cast<int*>(lds.km);
+    int* order = reinterpret_cast<int*>(lds.vm);
+    auto clamped = [&](int x) { return min(max(x, 0), a.Pcap); };
+    const int len = clamped(a.prefix_lens[min(tid, a.B - 1)]), len0 = clamped(a.prefix_lens[0]);
+    if (tid < kPrefixSortSeqs) lens[tid] = tid < a.B ? len : -1;
+    const bool differ = __syncthreads_or(len != len0);
+    int place = tid;
+    if (differ) {
+        place = 0;
+        for (int j = 0; j < a.B; j += 4) {              // lens is padded with -1
+            const int4 x = *reinterpret_cast<const int4*>(lens + j);
+            place += (x.x > len) | (x.x == len & j < tid);
+            place += (x.y > len) | (x.y == len & j + 1 < tid);
+            place += (x.z > len) | (x.z == len & j + 2 < tid);
+            place += (x.w > len) | (x.w == len & j + 3 < tid);
+        }
+        if (tid < a.B) order[place] = tid;
+        __syncthreads();
+    }
+    if (writes && tid < a.B) a.places[tid] = place;
+    if (!differ) {
+        if (writes && tid < a.tiles) a.table[tid] = PrefixTable{tid, a.tiles, a.S};
+        return false;
+    }
+    // one workgroup for every tile that has tokens, the others in proportion to the tiles' units
+    const int step = PrefixShape<RW>::kRows / a.G;      // sequences per tile, the first of them the longest
+    long long all = 0;
+    int used = 0;
+    for (int t = 0; t < a.tiles; ++t) {
+        const int units = (lens[order[t * step]] + PrefixShape<RW>::kTokens - 1) / PrefixShape<RW>::kTokens;
+        all += units;
+        used += units > 0;
+    }
+    const long long spare = (long long)a.S * a.tiles - used;
+    tile = -1;
+    int first = 0;
+    for (int t = 0; t < a.tiles; ++t) {
+        const int units = (lens[order[t * step]] + PrefixShape<RW>::kTokens - 1) / PrefixShape<RW>::kTokens;
+        const int count = units > 0 ? 1 + (int)((double)(units * spare) / (double)all) : 0;
+        if (writes && tid == 0) a.table[t] = PrefixTable{first, 1, count};
+        if (w >= first && w < first + count) {
+            tile = t;
+            mine = PrefixTable{first, 1, count};
+        }
+        first += count;
+    }
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    return true;
+}
+
 }  // namespace
 
 template <int RW, bool I8>
@@ -210,20 +268,38 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, h = lane >> 5;
     const int rg = wave % RW, tg = wave / RW;
-    const int tile = (int)(blockIdx.x >> 3) % a.tiles;
+    // Workgroups of one run but different tiles read the same tokens: they are eight apart, on one XCD (consecutive
+    // workgroups go to the eight XCDs in turn).
+    const int slot = (int)(blockIdx.x >> 3) % a.tiles;
     const int pair = (int)(blockIdx.x >> 3) / a.tiles * 8 + (int)(blockIdx.x & 7);
     if (pair >= a.Hkv * a.S) return;
-    const int kvh = pair / a.S, run = pair % a.S;
-    const int rows = a.B * a.G;
+    const int kvh = pair / a.S, w = pair % a.S * a.tiles + slot;        // workgroup w of this KV head
+    const int rows = a.B * a.G, gs = __builtin_ctz(a.G);
+    PrefixTable mine{slot, a.tiles, a.S};
+    int tile = slot;
 
     // queries and lengths, asked for together
-    const int r = tile * Sh::kRows + 32 * rg + n, gs = __builtin_ctz(a.G), b = min(r >> gs, a.B - 1);
-    const bool live = r < rows;
+    int r = tile * Sh::kRows + 32 * rg + n, b = min(r >> gs, a.B - 1);
     v4u qw[8];
-    const uint16_t* qrow = a.q + ((size_t)b * a.Hq + kvh * a.G + (r & (a.G - 1))) * kD + 8 * h;
+    auto load_queries = [&]() {
+        const uint16_t* qrow = a.q + ((size_t)b * a.Hq + kvh * a.G + (r & (a.G - 1))) * kD + 8 * h;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) qw[s] = *reinterpret_cast<const v4u*>(qrow + 16 * s);
-    const int len = a.prefix_lens[b];
+        for (int s = 0; s < 8; ++s) qw[s] = *reinterpret_cast<const v4u*>(qrow + 16 * s);
+    };
+    load_queries();
+    int len = a.prefix_lens[b];
+    if constexpr (RW == 8) {
+        if (a.table && sort_by_length(a, lds, kvh == 0 && w == 0, w, tile, mine)) {
+            if (tile < 0) return;                       // lengths leave this workgroup without work
+            const int* order = reinterpret_cast<const int*>(lds.vm);
+            r = tile * Sh::kRows + 32 * rg + n;
+            b = order[min(r >> gs, a.B - 1)];
+            load_queries();
+            len = a.prefix_lens[b];
+        }
+    }
+    const int run = (w - mine.first) / mine.stride, S = mine.count;
+    const bool live = r < rows;
     if (tid < 4) lds.nonfinite[tid] = -1;
     v8bf q[8];
 #pragma unroll
@@ -245,7 +321,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     for (int w = 0; w < 8; ++w) all = max(all, reinterpret_cast<const int*>(lds.m[w])[0]);
     all = __builtin_amdgcn_readfirstlane(all);
     // equal runs of whole tiles, the first ones one longer
-    const int units = (all + Sh::kTokens - 1) / Sh::kTokens, each = units / a.S, more = units - each * a.S;
+    const int units = (all + Sh::kTokens - 1) / Sh::kTokens, each = units / S, more = units - each * S;
     const int first = each * run + min(run, more), last = first + each + (run < more);
 
     const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
@@ -455,7 +531,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
 
     // token groups joined in LDS, then one partial row per query row
     l = halves_sum(l);
-    const size_t out0 = ((size_t)(kvh * a.tiles + tile) * a.S + run) * Sh::kRows;
+    const size_t out0 = ((size_t)kvh * a.S * a.tiles + w) * Sh::kRows;
     if constexpr (Sh::kTokenGroups > 1) {
         if (h == 0) {
             lds.m[wave][n] = m;

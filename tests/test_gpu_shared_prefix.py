@@ -167,6 +167,29 @@ def test_many_sequences():
         check_attention(got, _reference(q, prefix, prefix_lens, cache, lens), P + 200, P_BF16)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("B,G,kind", [(70, 4, "equal"), (256, 2, "ragged"), (33, 8, "ragged"), (90, 8, "none"), (65, 8, "one"),
+                                      (257, 1, "one"), (256, 8, "two")])
+def test_sequences_in_several_row_tiles(B, G, kind, bits):
+    """More query rows than a tile holds: the sequences are taken in order of their lengths where these differ, and the
+    tiles get workgroups by theirs, some of them none."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B)
+    P = 1000
+    prefix_lens = {"equal": [P] * B, "none": [0] * B, "one": [P if b == B // 2 else 0 for b in range(B)],
+                   "two": [P if b % 2 else 3 for b in range(B)], "ragged": [(397 * b) % (P + 1) for b in range(B)]}[kind]
+    lens = [b % 3 for b in range(B)]
+    q = _normal(gen, B, 2 * G, D)
+    prefix, cache = random_cache(gen, 1, 2, _cap([P]), bits), random_cache(gen, B, 2, 64, bits)
+    ref = _reference(q, prefix, prefix_lens, cache, lens)
+    for splits in (0, 1, 5):
+        ws = ffd.new_shared_prefix_workspace(B, 2 * G, 2, _cap([P]), 64, splits)
+        ws.fill_(255)
+        got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), num_splits=splits, workspace=ws)
+        torch.cuda.synchronize()
+        check_attention(got, ref, P + 3, P_BF16)
+
+
 def test_equals_dense_attention_over_the_whole():
     """The same tokens as one bf16 cache per sequence through dense_decode_attention: the two round differently, each by
     a half step of bf16 and, here, of the probabilities."""
