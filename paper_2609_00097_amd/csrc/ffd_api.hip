@@ -414,21 +414,21 @@ KvSource source_of(const ffd_kv& c) {
                     static_cast<const uint16_t*>(c.k_absmax), static_cast<const uint16_t*>(c.v_absmax)};
 }
 
-// Partial states of a dense attention over whole caches, at the start of its workspace.
+// Partial states of a dense attention over whole caches: its rows, its table (null: S rows per head) and grid.
 struct OwnPartials {
     Partials p;
-    int2* table;                      // or null: S rows per head
+    int2* table;
     dim3 grid;
 };
-OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {
+size_t own_rows(int B, int Hq, int S) { return (size_t)B * Hq * (B <= kDenseBalanceMaxSeqs ? S + 1 : S); }
+OwnPartials own_partials(Partials p, void* table, int B, int Hkv, int S) {
     const bool balanced = B <= kDenseBalanceMaxSeqs;
-    OwnPartials o;
-    o.p = carve(workspace, (size_t)B * Hq * (balanced ? S + 1 : S));
-    o.table = balanced ? reinterpret_cast<int2*>(static_cast<uint8_t*>(workspace) +
-                                                 round_up(partials_bytes((size_t)B * Hq * (S + 1)), kAlign))
-                       : nullptr;
-    o.grid = balanced ? dim3((unsigned)((S + 1) * B * Hkv)) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B);
-    return o;
+    return OwnPartials{p, balanced ? static_cast<int2*>(table) : nullptr,
+                       balanced ? dim3((unsigned)((S + 1) * B * Hkv)) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B)};
+}
+OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      // as ffd_dense_workspace_bytes lays it out
+    const size_t rows = own_rows(B, Hq, S);
+    return own_partials(carve(workspace, rows), static_cast<uint8_t*>(workspace) + round_up(partials_bytes(rows), kAlign), B, Hkv, S);
 }
 
 void launch_own(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const int32_t* seq_lens, int B, int Hq, int Hkv,
@@ -443,10 +443,10 @@ void launch_own(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const
 struct PrefixPlan {
     int tile_rows, tiles, S;
     bool sorted;                      // the order of sequences and the tiles' workgroups follow the lengths
-    size_t rows;                      // partial rows in all
-    size_t table_off, places_off, own_off;      // in the workspace, behind the partial rows
+    size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
+    size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
 };
-PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_own) {
     const long long rows = (long long)B * (Hq / Hkv);
     PrefixPlan p;
     p.tile_rows = 16;
@@ -461,9 +461,10 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits) {
     p.S = (int)s;
     p.sorted = p.tiles > 1 && B <= kPrefixSortSeqs;
     p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
-    p.table_off = round_up(partials_bytes(p.rows), kAlign);
-    p.places_off = p.table_off + round_up(p.sorted ? p.tiles * sizeof(PrefixTable) : 0, kAlign);
-    p.own_off = p.places_off + round_up(p.sorted ? B * sizeof(int) : 0, kAlign);
+    p.all_rows = p.rows + own_rows(B, Hq, S_own);
+    p.places_off = round_up(partials_bytes(p.all_rows), kAlign);
+    p.own_table_off = p.places_off + round_up(p.sorted ? B * sizeof(PrefixPlace) : 0, kAlign);
+    p.total = p.own_table_off + (B <= kDenseBalanceMaxSeqs ? (size_t)B * Hkv * sizeof(int2) : 0);
     return p;
 }
 
@@ -817,9 +818,10 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
 }
 
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits) {
-    const size_t own = ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits);
-    if (own == 0 || B == 0 || check_pcap(Pcap) != FFD_OK || (long long)B * Hkv > (1LL << 20)) return 0;
-    return prefix_plan(B, Hq, Hkv, Pcap, num_splits).own_off + own;
+    if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || check_pcap(Pcap) != FFD_OK) return 0;
+    const int S = resolve_splits(B, Hkv, Lcap, num_splits, true);
+    if (S <= 0 || (long long)B * Hkv > (1LL << 20)) return 0;
+    return prefix_plan(B, Hq, Hkv, Pcap, num_splits, S).total;
 }
 
 int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
@@ -839,25 +841,24 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
         return FFD_ERR_WORKSPACE_TOO_SMALL;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const int G = Hq / Hkv;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits);
-    const Partials P = carve(workspace, plan.rows);
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
+    const Partials P = carve(workspace, plan.all_rows);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    PrefixTable* table = plan.sorted ? reinterpret_cast<PrefixTable*>(ws + plan.table_off) : nullptr;
-    int* places = plan.sorted ? reinterpret_cast<int*>(ws + plan.places_off) : nullptr;
-    const OwnPartials o = own_partials(ws + plan.own_off, B, Hq, Hkv, S);
+    PrefixPlace* places = plan.sorted ? reinterpret_cast<PrefixPlace*>(ws + plan.places_off) : nullptr;
+    const OwnPartials o = own_partials(Partials{P.m + plan.rows, P.l + plan.rows, P.acc + plan.rows * kD}, ws + plan.own_table_off, B, Hkv, S);
     const uint16_t* qp = static_cast<const uint16_t*>(q);
-    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, table, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
+    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
     const dim3 grid((unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles));
     if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, grid, stream, a);
     else launch_prefix<false>(plan.tile_rows, grid, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
     launch_own(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
     if ((st = launch_status()) != FFD_OK) return st;
-    const SharedMergeArgs m{P.m, P.l, P.acc, o.p.m, o.p.l, o.p.acc, o.table, table, places, static_cast<uint16_t*>(out), lse,
+    const SharedMergeArgs m{P.m, P.l, P.acc, plan.rows, o.table, places, static_cast<uint16_t*>(out), lse,
                             Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};
-    const dim3 merge_grid((unsigned)(B * Hq), kMergeSlices);
-    if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, merge_grid, dim3(64), 0, stream, m);
-    else hipLaunchKernelGGL(shared_merge_kernel<4>, merge_grid, dim3(256), 0, stream, m);
+    const dim3 wide((unsigned)(B * Hq)), deep((unsigned)(B * Hq), kMergeSlices);
+    if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, wide, dim3(256), 0, stream, m);
+    else hipLaunchKernelGGL(shared_merge_kernel<4>, deep, dim3(256), 0, stream, m);
     return launch_status();
 }
 

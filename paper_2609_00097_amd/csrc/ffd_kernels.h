@@ -194,12 +194,13 @@ struct OwnArgs {
 
 // Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in `tiles` tiles of R
 // rows (16 CT of prefix_kernel, up to 32 rows; 32 RW of prefix_tile_kernel), S * tiles workgroups per KV head, workgroup
-// w of them writing R partial rows from (kvh * S * tiles + w) * R on. Without a table tile t has S equal runs, those of
-// workgroups t, t + tiles, ..; with one (prefix_tile_kernel<8>) the sequences' order and the tiles' workgroups follow
+// w of them writing R partial rows from (kvh * S * tiles + w) * R on. Without `places` tile t has S equal runs, those of
+// workgroups t, t + tiles, ..; with it (prefix_tile_kernel<8>) the sequences' order and the tiles' workgroups follow
 // the lengths.
 constexpr int kPrefixSortSeqs = 256;           // most sequences that are sorted
-struct PrefixTable {
-    int first, stride, count;                  // workgroups of a tile
+struct alignas(16) PrefixPlace {
+    int first, stride, count;                  // workgroups of a sequence's tile
+    int place;                                 // the sequence's place among the query rows
 };
 struct PrefixArgs {
     const uint16_t* q;          // bf16 [B, Hq, 128]
@@ -208,19 +209,17 @@ struct PrefixArgs {
     float* part_m;
     float* part_l;
     float* part_acc;
-    PrefixTable* table;         // [tiles] or null
-    int* places;                // [B] with a table: each sequence's place among the query rows
+    PrefixPlace* places;        // [B] or null
     int B, Hq, Hkv, Pcap, G, S, tiles;
     float scale;
 };
 
 // Partial rows of the shared prefix and of the sequences' own caches, for the merge of both.
 struct SharedMergeArgs {
-    const float *prefix_m, *prefix_l, *prefix_acc;
-    const float *own_m, *own_l, *own_acc;
+    const float *m, *l, *acc;   // the prefix's rows, then the own caches' from prefix_rows on
+    size_t prefix_rows;
     const int2* table;          // own rows as in lse_merge_kernel
-    const PrefixTable* prefix_table;    // of PrefixArgs, or null
-    const int* places;
+    const PrefixPlace* places;  // of PrefixArgs, or null
     uint16_t* out;
     float* lse;
     int Hq, Hkv, G, tiles, tile_rows, S_prefix, S_own;

@@ -30,18 +30,33 @@ struct State {
 
 __device__ __forceinline__ float rescale(float m, float M) { return m == -INFINITY ? 0.f : __expf(m - M); }
 
-// Folds rows s0 + LANES u (u < U) below count into st; the row index is clamped, so that the loads are
+// Places of a head's partial rows: `count` of them, the first `split` at first + s * stride, the others at
+// rest + (s - split) * rest_stride.
+struct Rows {
+    size_t first, stride;
+    int split;
+    size_t rest, rest_stride;
+    int count;
+    __device__ __forceinline__ size_t operator()(int s) const { return s < split ? first + s * stride : rest + (s - split) * rest_stride; }
+};
+struct EvenRows {
+    size_t first, stride;
+    int count;
+    __device__ __forceinline__ size_t operator()(int s) const { return first + (size_t)s * stride; }
+};
+
+// Folds rows s0 + LANES u (u < U) below rows.count into st; the row index is clamped, so that the loads are
 // unconditional.
-template <int U, int LANES>
+template <int U, int LANES, class R>
 __device__ __forceinline__ void fold_rows(State& st, const float* __restrict__ part_m, const float* __restrict__ part_l,
-                                          const float* __restrict__ part_acc, size_t row0, size_t stride, int count,
-                                          int s0) {
+                                          const float* __restrict__ part_acc, const R& rows, int s0) {
+    const int count = rows.count;
     float m[U], l[U];
     float4 a[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int s = s0 + u * LANES;
-        const size_t row = row0 + (size_t)min(s, count - 1) * stride;
+        const size_t row = rows(min(s, count - 1));
         m[u] = part_m[row];
         l[u] = part_l[row];
         a[u] = *reinterpret_cast<const float4*>(part_acc + row * kD);
@@ -83,11 +98,11 @@ __device__ __forceinline__ float rows_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Joins the states of the workgroup's threads and writes head blockIdx.x's dims of slice blockIdx.y.
+// Joins the states of NW waves, tid a thread's number among them, and writes head blockIdx.x's dims of a slice.
 template <int NW>
-__device__ __forceinline__ void finish(State st, float (&part)[NW][8][8], uint16_t* __restrict__ out,
+__device__ __forceinline__ void finish(State st, float (&part)[NW][8][8], int tid, int slice, uint16_t* __restrict__ out,
                                        float* __restrict__ lse) {
-    const int tid = threadIdx.x, d4 = tid & 7, wave = tid >> 6, lane = tid & 63;
+    const int d4 = tid & 7, wave = tid >> 6, lane = tid & 63;
     const float M = rows_max(st.m);
     const float c = rescale(st.m, M);
     const float l = rows_sum(st.l * c);
@@ -123,8 +138,8 @@ __device__ __forceinline__ void finish(State st, float (&part)[NW][8][8], uint16
     uint2 packed;
     packed.x = (uint32_t)f32_to_bf16(o.x * inv) | ((uint32_t)f32_to_bf16(o.y * inv) << 16);
     packed.y = (uint32_t)f32_to_bf16(o.z * inv) | ((uint32_t)f32_to_bf16(o.w * inv) << 16);
-    *reinterpret_cast<uint2*>(out + (size_t)blockIdx.x * kD + blockIdx.y * kSliceDims + 4 * d4) = packed;
-    if (lse && blockIdx.y == 0 && d4 == 0) lse[blockIdx.x] = any ? Mx + logf(lx) : -INFINITY;
+    *reinterpret_cast<uint2*>(out + (size_t)blockIdx.x * kD + slice * kSliceDims + 4 * d4) = packed;
+    if (lse && slice == 0 && d4 == 0) lse[blockIdx.x] = any ? Mx + logf(lx) : -INFINITY;
 }
 
 }  // namespace
@@ -146,15 +161,15 @@ __global__ __launch_bounds__(64 * NW) void lse_merge_kernel(const float* __restr
         first = fl.x;
         S = fl.y - fl.x + 1;
     }
-    const size_t row0 = first * G + blockIdx.x % G;
+    const EvenRows rows{first * G + blockIdx.x % G, (size_t)G, S};
     const float* acc = part_acc + blockIdx.y * kSliceDims + 4 * d4;
     State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     if (S > 2 * kRowLanes) {                                // uniform
-        for (int s0 = 0; s0 < S; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, part_m, part_l, acc, row0, G, S, s0 + r);
+        for (int s0 = 0; s0 < S; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, part_m, part_l, acc, rows, s0 + r);
     } else if (S > 0) {
-        fold_rows<2, kRowLanes>(st, part_m, part_l, acc, row0, G, S, r);
+        fold_rows<2, kRowLanes>(st, part_m, part_l, acc, rows, r);
     }
-    finish<NW>(st, part, out, lse);
+    finish<NW>(st, part, tid, blockIdx.y, out, lse);
 }
 
 template __global__ void lse_merge_kernel<1>(const float*, const float*, const float*, int, const int2*, int, uint16_t*, float*);
@@ -162,36 +177,37 @@ template __global__ void lse_merge_kernel<4>(const float*, const float*, const f
 
 
 // The same over the rows of two attentions: the head's rows of the shared prefix, one of each workgroup of its tile, and
-// the own cache's.
+// the own cache's, all rows of one array. NW waves per slice as above; with one the workgroup's four waves take the four
+// slices (4096 heads of 18 rows: 14.5 us with a workgroup per slice, which is their dispatch).
 template <int NW>
-__global__ __launch_bounds__(64 * NW) void shared_merge_kernel(SharedMergeArgs a) {
+__global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
     constexpr int kRowLanes = 8 * NW;
-    alignas(16) __shared__ float part[NW][8][8];
-    const int tid = threadIdx.x, d4 = tid & 7, r = tid >> 3;
+    alignas(16) __shared__ float part[4 / NW][NW][8][8];
+    const int unit = threadIdx.x / (64 * NW), tid = threadIdx.x % (64 * NW), d4 = tid & 7, r = tid >> 3;
+    const int slice = NW == 1 ? unit : blockIdx.y;
     const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, kvh = h / a.G;
     const size_t x = (size_t)b * a.Hkv + kvh;
-    const int q_row = (a.prefix_table ? a.places[b] : b) * a.G + h % a.G, tile = q_row / a.tile_rows;
-    PrefixTable p{tile, a.tiles, a.S_prefix};
-    if (a.prefix_table) p = a.prefix_table[tile];
-    const size_t prefix0 = ((size_t)kvh * a.S_prefix * a.tiles + p.first) * a.tile_rows + q_row % a.tile_rows;
-    const size_t prefix_stride = (size_t)p.stride * a.tile_rows;
-    size_t first = x * a.S_own;
-    int S = a.S_own;
-    if (a.table) {
-        const int2 fl = a.table[x];
-        first = fl.x;
-        S = fl.y - fl.x + 1;
-    }
-    // without a table a head's rows lie side by side, with one those of a group's heads
-    const size_t own0 = a.table ? first * a.G + h % a.G : (size_t)blockIdx.x * a.S_own;
-    const size_t stride = a.table ? a.G : 1;
-    const int dims = blockIdx.y * kSliceDims + 4 * d4;
+    int2 fl = make_int2(0, -1);
+    PrefixPlace p{0, a.tiles, a.S_prefix, b};
+    if (a.table) fl = a.table[x];                           // both asked for before either is used
+    if (a.places) p = a.places[b];
+    const int q_row = p.place * a.G + h % a.G;
+    if (!a.places) p.first = q_row / a.tile_rows;
+    // own rows: without a table a head's lie side by side, with one those of a group's heads
+    const size_t own0 = a.prefix_rows + (a.table ? (size_t)fl.x * a.G + h % a.G : (size_t)blockIdx.x * a.S_own);
+    const int own = a.table ? fl.y - fl.x + 1 : a.S_own;
+    const Rows rows{((size_t)kvh * a.S_prefix * a.tiles + p.first) * a.tile_rows + q_row % a.tile_rows,
+                    (size_t)p.stride * a.tile_rows, p.count, own0, a.table ? (size_t)a.G : 1, p.count + own};
+    const float* acc = a.acc + slice * kSliceDims + 4 * d4;
     State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    for (int s0 = 0; s0 < p.count; s0 += 2 * kRowLanes)
-        fold_rows<2, kRowLanes>(st, a.prefix_m, a.prefix_l, a.prefix_acc + dims, prefix0, prefix_stride, p.count, s0 + r);
-    for (int s0 = 0; s0 < S; s0 += 2 * kRowLanes)
-        fold_rows<2, kRowLanes>(st, a.own_m, a.own_l, a.own_acc + dims, own0, stride, S, s0 + r);
-    finish<NW>(st, part, a.out, a.lse);
+    if (rows.count > 4 * kRowLanes) {                       // uniform
+        for (int s0 = 0; s0 < rows.count; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, a.m, a.l, acc, rows, s0 + r);
+    } else if (rows.count > 2 * kRowLanes) {
+        fold_rows<4, kRowLanes>(st, a.m, a.l, acc, rows, r);
+    } else if (rows.count > 0) {
+        fold_rows<2, kRowLanes>(st, a.m, a.l, acc, rows, r);
+    }
+    finish<NW>(st, part[unit], tid, slice, a.out, a.lse);
 }
 
 template __global__ void shared_merge_kernel<1>(SharedMergeArgs);

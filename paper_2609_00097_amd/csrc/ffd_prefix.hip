@@ -203,10 +203,10 @@ __device__ __forceinline__ void add_nonfinite(v16f (&o)[4], const KvSource& kv, 
 
 // Sequences that use different parts of the prefix, in order of their lengths: then the waves of a tile end together
 // and a tile is as long as its own sequences need. The tiles get workgroups by their lengths. Computed by every
-// workgroup alone; `writes`: this one leaves places and table for the merge. False, and nothing changed, where all
+// workgroup alone; `writes`: this one leaves the places for the merge. False, and nothing changed, where all
 // lengths are equal; else lds.vm holds the order, tile is this workgroup's (-1: none) and mine its tile's workgroups.
 template <int RW>
-__device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW>& lds, bool writes, int w, int& tile, PrefixTable& mine) {
+__device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW>& lds, bool writes, int w, int& tile, PrefixPlace& mine) {
     static_assert(sizeof(lds.km) >= kPrefixSortSeqs * sizeof(int) && sizeof(lds.vm) >= kPrefixSortSeqs * sizeof(int));
     const int tid = threadIdx.x;
     int* lens = reinterpret_cast<int*>(lds.km);
@@ -228,13 +228,12 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
         if (tid < a.B) order[place] = tid;
         __syncthreads();
     }
-    if (writes && tid < a.B) a.places[tid] = place;
+    const int step = PrefixShape<RW>::kRows / a.G;      // sequences per tile, the first of them the longest
     if (!differ) {
-        if (writes && tid < a.tiles) a.table[tid] = PrefixTable{tid, a.tiles, a.S};
+        if (writes && tid < a.B) a.places[tid] = PrefixPlace{tid / step, a.tiles, a.S, tid};
         return false;
     }
     // one workgroup for every tile that has tokens, the others in proportion to the tiles' units
-    const int step = PrefixShape<RW>::kRows / a.G;      // sequences per tile, the first of them the longest
     long long all = 0;
     int used = 0;
     for (int t = 0; t < a.tiles; ++t) {
@@ -248,10 +247,10 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
     for (int t = 0; t < a.tiles; ++t) {
         const int units = (lens[order[t * step]] + PrefixShape<RW>::kTokens - 1) / PrefixShape<RW>::kTokens;
         const int count = units > 0 ? 1 + (int)((double)(units * spare) / (double)all) : 0;
-        if (writes && tid == 0) a.table[t] = PrefixTable{first, 1, count};
+        if (writes && tid < a.B && place / step == t) a.places[tid] = PrefixPlace{first, 1, count, place};
         if (w >= first && w < first + count) {
             tile = t;
-            mine = PrefixTable{first, 1, count};
+            mine = PrefixPlace{first, 1, count, 0};
         }
         first += count;
     }
@@ -275,7 +274,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     if (pair >= a.Hkv * a.S) return;
     const int kvh = pair / a.S, w = pair % a.S * a.tiles + slot;        // workgroup w of this KV head
     const int rows = a.B * a.G, gs = __builtin_ctz(a.G);
-    PrefixTable mine{slot, a.tiles, a.S};
+    PrefixPlace mine{slot, a.tiles, a.S, 0};
     int tile = slot;
 
     // queries and lengths, asked for together
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     load_queries();
     int len = a.prefix_lens[b];
     if constexpr (RW == 8) {
-        if (a.table && sort_by_length(a, lds, kvh == 0 && w == 0, w, tile, mine)) {
+        if (a.places && sort_by_length(a, lds, kvh == 0 && w == 0, w, tile, mine)) {
             if (tile < 0) return;                       // lengths leave this workgroup without work
             const int* order = reinterpret_cast<const int*>(lds.vm);
             r = tile * Sh::kRows + 32 * rg + n;

@@ -111,8 +111,12 @@ def test_shared_prefix_workspace(so):
     need = size(2, 32, 8, 8192, 4096, 128, 0)
     assert need > dense and need % 4 == 0
     assert _shared(so, ws_bytes=need - 1) == 3
-    # given splits: rows rounded up to 16 times them, and the dense call's for the same splits
-    assert size(2, 32, 8, 8192, 4096, 128, 3) == 8 * 16 * 3 * 130 * 4 + so.ffd_dense_workspace_bytes(2, 32, 8, 4096, 128, 3)
+    # given splits: rows rounded up to 16 times them, and those of the dense call for the same splits
+    up = lambda x: -(-x // 256) * 256
+    assert size(2, 32, 8, 8192, 4096, 128, 3) == up((8 * 16 * 3 + 2 * 32 * (3 + 1)) * 130 * 4) + 2 * 8 * 8
+    # two tiles of 256 rows: the sequences' places
+    assert size(70, 32, 8, 8192, 4096, 128, 3) == up((8 * 2 * 256 * 3 + 70 * 32 * 4) * 130 * 4) + up(70 * 16) + 70 * 8 * 8
+    assert size(300, 32, 8, 8192, 4096, 128, 3) == up((8 * 5 * 256 * 3 + 300 * 32 * 3) * 130 * 4)
     for bad in ((0, 32, 8, 8192, 4096, 128, 0), (2, 32, 8, 100, 4096, 128, 0), (2, 32, 8, 8192, 4096, 96, 0),
                 (2, 30, 8, 8192, 4096, 128, 0), (2, 32, 8, 8192, 4096, 128, 5000)):
         assert size(*bad) == 0
