@@ -30,56 +30,57 @@ struct State {
 
 __device__ __forceinline__ float rescale(float m, float M) { return m == -INFINITY ? 0.f : __expf(m - M); }
 
-// Places of a head's partial rows: `count` of them, the first `split` at first + s * stride, the others at
-// rest + (s - split) * rest_stride.
+// Places of partial rows: `count` of them from `first` on.
 struct Rows {
     size_t first, stride;
-    int split;
-    size_t rest, rest_stride;
     int count;
-    __device__ __forceinline__ size_t operator()(int s) const { return s < split ? first + s * stride : rest + (s - split) * rest_stride; }
-};
-struct EvenRows {
-    size_t first, stride;
-    int count;
-    __device__ __forceinline__ size_t operator()(int s) const { return first + (size_t)s * stride; }
 };
 
-// Folds rows s0 + LANES u (u < U) below rows.count into st; the row index is clamped, so that the loads are
-// unconditional.
-template <int U, int LANES, class R>
-__device__ __forceinline__ void fold_rows(State& st, const float* __restrict__ part_m, const float* __restrict__ part_l,
-                                          const float* __restrict__ part_acc, const R& rows, int s0) {
-    const int count = rows.count;
+// Rows s0 + LANES u (u < U) below rows.count: loaded, and folded into a state. The row index is clamped, so that the
+// loads are unconditional.
+template <int U, int LANES>
+struct Batch {
     float m[U], l[U];
     float4 a[U];
+    __device__ __forceinline__ void load(const float* __restrict__ part_m, const float* __restrict__ part_l,
+                                         const float* __restrict__ part_acc, const Rows& rows, int s0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int s = s0 + u * LANES;
-        const size_t row = rows(min(s, count - 1));
-        m[u] = part_m[row];
-        l[u] = part_l[row];
-        a[u] = *reinterpret_cast<const float4*>(part_acc + row * kD);
-        if (s >= count) m[u] = -INFINITY;
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * LANES;
+            const size_t row = rows.first + (size_t)min(s, rows.count - 1) * rows.stride;
+            m[u] = part_m[row];
+            l[u] = part_l[row];
+            a[u] = *reinterpret_cast<const float4*>(part_acc + row * kD);
+            if (s >= rows.count) m[u] = -INFINITY;
+        }
     }
-    float M = st.m;
+    __device__ __forceinline__ void fold(State& st) const {
+        float M = st.m;
 #pragma unroll
-    for (int u = 0; u < U; ++u) M = fmaxf(M, m[u]);
-    const float c = rescale(st.m, M);
-    st.m = M;
-    st.l *= c;
+        for (int u = 0; u < U; ++u) M = fmaxf(M, m[u]);
+        const float c = rescale(st.m, M);
+        st.m = M;
+        st.l *= c;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) st.a[e] *= c;
+        for (int e = 0; e < 4; ++e) st.a[e] *= c;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const float w = rescale(m[u], M);
-        const bool any = m[u] != -INFINITY;         // else l and a may be NaN
-        st.l = fmaf(w, any ? l[u] : 0.f, st.l);
-        st.a[0] = fmaf(w, any ? a[u].x : 0.f, st.a[0]);
-        st.a[1] = fmaf(w, any ? a[u].y : 0.f, st.a[1]);
-        st.a[2] = fmaf(w, any ? a[u].z : 0.f, st.a[2]);
-        st.a[3] = fmaf(w, any ? a[u].w : 0.f, st.a[3]);
+        for (int u = 0; u < U; ++u) {
+            const float w = rescale(m[u], M);
+            const bool any = m[u] != -INFINITY;         // else l and a may be NaN
+            st.l = fmaf(w, any ? l[u] : 0.f, st.l);
+            st.a[0] = fmaf(w, any ? a[u].x : 0.f, st.a[0]);
+            st.a[1] = fmaf(w, any ? a[u].y : 0.f, st.a[1]);
+            st.a[2] = fmaf(w, any ? a[u].z : 0.f, st.a[2]);
+            st.a[3] = fmaf(w, any ? a[u].w : 0.f, st.a[3]);
+        }
     }
+};
+template <int U, int LANES>
+__device__ __forceinline__ void fold_rows(State& st, const float* __restrict__ part_m, const float* __restrict__ part_l,
+                                          const float* __restrict__ part_acc, const Rows& rows, int s0) {
+    Batch<U, LANES> x;
+    x.load(part_m, part_l, part_acc, rows, s0);
+    x.fold(st);
 }
 
 // max and sum over the lanes that differ in bits 3, 4 and 5 (the rows of a wave)
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(64 * NW) void lse_merge_kernel(const float* __restr
         first = fl.x;
         S = fl.y - fl.x + 1;
     }
-    const EvenRows rows{first * G + blockIdx.x % G, (size_t)G, S};
+    const Rows rows{first * G + blockIdx.x % G, (size_t)G, S};
     const float* acc = part_acc + blockIdx.y * kSliceDims + 4 * d4;
     State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     if (S > 2 * kRowLanes) {                                // uniform
@@ -187,26 +188,29 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
     const int slice = NW == 1 ? unit : blockIdx.y;
     const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, kvh = h / a.G;
     const size_t x = (size_t)b * a.Hkv + kvh;
+    const float* acc = a.acc + slice * kSliceDims + 4 * d4;
     int2 fl = make_int2(0, -1);
     PrefixPlace p{0, a.tiles, a.S_prefix, b};
     if (a.table) fl = a.table[x];                           // both asked for before either is used
     if (a.places) p = a.places[b];
     const int q_row = p.place * a.G + h % a.G;
     if (!a.places) p.first = q_row / a.tile_rows;
-    // own rows: without a table a head's lie side by side, with one those of a group's heads
-    const size_t own0 = a.prefix_rows + (a.table ? (size_t)fl.x * a.G + h % a.G : (size_t)blockIdx.x * a.S_own);
-    const int own = a.table ? fl.y - fl.x + 1 : a.S_own;
-    const Rows rows{((size_t)kvh * a.S_prefix * a.tiles + p.first) * a.tile_rows + q_row % a.tile_rows,
-                    (size_t)p.stride * a.tile_rows, p.count, own0, a.table ? (size_t)a.G : 1, p.count + own};
-    const float* acc = a.acc + slice * kSliceDims + 4 * d4;
+    const Rows prefix{((size_t)kvh * a.S_prefix * a.tiles + p.first) * a.tile_rows + q_row % a.tile_rows,
+                      (size_t)p.stride * a.tile_rows, p.count};
+    // the prefix's first rows under way before the own ones are located (any row where there is none: nothing is
+    // folded); those lie side by side without a table, with one with those of the group's other heads
+    constexpr int U = NW == 1 ? 4 : 2;
+    Batch<U, kRowLanes> x0;
+    Batch<1, kRowLanes> y0;
+    x0.load(a.m, a.l, acc, prefix.count > 0 ? prefix : Rows{0, 0, 1}, r);
+    const Rows own{a.prefix_rows + (a.table ? (size_t)fl.x * a.G + h % a.G : (size_t)blockIdx.x * a.S_own),
+                   a.table ? (size_t)a.G : 1, a.table ? fl.y - fl.x + 1 : a.S_own};
+    y0.load(a.m, a.l, acc, own, r);
     State st{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    if (rows.count > 4 * kRowLanes) {                       // uniform
-        for (int s0 = 0; s0 < rows.count; s0 += 8 * kRowLanes) fold_rows<8, kRowLanes>(st, a.m, a.l, acc, rows, s0 + r);
-    } else if (rows.count > 2 * kRowLanes) {
-        fold_rows<4, kRowLanes>(st, a.m, a.l, acc, rows, r);
-    } else if (rows.count > 0) {
-        fold_rows<2, kRowLanes>(st, a.m, a.l, acc, rows, r);
-    }
+    if (prefix.count > 0) x0.fold(st);                      // uniform
+    y0.fold(st);
+    for (int s0 = U * kRowLanes; s0 < prefix.count; s0 += U * kRowLanes) fold_rows<U, kRowLanes>(st, a.m, a.l, acc, prefix, s0 + r);
+    for (int s0 = kRowLanes; s0 < own.count; s0 += 2 * kRowLanes) fold_rows<2, kRowLanes>(st, a.m, a.l, acc, own, s0 + r);
     finish<NW>(st, part[unit], tid, slice, a.out, a.lse);
 }
 
