@@ -297,12 +297,19 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
 
 /*
  * Exact dense decode attention over an 8-bit cache: ffd_dense_decode_attention with k = n M / 127 and v likewise,
- * neither rounded to bf16. Arguments, splits and workspace (ffd_dense_workspace_bytes) are those of that call; the
- * cache holds B sequences. B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
+ * neither rounded to bf16. Arguments are those of that call; the cache holds B sequences, the workspace takes
+ * ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
  */
 int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
                              int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ffd_kv8_decode_attention: fp32 partials of B * Hq * (S + 1) rows (beyond 256 sequences B * Hq * S),
+ * (D + 2) * 4 bytes each, on a 256-byte boundary, then, up to 256 sequences, a table of B * Hkv * 8 bytes; S is
+ * num_splits, or automatically as of ffd_dense_decode_attention, and in batches of 64 groups or more with at least 64
+ * blocks of the capacity for each of three workgroups per compute unit up to eight workgroups per unit. 0 on invalid or
+ * unsupported input. */
+size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_splits);
 
 /*
  * Exact dense decode attention of a batch over a shared prefix and each sequence's own tokens: sequence b attends

@@ -400,6 +400,19 @@ int decode_checks(const void* q, const void* k_codes, const void* k_absmax, cons
     return FFD_OK;
 }
 
+// Splits of the attention over an 8-bit cache: the dense path's, but eight workgroups per CU where a batch of 64 groups
+// or more has 64 blocks of the capacity for each of the three per CU: the lengths of such a batch differ, and what is
+// left over when most workgroups have ended is a part of a smaller run. Three / eight per CU: 32 sequences of 1K to 32K
+// 196 / 181 us, 64 of 500 to 16K 235 / 216, 16 of 1 to 64K with eight heads per KV head 234 / 226; below the limit,
+// 32 of 8K 101 / 105 us, 64 of 100 to 2K 36 / 38.
+constexpr int kKv8WideBlocks = 64, kKv8WidePerCu = 8;
+int kv8_splits(int B, int Hkv, int Lcap, int num_splits) {
+    const int s = resolve_splits(B, Hkv, Lcap, num_splits, true);
+    const long long pairs = (long long)B * Hkv, blocks = pairs * (Lcap / FFD_BLOCK), wide = (long long)kKv8WidePerCu * device_cus();
+    if (s <= 0 || num_splits > 0 || pairs < 64 || blocks < kKv8WideBlocks * (long long)dense_target_workgroups(pairs)) return s;
+    return (int)std::max<long long>(s, wide / pairs - 1);
+}
+
 // Pointers of a cache argument: all there and aligned; *bits is 8 or 16. An 8-bit one is required where only8.
 int check_kv(const ffd_kv* c, bool only8, int* bits) {
     if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return FFD_ERR_INVALID_ARGUMENT;
@@ -798,6 +811,13 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
     return launch_status();
 }
 
+size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_splits) {
+    if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || (long long)B * Hkv > (1LL << 20)) return 0;
+    const int S = kv8_splits(B, Hkv, Lcap, num_splits);
+    if (S <= 0) return 0;
+    return round_up(partials_bytes(own_rows(B, Hq, S)), kAlign) + (B <= kDenseBalanceMaxSeqs ? (size_t)B * Hkv * sizeof(int2) : 0);
+}
+
 int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
                              int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
@@ -808,7 +828,8 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
     if (st != FFD_OK || B == 0) return st;
     if ((long long)B * Hkv > (1LL << 20)) return FFD_ERR_UNSUPPORTED;
     if ((st = check_kv(cache, true, &bits)) != FFD_OK) return st;
-    if (workspace_bytes < ffd_dense_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < ffd_kv8_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
+    S = kv8_splits(B, Hkv, Lcap, num_splits);
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
     launch_own(o, static_cast<const uint16_t*>(q), *cache, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);

@@ -25,8 +25,8 @@ NOALLOC_SCRATCH_BYTES = 16 << 20     # FFD_NOALLOC_SCRATCH_BYTES
 
 EXPORTS = ("ffd_quantize_keys", "ffd_append_kv", "ffd_decode_attention", "ffd_decode_attention_ex",
            "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_write_kv8", "ffd_read_kv8",
-           "ffd_kv8_decode_attention", "ffd_shared_prefix_decode_attention", "ffd_shared_prefix_workspace_bytes",
-           "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits",
+           "ffd_kv8_decode_attention", "ffd_kv8_workspace_bytes", "ffd_shared_prefix_decode_attention",
+           "ffd_shared_prefix_workspace_bytes", "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits",
            "ffd_workspace_bytes", "ffd_dense_workspace_bytes", "ffd_status_string")
 
 
@@ -91,7 +91,7 @@ def lib() -> ctypes.CDLL:
     so.ffd_fused_splits.argtypes = [I, I, I, I]
     so.ffd_select_kernels.argtypes = [I, I, I, I]
     so.ffd_dense_resolve_splits.argtypes = [I, I, I, I]
-    for name in ("ffd_workspace_bytes", "ffd_dense_workspace_bytes"):
+    for name in ("ffd_workspace_bytes", "ffd_dense_workspace_bytes", "ffd_kv8_workspace_bytes"):
         getattr(so, name).argtypes = [I, I, I, I, I, I]
         getattr(so, name).restype = SZ
     so.ffd_status_string.argtypes = [I]
@@ -515,13 +515,23 @@ def _need_workspace(workspace, device):
     return workspace.nbytes
 
 
+def kv8_workspace_bytes(B: int, Hq: int, Hkv: int, Lcap: int, num_splits: int = 0) -> int:
+    """Bytes for ``kv8_decode_attention``."""
+    return lib().ffd_kv8_workspace_bytes(B, Hq, Hkv, Lcap, HEAD_DIM, num_splits)
+
+
+def new_kv8_workspace(B: int, Hq: int, Hkv: int, Lcap: int, num_splits: int = 0, device="cuda"):
+    """A workspace for ``kv8_decode_attention`` (one per stream)."""
+    return torch.empty(max(kv8_workspace_bytes(B, Hq, Hkv, Lcap, num_splits), 16), dtype=torch.uint8, device=device)
+
+
 def kv8_decode_attention(q, cache, seq_lens, *, num_splits: int = 0, softmax_scale: float = 0.0,
                          return_lse: bool = True, workspace=None, out=None, lse=None):
     """Exact dense decode attention over an 8-bit cache: ``dense_decode_attention`` on the values that it stands
-    for. Returns ``(out, lse)``. ``workspace``: ``new_workspace(..., dense=True)``'s."""
+    for. Returns ``(out, lse)``. ``workspace``: ``new_kv8_workspace``'s."""
     device, B, Hq, Hkv, Lcap, kv, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, False)
     if workspace is None:
-        workspace = new_workspace(B, Hq, Hkv, Lcap, num_splits, q.device, dense=True)
+        workspace = new_kv8_workspace(B, Hq, Hkv, Lcap, num_splits, q.device)
     _launch("ffd_kv8_decode_attention", lib().ffd_kv8_decode_attention, device, q.data_ptr(), ctypes.byref(kv),
             seq_lens.data_ptr(), B, Hq, Hkv, Lcap, HEAD_DIM, num_splits, softmax_scale, out.data_ptr(), _ptr(lse),
             workspace.data_ptr(), _need_workspace(workspace, device))

@@ -231,6 +231,22 @@ def test_attention_of_more_sequences_than_the_balanced_mode_takes():
         check_attention(got, attention(q, [(*values(cache), lens)]), 700, P_SPLIT)
 
 
+def test_attention_with_many_workgroups_per_compute_unit():
+    """A batch whose capacity makes its automatic splits finer, with lengths far apart."""
+    from paper_2609_00097_amd import ffd
+    B, Hkv, L = 64, 1, 65536
+    lens = [1 + (9973 * b * b) % 2500 for b in range(B)]
+    lens[5], lens[40] = 0, 20000
+    assert ffd.kv8_workspace_bytes(B, Hkv, Hkv, L) > ffd.workspace_bytes(B, Hkv, Hkv, L, dense=True)
+    gen = _gen(14)
+    q, cache = _normal(gen, B, Hkv, D), random_cache(gen, B, Hkv, 20032)
+    cache = tuple(torch.nn.functional.pad(t, (0, 0) * (t.dim() == 4) + (0, L - 20032)) for t in cache)
+    got = ffd.kv8_decode_attention(q, cache, _int32(lens))
+    torch.cuda.synchronize()
+    k, v = values([t[:, :, :20032] for t in cache])
+    check_attention(got, attention(q, [(k, v, lens)]), 20000, P_SPLIT)
+
+
 def test_attention_over_nan_tokens_and_large_scores():
     """A token with a NaN among those that a sequence sees makes its rows NaN, also where there is no other; scores
     of several hundred, of both signs."""
@@ -298,7 +314,7 @@ def test_captured_steps_grow_the_cache():
     lens_g, lens_e = start.clone(), start.clone()
     k_new, v_new = _normal(gen, B, Hkv, D), _normal(gen, B, Hkv, D)
     q = _normal(gen, B, Hq, D)
-    ws = ffd.new_workspace(B, Hq, Hkv, L, dense=True)
+    ws = ffd.new_kv8_workspace(B, Hq, Hkv, L)
     out, lse = torch.empty_like(q), torch.empty(B, Hq, device="cuda")
 
     def step():

@@ -105,6 +105,21 @@ def test_shared_prefix_caches_are_whole(so):
     assert _shared(so, prefix=bf16, own=bf16, ws_bytes=16) == 3          # the size is the first thing that is wrong
 
 
+def test_kv8_workspace(so):
+    size = so.ffd_kv8_workspace_bytes
+    up = lambda x: -(-x // 256) * 256
+    assert size(4, 32, 8, 131072, 128, 0) == so.ffd_dense_workspace_bytes(4, 32, 8, 131072, 128, 0)
+    assert size(32, 32, 8, 8192, 128, 0) == so.ffd_dense_workspace_bytes(32, 32, 8, 8192, 128, 0)
+    # 512 groups of 256 blocks: 170 for each of 768 workgroups, so 2048 of them (no GPU here: 256 CUs), S = 4 - 1
+    assert size(64, 32, 8, 16384, 128, 0) == up(64 * 32 * (3 + 1) * 130 * 4) + 64 * 8 * 8
+    assert size(64, 32, 8, 16384, 128, 1) == up(64 * 32 * 2 * 130 * 4) + 64 * 8 * 8
+    assert size(300, 8, 8, 4096, 128, 1) == up(300 * 8 * 130 * 4)
+    for bad in ((0, 32, 8, 4096, 128, 0), (1, 30, 8, 4096, 128, 0), (1, 32, 8, 100, 128, 0), (1, 32, 8, 4096, 64, 0),
+                (1, 32, 8, 4096, 128, 5000), (60000, 64, 64, 64, 128, 0)):
+        assert size(*bad) == 0
+    assert _attend(so, ws_bytes=size(1, 32, 8, 4096, 128, 0) - 1) == 3
+
+
 def test_shared_prefix_workspace(so):
     size = so.ffd_shared_prefix_workspace_bytes
     dense = so.ffd_dense_workspace_bytes(2, 32, 8, 4096, 128, 0)
