@@ -43,22 +43,26 @@ constexpr int kPThreads = kPrefixTileThreads;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;                  // growth of the maximum, in powers of two, that rescales
 
-template <int RW>
+template <int RW, bool I8>
 struct PrefixShape {
-    static constexpr int kTokenGroups = 8 / RW;
-    static constexpr int kSub = RW == 2 ? 1 : 2;                        // 32-token tiles of a wave
+    static constexpr bool kRoles = I8 && RW <= 4;                       // waves 4 .. 7 stage, waves 0 .. 3 do the rest
+    static constexpr bool kPhased = RW > 2 && !kRoles;
+    static constexpr int kMathWaves = kRoles ? 4 : 8;
+    static constexpr int kTokenGroups = kMathWaves / RW;
+    static constexpr int kSub = kRoles || kPhased ? 2 : 1;              // 32-token tiles of a wave
     static constexpr int kTokens = 32 * kSub * kTokenGroups;            // tokens of a tile of the workgroup
     static constexpr int kRows = 32 * RW;
     static constexpr int kBytes = kTokens * 2 * kD;                     // of a tile's keys, or values, in LDS
-    static constexpr int kLoads = kTokens / 32;                         // 16-byte chunks per thread of half of them
-    static constexpr bool kPhased = RW > 2;
+    static constexpr int kParts = kRoles ? 1 : 2;                       // teams that stage a tile
+    static constexpr int kPartTokens = kTokens / kParts;
+    static constexpr int kLoads = kPartTokens / 16;                     // 16-byte chunks of bf16 keys per thread
 };
-constexpr int kTeam = kPThreads / 2;           // threads that stage one half of a tile
+constexpr int kTeam = kPThreads / 2;           // threads of a team, four waves
 constexpr int kJoinPad = kD + 4;
 
-template <int RW>
+template <int RW, bool I8>
 struct PrefixLds {
-    using Sh = PrefixShape<RW>;
+    using Sh = PrefixShape<RW, I8>;
     union {
         struct {
             alignas(16) uint8_t keys[2][Sh::kBytes];
@@ -94,32 +98,32 @@ __device__ __forceinline__ uint2 expand4(uint32_t w) {          // four codes as
                       __builtin_amdgcn_perm(__float_as_uint(byte_value<3>(w)), __float_as_uint(byte_value<2>(w)), 0x07060302u));
 }
 
-// Half of a tile on its way from memory to LDS, in the registers of a team: rows [team kTokens / 2, ..) of the tile.
-// `last` is the last row of the tile that any query sees; rows behind it repeat it.
+// A team's part of a tile on its way from memory to LDS, in registers: rows [part kPartTokens, ..) of the tile. `last` is
+// the last row of the tile that any query sees; rows behind it repeat it.
 template <int RW, bool I8> struct Staged;
 template <int RW> struct Staged<RW, false> {
-    using Sh = PrefixShape<RW>;
+    using Sh = PrefixShape<RW, false>;
     v4u k[Sh::kLoads], v[Sh::kLoads];
-    static __device__ __forceinline__ int row_of(int j, int team, int id) { return team * (Sh::kTokens / 2) + (id >> 4) + j * (kTeam / 16); }
-    static __device__ __forceinline__ void load(v4u (&x)[Sh::kLoads], const uint8_t* from, int t0, int last, int team, int id) {
+    static __device__ __forceinline__ int row_of(int j, int part, int id) { return part * Sh::kPartTokens + (id >> 4) + j * (kTeam / 16); }
+    static __device__ __forceinline__ void load(v4u (&x)[Sh::kLoads], const uint8_t* from, int t0, int last, int part, int id) {
         const uint8_t* base = from + (size_t)t0 * (2 * kD);
 #pragma unroll
         for (int j = 0; j < Sh::kLoads; ++j)
-            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, team, id), last) * (2 * kD) + 16 * (id & 15));
+            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, part, id), last) * (2 * kD) + 16 * (id & 15));
     }
-    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int team, int id) { load(k, kv.k, t0, last, team, id); }
-    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int team, int id) { load(v, kv.v, t0, last, team, id); }
-    __device__ __forceinline__ void store_keys(PrefixLds<RW>& lds, int u, int, int team, int id) const {
+    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int part, int id) { load(k, kv.k, t0, last, part, id); }
+    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int part, int id) { load(v, kv.v, t0, last, part, id); }
+    __device__ __forceinline__ void store_keys(PrefixLds<RW, false>& lds, int u, int, int part, int id) const {
 #pragma unroll
         for (int j = 0; j < Sh::kLoads; ++j) {
-            const int row = row_of(j, team, id);
+            const int row = row_of(j, part, id);
             *reinterpret_cast<v4u*>(&lds.keys[u & 1][row * (2 * kD) + 16 * key_chunk(row, id & 15)]) = k[j];
         }
     }
-    __device__ __forceinline__ void store_values(PrefixLds<RW>& lds, int u, int team, int id) const {
+    __device__ __forceinline__ void store_values(PrefixLds<RW, false>& lds, int u, int part, int id) const {
 #pragma unroll
         for (int j = 0; j < Sh::kLoads; ++j) {
-            const int row = row_of(j, team, id);
+            const int row = row_of(j, part, id);
             v4u x = v[j];
             const uint32_t big = pk_max_u16(pk_max_u16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max_u16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
             if (max(big & 0xffffu, big >> 16) >= 0x7f80u) {
@@ -135,18 +139,18 @@ template <int RW> struct Staged<RW, false> {
     }
 };
 template <int RW> struct Staged<RW, true> {
-    using Sh = PrefixShape<RW>;
+    using Sh = PrefixShape<RW, true>;
     static constexpr int kLoads = Sh::kLoads / 2;
-    static constexpr int kScales = Sh::kTokens / 2;
+    static constexpr int kScales = Sh::kPartTokens;
     static_assert(2 * kScales <= kTeam, "one absmax per thread");
     v4u k[kLoads], v[kLoads];
     uint32_t m;                                 // absmax of a key (threads below kScales) or value (the next kScales)
-    static __device__ __forceinline__ int row_of(int j, int team, int id) { return team * (Sh::kTokens / 2) + (id >> 3) + j * (kTeam / 8); }
-    static __device__ __forceinline__ void load(v4u (&x)[kLoads], const uint8_t* from, int t0, int last, int team, int id) {
+    static __device__ __forceinline__ int row_of(int j, int part, int id) { return part * Sh::kPartTokens + (id >> 3) + j * (kTeam / 8); }
+    static __device__ __forceinline__ void load(v4u (&x)[kLoads], const uint8_t* from, int t0, int last, int part, int id) {
         const uint8_t* base = from + (size_t)t0 * kD;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, team, id), last) * kD + 16 * (id & 7));
+            x[j] = *reinterpret_cast<const v4u*>(base + (uint32_t)min(row_of(j, part, id), last) * kD + 16 * (id & 7));
     }
     static __device__ __forceinline__ void expand(uint8_t* tile, int row, int c, bool keys, const v4u& w) {
 #pragma unroll
@@ -156,18 +160,18 @@ template <int RW> struct Staged<RW, true> {
             *reinterpret_cast<v4u*>(tile + row * (2 * kD) + 16 * at) = v4u{a.x, a.y, b.x, b.y};
         }
     }
-    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int team, int id) {
-        load(k, kv.k, t0, last, team, id);
+    __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int part, int id) {
+        load(k, kv.k, t0, last, part, id);
         m = 0;                                  // the values' absmaxes come with the keys: they are needed with the scores
         if (id < 2 * kScales)
-            m = (id < kScales ? kv.k_absmax : kv.v_absmax)[(size_t)t0 + min(team * kScales + (id & (kScales - 1)), last)];
+            m = (id < kScales ? kv.k_absmax : kv.v_absmax)[(size_t)t0 + min(part * kScales + (id & (kScales - 1)), last)];
     }
-    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int team, int id) { load(v, kv.v, t0, last, team, id); }
-    __device__ __forceinline__ void store_keys(PrefixLds<RW>& lds, int u, int last, int team, int id) const {
+    __device__ __forceinline__ void load_values(const KvSource& kv, int t0, int last, int part, int id) { load(v, kv.v, t0, last, part, id); }
+    __device__ __forceinline__ void store_keys(PrefixLds<RW, true>& lds, int u, int last, int part, int id) const {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) expand(lds.keys[u & 1], row_of(j, team, id), 2 * (id & 7), true, k[j]);
+        for (int j = 0; j < kLoads; ++j) expand(lds.keys[u & 1], row_of(j, part, id), 2 * (id & 7), true, k[j]);
         if (id < 2 * kScales) {
-            const int t = team * kScales + (id & (kScales - 1));
+            const int t = part * kScales + (id & (kScales - 1));
             const float x = t <= last ? bf16_to_f32((uint16_t)m) * (1.f / 127.f) : 0.f;
             const bool finite = fabsf(x) < INFINITY;
             if (id < kScales) {
@@ -178,9 +182,9 @@ template <int RW> struct Staged<RW, true> {
             }
         }
     }
-    __device__ __forceinline__ void store_values(PrefixLds<RW>& lds, int u, int team, int id) const {
+    __device__ __forceinline__ void store_values(PrefixLds<RW, true>& lds, int u, int part, int id) const {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) expand(lds.values[u & 1], row_of(j, team, id), 2 * (id & 7), false, v[j]);
+        for (int j = 0; j < kLoads; ++j) expand(lds.values[u & 1], row_of(j, part, id), 2 * (id & 7), false, v[j]);
     }
 };
 
@@ -205,8 +209,8 @@ __device__ __forceinline__ void add_nonfinite(v16f (&o)[4], const KvSource& kv, 
 // and a tile is as long as its own sequences need. The tiles get workgroups by their lengths. Computed by every
 // workgroup alone; `writes`: this one leaves the places for the merge. False, and nothing changed, where all
 // lengths are equal; else lds.vm holds the order, tile is this workgroup's (-1: none) and mine its tile's workgroups.
-template <int RW>
-__device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW>& lds, bool writes, int w, int& tile, PrefixPlace& mine) {
+template <int RW, bool I8>
+__device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW, I8>& lds, bool writes, int w, int& tile, PrefixPlace& mine) {
     static_assert(sizeof(lds.km) >= kPrefixSortSeqs * sizeof(int) && sizeof(lds.vm) >= kPrefixSortSeqs * sizeof(int));
     const int tid = threadIdx.x;
     int* lens = reinterpret_cast<int*>(lds.km);
@@ -228,7 +232,7 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
         if (tid < a.B) order[place] = tid;
         __syncthreads();
     }
-    const int step = PrefixShape<RW>::kRows / a.G;      // sequences per tile, the first of them the longest
+    const int step = PrefixShape<RW, I8>::kRows / a.G;      // sequences per tile, the first of them the longest
     if (!differ) {
         if (writes && tid < a.B) a.places[tid] = PrefixPlace{tid / step, a.tiles, a.S, tid};
         return false;
@@ -237,7 +241,7 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
     long long all = 0;
     int used = 0;
     for (int t = 0; t < a.tiles; ++t) {
-        const int units = (lens[order[t * step]] + PrefixShape<RW>::kTokens - 1) / PrefixShape<RW>::kTokens;
+        const int units = (lens[order[t * step]] + PrefixShape<RW, I8>::kTokens - 1) / PrefixShape<RW, I8>::kTokens;
         all += units;
         used += units > 0;
     }
@@ -245,7 +249,7 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
     tile = -1;
     int first = 0;
     for (int t = 0; t < a.tiles; ++t) {
-        const int units = (lens[order[t * step]] + PrefixShape<RW>::kTokens - 1) / PrefixShape<RW>::kTokens;
+        const int units = (lens[order[t * step]] + PrefixShape<RW, I8>::kTokens - 1) / PrefixShape<RW, I8>::kTokens;
         const int count = units > 0 ? 1 + (int)((double)(units * spare) / (double)all) : 0;
         if (writes && tid < a.B && place / step == t) a.places[tid] = PrefixPlace{first, 1, count, place};
         if (w >= first && w < first + count) {
@@ -262,11 +266,11 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
 
 template <int RW, bool I8>
 __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a) {
-    using Sh = PrefixShape<RW>;
-    __shared__ PrefixLds<RW> lds;
+    using Sh = PrefixShape<RW, I8>;
+    __shared__ PrefixLds<RW, I8> lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, h = lane >> 5;
-    const int rg = wave % RW, tg = wave / RW;
+    const int rg = wave % RW, tg = wave % Sh::kMathWaves / RW;
     // Workgroups of one run but different tiles read the same tokens: they are eight apart, on one XCD (consecutive
     // workgroups go to the eight XCDs in turn).
     const int slot = (int)(blockIdx.x >> 3) % a.tiles;
@@ -345,9 +349,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     v8bf p[2 * Sh::kSub];
     auto first_token = [&](int u) { return u * Sh::kTokens + wave_row; };
 
-    // Reads of LDS that can be under way before their use. Without phases (one tile of 32 tokens, registers to spare) a
-    // tile's scales and first value operands are asked for with its keys: read where they are used, each is another
-    // latency of LDS in the wave's chain (16 sequences on 128K in 8 bits: 80 us of kernel).
+    // With 32 tokens per wave there are registers to ask for a tile's first value operands with its scores; read where
+    // they are used, they are another latency of LDS in the wave's chain.
+    constexpr bool kEarly = Sh::kSub == 1;
     v4f km[Sh::kSub][4], vm[Sh::kSub][4];
     v8s head_values[4];
     int flag = 0;
@@ -370,10 +374,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     auto scores = [&](int u) {
         if (first_token(u) >= longest) return;          // uniform, here and below
         const uint8_t* keys = lds.keys[u & 1];
-        if constexpr (!Sh::kPhased) {
-            if constexpr (I8) read_scales(km, lds.km[u & 3]);
-            flag = lds.nonfinite[u & 3];
-        }
+        if constexpr (kEarly) flag = lds.nonfinite[u & 3];
         v8bf kf[2][4];
 #pragma unroll
         for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
@@ -393,8 +394,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
             }
         }
-        if constexpr (!Sh::kPhased) {
-            if constexpr (I8) read_scales(vm, lds.vm[u & 3]);
+        if constexpr (kEarly) {
 #pragma unroll
             for (int d = 0; d < 4; ++d) head_values[d] = value_operand(lds.values[u & 1], 0, d);
         }
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         const int w0 = first_token(u);
         if (w0 >= longest) return;
         if constexpr (I8) {
-            if constexpr (Sh::kPhased) read_scales(km, lds.km[u & 3]);
+            read_scales(km, lds.km[u & 3]);
 #pragma unroll
             for (int x = 0; x < Sh::kSub; ++x)
 #pragma unroll
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         }
         const float m0 = m == -INFINITY ? 0.f : m;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (I8 && Sh::kPhased) read_scales(vm, lds.vm[u & 3]);
+        if constexpr (I8) read_scales(vm, lds.vm[u & 3]);
 #pragma unroll
         for (int x = 0; x < Sh::kSub; ++x) {
             float e[16];
@@ -467,31 +467,60 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         for (int y = 0; y < 2 * Sh::kSub; ++y)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const v8s f = y == 0 && !Sh::kPhased ? head_values[d] : value_operand(values, y, d);
+                const v8s f = y == 0 && kEarly ? head_values[d] : value_operand(values, y, d);
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
             }
-        if constexpr (Sh::kPhased) flag = lds.nonfinite[u & 3];
+        if constexpr (!kEarly) flag = lds.nonfinite[u & 3];
         if (__builtin_amdgcn_readfirstlane(flag) == u) add_nonfinite<I8>(o, kv, w0, min(w0 + 32 * Sh::kSub, all), lim, h);
     };
 
     // Staging. Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for
     // one tile's registers would fall on the next one's loads.
-    const int team = wave >> 2, id = tid & (kTeam - 1);
-    Staged<RW, I8> st;
+    const int team = wave >> 2, part = Sh::kParts == 2 ? team : 0, id = tid & (kTeam - 1);
     auto last_row = [&](int u) { return all - 1 - u * Sh::kTokens; };
-    auto load_keys = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_keys(kv, u * Sh::kTokens, last_row(u), team, id); };
-    auto load_values = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_values(kv, u * Sh::kTokens, last_row(u), team, id); };
+    auto load_keys = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_keys(kv, u * Sh::kTokens, last_row(u), part, id); };
+    auto load_values = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_values(kv, u * Sh::kTokens, last_row(u), part, id); };
+    auto store_keys = [&](const Staged<RW, I8>& x, int u) { x.store_keys(lds, u, last_row(min(u, last - 1)), part, id); };
+    auto store_values = [&](const Staged<RW, I8>& x, int u) { x.store_values(lds, u, part, id); };
     if (first < last) {
-        Staged<RW, I8> head;
-        load_keys(head, first);
-        load_values(st, first);
-        load_keys(st, first + 1);
-        head.store_keys(lds, first, last_row(first), team, id);
-        if constexpr (Sh::kPhased) {
+        Staged<RW, I8> st, head;
+        if constexpr (Sh::kRoles) {
+            if (team == 1) {
+                // two tiles under way, in turn in the two sets of registers
+                auto refill = [&](Staged<RW, I8>& x, int u) {
+                    store_keys(x, u);
+                    store_values(x, u);
+                    load_keys(x, u + 2);
+                    load_values(x, u + 2);
+                    __syncthreads();
+                };
+                load_keys(head, first);
+                load_values(head, first);
+                load_keys(st, first + 1);
+                load_values(st, first + 1);
+                refill(head, first);
+                for (int u = first; u < last; u += 2) {
+                    refill(st, u + 1);
+                    if (u + 1 < last) refill(head, u + 2);
+                }
+            } else {
+                __syncthreads();
+                for (int u = first; u < last; ++u) {
+                    scores(u);
+                    softmax(u);
+                    products(u);
+                    __syncthreads();
+                }
+            }
+        } else if constexpr (Sh::kPhased) {
+            load_keys(head, first);
+            load_values(st, first);
+            load_keys(st, first + 1);
+            store_keys(head, first);
             // this team's half of the keys of tile u and the values of u - 1 to LDS; those after them are asked for
             auto stage = [&](int u) {
-                st.store_keys(lds, u, last_row(min(u, last - 1)), team, id);
-                st.store_values(lds, u - 1, team, id);
+                store_keys(st, u);
+                store_values(st, u - 1);
                 load_keys(st, u + 1);
                 load_values(st, u);
             };
@@ -512,15 +541,19 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             }
             if (team == 0) __syncthreads();
         } else {
-            st.store_values(lds, first, team, id);
+            load_keys(head, first);
+            load_values(head, first);
+            load_keys(st, first + 1);
             load_values(st, first + 1);
+            store_keys(head, first);
+            store_values(head, first);
             __syncthreads();
             for (int u = first; u < last; ++u) {
                 scores(u);
                 softmax(u);
                 products(u);
-                st.store_keys(lds, u + 1, last_row(min(u + 1, last - 1)), team, id);
-                st.store_values(lds, u + 1, team, id);
+                store_keys(st, u + 1);
+                store_values(st, u + 1);
                 load_keys(st, u + 2);
                 load_values(st, u + 2);
                 __syncthreads();
@@ -531,6 +564,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     // token groups joined in LDS, then one partial row per query row
     l = halves_sum(l);
     const size_t out0 = ((size_t)kvh * a.S * a.tiles + w) * Sh::kRows;
+    const bool math = wave < Sh::kMathWaves;
     if constexpr (Sh::kTokenGroups > 1) {
         if (h == 0) {
             lds.m[wave][n] = m;
@@ -548,7 +582,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         const float f = m == -INFINITY ? 0.f : exp2_hw(m - M);
 #pragma unroll
         for (int x = Sh::kTokenGroups - 1; x >= 0; --x) {
-            if (tg == x) {
+            if (math && tg == x) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -568,12 +602,12 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         for (int i = tid; i < count * (kD / 4); i += kPThreads)
             *reinterpret_cast<float4*>(a.part_acc + (out0 + (i >> 5)) * kD + 4 * (i & 31)) =
                 *reinterpret_cast<const float4*>(&lds.join[i >> 5][4 * (i & 31)]);
-        if (tg == 0 && h == 0 && live) {
+        if (math && tg == 0 && h == 0 && live) {
             a.part_m[out0 + 32 * rg + n] = M * 0.69314718055994531f;
             a.part_l[out0 + 32 * rg + n] = L;
         }
     } else {
-        if (live) {
+        if (math && live) {
             const size_t row = out0 + 32 * rg + n;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
