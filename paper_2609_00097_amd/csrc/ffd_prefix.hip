@@ -370,29 +370,28 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
-    // s = K Q^T of tile u; the next four key operands are on their way from LDS while four are used.
-    auto scores = [&](int u) {
-        if (first_token(u) >= longest) return;          // uniform, here and below
+    // s = K Q^T of tile u; the next four key operands are on their way from LDS while four are used. The first four can
+    // be asked for earlier.
+    v8bf kf[2][4];
+    auto read_key_operands = [&](int u, int j) {
         const uint8_t* keys = lds.keys[u & 1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
+    };
+    auto scores = [&](int u) {
         if constexpr (kEarly) flag = lds.nonfinite[u & 3];
-        v8bf kf[2][4];
 #pragma unroll
-        for (int j = 0; j < 2 * Sh::kSub + 1; ++j) {
-            if (j < 2 * Sh::kSub) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
-            }
+        for (int j = 1; j < 2 * Sh::kSub + 1; ++j) {
+            if (j < 2 * Sh::kSub) read_key_operands(u, j);
             __builtin_amdgcn_sched_barrier(0);
-            if (j > 0) {
-                const int x = (j - 1) >> 1, k = (j - 1) & 1;
-                if (k == 0) {
+            const int x = (j - 1) >> 1, k = (j - 1) & 1;
+            if (k == 0) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
         }
         if constexpr (kEarly) {
 #pragma unroll
@@ -403,7 +402,6 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     // p = the probabilities of tile u against the maximum m, which follows the running one; their sum into l.
     auto softmax = [&](int u) {
         const int w0 = first_token(u);
-        if (w0 >= longest) return;
         if constexpr (I8) {
             read_scales(km, lds.km[u & 3]);
 #pragma unroll
@@ -458,10 +456,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
 
-    // o += V^T P^T of tile u.
+    // o += V^T P^T of tile u, and the infinities and NaN among its values.
     auto products = [&](int u) {
-        const int w0 = first_token(u);
-        if (w0 >= longest) return;
         const uint8_t* values = lds.values[u & 1];
 #pragma unroll
         for (int y = 0; y < 2 * Sh::kSub; ++y)
@@ -470,9 +466,14 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 const v8s f = y == 0 && kEarly ? head_values[d] : value_operand(values, y, d);
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
             }
+    };
+    auto nonfinite = [&](int u) {
         if constexpr (!kEarly) flag = lds.nonfinite[u & 3];
+        const int w0 = first_token(u);
         if (__builtin_amdgcn_readfirstlane(flag) == u) add_nonfinite<I8>(o, kv, w0, min(w0 + 32 * Sh::kSub, all), lim, h);
     };
+    // the tile from which on this wave's rows see no token any more
+    const int mine_last = max(first, min(last, (longest - wave_row + Sh::kTokens - 1) / Sh::kTokens));
 
     // Staging. Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for
     // one tile's registers would fall on the next one's loads.
@@ -505,12 +506,15 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 }
             } else {
                 __syncthreads();
-                for (int u = first; u < last; ++u) {
+                for (int u = first; u < mine_last; ++u) {
+                    read_key_operands(u, 0);
                     scores(u);
                     softmax(u);
                     products(u);
+                    nonfinite(u);
                     __syncthreads();
                 }
+                for (int u = mine_last; u < last; ++u) __syncthreads();
             }
         } else if constexpr (Sh::kPhased) {
             load_keys(head, first);
@@ -529,14 +533,30 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 stage(first + 1);
                 __syncthreads();
             }
-            for (int u = first; u <= last; ++u) {
-                if (u > first) products(u - 1);
-                if (u < last) scores(u);
+            // a tile's two phases: scores after the products of the tile before, then softmax
+            auto vector_phase = [&](int u) {
                 __syncthreads();
-                if (u < last) {
-                    softmax(u);
-                    stage(u + 1 + team);
+                softmax(u);
+                stage(u + 1 + team);
+                __syncthreads();
+            };
+            if (first < mine_last) {
+                read_key_operands(first, 0);
+                scores(first);
+                vector_phase(first);
+                for (int u = first + 1; u < mine_last; ++u) {
+                    read_key_operands(u, 0);
+                    products(u - 1);
+                    scores(u);
+                    nonfinite(u - 1);
+                    vector_phase(u);
                 }
+                products(mine_last - 1);
+                nonfinite(mine_last - 1);
+            }
+            for (int u = mine_last; u <= last; ++u) {
+                __syncthreads();
+                if (u < last) stage(u + 1 + team);
                 __syncthreads();
             }
             if (team == 0) __syncthreads();
@@ -549,9 +569,13 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             store_values(head, first);
             __syncthreads();
             for (int u = first; u < last; ++u) {
-                scores(u);
-                softmax(u);
-                products(u);
+                if (u < mine_last) {
+                    read_key_operands(u, 0);
+                    scores(u);
+                    softmax(u);
+                    products(u);
+                    nonfinite(u);
+                }
                 store_keys(st, u + 1);
                 store_values(st, u + 1);
                 load_keys(st, u + 2);
