@@ -418,10 +418,16 @@ def _kv_cache(cache, name, device, rows):
         return KvCache(k.data_ptr(), None, v.data_ptr(), None)
     k, k_absmax, v, v_absmax = cache
     vectors = rows[:3]
-    _need_on(device, k, name, torch.int8, rows, " k_codes")
-    _need_on(device, k_absmax, name, torch.bfloat16, vectors, " k_absmax")
-    _need_on(device, v, name, torch.int8, rows, " v_codes")
-    _need_on(device, v_absmax, name, torch.bfloat16, vectors, " v_absmax")
+    if not (type(k) is type(k_absmax) is type(v) is type(v_absmax) is torch.Tensor       # the usual tensors, cheaply
+            and k.dtype is torch.int8 and v.dtype is torch.int8
+            and k_absmax.dtype is torch.bfloat16 and v_absmax.dtype is torch.bfloat16
+            and k.shape == rows and v.shape == rows and k_absmax.shape == vectors and v_absmax.shape == vectors
+            and k.get_device() == k_absmax.get_device() == v.get_device() == v_absmax.get_device() == device >= 0
+            and k.is_contiguous() and v.is_contiguous() and k_absmax.is_contiguous() and v_absmax.is_contiguous()):
+        _need_on(device, k, name, torch.int8, rows, " k_codes")
+        _need_on(device, k_absmax, name, torch.bfloat16, vectors, " k_absmax")
+        _need_on(device, v, name, torch.int8, rows, " v_codes")
+        _need_on(device, v_absmax, name, torch.bfloat16, vectors, " v_absmax")
     return KvCache(k.data_ptr(), k_absmax.data_ptr(), v.data_ptr(), v_absmax.data_ptr())
 
 
@@ -429,7 +435,11 @@ _Strides = ctypes.c_int64 * 3
 
 
 def _strided(t, name, device, shape):
-    """The three strides, in elements, of ``t`` as [B, T, Hkv, 128]. Only the dims of a vector need to be contiguous."""
+    """The three strides, in elements, of ``t`` as [B, T, Hkv, 128]; None where it is contiguous. Only the dims of a vector
+    need to be."""
+    if (type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device >= 0
+            and t.is_contiguous()):
+        return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != torch.bfloat16 or t.get_device() != device:
