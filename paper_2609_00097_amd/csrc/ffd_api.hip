@@ -427,28 +427,21 @@ KvSource source_of(const ffd_kv& c) {
                     static_cast<const uint16_t*>(c.k_absmax), static_cast<const uint16_t*>(c.v_absmax)};
 }
 
-// Partial states of a dense attention over whole caches: its rows, its table (null: S rows per head) and grid.
+// Partial states of a dense attention over whole caches: its rows, its table (null: S rows per head) and workgroups.
 struct OwnPartials {
     Partials p;
     int2* table;
-    dim3 grid;
+    unsigned wgs;
 };
 size_t own_rows(int B, int Hq, int S) { return (size_t)B * Hq * (B <= kDenseBalanceMaxSeqs ? S + 1 : S); }
 OwnPartials own_partials(Partials p, void* table, int B, int Hkv, int S) {
     const bool balanced = B <= kDenseBalanceMaxSeqs;
     return OwnPartials{p, balanced ? static_cast<int2*>(table) : nullptr,
-                       balanced ? dim3((unsigned)((S + 1) * B * Hkv)) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B)};
+                       (unsigned)((balanced ? S + 1 : S) * B * Hkv)};
 }
 OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      // as ffd_dense_workspace_bytes lays it out
     const size_t rows = own_rows(B, Hq, S);
     return own_partials(carve(workspace, rows), static_cast<uint8_t*>(workspace) + round_up(partials_bytes(rows), kAlign), B, Hkv, S);
-}
-
-void launch_own(const OwnPartials& o, const uint16_t* q, const ffd_kv& kv, const int32_t* seq_lens, int B, int Hq, int Hkv,
-                int Lcap, int S, float scale, hipStream_t stream) {
-    OwnArgs a{q, source_of(kv), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, Hq / Hkv, S, scale};
-    if (kv.k_absmax) hipLaunchKernelGGL(own_decode_kernel<true>, o.grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL(own_decode_kernel<false>, o.grid, dim3(kThreads), 0, stream, a);
 }
 
 // Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head (a prefix is then
@@ -481,14 +474,26 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_o
     return p;
 }
 
+void launch_own(bool i8, unsigned wgs, hipStream_t stream, const OwnArgs& o) {
+    if (i8) hipLaunchKernelGGL(own_decode_kernel<true>, dim3(wgs), dim3(kThreads), 0, stream, o);
+    else hipLaunchKernelGGL(own_decode_kernel<false>, dim3(wgs), dim3(kThreads), 0, stream, o);
+}
+
+// Few rows: one launch for both, the prefix's workgroups first (whole calls: four sequences on 2K tokens 16.7 us with two
+// launches, 14.6 with one; eight on 64K with 1K of their own 70.6 and 65.0, with 16K 157 and 150). A large tile's
+// workgroup has its CU to itself, so the own caches wait for it in either form, and two launches are the faster: 64.2 us
+// against 67.5 for 32 sequences on 32K, 93.5 against 97 for 16 on 128K in 8 bits.
 template <bool I8>
-void launch_prefix(int tile_rows, dim3 grid, hipStream_t stream, const PrefixArgs& a) {
-    const dim3 small(kThreads), large(kPrefixTileThreads);
-    if (tile_rows == 16) hipLaunchKernelGGL((prefix_kernel<1, I8>), grid, small, 0, stream, a);
-    else if (tile_rows == 32) hipLaunchKernelGGL((prefix_kernel<2, I8>), grid, small, 0, stream, a);
-    else if (tile_rows == 64) hipLaunchKernelGGL((prefix_tile_kernel<2, I8>), grid, large, 0, stream, a);
-    else if (tile_rows == 128) hipLaunchKernelGGL((prefix_tile_kernel<4, I8>), grid, large, 0, stream, a);
-    else hipLaunchKernelGGL((prefix_tile_kernel<8, I8>), grid, large, 0, stream, a);
+void launch_prefix(int tile_rows, hipStream_t stream, const PrefixArgs& a, bool own8, unsigned own_wgs, const OwnArgs& o) {
+    const dim3 wgs((unsigned)a.wgs), both(a.wgs + own_wgs), small(kThreads), large(kPrefixTileThreads);
+    if (tile_rows == 16 && own8) hipLaunchKernelGGL((prefix_kernel<1, I8, true>), both, small, 0, stream, a, o);
+    else if (tile_rows == 16) hipLaunchKernelGGL((prefix_kernel<1, I8, false>), both, small, 0, stream, a, o);
+    else if (tile_rows == 32 && own8) hipLaunchKernelGGL((prefix_kernel<2, I8, true>), both, small, 0, stream, a, o);
+    else if (tile_rows == 32) hipLaunchKernelGGL((prefix_kernel<2, I8, false>), both, small, 0, stream, a, o);
+    else if (tile_rows == 64) hipLaunchKernelGGL((prefix_tile_kernel<2, I8>), wgs, large, 0, stream, a);
+    else if (tile_rows == 128) hipLaunchKernelGGL((prefix_tile_kernel<4, I8>), wgs, large, 0, stream, a);
+    else hipLaunchKernelGGL((prefix_tile_kernel<8, I8>), wgs, large, 0, stream, a);
+    if (tile_rows > 32) launch_own(own8, own_wgs, stream, o);
 }
 
 int check_pcap(int Pcap) {
@@ -757,8 +762,9 @@ int ffd_dense_decode_attention(const void* q, const void* k, const void* v, cons
     const int G = Hq / Hkv;
     DenseArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), seq_lens,
                 o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, S, scale};
-    if (G <= 4) hipLaunchKernelGGL(dense_decode_kernel<1>, o.grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL(dense_decode_kernel<2>, o.grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid = o.table ? dim3(o.wgs) : dim3((unsigned)S, (unsigned)Hkv, (unsigned)B);
+    if (G <= 4) hipLaunchKernelGGL(dense_decode_kernel<1>, grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(dense_decode_kernel<2>, grid, dim3(kThreads), 0, stream, a);
     st = launch_status();
     if (st != FFD_OK) return st;
     launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? G : 1, static_cast<uint16_t*>(out), lse);
@@ -832,7 +838,9 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
     S = kv8_splits(B, Hkv, Lcap, num_splits);
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
-    launch_own(o, static_cast<const uint16_t*>(q), *cache, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    const OwnArgs a{static_cast<const uint16_t*>(q), source_of(*cache), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv,
+                    Lcap, Hq / Hkv, S, scale};
+    launch_own(true, o.wgs, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
     launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
     return launch_status();
@@ -868,12 +876,12 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     PrefixPlace* places = plan.sorted ? reinterpret_cast<PrefixPlace*>(ws + plan.places_off) : nullptr;
     const OwnPartials o = own_partials(Partials{P.m + plan.rows, P.l + plan.rows, P.acc + plan.rows * kD}, ws + plan.own_table_off, B, Hkv, S);
     const uint16_t* qp = static_cast<const uint16_t*>(q);
-    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles, scale};
-    const dim3 grid((unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles));
-    if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, grid, stream, a);
-    else launch_prefix<false>(plan.tile_rows, grid, stream, a);
-    if ((st = launch_status()) != FFD_OK) return st;
-    launch_own(o, qp, *own, seq_lens, B, Hq, Hkv, Lcap, S, scale, stream);
+    const unsigned wgs = (unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles);
+    const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles,
+                       (int)wgs, scale};
+    const OwnArgs oa{qp, source_of(*own), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, S, scale};
+    if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);
+    else launch_prefix<false>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);
     if ((st = launch_status()) != FFD_OK) return st;
     const SharedMergeArgs m{P.m, P.l, P.acc, plan.rows, o.table, places, static_cast<uint16_t*>(out), lse,
                             Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};

@@ -171,7 +171,7 @@ struct ReadKv8Args {
 };
 constexpr int kReadTokens = 64;                // tokens per workgroup of the read
 
-// Attention over one cache, bf16 (absmax null) or 8-bit, see ffd_attend.hip.
+// Attention over one cache, bf16 (absmax null) or 8-bit, see ffd_attend.h.
 struct KvSource {
     const uint8_t* k;           // [.., cap, 128] bf16 or int8
     const uint8_t* v;
@@ -211,6 +211,7 @@ struct PrefixArgs {
     float* part_acc;
     PrefixPlace* places;        // [B] or null
     int B, Hq, Hkv, Pcap, G, S, tiles;
+    int wgs;                    // workgroups of the prefix; those behind them take the own caches
     float scale;
 };
 
@@ -269,8 +270,8 @@ template <int BITS> __global__ void append_kv_kernel(AppendArgs a);
 __global__ void write_kv8_kernel(WriteKv8Args a);
 __global__ void read_kv8_kernel(ReadKv8Args a);
 template <bool I8> __global__ void own_decode_kernel(OwnArgs a);
-// CT (1, 2): tiles of 16 query rows per workgroup; I8: an 8-bit prefix.
-template <int CT, bool I8> __global__ void prefix_kernel(PrefixArgs a);
+// CT (1, 2): tiles of 16 query rows per workgroup; I8: an 8-bit prefix, OWN8: 8-bit own caches.
+template <int CT, bool I8, bool OWN8> __global__ void prefix_kernel(PrefixArgs a, OwnArgs own);
 constexpr int kPrefixTileThreads = 512;
 // RW (2, 4, 8): groups of 32 query rows per workgroup.
 template <int RW, bool I8> __global__ void prefix_tile_kernel(PrefixArgs a);
