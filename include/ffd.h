@@ -280,6 +280,7 @@ typedef struct ffd_kv {
  *   k_new, v_new   bf16 [B, T, Hkv, D], the dims of a vector contiguous; k_strides, v_strides are HOST arrays of
  *                  three strides in elements (sequence, token, head), each >= 0 and a multiple of 8, or NULL for a
  *                  contiguous tensor.
+ *                  T <= 2^28, else FFD_ERR_UNSUPPORTED.
  *   start          int32 [B] (device);  counts  int32 [B] (device) or NULL for T everywhere; values above T mean T,
  *                  negative ones 0.
  */
@@ -298,7 +299,8 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
 /*
  * Exact dense decode attention over an 8-bit cache: ffd_dense_decode_attention with k = n M / 127 and v likewise,
  * neither rounded to bf16. Arguments are those of that call; the cache holds B sequences, the workspace takes
- * ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
+ * ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20 and B * Hkv * (S + 1) < 2^23 (S as there), else
+ * FFD_ERR_UNSUPPORTED.
  */
 int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
                              int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
@@ -324,7 +326,8 @@ size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_
  *   out, lse      as ffd_dense_decode_attention; a sequence with no token at all gets out = 0, lse = -inf
  *   workspace     ffd_shared_prefix_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that
  *                 overlap in time need separate workspaces.
- * B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
+ * B * Hkv <= 2^20 and B * Hkv * (splits + 1) < 2^23, fewer than 2^22 runs of the prefix over all KV heads and tiles,
+ * else FFD_ERR_UNSUPPORTED.
  */
 int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
                                        const ffd_kv* own, const int32_t* seq_lens, int B, int Hq, int Hkv, int Lcap,

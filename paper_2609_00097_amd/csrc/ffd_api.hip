@@ -413,6 +413,11 @@ int kv8_splits(int B, int Hkv, int Lcap, int num_splits) {
     return (int)std::max<long long>(s, wide / pairs - 1);
 }
 
+// What a launch takes: fewer than 2^32 threads (both attentions may share it), and pairs as the int indices of the kernels and the merge take them.
+bool own_fits(int B, int Hkv, int S) {
+    return (long long)B * Hkv <= (1LL << 20) && (S + 1LL) * B * Hkv * kThreads < (1LL << 31);
+}
+
 // Pointers of a cache argument: all there and aligned; *bits is 8 or 16. An 8-bit one is required where only8.
 int check_kv(const ffd_kv* c, bool only8, int* bits) {
     if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return FFD_ERR_INVALID_ARGUMENT;
@@ -448,6 +453,7 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      
 // read once), at most 256; as many runs as give each CU one workgroup (two of the small ones that fit there).
 struct PrefixPlan {
     int tile_rows, tiles, S;
+    long long wgs;
     bool sorted;                      // the order of sequences and the tiles' workgroups follow the lengths
     size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
     size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
@@ -465,6 +471,7 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_o
         s = std::max(1LL, std::min(s, (long long)FFD_MAX_SPLITS));
     }
     p.S = (int)s;
+    p.wgs = ((long long)Hkv * p.S + 7) / 8 * 8 * p.tiles;
     p.sorted = p.tiles > 1 && B <= kPrefixSortSeqs;
     p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
     p.all_rows = p.rows + own_rows(B, Hq, S_own);
@@ -473,6 +480,8 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_o
     p.total = p.own_table_off + (B <= kDenseBalanceMaxSeqs ? (size_t)B * Hkv * sizeof(int2) : 0);
     return p;
 }
+
+bool prefix_fits(const PrefixPlan& p) { return p.wgs * kPrefixTileThreads < (1LL << 31); }
 
 void launch_own(bool i8, unsigned wgs, hipStream_t stream, const OwnArgs& o) {
     if (i8) hipLaunchKernelGGL(own_decode_kernel<true>, dim3(wgs), dim3(kThreads), 0, stream, o);
@@ -777,6 +786,7 @@ int ffd_write_kv8(const void* k_new, const void* v_new, const int64_t* k_strides
     int st = check_shapes(B, Hkv, Hkv, Lcap, D);
     if (st != FFD_OK) return st;
     if (T < 0) return FFD_ERR_INVALID_ARGUMENT;
+    if (T > 1 << 28) return FFD_ERR_UNSUPPORTED;
     const int64_t contiguous[3] = {(int64_t)T * Hkv * D, (int64_t)Hkv * D, D};
     if (!k_strides) k_strides = contiguous;
     if (!v_strides) v_strides = contiguous;
@@ -818,9 +828,9 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
 }
 
 size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_splits) {
-    if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || (long long)B * Hkv > (1LL << 20)) return 0;
+    if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0) return 0;
     const int S = kv8_splits(B, Hkv, Lcap, num_splits);
-    if (S <= 0) return 0;
+    if (S <= 0 || !own_fits(B, Hkv, S)) return 0;
     return round_up(partials_bytes(own_rows(B, Hq, S)), kAlign) + (B <= kDenseBalanceMaxSeqs ? (size_t)B * Hkv * sizeof(int2) : 0);
 }
 
@@ -832,10 +842,10 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
     int st = attention_common_checks(q, cache ? cache->v : nullptr, seq_lens, B, Hq, Hkv, Lcap, D, num_splits,
                                      softmax_scale, out, lse, workspace, workspace_bytes, true, &S);
     if (st != FFD_OK || B == 0) return st;
-    if ((long long)B * Hkv > (1LL << 20)) return FFD_ERR_UNSUPPORTED;
+    S = kv8_splits(B, Hkv, Lcap, num_splits);
+    if (!own_fits(B, Hkv, S)) return FFD_ERR_UNSUPPORTED;
     if ((st = check_kv(cache, true, &bits)) != FFD_OK) return st;
     if (workspace_bytes < ffd_kv8_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
-    S = kv8_splits(B, Hkv, Lcap, num_splits);
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
     const OwnArgs a{static_cast<const uint16_t*>(q), source_of(*cache), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv,
@@ -849,8 +859,9 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits) {
     if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || check_pcap(Pcap) != FFD_OK) return 0;
     const int S = resolve_splits(B, Hkv, Lcap, num_splits, true);
-    if (S <= 0 || (long long)B * Hkv > (1LL << 20)) return 0;
-    return prefix_plan(B, Hq, Hkv, Pcap, num_splits, S).total;
+    if (S <= 0 || !own_fits(B, Hkv, S)) return 0;
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
+    return prefix_fits(plan) ? plan.total : 0;
 }
 
 int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
@@ -863,22 +874,22 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
                                      softmax_scale, out, lse, workspace, workspace_bytes, true, &S);
     if (st != FFD_OK) return st;
     if ((st = check_pcap(Pcap)) != FFD_OK || B == 0) return st;
-    if ((long long)B * Hkv > (1LL << 20)) return FFD_ERR_UNSUPPORTED;
+    if (!own_fits(B, Hkv, S)) return FFD_ERR_UNSUPPORTED;
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
+    if (!prefix_fits(plan)) return FFD_ERR_UNSUPPORTED;
     if ((st = check_kv(prefix, false, &prefix_bits)) != FFD_OK || (st = check_kv(own, false, &own_bits)) != FFD_OK) return st;
     if (!prefix_lens || (reinterpret_cast<uintptr_t>(prefix_lens) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
     if (workspace_bytes < ffd_shared_prefix_workspace_bytes(B, Hq, Hkv, Pcap, Lcap, D, num_splits))
         return FFD_ERR_WORKSPACE_TOO_SMALL;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const int G = Hq / Hkv;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
     const Partials P = carve(workspace, plan.all_rows);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     PrefixPlace* places = plan.sorted ? reinterpret_cast<PrefixPlace*>(ws + plan.places_off) : nullptr;
     const OwnPartials o = own_partials(Partials{P.m + plan.rows, P.l + plan.rows, P.acc + plan.rows * kD}, ws + plan.own_table_off, B, Hkv, S);
     const uint16_t* qp = static_cast<const uint16_t*>(q);
-    const unsigned wgs = (unsigned)((((long long)Hkv * plan.S + 7) / 8) * 8 * plan.tiles);
     const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles,
-                       (int)wgs, scale};
+                       (int)plan.wgs, scale};
     const OwnArgs oa{qp, source_of(*own), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, S, scale};
     if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);
     else launch_prefix<false>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);

@@ -247,6 +247,48 @@ def _capture(fn):
     return g
 
 
+@pytest.mark.parametrize("B,bits", [(3, 8), (12, 16), (40, 8), (70, 16)])
+def test_workspaces_hold_anything(B, bits):
+    """A workspace of NaN (all bits set) changes nothing, in the middle of sequences without tokens."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B)
+    Hq, Hkv, P, L = 8, 2, 640, 192
+    q, prefix, cache = _normal(gen, B, Hq, D), random_cache(gen, 1, Hkv, P, bits), random_cache(gen, B, Hkv, L, bits)
+    prefix_lens, lens = _int32([(97 * b) % P * (b % 3 > 0) for b in range(B)]), _int32([(29 * b) % L * (b % 2) for b in range(B)])
+    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, P, L)
+    want = ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens, workspace=ws.zero_())
+    got = ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens, workspace=ws.fill_(255))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    if bits == 8:
+        ws = ffd.new_kv8_workspace(B, Hq, Hkv, L)
+        want = ffd.kv8_decode_attention(q, cache, lens, workspace=ws.zero_())
+        got = ffd.kv8_decode_attention(q, cache, lens, workspace=ws.fill_(255))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_two_calls_at_once():
+    """Two streams with a workspace each, a small batch and one of two row tiles, give what one after the other does."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(51)
+    jobs = []
+    for B, P in ((4, 8192), (66, 4096)):
+        lens, cache = _int32([(31 * b) % 256 for b in range(B)]), random_cache(gen, B, 2, 256, 16)
+        prefix_lens = _int32([P - 50 * b for b in range(B)])
+        jobs.append((_normal(gen, B, 8, D), random_cache(gen, 1, 2, P, 8), prefix_lens, cache, lens))
+    spaces = [ffd.new_shared_prefix_workspace(len(j[0]), 8, 2, j[1][0].shape[2], 256) for j in jobs]
+    want = [ffd.shared_prefix_decode_attention(*j, workspace=w) for j, w in zip(jobs, spaces)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[] for _ in jobs]
+    for _ in range(8):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(ffd.shared_prefix_decode_attention(*jobs[i], workspace=spaces[i]))
+    torch.cuda.synchronize()
+    for results, (out, lse) in zip(got, want):
+        assert all(torch.equal(o, out) and torch.equal(l, lse) for o, l in results)
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 def test_a_served_batch(bits):
     """As a serving program uses them together: a prompt is written once, a captured step (write or copy the new

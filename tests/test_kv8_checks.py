@@ -137,6 +137,19 @@ def test_shared_prefix_workspace(so):
         assert size(*bad) == 0
 
 
+def test_launches_past_the_limits_are_refused(so):
+    huge = dict(ws_bytes=1 << 62)
+    assert so.ffd_kv8_workspace_bytes(16, 65535, 65535, 64, 128, 64) == 0        # 2^20 groups of 65 workgroups
+    assert _attend(so, B=16, Hq=65535, Hkv=65535, Lcap=64, splits=64, **huge) == 2
+    assert so.ffd_shared_prefix_workspace_bytes(16, 65535, 65535, 64, 64, 128, 64) == 0
+    assert _shared(so, B=16, Hq=65535, Hkv=65535, Pcap=64, Lcap=64, splits=64, **huge) == 2
+    # 8000 groups of 1025 workgroups pass the first limit, 8000 heads of 1024 runs of the prefix do not
+    assert so.ffd_kv8_workspace_bytes(1, 8000, 8000, 64, 128, 1024) > 0
+    assert so.ffd_shared_prefix_workspace_bytes(1, 8000, 8000, 64, 64, 128, 1024) == 0
+    assert _shared(so, B=1, Hq=8000, Hkv=8000, Pcap=64, Lcap=64, splits=1024, **huge) == 2
+    assert so.ffd_write_kv8(FAKE, FAKE, None, None, _kv(), FAKE, None, 1, (1 << 28) + 1, 8, 4096, 128, None) == 2
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     from paper_2609_00097_amd import ffd
     cache = ffd.empty_kv8(2, 8, 128, device="cpu")
