@@ -140,6 +140,12 @@ template <> struct ValueTile<false> {
         }
         return max(m & 0xffffu, m >> 16) < 0x7f80u;
     }
+    // Rows at and behind `end` of the tile to zero.
+    __device__ __forceinline__ void clear_from(int end, int g) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (value_token(e, g) >= end) v[e] = make_uint4(0u, 0u, 0u, 0u);
+    }
     // Infinities and NaN to zero.
     __device__ __forceinline__ void make_finite() {
         auto fix = [](uint32_t w) {
@@ -223,7 +229,7 @@ __device__ __forceinline__ void add_nonfinite(RowState<CT>& st, const uint16_t* 
 // lane's row sees) clamps the rows read: those behind it may hold anything. Row n of tile c sees tokens below lim[c];
 // tiles that end at or before `full` are seen whole by every row. zscale turns a product into z2. SPLIT: rows n and
 // n + 8 are the same query, and their probabilities the high and the low half of one: p = hi + lo, both bf16, so
-// that p is rounded to 2^-17 and not to 2^-9 (the instruction has the rows to spare).
+// that p is rounded to 2^-17 and not to 2^-9 (the instruction has the rows to spare); all rows see `rows` tokens then.
 template <int CT, bool I8, bool SPLIT>
 __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4], const KvSource& kv, int begin, int end,
                                        int rows, const int (&lim)[CT], int full, float zscale, int wave, int n, int g) {
@@ -306,7 +312,9 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
             }
             p[c] = __builtin_bit_cast(v8bf, make_uint4(w[0], w[1], w[2], w[3]));
         }
-        if constexpr (!I8) {
+        if constexpr (SPLIT && !I8) {
+            if (masked) vt.clear_from(rows - t0, g);        // behind the last token: zero times infinity
+        } else if constexpr (!I8) {
             if (masked && __ballot(!vt.all_finite()) != 0) {
                 vt.make_finite();
                 add_nonfinite<CT>(st, reinterpret_cast<const uint16_t*>(kv.v), t0, rows, lim, g);
@@ -407,8 +415,7 @@ __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, in
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
     const bool balanced = a.table != nullptr;
-    const int s = wg % a.S;
-    int kvh = wg / a.S % a.Hkv, b = wg / a.S / a.Hkv, L = 0, jb = 0, je = 0;
+    int kvh, b, L, jb, je, s = 0;
     if (balanced) {
         if (!balanced_share(a, wg, lane, b, kvh, L, jb, je)) return;
         b = __builtin_amdgcn_readfirstlane(b);
@@ -416,6 +423,9 @@ __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, in
         jb = __builtin_amdgcn_readfirstlane(jb);
         je = __builtin_amdgcn_readfirstlane(je);
     } else {
+        s = wg % a.S;
+        kvh = wg / a.S % a.Hkv;
+        b = wg / a.S / a.Hkv;
         L = min(max(a.seq_lens[b], 0), a.Lcap);
         const int nblk = (L + kBlock - 1) / kBlock, bps = (nblk + a.S - 1) / a.S;
         jb = min(s * bps, nblk);
@@ -438,7 +448,8 @@ __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, in
     for (int i = tid; i < G * kD; i += kThreads) {
         const int h = i >> 7, d = i & (kD - 1);
         const size_t row = out0 + h * stride;
-        a.part_acc[row * kD + d] = (lds.acc[0][h][d] + lds.acc[1][h][d]) + (lds.acc[0][h + 8][d] + lds.acc[1][h + 8][d]);
+        const float hi = lds.acc[0][h][d] + lds.acc[1][h][d], lo = lds.acc[0][h + 8][d] + lds.acc[1][h + 8][d];
+        a.part_acc[row * kD + d] = fabsf(hi) < INFINITY ? hi + lo : hi;     // a low half may be zero: not times infinity
         if (d == 0) {
             float m, l;
             joined_ml(lds, h, m, l);

@@ -110,6 +110,28 @@ def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies):
     check_attention((o[fine], lse.cpu()[fine]), tuple(t[fine] for t in clean), 310, P_BF16)
 
 
+@pytest.mark.parametrize("G", [1, 4, 8])
+def test_infinities_and_nan_in_own_caches(G):
+    """In tiles that end inside the sequence and in whole ones, behind them and at the last token."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(7)
+    lens, prefix_lens = [100, 128, 1, 45, 300, 31], [0, 5, 10, 0, 64, 0]
+    B = len(lens)
+    q = _normal(gen, B, G, D)
+    prefix, cache = random_cache(gen, 1, 1, 64, 16), random_cache(gen, B, 1, 320, 16)
+    clean = _reference(q, prefix, prefix_lens, cache, lens)
+    _spoil(cache, lens)
+    special = [(0, 7, 3, math.inf), (0, 99, 9, -math.inf), (1, 64, 17, math.nan), (1, 127, 5, math.inf), (2, 0, 100, math.inf),
+               (3, 44, 127, -math.inf), (4, 200, 64, math.inf), (4, 290, 0, -math.inf), (5, 2, 2, math.inf)]
+    for b, t, d, x in special:
+        cache[1][b, 0, t, d] = x
+    out, lse = (t.cpu() for t in ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens)))
+    for b, t, d, x in special:
+        assert out[b, :, d].isnan().all() if math.isnan(x) else bool((out[b, :, d] == x).all()), f"sequence {b}, token {t}"
+        out[b, :, d] = clean[0][b, :, d].bfloat16()
+    check_attention((out, lse), clean, 364, P_BF16)
+
+
 @pytest.mark.parametrize("G", [1, 8])
 def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G):
     from paper_2609_00097_amd import ffd
