@@ -336,8 +336,8 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
 
 /* Workspace bytes of ffd_shared_prefix_decode_attention: (D + 2) * 4 bytes for each query row (their number per KV head
  * rounded up to the kernel's row tiles) and run of the prefix, and for each row of ffd_dense_decode_attention's partials;
- * then, each on a 256-byte boundary, for up to 256 sequences 16 bytes each where there are several row tiles, and
- * a table of B * Hkv * 8 bytes. 0 on invalid or unsupported input. */
+ * then, each on a 256-byte boundary, for up to 256 sequences 16 bytes each where there are several tiles of 256 rows,
+ * and a table of B * Hkv * 8 bytes. 0 on invalid or unsupported input. */
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits);
 
 /* The split count S for this num_splits (0 = automatic), which sizes the workspace: num_splits itself, or

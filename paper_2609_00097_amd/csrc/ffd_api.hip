@@ -450,7 +450,12 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      
 }
 
 // Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head (a prefix is then
-// read once), at most 256; as many runs as give each CU one workgroup (two of the small ones that fit there).
+// read once), at most 256, and as many runs as give each CU one workgroup (64K, eight KV heads, whole calls: 16 rows 52
+// us, with two per CU 56, 32 rows 54 and 58; 128 rows 71, with two waves of workgroups 97).
+// More than 32 rows over little work are several tiles of 32, whose workgroups start sooner and take the own caches along,
+// though each reads the prefix (out of its XCD's L2): up to 80K query rows times tokens per CU. Tiles of 32 / one tile of
+// them all, eight KV heads: 64 rows on 4K 15 / 25 us, on 16K 22.7 / 30.5, on 40K 47.7 / 51.0, 128 rows on 4K 17.5 / 26.9,
+// on 16K 32.4 / 35.3, on 20K (the limit) 42.9 / 43.4, on 32K 54.6 / 45.6; 256 on 8K 32.3 / 37.6, on 16K 52.6 / 46.8.
 struct PrefixPlan {
     int tile_rows, tiles, S;
     long long wgs;
@@ -458,21 +463,23 @@ struct PrefixPlan {
     size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
     size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
 };
+constexpr long long kSmallTileWork = 80 << 10;       // query rows times prefix tokens, per CU
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_own) {
     const long long rows = (long long)B * (Hq / Hkv);
     PrefixPlan p;
     p.tile_rows = 16;
     while (p.tile_rows < rows && p.tile_rows < 256) p.tile_rows *= 2;
+    if (rows > 32 && rows * Hkv * Pcap <= kSmallTileWork * device_cus()) p.tile_rows = 32;
     p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
     long long s = num_splits;
     if (s == 0) {
-        s = (p.tile_rows <= 32 ? 2LL : 1LL) * device_cus() / ((long long)Hkv * p.tiles);
+        s = (long long)device_cus() / ((long long)Hkv * p.tiles);
         s = std::min(s, (long long)(Pcap + 127) / 128);
         s = std::max(1LL, std::min(s, (long long)FFD_MAX_SPLITS));
     }
     p.S = (int)s;
     p.wgs = ((long long)Hkv * p.S + 7) / 8 * 8 * p.tiles;
-    p.sorted = p.tiles > 1 && B <= kPrefixSortSeqs;
+    p.sorted = p.tile_rows == 256 && p.tiles > 1 && B <= kPrefixSortSeqs;
     p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
     p.all_rows = p.rows + own_rows(B, Hq, S_own);
     p.places_off = round_up(partials_bytes(p.all_rows), kAlign);

@@ -23,7 +23,10 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, OwnAr
     JoinLds<CT>& lds = sm.lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
-    const int pair = blockIdx.x;                        // one row tile
+    // Workgroups of one run but different tiles read the same tokens: they are eight apart, on one XCD (consecutive
+    // workgroups go to the eight XCDs in turn).
+    const int tile = (int)(blockIdx.x >> 3) % a.tiles;
+    const int pair = (int)(blockIdx.x >> 3) / a.tiles * 8 + (int)(blockIdx.x & 7);
     if (pair >= a.Hkv * a.S) return;
     const int kvh = pair / a.S, run = pair % a.S;
     const int rows = a.B * a.G;
@@ -32,13 +35,13 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, OwnAr
     int len[CT], lim[CT], longest = 0, shortest = INT32_MAX;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {                      // queries and lengths, asked for together
-        const int r = 16 * c + n, b = min(r >> gs, a.B - 1);
+        const int r = (tile * CT + c) * 16 + n, b = min(r >> gs, a.B - 1);
         load_query<I8>(q[c], a.q + ((size_t)b * a.Hq + kvh * a.G + (r & (a.G - 1))) * kD, g);
         len[c] = a.prefix_lens[b];
     }
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const bool live = 16 * c + n < rows;
+        const bool live = (tile * CT + c) * 16 + n < rows;
         lim[c] = live ? min(max(len[c], 0), a.Pcap) : INT32_MAX;
         longest = max(longest, live ? lim[c] : 0);
         shortest = min(shortest, lim[c]);
@@ -61,8 +64,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, OwnAr
     st.clear();
     attend<CT, I8, false>(st, q, kv, begin, end, longest, lim, shortest, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
     join_waves(lds, st, wave, n, g);
-    const size_t out0 = (size_t)pair * (16 * CT);
-    for (int i = tid; i < rows * (kD / 4); i += kThreads) {
+    const size_t out0 = ((size_t)pair * a.tiles + tile) * (16 * CT);
+    const int live = min(16 * CT, rows - tile * 16 * CT);
+    for (int i = tid; i < live * (kD / 4); i += kThreads) {
         const int r = i >> 5, d4 = i & 31;
         const float4 x = *reinterpret_cast<const float4*>(&lds.acc[0][r][4 * d4]);
         const float4 y = *reinterpret_cast<const float4*>(&lds.acc[1][r][4 * d4]);

@@ -193,7 +193,7 @@ struct OwnArgs {
 };
 
 // Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in `tiles` tiles of R
-// rows (16 CT of prefix_kernel, up to 32 rows; 32 RW of prefix_tile_kernel), S * tiles workgroups per KV head, workgroup
+// rows (16 CT of prefix_kernel; 32 RW of prefix_tile_kernel), S * tiles workgroups per KV head, workgroup
 // w of them writing R partial rows from (kvh * S * tiles + w) * R on. Without `places` tile t has S equal runs, those of
 // workgroups t, t + tiles, ..; with it (prefix_tile_kernel<8>) the sequences' order and the tiles' workgroups follow
 // the lengths.

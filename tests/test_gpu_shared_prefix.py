@@ -32,14 +32,31 @@ def _spoil(cache, lens):
             t[b, :, max(n, 0):] = 127 if t.dtype == torch.int8 else math.nan
 
 
+def _with_room(prefix, rows, room):
+    """The prefix in a capacity for which more than 32 query rows are not cut into tiles of 32, NaN behind its tokens."""
+    if not room or rows <= 32:
+        return prefix
+    Hkv, P = prefix[0].shape[1:3]
+    work = 81 * 1024 * torch.cuda.get_device_properties(0).multi_processor_count
+    cap = 64 * -(-work // (64 * rows * Hkv))
+    if cap <= P:
+        return prefix
+    whole = tuple(torch.empty(1, Hkv, cap, *t.shape[3:], dtype=t.dtype, device="cuda") for t in prefix)
+    _spoil(whole, [P])
+    for big, t in zip(whole, prefix):
+        big[:, :, :P] = t
+    return whole
+
+
 def _reference(q, prefix, prefix_lens, cache, lens, scale=None):
     return attention(q, [(*values(prefix), prefix_lens), (*values(cache), lens)], scale)
 
 
 # query rows of a KV head (B * G) around the kernel's tiles of 16, 32 and 64 rows
 @pytest.mark.parametrize("B,Hq,Hkv", [(1, 1, 1), (1, 16, 2), (4, 8, 2), (17, 2, 2), (8, 8, 2), (33, 1, 1), (16, 4, 1), (13, 10, 2)])
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("prefix_bits,own_bits", [(16, 16), (8, 8), (8, 16), (16, 8)])
-def test_full_prefix(B, Hq, Hkv, prefix_bits, own_bits):
+def test_full_prefix(B, Hq, Hkv, prefix_bits, own_bits, room):
     from paper_2609_00097_amd import ffd
     if Hq // Hkv not in (1, 2, 4, 8):
         Hq = 8 * Hkv
@@ -49,12 +66,13 @@ def test_full_prefix(B, Hq, Hkv, prefix_bits, own_bits):
     prefix, cache = random_cache(gen, 1, Hkv, _cap([P]), prefix_bits), random_cache(gen, B, Hkv, _cap(lens), own_bits)
     _spoil(prefix, [P])
     _spoil(cache, lens)
-    print(f"case shared B={B} Hq={Hq} Hkv={Hkv} bits {prefix_bits} {own_bits}", flush=True)
-    got = ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens))
+    print(f"case shared B={B} Hq={Hq} Hkv={Hkv} bits {prefix_bits} {own_bits} room {room}", flush=True)
+    got = ffd.shared_prefix_decode_attention(q, _with_room(prefix, B * (Hq // Hkv), room), _int32([P] * B), cache, _int32(lens))
     torch.cuda.synchronize()
     check_attention(got, _reference(q, prefix, [P] * B, cache, lens), P + 130, P_BF16)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("prefix_lens,lens", [
     ([0, 1, 31, 32, 33, 127, 128, 129], [0, 0, 1, 64, 65, 3, 0, 0]),
@@ -63,25 +81,28 @@ def test_full_prefix(B, Hq, Hkv, prefix_bits, own_bits):
     ([64], [0]),
     ([0, 0], [0, 0]),
 ])
-def test_parts_of_the_prefix(bits, prefix_lens, lens):
+def test_parts_of_the_prefix(bits, prefix_lens, lens, room):
     from paper_2609_00097_amd import ffd
     gen = _gen(len(lens) + bits)
     B, Hq, Hkv, Pcap = len(lens), 16, 2, 4032
     q = _normal(gen, B, Hq, D)
     prefix, cache = random_cache(gen, 1, Hkv, Pcap, bits), random_cache(gen, B, Hkv, 128, bits)
+    if room:                                              # the longest one is not clamped then
+        prefix_lens = [min(n, Pcap) for n in prefix_lens]
     clamped = [min(max(n, 0), Pcap) for n in prefix_lens]
     own = [min(max(n, 0), 128) for n in lens]
     _spoil(prefix, [max(clamped)])
     _spoil(cache, own)
-    print(f"case shared parts {prefix_lens} {lens} bits {bits}", flush=True)
-    got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+    print(f"case shared parts {prefix_lens} {lens} bits {bits} room {room}", flush=True)
+    got = ffd.shared_prefix_decode_attention(q, _with_room(prefix, 8 * B, room), _int32(prefix_lens), cache, _int32(lens))
     torch.cuda.synchronize()
     check_attention(got, _reference(q, prefix, clamped, cache, own), Pcap + 128, P_BF16)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("G", [1, 2, 4, 8])
 @pytest.mark.parametrize("copies", [1, 9])
-def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies):
+def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies, room):
     """Keys and values of prefix tokens that some sequences use and others do not, within one tile of tokens and in
     tiles of their own; from 5 to 360 query rows."""
     from paper_2609_00097_amd import ffd
@@ -95,6 +116,7 @@ def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies):
     prefix[1][0, 0, 50, 17] = math.nan
     prefix[0][0, 0, 250, 3] = math.nan
     prefix[1][0, 0, 299, 100] = -math.inf
+    prefix = _with_room(prefix, B * G, room)
     out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
     torch.cuda.synchronize()
     used = torch.tensor(prefix_lens)
@@ -132,8 +154,9 @@ def test_infinities_and_nan_in_own_caches(G):
     check_attention((out, lse), clean, 364, P_BF16)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("G", [1, 8])
-def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G):
+def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G, room):
     from paper_2609_00097_amd import ffd
     gen = _gen(6)
     prefix_lens, lens = [40, 44, 60, 200, 300] * 5, [3, 0, 10, 0, 1] * 5
@@ -142,6 +165,7 @@ def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G):
     clean = _reference(q, prefix, prefix_lens, cache, lens)
     prefix[3][0, 0, 42] = math.nan                        # a value
     prefix[1][0, 0, 250] = math.nan                       # a key
+    prefix = _with_room(prefix, 25 * G, room)
     out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
     torch.cuda.synchronize()
     fine = torch.tensor(prefix_lens) <= 42
@@ -149,15 +173,17 @@ def test_a_nan_token_of_an_8_bit_prefix_reaches_only_the_rows_that_see_it(G):
     check_attention((out.cpu()[fine], lse.cpu()[fine]), tuple(t[fine] for t in clean), 310, P_BF16)
 
 
-def test_splits_scale_and_given_outputs():
+@pytest.mark.parametrize("room", [False, True])
+def test_splits_scale_and_given_outputs(room):
     from paper_2609_00097_amd import ffd
     gen = _gen(7)
-    B, Hq, Hkv, P, lens = 6, 8, 2, 2500, [700, 0, 1, 64, 333, 10]
+    B, Hq, Hkv, P, lens = (12 if room else 6), 8, 2, 2500, [700, 0, 1, 64, 333, 10] * (2 if room else 1)
     q, prefix, cache = _normal(gen, B, Hq, D), random_cache(gen, 1, Hkv, _cap([P])), random_cache(gen, B, Hkv, 704, 16)
     ref = _reference(q, prefix, [P] * B, cache, lens, 0.15)
+    prefix = _with_room(prefix, 4 * B, room)
     for splits in (1, 2, 9, 40, 0):                       # 40: more runs than the prefix has rounds
         out, lse = torch.full_like(q, 7.0), torch.full((B, Hq), 7.0, device="cuda")
-        ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, _cap([P]), 704, splits)
+        ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, prefix[0].shape[2], 704, splits)
         ws.fill_(255)                                     # NaN wherever the call reads what it has not written
         got = ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens), num_splits=splits,
                                                  softmax_scale=0.15, workspace=ws, out=out, lse=lse)
@@ -175,7 +201,8 @@ def test_splits_scale_and_given_outputs():
         ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), (cache[0], cache[1][:, :, :64]), _int32(lens))
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("room", [False, True])
+def test_many_sequences(room):
     """300 sequences (the own caches beyond the balanced mode) in several row tiles, the last one in part."""
     from paper_2609_00097_amd import ffd
     gen = _gen(9)
@@ -184,15 +211,16 @@ def test_many_sequences():
     q = _normal(gen, B, Hq, D)
     for bits in (16, 8):
         prefix, cache = random_cache(gen, 1, Hkv, _cap([P]), bits), random_cache(gen, B, Hkv, 256, bits)
-        got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+        got = ffd.shared_prefix_decode_attention(q, _with_room(prefix, 4 * B, room), _int32(prefix_lens), cache, _int32(lens))
         torch.cuda.synchronize()
         check_attention(got, _reference(q, prefix, prefix_lens, cache, lens), P + 200, P_BF16)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("B,G,kind", [(70, 4, "equal"), (256, 2, "ragged"), (33, 8, "ragged"), (90, 8, "none"), (65, 8, "one"),
                                       (257, 1, "one"), (256, 8, "two")])
-def test_sequences_in_several_row_tiles(B, G, kind, bits):
+def test_sequences_in_several_row_tiles(B, G, kind, bits, room):
     """More query rows than a tile holds: the sequences are taken in order of their lengths where these differ, and the
     tiles get workgroups by theirs, some of them none."""
     from paper_2609_00097_amd import ffd
@@ -204,8 +232,9 @@ def test_sequences_in_several_row_tiles(B, G, kind, bits):
     q = _normal(gen, B, 2 * G, D)
     prefix, cache = random_cache(gen, 1, 2, _cap([P]), bits), random_cache(gen, B, 2, 64, bits)
     ref = _reference(q, prefix, prefix_lens, cache, lens)
+    prefix = _with_room(prefix, B * G, room)
     for splits in (0, 1, 5):
-        ws = ffd.new_shared_prefix_workspace(B, 2 * G, 2, _cap([P]), 64, splits)
+        ws = ffd.new_shared_prefix_workspace(B, 2 * G, 2, prefix[0].shape[2], 64, splits)
         ws.fill_(255)
         got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), num_splits=splits, workspace=ws)
         torch.cuda.synchronize()
@@ -269,15 +298,17 @@ def _capture(fn):
     return g
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("B,bits", [(3, 8), (12, 16), (40, 8), (70, 16)])
-def test_workspaces_hold_anything(B, bits):
+def test_workspaces_hold_anything(B, bits, room):
     """A workspace of NaN (all bits set) changes nothing, in the middle of sequences without tokens."""
     from paper_2609_00097_amd import ffd
     gen = _gen(B)
     Hq, Hkv, P, L = 8, 2, 640, 192
     q, prefix, cache = _normal(gen, B, Hq, D), random_cache(gen, 1, Hkv, P, bits), random_cache(gen, B, Hkv, L, bits)
     prefix_lens, lens = _int32([(97 * b) % P * (b % 3 > 0) for b in range(B)]), _int32([(29 * b) % L * (b % 2) for b in range(B)])
-    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, P, L)
+    prefix = _with_room(prefix, 4 * B, room)
+    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, prefix[0].shape[2], L)
     want = ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens, workspace=ws.zero_())
     got = ffd.shared_prefix_decode_attention(q, prefix, prefix_lens, cache, lens, workspace=ws.fill_(255))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
@@ -288,7 +319,8 @@ def test_workspaces_hold_anything(B, bits):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_two_calls_at_once():
+@pytest.mark.parametrize("room", [False, True])
+def test_two_calls_at_once(room):
     """Two streams with a workspace each, a small batch and one of two row tiles, give what one after the other does."""
     from paper_2609_00097_amd import ffd
     gen = _gen(51)
@@ -296,7 +328,8 @@ def test_two_calls_at_once():
     for B, P in ((4, 8192), (66, 4096)):
         lens, cache = _int32([(31 * b) % 256 for b in range(B)]), random_cache(gen, B, 2, 256, 16)
         prefix_lens = _int32([P - 50 * b for b in range(B)])
-        jobs.append((_normal(gen, B, 8, D), random_cache(gen, 1, 2, P, 8), prefix_lens, cache, lens))
+        prefix = _with_room(random_cache(gen, 1, 2, P, 8), 4 * B, room)
+        jobs.append((_normal(gen, B, 8, D), prefix, prefix_lens, cache, lens))
     spaces = [ffd.new_shared_prefix_workspace(len(j[0]), 8, 2, j[1][0].shape[2], 256) for j in jobs]
     want = [ffd.shared_prefix_decode_attention(*j, workspace=w) for j, w in zip(jobs, spaces)]
     torch.cuda.synchronize()

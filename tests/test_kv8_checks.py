@@ -130,7 +130,9 @@ def test_shared_prefix_workspace(so):
     up = lambda x: -(-x // 256) * 256
     assert size(2, 32, 8, 8192, 4096, 128, 3) == up((8 * 16 * 3 + 2 * 32 * (3 + 1)) * 130 * 4) + 2 * 8 * 8
     # two tiles of 256 rows: the sequences' places
-    assert size(70, 32, 8, 8192, 4096, 128, 3) == up((8 * 2 * 256 * 3 + 70 * 32 * 4) * 130 * 4) + up(70 * 16) + 70 * 8 * 8
+    assert size(70, 32, 8, 16384, 4096, 128, 3) == up((8 * 2 * 256 * 3 + 70 * 32 * 4) * 130 * 4) + up(70 * 16) + 70 * 8 * 8
+    # little work: nine tiles of 32 rows
+    assert size(70, 32, 8, 4096, 4096, 128, 3) == up((8 * 9 * 32 * 3 + 70 * 32 * 4) * 130 * 4) + 70 * 8 * 8
     assert size(300, 32, 8, 8192, 4096, 128, 3) == up((8 * 5 * 256 * 3 + 300 * 32 * 3) * 130 * 4)
     for bad in ((0, 32, 8, 8192, 4096, 128, 0), (2, 32, 8, 100, 4096, 128, 0), (2, 32, 8, 8192, 4096, 96, 0),
                 (2, 30, 8, 8192, 4096, 128, 0), (2, 32, 8, 8192, 4096, 128, 5000)):
