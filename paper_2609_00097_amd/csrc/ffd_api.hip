@@ -453,9 +453,10 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      
 // read once), at most 256, and as many runs as give each CU one workgroup (64K, eight KV heads, whole calls: 16 rows 52
 // us, with two per CU 56, 32 rows 54 and 58; 128 rows 71, with two waves of workgroups 97).
 // More than 32 rows over little work are several tiles of 32, whose workgroups start sooner and take the own caches along,
-// though each reads the prefix (out of its XCD's L2): up to 80K query rows times tokens per CU. Tiles of 32 / one tile of
-// them all, eight KV heads: 64 rows on 4K 15 / 25 us, on 16K 22.7 / 30.5, on 40K 47.7 / 51.0, 128 rows on 4K 17.5 / 26.9,
-// on 16K 32.4 / 35.3, on 20K (the limit) 42.9 / 43.4, on 32K 54.6 / 45.6; 256 on 8K 32.3 / 37.6, on 16K 52.6 / 46.8.
+// though each reads the prefix (out of its XCD's L2): up to 64K query rows times tokens per CU. Whole calls with up to 512
+// own tokens, eight KV heads, tiles of 32 / one tile of them all, bf16: 64 rows on 4K 17 / 27 us, on 16K 26.7 / 33.2, on
+// 32K 40.5 / 44.4 (8 bits 37.6 / 35.5); 128 rows on 4K 23 / 32, on 16K 36.9 / 40.9 (37.5 / 36.0), on 20K 44.1 / 43.7 (42.9 /
+// 38.4); 256 rows on 4K 28.6 / 40.3, on 8K 38.3 / 44.0, on 12K 50.8 / 51.5.
 struct PrefixPlan {
     int tile_rows, tiles, S;
     long long wgs;
@@ -463,7 +464,7 @@ struct PrefixPlan {
     size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
     size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
 };
-constexpr long long kSmallTileWork = 80 << 10;       // query rows times prefix tokens, per CU
+constexpr long long kSmallTileWork = 64 << 10;       // query rows times prefix tokens, per CU
 PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_own) {
     const long long rows = (long long)B * (Hq / Hkv);
     PrefixPlan p;

@@ -202,6 +202,16 @@ struct RowState {
             for (int i = 0; i < 8; ++i) o[c][i] = v4f{0.f, 0.f, 0.f, 0.f};
         }
     }
+    __device__ __forceinline__ bool all_finite() const {
+        float x = 0.f;                          // stays zero where every o is finite
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x = fmaf(o[c][i][r], 0.f, x);
+        return x == 0.f;
+    }
 };
 
 // What the instruction cannot do in a tile that some rows see only in part: infinities and NaN among the values of a
@@ -227,10 +237,14 @@ __device__ __forceinline__ void add_nonfinite(RowState<CT>& st, const uint16_t* 
 
 // Attends over tokens [begin, end) of kv: this wave's tiles of every round. `rows` (end of the tokens that any
 // lane's row sees) clamps the rows read: those behind it may hold anything. Row n of tile c sees tokens below lim[c];
-// tiles that end at or before `full` are seen whole by every row. zscale turns a product into z2. SPLIT: rows n and
-// n + 8 are the same query, and their probabilities the high and the low half of one: p = hi + lo, both bf16, so
-// that p is rounded to 2^-17 and not to 2^-9 (the instruction has the rows to spare); all rows see `rows` tokens then.
-template <int CT, bool I8, bool SPLIT>
+// tiles that end at or before `full` are seen whole by every row. zscale turns a product into z2.
+//
+// Probabilities are given to the instruction as p = hi + lo, both bf16, so that they are rounded to 2^-17 and not to
+// 2^-9: kSpareRows: rows n and n + 8 are the same query, one with hi and the other with lo, and all see `rows` tokens;
+// kTwoParts: two instructions. A lo may be zero or negative, so that an infinite value becomes NaN with it: kOnePart
+// is hi alone, for the caller to repeat a run with where kTwoParts left anything that is not finite.
+enum Parts { kSpareRows, kTwoParts, kOnePart };
+template <int CT, bool I8, Parts PARTS>
 __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4], const KvSource& kv, int begin, int end,
                                        int rows, const int (&lim)[CT], int full, float zscale, int wave, int n, int g) {
     int t0 = begin + kTile * wave;
@@ -264,7 +278,7 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
         }
         kt.load(kv, next, rows - 1 - next, n, g);
 
-        v8bf p[CT];
+        v8bf p[CT], lo[CT];
         float vs[8];
         if constexpr (I8) {
 #pragma unroll
@@ -301,18 +315,17 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
                 if constexpr (I8) x[e] = masked && !(t0 + value_token(e, g) < lim[c]) ? 0.f : x[e] * vs[e];
             }
             st.l[c] += sum;
-            uint32_t w[4];
+            uint32_t w[4], low[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-                if constexpr (SPLIT) {
-                    const uint32_t low = pack_bf16(x[2 * e] - bf16_lo(w[e]), x[2 * e + 1] - bf16_hi(w[e]));
-                    w[e] = n < 8 ? w[e] : low;
-                }
+                if constexpr (PARTS != kOnePart) low[e] = pack_bf16(x[2 * e] - bf16_lo(w[e]), x[2 * e + 1] - bf16_hi(w[e]));
+                if constexpr (PARTS == kSpareRows) w[e] = n < 8 ? w[e] : low[e];
             }
             p[c] = __builtin_bit_cast(v8bf, make_uint4(w[0], w[1], w[2], w[3]));
+            if constexpr (PARTS == kTwoParts) lo[c] = __builtin_bit_cast(v8bf, make_uint4(low[0], low[1], low[2], low[3]));
         }
-        if constexpr (SPLIT && !I8) {
+        if constexpr (PARTS == kSpareRows && !I8) {
             if (masked) vt.clear_from(rows - t0, g);        // behind the last token: zero times infinity
         } else if constexpr (!I8) {
             if (masked && __ballot(!vt.all_finite()) != 0) {
@@ -327,6 +340,12 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int c = 0; c < CT; ++c) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], p[c], st.o[c][i], 0, 0, 0);
+        if constexpr (PARTS == kTwoParts) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], lo[c], st.o[c][i], 0, 0, 0);
+        }
         t0 += kRound;
         if (t0 >= end) break;
     }
@@ -441,7 +460,7 @@ __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, in
     RowState<1> st;
     st.clear();
     const int lim[1] = {L};
-    attend<1, I8, true>(st, q, kv, kBlock * jb, min(kBlock * je, L), L, lim, L, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
+    attend<1, I8, kSpareRows>(st, q, kv, kBlock * jb, min(kBlock * je, L), L, lim, L, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
     join_waves(lds, st, wave, n, g);
     const size_t out0 = balanced ? (size_t)wg * G : ((size_t)b * a.Hq + hq0) * a.S + s;
     const size_t stride = balanced ? 1 : a.S;

@@ -11,7 +11,7 @@ __global__ __launch_bounds__(kThreads, 2) void own_decode_kernel(OwnArgs a) {
 
 // The batch over its shared prefix, and in the workgroups behind those over the sequences' own caches: one launch.
 template <int CT, bool I8, bool OWN8>
-__global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, OwnArgs own) {
+__global__ __launch_bounds__(kThreads, CT == 1 ? 3 : 2) void prefix_kernel(PrefixArgs a, OwnArgs own) {
     __shared__ union {
         JoinLds<CT> lds;
         JoinLds<1> own_lds;
@@ -62,7 +62,12 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(PrefixArgs a, OwnAr
                       I8 ? a.kv.v_absmax + row0 : nullptr};
     RowState<CT> st;
     st.clear();
-    attend<CT, I8, false>(st, q, kv, begin, end, longest, lim, shortest, a.scale * kLog2e / (I8 ? 127.f : 1.f), wave, n, g);
+    const float zscale = a.scale * kLog2e / (I8 ? 127.f : 1.f);
+    attend<CT, I8, kTwoParts>(st, q, kv, begin, end, longest, lim, shortest, zscale, wave, n, g);
+    if (!I8 && __ballot(!st.all_finite()) != 0) {
+        st.clear();
+        attend<CT, I8, kOnePart>(st, q, kv, begin, end, longest, lim, shortest, zscale, wave, n, g);
+    }
     join_waves(lds, st, wave, n, g);
     const size_t out0 = ((size_t)pair * a.tiles + tile) * (16 * CT);
     const int live = min(16 * CT, rows - tile * 16 * CT);

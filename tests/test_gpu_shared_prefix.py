@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from tests.kv8_reference import D, P_BF16, attention, check_attention, random_cache, values
+from tests.kv8_reference import D, P_BF16, P_SPLIT, attention, check_attention, random_cache, values
 
 pytestmark = pytest.mark.gpu
 
@@ -130,6 +130,39 @@ def test_infinities_and_nan_reach_only_the_rows_that_see_them(G, copies, room):
     o, fine = out.cpu().clone(), used <= 299
     o[want] = clean[0][want].bfloat16()
     check_attention((o[fine], lse.cpu()[fine]), tuple(t[fine] for t in clean), 310, P_BF16)
+
+
+@pytest.mark.parametrize("B,G,bits", [(1, 1, 16), (4, 4, 16), (4, 4, 8), (4, 8, 16), (4, 8, 8), (40, 4, 16), (33, 8, 8)])
+def test_probabilities_of_small_tiles_have_two_parts(B, G, bits):
+    """Tiles of 16 and 32 query rows round a probability to 2^-16, not to 2^-8."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B + G)
+    P, lens = 1000, [(19 * b) % 60 for b in range(B)]
+    prefix_lens = [P - 13 * b for b in range(B)]
+    q = _normal(gen, B, 2 * G, D)
+    prefix, cache = random_cache(gen, 1, 2, _cap([P]), bits), random_cache(gen, B, 2, 64, bits)
+    _spoil(prefix, [P])
+    got = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
+    check_attention(got, _reference(q, prefix, prefix_lens, cache, lens), P + 60, P_SPLIT)
+
+
+@pytest.mark.parametrize("room", [False, True])
+@pytest.mark.parametrize("B,G", [(2, 1), (3, 4), (4, 8), (9, 8), (20, 8), (40, 8)])
+def test_infinite_values_that_every_row_sees(B, G, room):
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B * G)
+    P, special = 700, [(5, 3, math.inf), (333, 127, -math.inf), (334, 64, math.inf), (690, 0, -math.inf), (200, 50, math.nan)]
+    q, prefix, cache = _normal(gen, B, G, D), random_cache(gen, 1, 1, _cap([P]), 16), random_cache(gen, B, 1, 64, 16)
+    lens = [b % 3 for b in range(B)]
+    clean = _reference(q, prefix, [P] * B, cache, lens)
+    for t, d, x in special:
+        prefix[1][0, 0, t, d] = x
+    prefix = _with_room(prefix, B * G, room)
+    out, lse = (t.cpu() for t in ffd.shared_prefix_decode_attention(q, prefix, _int32([P] * B), cache, _int32(lens)))
+    for t, d, x in special:
+        assert out[:, :, d].isnan().all() if math.isnan(x) else bool((out[:, :, d] == x).all()), f"token {t}"
+        out[:, :, d] = clean[0][:, :, d].bfloat16()
+    check_attention((out, lse), clean, P + 3, P_BF16)
 
 
 @pytest.mark.parametrize("G", [1, 4, 8])
