@@ -179,7 +179,8 @@ template __global__ void lse_merge_kernel<4>(const float*, const float*, const f
 
 // The same over the rows of two attentions: the head's rows of the shared prefix, one of each workgroup of its tile, and
 // the own cache's, all rows of one array. NW waves per slice as above; with one the workgroup's four waves take the four
-// slices (4096 heads of 18 rows: 14.5 us with a workgroup per slice, which is their dispatch).
+// slices, so that there are fewer workgroups to dispatch (4096 heads of 18 rows: 14.5 us with a workgroup per slice, 12.1
+// so; 1024 of 34 5.9).
 template <int NW>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
     constexpr int kRowLanes = 8 * NW;
