@@ -19,9 +19,13 @@
 //
 // 8-bit codes become bf16 integers on their way into LDS; M / 127 of a key multiplies its score, that of a value its
 // probability. The maximum that the exponents are taken against follows the running one only when that has grown by
-// 2^8, so that the accumulators are rarely rescaled. Probabilities are rounded to one bf16 for the instruction (half a
-// step, 2^-8, at most, and independent from token to token: over many tokens an error as large as that of rounding the
-// output itself); a second part as for small tiles would be half again as many matrix instructions.
+// 2^8, so that the accumulators are rarely rescaled.
+//
+// Probabilities. In bf16, up to 64 rows, they are given to the instruction in two parts as for small tiles, which costs
+// nothing there. Otherwise they are rounded to one bf16 (half a step, 2^-8, at most, and independent from token to token:
+// over the many tokens of the prefixes that come here an error about as large as that of rounding the output itself, and
+// of the two 1.4 times that); the second part, half again as many matrix instructions, was measured at 59 -> 68 us for
+// 128 rows, 87 -> 110 for 256, 68 -> 78 for 64 in 8 bits.
 //
 // Three ways to keep a CU's SIMDs, two waves each, on loads, matrix and vector instructions at once, by what there is
 // most of. bf16, 64 rows (the plain loop): the loads; every wave does all there is to do to a tile, then stages its
@@ -58,6 +62,7 @@ template <int RW, bool I8>
 struct PrefixShape {
     static constexpr bool kRoles = I8 && RW <= 4;                       // waves 4 .. 7 stage, waves 0 .. 3 do the rest
     static constexpr bool kPhased = RW > 2 && !kRoles;
+    static constexpr bool kTwoParts = RW == 2 && !I8;                   // probabilities in two bf16 parts
     static constexpr int kMathWaves = kRoles ? 4 : 8;
     static constexpr int kTokenGroups = kMathWaves / RW;
     static constexpr int kSub = kRoles || kPhased ? 2 : 1;              // 32-token tiles of a wave
@@ -357,7 +362,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const uint32_t v_at = (wave_row + v_row) * (2 * kD) + 16 * value_chunk<I8>(v_row, v_c) + 8 * (i16 & 1);
 
     v16f s[Sh::kSub];
-    v8bf p[2 * Sh::kSub];
+    v8bf p[2 * Sh::kSub], lo[2 * Sh::kSub];
     auto first_token = [&](int u) { return u * Sh::kTokens + wave_row; };
 
     // With 32 tokens per wave there are registers to ask for a tile's first value operands with its scores; read where
@@ -461,8 +466,17 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             }
 #pragma unroll
             for (int y = 0; y < 2; ++y)
-                p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{pack_bf16(e[8 * y], e[8 * y + 1]), pack_bf16(e[8 * y + 2], e[8 * y + 3]),
-                                                            pack_bf16(e[8 * y + 4], e[8 * y + 5]), pack_bf16(e[8 * y + 6], e[8 * y + 7])});
+            {
+                uint32_t w[4], low[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float x0 = e[8 * y + 2 * k], x1 = e[8 * y + 2 * k + 1];
+                    w[k] = pack_bf16(x0, x1);
+                    if constexpr (Sh::kTwoParts) low[k] = pack_bf16(x0 - bf16_lo(w[k]), x1 - bf16_hi(w[k]));
+                }
+                p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
+                if constexpr (Sh::kTwoParts) lo[2 * x + y] = __builtin_bit_cast(v8bf, v4u{low[0], low[1], low[2], low[3]});
+            }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
@@ -476,6 +490,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             for (int d = 0; d < 4; ++d) {
                 const v8s f = y == 0 && kEarly ? head_values[d] : value_operand(values, y, d);
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
+                if constexpr (Sh::kTwoParts)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), lo[y], o[d], 0, 0, 0);
             }
     };
     auto nonfinite = [&](int u) {
