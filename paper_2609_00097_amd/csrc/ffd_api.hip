@@ -413,6 +413,21 @@ int kv8_splits(int B, int Hkv, int Lcap, int num_splits) {
     return (int)std::max<long long>(s, wide / pairs - 1);
 }
 
+// Caches so short, or so many of them, that one workgroup takes all tokens of a (sequence, KV head): one launch without
+// partial states. Split / whole, whole calls of kv8_decode_attention: 2 groups of 512 tokens 11.3 / 7.7 us, 64 of 1K 12.1 / 11.6, 256 of 1K 19 / 14, 512 of 64 (eight
+// heads) 15.0 / 7.3, 2048 of up to 1K 77 / 63; beyond the limits 64 of 2K 13.2 / 19.0, 256 of up to 4K 28 / 39; 2048 of up to
+// 4K 230 / 226 and, one sequence eight times as long as the others, 72 / 65, of 8K 412 / 418.
+constexpr int kWholeTokens = 1024, kWholeTokensMany = 4096, kWholeManyPerCu = 8;
+bool many_groups(int B, int Hkv) { return (long long)B * Hkv >= (long long)kWholeManyPerCu * device_cus(); }
+bool kv8_whole(int B, int Hkv, int Lcap, int num_splits) {
+    return num_splits == 0 && Lcap <= (many_groups(B, Hkv) ? kWholeTokensMany : kWholeTokens);
+}
+// Beside a prefix, where it saves the merge rows only: 2048 groups of 64 tokens 54 / 46 us, of 512 83 / 75, of 1K 135 / 135
+// (8 bits 92 / 84); fewer groups lose (512 of 1K 44.5 / 49.8, 64 of 1K 16 / 20).
+bool own_whole(int B, int Hkv, int Lcap, int num_splits) {
+    return num_splits == 0 && many_groups(B, Hkv) && Lcap <= kWholeTokens;
+}
+
 // What a launch takes: fewer than 2^32 threads (both attentions may share it), and pairs as the int indices of the kernels and the merge take them.
 bool own_fits(int B, int Hkv, int S) {
     return (long long)B * Hkv <= (1LL << 20) && (S + 1LL) * B * Hkv * kThreads < (1LL << 31);
@@ -438,9 +453,11 @@ struct OwnPartials {
     int2* table;
     unsigned wgs;
 };
-size_t own_rows(int B, int Hq, int S) { return (size_t)B * Hq * (B <= kDenseBalanceMaxSeqs ? S + 1 : S); }
-OwnPartials own_partials(Partials p, void* table, int B, int Hkv, int S) {
-    const bool balanced = B <= kDenseBalanceMaxSeqs;
+size_t own_rows(int B, int Hq, int S, bool whole = false) {
+    return (size_t)B * Hq * (B <= kDenseBalanceMaxSeqs && !whole ? S + 1 : S);
+}
+OwnPartials own_partials(Partials p, void* table, int B, int Hkv, int S, bool whole = false) {
+    const bool balanced = B <= kDenseBalanceMaxSeqs && !whole;
     return OwnPartials{p, balanced ? static_cast<int2*>(table) : nullptr,
                        (unsigned)((balanced ? S + 1 : S) * B * Hkv)};
 }
@@ -460,12 +477,14 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      
 struct PrefixPlan {
     int tile_rows, tiles, S;
     long long wgs;
+    int S_own;
+    bool own_whole;
     bool sorted;                      // the order of sequences and the tiles' workgroups follow the lengths
     size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
     size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
 };
 constexpr long long kSmallTileWork = 64 << 10;       // query rows times prefix tokens, per CU
-PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_own) {
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int Lcap, int num_splits, int S_own) {
     const long long rows = (long long)B * (Hq / Hkv);
     PrefixPlan p;
     p.tile_rows = 16;
@@ -482,7 +501,9 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_o
     p.wgs = ((long long)Hkv * p.S + 7) / 8 * 8 * p.tiles;
     p.sorted = p.tile_rows == 256 && p.tiles > 1 && B <= kPrefixSortSeqs;
     p.rows = (size_t)Hkv * p.tiles * p.S * p.tile_rows;
-    p.all_rows = p.rows + own_rows(B, Hq, S_own);
+    p.own_whole = own_whole(B, Hkv, Lcap, num_splits);
+    p.S_own = p.own_whole ? 1 : S_own;
+    p.all_rows = p.rows + own_rows(B, Hq, p.S_own, p.own_whole);
     p.places_off = round_up(partials_bytes(p.all_rows), kAlign);
     p.own_table_off = p.places_off + round_up(p.sorted ? B * sizeof(PrefixPlace) : 0, kAlign);
     p.total = p.own_table_off + (B <= kDenseBalanceMaxSeqs ? (size_t)B * Hkv * sizeof(int2) : 0);
@@ -492,8 +513,8 @@ PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int num_splits, int S_o
 bool prefix_fits(const PrefixPlan& p) { return p.wgs * kPrefixTileThreads < (1LL << 31); }
 
 void launch_own(bool i8, unsigned wgs, hipStream_t stream, const OwnArgs& o) {
-    if (i8) hipLaunchKernelGGL(own_decode_kernel<true>, dim3(wgs), dim3(kThreads), 0, stream, o);
-    else hipLaunchKernelGGL(own_decode_kernel<false>, dim3(wgs), dim3(kThreads), 0, stream, o);
+    if (i8) hipLaunchKernelGGL((own_decode_kernel<true, false>), dim3(wgs), dim3(kThreads), 0, stream, o);
+    else hipLaunchKernelGGL((own_decode_kernel<false, false>), dim3(wgs), dim3(kThreads), 0, stream, o);
 }
 
 // Few rows: one launch for both, the prefix's workgroups first (whole calls: four sequences on 2K tokens 16.7 us with two
@@ -856,8 +877,13 @@ int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* 
     if (workspace_bytes < ffd_kv8_workspace_bytes(B, Hq, Hkv, Lcap, D, num_splits)) return FFD_ERR_WORKSPACE_TOO_SMALL;
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)D);
     const OwnPartials o = own_partials(workspace, B, Hq, Hkv, S);
-    const OwnArgs a{static_cast<const uint16_t*>(q), source_of(*cache), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv,
-                    Lcap, Hq / Hkv, S, scale};
+    OwnArgs a{static_cast<const uint16_t*>(q), source_of(*cache), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv,
+              Lcap, Hq / Hkv, S, scale, static_cast<uint16_t*>(out), lse};
+    if (kv8_whole(B, Hkv, Lcap, num_splits)) {
+        a.S = 1;
+        hipLaunchKernelGGL((own_decode_kernel<true, true>), dim3((unsigned)(B * Hkv)), dim3(kThreads), 0, stream, a);
+        return launch_status();
+    }
     launch_own(true, o.wgs, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;
     launch_merge(B * Hq, stream, o.p.m, o.p.l, o.p.acc, S, o.table, o.table ? Hq / Hkv : 1, static_cast<uint16_t*>(out), lse);
@@ -868,7 +894,7 @@ size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int L
     if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || check_pcap(Pcap) != FFD_OK) return 0;
     const int S = resolve_splits(B, Hkv, Lcap, num_splits, true);
     if (S <= 0 || !own_fits(B, Hkv, S)) return 0;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S);
     return prefix_fits(plan) ? plan.total : 0;
 }
 
@@ -883,7 +909,7 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     if (st != FFD_OK) return st;
     if ((st = check_pcap(Pcap)) != FFD_OK || B == 0) return st;
     if (!own_fits(B, Hkv, S)) return FFD_ERR_UNSUPPORTED;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, num_splits, S);
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S);
     if (!prefix_fits(plan)) return FFD_ERR_UNSUPPORTED;
     if ((st = check_kv(prefix, false, &prefix_bits)) != FFD_OK || (st = check_kv(own, false, &own_bits)) != FFD_OK) return st;
     if (!prefix_lens || (reinterpret_cast<uintptr_t>(prefix_lens) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
@@ -894,16 +920,18 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     const Partials P = carve(workspace, plan.all_rows);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     PrefixPlace* places = plan.sorted ? reinterpret_cast<PrefixPlace*>(ws + plan.places_off) : nullptr;
-    const OwnPartials o = own_partials(Partials{P.m + plan.rows, P.l + plan.rows, P.acc + plan.rows * kD}, ws + plan.own_table_off, B, Hkv, S);
+    const OwnPartials o = own_partials(Partials{P.m + plan.rows, P.l + plan.rows, P.acc + plan.rows * kD}, ws + plan.own_table_off, B, Hkv,
+                                       plan.S_own, plan.own_whole);
     const uint16_t* qp = static_cast<const uint16_t*>(q);
     const PrefixArgs a{qp, source_of(*prefix), prefix_lens, P.m, P.l, P.acc, places, B, Hq, Hkv, Pcap, G, plan.S, plan.tiles,
                        (int)plan.wgs, scale};
-    const OwnArgs oa{qp, source_of(*own), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, S, scale};
+    const OwnArgs oa{qp, source_of(*own), seq_lens, o.p.m, o.p.l, o.p.acc, o.table, B, Hq, Hkv, Lcap, G, plan.S_own,
+                     scale, nullptr, nullptr};
     if (prefix_bits == 8) launch_prefix<true>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);
     else launch_prefix<false>(plan.tile_rows, stream, a, own_bits == 8, o.wgs, oa);
     if ((st = launch_status()) != FFD_OK) return st;
     const SharedMergeArgs m{P.m, P.l, P.acc, plan.rows, o.table, places, static_cast<uint16_t*>(out), lse,
-                            Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, S};
+                            Hq, Hkv, G, plan.tiles, plan.tile_rows, plan.S, plan.S_own};
     const dim3 wide((unsigned)(B * Hq)), deep((unsigned)(B * Hq), kMergeSlices);
     if (B * Hq >= kMergeOneWaveHeads) hipLaunchKernelGGL(shared_merge_kernel<1>, wide, dim3(256), 0, stream, m);
     else hipLaunchKernelGGL(shared_merge_kernel<4>, deep, dim3(256), 0, stream, m);

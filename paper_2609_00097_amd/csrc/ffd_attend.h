@@ -433,12 +433,12 @@ __device__ __forceinline__ void load_query(v8bf (&q)[4], const uint16_t* row, in
 
 // Decode over an 8-bit (I8) or bf16 cache: workgroup wg takes a run of blocks of a (sequence, KV head), as in
 // dense_decode_kernel. The group's G <= 8 queries are rows 0 .. G - 1 and, for the low halves of the probabilities,
-// 8 .. 8 + G - 1.
-template <bool I8>
+// 8 .. 8 + G - 1. WHOLE: a workgroup takes all of its pair's tokens (no table, S = 1) and writes the result itself.
+template <bool I8, bool WHOLE = false>
 __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, int wg) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15;
-    const bool balanced = a.table != nullptr;
+    const bool balanced = !WHOLE && a.table != nullptr;
     int kvh, b, L, jb, je, s = 0;
     if (balanced) {
         if (!balanced_share(a, wg, lane, b, kvh, L, jb, je)) return;
@@ -473,12 +473,21 @@ __device__ __forceinline__ void own_decode(const OwnArgs& a, JoinLds<1>& lds, in
         const int h = i >> 7, d = i & (kD - 1);
         const size_t row = out0 + h * stride;
         const float hi = lds.acc[0][h][d] + lds.acc[1][h][d], lo = lds.acc[0][h + 8][d] + lds.acc[1][h + 8][d];
-        a.part_acc[row * kD + d] = fabsf(hi) < INFINITY ? hi + lo : hi;     // a low half may be zero: not times infinity
-        if (d == 0) {
+        const float o = fabsf(hi) < INFINITY ? hi + lo : hi;                // a low half may be zero: not times infinity
+        if constexpr (WHOLE) {
             float m, l;
             joined_ml(lds, h, m, l);
-            a.part_m[row] = m;
-            a.part_l[row] = l;
+            const bool any = m != -INFINITY;
+            a.out[row * kD + d] = f32_to_bf16(any ? o / l : 0.f);
+            if (d == 0 && a.lse) a.lse[row] = any ? m + logf(l) : -INFINITY;
+        } else {
+            a.part_acc[row * kD + d] = o;
+            if (d == 0) {
+                float m, l;
+                joined_ml(lds, h, m, l);
+                a.part_m[row] = m;
+                a.part_l[row] = l;
+            }
         }
     }
 }

@@ -3,10 +3,10 @@
 
 namespace ffd {
 
-template <bool I8>
+template <bool I8, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 2) void own_decode_kernel(OwnArgs a) {
     __shared__ JoinLds<1> lds;
-    own_decode<I8>(a, lds, blockIdx.x);
+    own_decode<I8, WHOLE>(a, lds, blockIdx.x);
 }
 
 // The batch over its shared prefix, and in the workgroups behind those over the sequences' own caches: one launch. Without
@@ -88,8 +88,9 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 3 : 2) void prefix_kernel(Prefi
     }
 }
 
-template __global__ void own_decode_kernel<false>(OwnArgs);
-template __global__ void own_decode_kernel<true>(OwnArgs);
+template __global__ void own_decode_kernel<false, false>(OwnArgs);
+template __global__ void own_decode_kernel<true, false>(OwnArgs);
+template __global__ void own_decode_kernel<true, true>(OwnArgs);
 template __global__ void prefix_kernel<1, false, false>(PrefixArgs, OwnArgs);
 template __global__ void prefix_kernel<1, false, true>(PrefixArgs, OwnArgs);
 template __global__ void prefix_kernel<1, true, false>(PrefixArgs, OwnArgs);

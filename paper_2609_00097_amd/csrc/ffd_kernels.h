@@ -190,6 +190,8 @@ struct OwnArgs {
     int2* table;
     int B, Hq, Hkv, Lcap, G, S;
     float scale;
+    uint16_t* out;              // WHOLE, else unused
+    float* lse;
 };
 
 // Attention of all sequences' queries over their shared prefix: the B * G query rows of a KV head in `tiles` tiles of R
@@ -269,7 +271,8 @@ template <int BITS> __global__ void quantize_keys_kernel(QuantArgs a);
 template <int BITS> __global__ void append_kv_kernel(AppendArgs a);
 __global__ void write_kv8_kernel(WriteKv8Args a);
 __global__ void read_kv8_kernel(ReadKv8Args a);
-template <bool I8> __global__ void own_decode_kernel(OwnArgs a);
+// WHOLE: a workgroup per (sequence, KV head), which writes out and lse.
+template <bool I8, bool WHOLE> __global__ void own_decode_kernel(OwnArgs a);
 // CT (1, 2): tiles of 16 query rows per workgroup; I8: an 8-bit prefix, OWN8: 8-bit own caches.
 template <int CT, bool I8, bool OWN8> __global__ void prefix_kernel(PrefixArgs a, OwnArgs own);
 constexpr int kPrefixTileThreads = 512;

@@ -231,6 +231,31 @@ def test_attention_of_more_sequences_than_the_balanced_mode_takes():
         check_attention(got, attention(q, [(*values(cache), lens)]), 700, P_SPLIT)
 
 
+@pytest.mark.parametrize("B,Hkv,G,L", [(3, 2, 8, 64), (5, 2, 4, 1024), (5, 2, 1, 1088), (256, 8, 2, 1088), (300, 7, 1, 128)])
+def test_attention_in_one_launch(B, Hkv, G, L):
+    """Around the capacities up to which a workgroup takes all tokens of a pair and writes the result: every length class,
+    NaN behind the tokens, and the same as split runs within the bounds."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B + L)
+    lens = [L, 0, 1, 63, 130][:B] + [(53 * b) % (L + 1) for b in range(5, B)]
+    lens = [min(n, L) for n in lens]
+    q, cache = _normal(gen, B, Hkv * G, D), random_cache(gen, B, Hkv, L)
+    for t in cache:
+        for b, n in enumerate(lens):
+            t[b, :, n:] = 127 if t.dtype == torch.int8 else math.nan
+    some = list(range(min(B, 5))) + ([B // 2, B - 1] if B > 5 else [])
+    ref = attention(q[some], [(*values(tuple(t[some] for t in cache)), [lens[b] for b in some])])
+    for splits in (0, 1, 3):
+        ws = ffd.new_kv8_workspace(B, Hkv * G, Hkv, L, splits).fill_(255)
+        out, lse = torch.full_like(q, 7.0), torch.full((B, Hkv * G), 7.0, device="cuda")
+        ffd.kv8_decode_attention(q, cache, _int32(lens), num_splits=splits, workspace=ws, out=out, lse=lse)
+        check_attention((out[some], lse[some]), ref, L, P_SPLIT)
+        assert bool((out != 7.0).any(-1).all()) and bool((lse != 7.0).all())
+    got = ffd.kv8_decode_attention(q, cache, _int32(lens), return_lse=False)
+    assert got[1] is None
+    check_attention((got[0][some], ref[1].float()), ref, L, P_SPLIT)
+
+
 def test_attention_with_many_workgroups_per_compute_unit():
     """A batch whose capacity makes its automatic splits finer, with lengths far apart."""
     from paper_2609_00097_amd import ffd

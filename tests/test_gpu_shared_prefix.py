@@ -274,6 +274,22 @@ def test_sequences_in_several_row_tiles(B, G, kind, bits, room):
         check_attention(got, ref, P + 3, P_BF16)
 
 
+@pytest.mark.parametrize("own_bits,L", [(16, 128), (8, 960), (16, 1088)])
+def test_many_groups_with_short_caches(own_bits, L):
+    """2048 (sequence, KV head) pairs on both sides of the capacity up to which one workgroup takes a pair's tokens."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(L)
+    B, Hkv, G, P = 256, 8, 2, 200
+    lens, prefix_lens = [(53 * b) % (L + 1) for b in range(B)], [(31 * b) % (P + 1) for b in range(B)]
+    q, prefix, cache = _normal(gen, B, Hkv * G, D), random_cache(gen, 1, Hkv, _cap([P]), 16), random_cache(gen, B, Hkv, L, own_bits)
+    _spoil(cache, lens)
+    ws = ffd.new_shared_prefix_workspace(B, Hkv * G, Hkv, _cap([P]), L).fill_(255)
+    out, lse = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), workspace=ws)
+    some = [0, 1, 100, 211, 255]
+    ref = _reference(q[some], prefix, [prefix_lens[b] for b in some], tuple(t[some] for t in cache), [lens[b] for b in some])
+    check_attention((out[some], lse[some]), ref, P + L, P_SPLIT)
+
+
 def test_equals_dense_attention_over_the_whole():
     """The same tokens as one bf16 cache per sequence through dense_decode_attention: the two round differently, each by
     a half step of bf16 and, here, of the probabilities."""
