@@ -393,8 +393,9 @@ def test_two_calls_at_once(room):
         assert all(torch.equal(o, out) and torch.equal(l, lse) for o, l in results)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
-def test_a_served_batch(bits):
+def test_a_served_batch(bits, room):
     """As a serving program uses them together: a prompt is written once, a captured step (write or copy the new
     token, advance, attend over prompt and own tokens) is replayed between eager work on the same workspace, and one
     sequence starts anew without the prompt. Every step equals the eager call and the 64-bit form."""
@@ -412,11 +413,12 @@ def test_a_served_batch(bits):
         prefix = tuple(torch.zeros(1, Hkv, _cap([P]), D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
         cache = tuple(torch.zeros(B, Hkv, L, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
         prefix[0][:, :, :P], prefix[1][:, :, :P] = prompt_k.transpose(1, 2), prompt_v.transpose(1, 2)
+    prefix = _with_room(prefix, 8 * B, room)
     prefix_lens, lens = _int32([P, P, 350, P, 0]), _int32([0, 3, 0, 17, 0])
     for t in cache:
         t.zero_()
     k_new, v_new, q = (_normal(gen, B, n, D) for n in (Hkv, Hkv, Hq))
-    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, _cap([P]), L)
+    ws = ffd.new_shared_prefix_workspace(B, Hq, Hkv, prefix[0].shape[2], L)
     out, lse = torch.empty_like(q), torch.empty(B, Hq, device="cuda")
 
     def write():
