@@ -283,6 +283,7 @@ __device__ __forceinline__ bool sort_by_length(const PrefixArgs& a, PrefixLds<RW
 template <int RW, bool I8>
 __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a) {
     using Sh = PrefixShape<RW, I8>;
+    constexpr bool kGuess = RW < 8 && !I8;      // 256 rows: the runs may follow the lengths; 8 bits: no registers to spare
     __shared__ PrefixLds<RW, I8> lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, h = lane >> 5;
@@ -296,6 +297,16 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const int rows = a.B * a.G, gs = __builtin_ctz(a.G);
     PrefixPlace mine{slot, a.tiles, a.S, 0};
     int tile = slot;
+    const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
+    const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
+                      I8 ? a.kv.v_absmax + row0 : nullptr};
+    const int team = wave >> 2, part = Sh::kParts == 2 ? team : 0, id = tid & (kTeam - 1);
+    // equal runs of whole tiles, the first ones one longer
+    auto run_begin = [&](int tokens, int run, int S, int& count) {
+        const int units = (tokens + Sh::kTokens - 1) / Sh::kTokens, each = units / S, more = units - each * S;
+        count = each + (run < more);
+        return each * run + min(run, more);
+    };
 
     // queries and lengths, asked for together
     int r = tile * Sh::kRows + 32 * rg + n, b = min(r >> gs, a.B - 1);
@@ -316,6 +327,19 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             load_queries();
             len = a.prefix_lens[b];
         }
+    }
+    // The first tile is asked for before the lengths are there, as it is if they are the capacity (32 sequences on 32K
+    // tokens: 60.4 us with two dependent loads at the start, 59.4 so).
+    Staged<RW, I8> st, head;
+    int guess = -1;
+    if constexpr (kGuess) {
+        int count;
+        guess = run_begin(a.Pcap, pair % a.S, a.S, count);
+        const int last = a.Pcap - 1 - guess * Sh::kTokens;
+        if (count == 0 || last < Sh::kTokens - 1) guess = -1;
+        const int u = max(guess, 0);
+        head.load_keys(kv, u * Sh::kTokens, max(last, 0), part, id);
+        if constexpr (!Sh::kPhased) head.load_values(kv, u * Sh::kTokens, max(last, 0), part, id);
     }
     const int run = (w - mine.first) / mine.stride, S = mine.count;
     const bool live = r < rows;
@@ -339,13 +363,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
 #pragma unroll
     for (int w = 0; w < 8; ++w) all = max(all, reinterpret_cast<const int*>(lds.m[w])[0]);
     all = __builtin_amdgcn_readfirstlane(all);
-    // equal runs of whole tiles, the first ones one longer
-    const int units = (all + Sh::kTokens - 1) / Sh::kTokens, each = units / S, more = units - each * S;
-    const int first = each * run + min(run, more), last = first + each + (run < more);
+    int count;
+    const int first = run_begin(all, run, S, count), last = first + count;
+    const bool guessed = kGuess && guess == first && (first + 1) * Sh::kTokens <= all;      // uniform
 
-    const size_t row0 = (size_t)kvh * a.Pcap, bytes = I8 ? kD : 2 * kD;
-    const KvSource kv{a.kv.k + row0 * bytes, a.kv.v + row0 * bytes, I8 ? a.kv.k_absmax + row0 : nullptr,
-                      I8 ? a.kv.v_absmax + row0 : nullptr};
     const float zscale = a.scale * kLog2e;
     v16f o[4];
 #pragma unroll
@@ -504,14 +525,12 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
 
     // Staging. Behind the run's end its last tile is staged again: with a branch around loads or stores the wait for
     // one tile's registers would fall on the next one's loads.
-    const int team = wave >> 2, part = Sh::kParts == 2 ? team : 0, id = tid & (kTeam - 1);
     auto last_row = [&](int u) { return all - 1 - u * Sh::kTokens; };
     auto load_keys = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_keys(kv, u * Sh::kTokens, last_row(u), part, id); };
     auto load_values = [&](Staged<RW, I8>& x, int u) { u = min(u, last - 1); x.load_values(kv, u * Sh::kTokens, last_row(u), part, id); };
     auto store_keys = [&](const Staged<RW, I8>& x, int u) { x.store_keys(lds, u, last_row(min(u, last - 1)), part, id); };
     auto store_values = [&](const Staged<RW, I8>& x, int u) { x.store_values(lds, u, part, id); };
     if (first < last) {
-        Staged<RW, I8> st, head;
         if constexpr (Sh::kRoles) {
             if (team == 1) {
                 // two tiles under way, in turn in the two sets of registers
@@ -544,7 +563,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 for (int u = mine_last; u < last; ++u) __syncthreads();
             }
         } else if constexpr (Sh::kPhased) {
-            load_keys(head, first);
+            if (!guessed) load_keys(head, first);
             load_values(st, first);
             load_keys(st, first + 1);
             store_keys(head, first);
@@ -588,8 +607,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             }
             if (team == 0) __syncthreads();
         } else {
-            load_keys(head, first);
-            load_values(head, first);
+            if (!guessed) {
+                load_keys(head, first);
+                load_values(head, first);
+            }
             load_keys(st, first + 1);
             load_values(st, first + 1);
             store_keys(head, first);

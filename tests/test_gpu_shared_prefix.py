@@ -306,6 +306,34 @@ def test_equals_dense_attention_over_the_whole():
     check_attention(got, ref, P + n, P_BF16)
 
 
+@pytest.mark.parametrize("B", [40, 100])
+@pytest.mark.parametrize("short", [0, 1, 5000])
+def test_a_prefix_filled_to_its_capacity(B, short):
+    """One token per sequence, at the starts of runs and a token before them, has nearly all of the weight: the staged
+    kernel's first tiles, which are asked for as if the lengths were the capacity, with that and with shorter lengths."""
+    from paper_2609_00097_amd import ffd
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    P = 64 * -(-(65 * 1024 * cus) // (64 * B))
+    gen = _gen(B)
+    k, v = torch.zeros(1, 1, P, D, dtype=torch.bfloat16, device="cuda"), _normal(gen, 1, 1, P, D)
+    units = -(-(P - short) // 128)
+    at = []
+    for j in range(B):
+        run = j * cus // B
+        start = 128 * (units // cus * run + min(run, units % cus))
+        at.append(min(max(start - (j & 1), 0), P - short - 1))
+        k[0, 0, at[j], j] = 1
+    k[:, :, P - short:] = math.nan
+    v[:, :, P - short:] = math.nan
+    q = torch.zeros(B, 1, D, dtype=torch.bfloat16, device="cuda")
+    q[torch.arange(B), 0, torch.arange(B)] = 30.0
+    cache = random_cache(gen, B, 1, 64, 16)
+    out, _ = ffd.shared_prefix_decode_attention(q, (k, v), _int32([P - short] * B), cache, _int32([0] * B), softmax_scale=1.0)
+    # the others' weight is at most P e^-30, 4e-8, of values below 6; the one's, a probability near 1, two roundings
+    want = v[0, 0, at].double()
+    assert bool(((out[:, 0].double() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -16).all())
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 def test_prefix_behind_32_bit_offsets(bits):
     """Rows of the prefix beyond 4 GiB: everything zero but tokens near the end, whose weights are known."""
