@@ -6,7 +6,7 @@
 // HBM's, beyond them the matrix cores'. Next to these, a score costs about eight VALU slots (scale and subtract,
 // exponential, maximum, sum, conversion), as much time as its matrix instructions.
 // Measured, eight KV heads, of which about 13 us are the start, the join of the token groups and the partial rows: 64K
-// tokens in bf16, 64 rows 57 us (4.7 TB/s), 128 59 (4.6 TB/s), 256 87 (790 TFLOP/s), 512 157 to 210 as the clock allows
+// tokens in bf16, 64 rows 56 us (4.8 TB/s), 128 57 (4.7 TB/s), 256 87 (790 TFLOP/s), 512 157 to 210 as the clock allows
 // (875 to 660); 128K in 8 bits, 64 rows 68 us (4.0 TB/s), 128 113 (610 TFLOP/s); 64K, 256 rows 106 (650).
 //
 // Mapping. Eight waves: RW row groups of 32 query rows by 8 / RW token groups. Scores are computed transposed by
