@@ -298,7 +298,7 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
 
 /*
  * Exact dense decode attention over an 8-bit cache: ffd_dense_decode_attention with k = n M / 127 and v likewise,
- * neither rounded to bf16. Arguments are those of that call; the cache holds B sequences, the workspace takes
+ * neither rounded to bf16. Scores and sums are fp32, a probability is rounded to 2^-16 of itself. Arguments are those of that call; the cache holds B sequences, the workspace takes
  * ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20 and B * Hkv * (S + 1) < 2^23 (S as there), else
  * FFD_ERR_UNSUPPORTED.
  */
@@ -316,7 +316,8 @@ size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_
 /*
  * Exact dense decode attention of a batch over a shared prefix and each sequence's own tokens: sequence b attends
  * over the first prefix_lens[b] tokens of the prefix and then tokens [0, seq_lens[b]) of its own cache, with one
- * softmax over both. The prefix is read once for the batch, up to its longest use.
+ * softmax over both. The prefix is read once for the batch, up to its longest use. Rounding is that of
+ * ffd_kv8_decode_attention, whatever else the batch holds.
  *   prefix        cache of one sequence, [Hkv, Pcap, ..], bf16 or 8 bits; Pcap a multiple of 64
  *   prefix_lens   int32 [B] (device), clamped to [0, Pcap]; 0 for a sequence that does not begin with the prefix
  *   own           cache of B sequences, [B, Hkv, Lcap, ..], bf16 or 8 bits (apart from the prefix's form)

@@ -244,8 +244,8 @@ __device__ __forceinline__ void add_nonfinite(RowState<CT>& st, const uint16_t* 
 // lane's row sees) clamps the rows read: those behind it may hold anything. Row n of tile c sees tokens below lim[c];
 // tiles that end at or before `full` are seen whole by every row. zscale turns a product into z2.
 //
-// Probabilities are given to the instruction as p = hi + lo, both bf16, so that they are rounded to 2^-17 and not to
-// 2^-9: kSpareRows: rows n and n + 8 are the same query, one with hi and the other with lo, and all see `rows` tokens;
+// Probabilities are given to the instruction as p = hi + lo, both bf16, so that they are rounded to 2^-16 and not to
+// 2^-8: kSpareRows: rows n and n + 8 are the same query, one with hi and the other with lo, and all see `rows` tokens;
 // kTwoParts: two instructions. A lo may be zero or negative, so that an infinite value becomes NaN with it: kOnePart
 // is hi alone, for the caller to repeat a run with where kTwoParts left anything that is not finite.
 enum Parts { kSpareRows, kTwoParts, kOnePart };

@@ -2,12 +2,13 @@
 // the mathematics; ffd_attend.hip serves fewer rows and short prefixes): tokens staged in LDS once for all rows of a
 // workgroup.
 //
-// Bound. A prefix token costs 512 bytes (8 bits: 260) and 512 operations per query row: up to about 128 rows
-// HBM's, beyond them the matrix cores'. Next to these, a score costs about eight VALU slots (scale and subtract,
-// exponential, maximum, sum, conversion), as much time as its matrix instructions.
+// Bound. A prefix token costs 512 bytes (8 bits: 260) and 768 operations per query row, 256 of them for the second part
+// of its probability: up to about 128 rows HBM's, beyond them the matrix cores'. Next to these, a score costs about ten
+// VALU slots (scale and subtract, exponential, maximum, sum, two conversions), as much time as its matrix instructions.
 // Measured, eight KV heads, of which about 13 us are the start, the join of the token groups and the partial rows: 64K
-// tokens in bf16, 64 rows 56 us (4.8 TB/s), 128 57 (4.7 TB/s), 256 87 (790 TFLOP/s), 512 157 to 210 as the clock allows
-// (875 to 660); 128K in 8 bits, 64 rows 68 us (4.0 TB/s), 128 113 (610 TFLOP/s); 64K, 256 rows 106 (650).
+// tokens in bf16, 64 rows 57 us (4.7 TB/s), 128 66 (4.1 TB/s), 256 105 (985 TFLOP/s, the second part's included), 512 204
+// to 228 as the clock allows (1010 to 900); 128K in 8 bits, 64 rows 76 us (3.6 TB/s), 128 122 to 130 (840 to 800 TFLOP/s); 64K, 256
+// rows 116 (890).
 //
 // Mapping. Eight waves: RW row groups of 32 query rows by 8 / RW token groups. Scores are computed transposed by
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T: lane (n, h) = (lane & 31, lane >> 5) holds, of query row n, tokens
@@ -21,16 +22,17 @@
 // probability. The maximum that the exponents are taken against follows the running one only when that has grown by
 // 2^8, so that the accumulators are rarely rescaled.
 //
-// Probabilities. In bf16, up to 64 rows, they are given to the instruction in two parts as for small tiles, which costs
-// nothing there. Otherwise they are rounded to one bf16 (half a step, 2^-8, at most, and independent from token to token:
-// over the many tokens of the prefixes that come here an error about as large as that of rounding the output itself, and
-// of the two 1.4 times that); the second part, half again as many matrix instructions, was measured at 59 -> 68 us for
-// 128 rows, 87 -> 110 for 256, 68 -> 78 for 64 in 8 bits.
+// Probabilities are given to the instruction in two bf16 parts, p = hi + lo, as for small tiles: rounded to 2^-16, so that
+// a result is as exact, and the same but for the order of sums, whatever number of rows it is computed with. One part
+// (2^-8) would save 8 us of 66 for 128 rows, 17 of 105 for 256, 8 of 76 for 64 in 8 bits, but its error does not average
+// out where many scores are equal, or where one token has most of the weight and the exponents' reference lags behind its
+// score: up to 2^-8 of the values, as much again as the rounding of the output.
 //
 // Three ways to keep a CU's SIMDs, two waves each, on loads, matrix and vector instructions at once, by what there is
 // most of. bf16, 64 rows (the plain loop): the loads; every wave does all there is to do to a tile, then stages its
 // part of the next, one barrier a tile. 8 bits, 64 and 128 rows (roles): the conversion of the codes; four waves, one on
-// each SIMD, stage, the others attend (64 rows on 128K tokens 75 us in phases, 68 so). All else: phases.
+// each SIMD, stage, the others attend (64 rows on 128K tokens, probabilities in one part: 75 us in phases, 68 so). All
+// else: phases.
 //
 // Phases. A tile has a matrix phase (the values' product of the tile before, then this one's scores) and a vector
 // phase (softmax; staging), each closed by a barrier. The two teams of four waves, one wave of each on every SIMD, are
@@ -62,7 +64,6 @@ template <int RW, bool I8>
 struct PrefixShape {
     static constexpr bool kRoles = I8 && RW <= 4;                       // waves 4 .. 7 stage, waves 0 .. 3 do the rest
     static constexpr bool kPhased = RW > 2 && !kRoles;
-    static constexpr bool kTwoParts = RW == 2 && !I8;                   // probabilities in two bf16 parts
     static constexpr int kMathWaves = kRoles ? 4 : 8;
     static constexpr int kTokenGroups = kMathWaves / RW;
     static constexpr int kSub = kRoles || kPhased ? 2 : 1;              // 32-token tiles of a wave
@@ -486,17 +487,16 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
                 for (int i = 0; i < 16; ++i) e[i] *= vm[x][i >> 2][i & 3];
             }
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-            {
+            for (int y = 0; y < 2; ++y) {
                 uint32_t w[4], low[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float x0 = e[8 * y + 2 * k], x1 = e[8 * y + 2 * k + 1];
                     w[k] = pack_bf16(x0, x1);
-                    if constexpr (Sh::kTwoParts) low[k] = pack_bf16(x0 - bf16_lo(w[k]), x1 - bf16_hi(w[k]));
+                    low[k] = pack_bf16(x0 - bf16_lo(w[k]), x1 - bf16_hi(w[k]));
                 }
                 p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
-                if constexpr (Sh::kTwoParts) lo[2 * x + y] = __builtin_bit_cast(v8bf, v4u{low[0], low[1], low[2], low[3]});
+                lo[2 * x + y] = __builtin_bit_cast(v8bf, v4u{low[0], low[1], low[2], low[3]});
             }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -511,8 +511,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             for (int d = 0; d < 4; ++d) {
                 const v8s f = y == 0 && kEarly ? head_values[d] : value_operand(values, y, d);
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), p[y], o[d], 0, 0, 0);
-                if constexpr (Sh::kTwoParts)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), lo[y], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, f), lo[y], o[d], 0, 0, 0);
             }
     };
     auto nonfinite = [&](int u) {
