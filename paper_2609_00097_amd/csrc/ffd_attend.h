@@ -219,9 +219,9 @@ struct RowState {
     }
 };
 
-// What the instruction cannot do in a tile that some rows see only in part: infinities and NaN among the values of a
-// token reach the rows that see it and no other (zero times infinity would reach all). The values have been made
-// finite; here they are added to the rows that see them, token by token.
+// What the instruction cannot do in a tile that some rows see only in part, or with a probability's low part: infinities
+// and NaN among the values of a token reach the rows that see it and no other (zero times infinity would reach all).
+// The values have been made finite; here they are added to the rows that see them, token by token.
 template <int CT>
 __device__ __forceinline__ void add_nonfinite(RowState<CT>& st, const uint16_t* v, int t0, int rows, const int (&lim)[CT], int g) {
 #pragma unroll 1
@@ -246,9 +246,10 @@ __device__ __forceinline__ void add_nonfinite(RowState<CT>& st, const uint16_t* 
 //
 // Probabilities are given to the instruction as p = hi + lo, both bf16, so that they are rounded to 2^-16 and not to
 // 2^-8: kSpareRows: rows n and n + 8 are the same query, one with hi and the other with lo, and all see `rows` tokens;
-// kTwoParts: two instructions. A lo may be zero or negative, so that an infinite value becomes NaN with it: kOnePart
-// is hi alone, for the caller to repeat a run with where kTwoParts left anything that is not finite.
-enum Parts { kSpareRows, kTwoParts, kOnePart };
+// kTwoParts: two instructions. A lo may be zero or negative, so that an infinite value becomes NaN with it: kTwoPartsFinite
+// takes infinities and NaN out of every tile, not only of those that are masked, for the caller to repeat a run with
+// where kTwoParts left anything that is not finite (to look for them in each tile would cost all other runs).
+enum Parts { kSpareRows, kTwoParts, kTwoPartsFinite };
 template <int CT, bool I8, Parts PARTS>
 __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4], const KvSource& kv, int begin, int end,
                                        int rows, const int (&lim)[CT], int full, float zscale, int wave, int n, int g) {
@@ -324,16 +325,16 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-                if constexpr (PARTS != kOnePart) low[e] = pack_bf16(x[2 * e] - bf16_lo(w[e]), x[2 * e + 1] - bf16_hi(w[e]));
+                low[e] = pack_bf16(x[2 * e] - bf16_lo(w[e]), x[2 * e + 1] - bf16_hi(w[e]));
                 if constexpr (PARTS == kSpareRows) w[e] = n < 8 ? w[e] : low[e];
             }
             p[c] = __builtin_bit_cast(v8bf, make_uint4(w[0], w[1], w[2], w[3]));
-            if constexpr (PARTS == kTwoParts) lo[c] = __builtin_bit_cast(v8bf, make_uint4(low[0], low[1], low[2], low[3]));
+            if constexpr (PARTS != kSpareRows) lo[c] = __builtin_bit_cast(v8bf, make_uint4(low[0], low[1], low[2], low[3]));
         }
         if constexpr (PARTS == kSpareRows && !I8) {
             if (masked) vt.clear_from(rows - t0, g);        // behind the last token: zero times infinity
         } else if constexpr (!I8) {
-            if (masked && __ballot(!vt.all_finite()) != 0) {
+            if ((masked || PARTS == kTwoPartsFinite) && __ballot(!vt.all_finite()) != 0) {
                 vt.make_finite();
                 add_nonfinite<CT>(st, reinterpret_cast<const uint16_t*>(kv.v), t0, rows, lim, g);
             }
@@ -345,7 +346,7 @@ __device__ __forceinline__ void attend(RowState<CT>& st, const v8bf (&q)[CT][4],
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int c = 0; c < CT; ++c) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], p[c], st.o[c][i], 0, 0, 0);
-        if constexpr (PARTS == kTwoParts) {
+        if constexpr (PARTS != kSpareRows) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll

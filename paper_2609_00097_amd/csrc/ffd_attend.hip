@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 3 : 2) void prefix_kernel(Prefi
     attend<CT, I8, kTwoParts>(st, q, kv, begin, end, longest, lim, shortest, zscale, wave, n, g);
     if (!I8 && __ballot(!st.all_finite()) != 0) {
         st.clear();
-        attend<CT, I8, kOnePart>(st, q, kv, begin, end, longest, lim, shortest, zscale, wave, n, g);
+        attend<CT, I8, kTwoPartsFinite>(st, q, kv, begin, end, longest, lim, shortest, zscale, wave, n, g);
     }
     join_waves(lds, st, wave, n, g);
     const size_t out0 = ((size_t)pair * a.tiles + tile) * (16 * CT);

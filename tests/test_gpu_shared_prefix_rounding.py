@@ -129,3 +129,32 @@ def test_random_scores(B, G, large, bits, own_bits):
     print(f"case random B={B} G={G} large={large} bits {bits} {own_bits}", flush=True)
     out, _ = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens))
     check_rounded(out, ref, P + 60, P_SPLIT)
+
+
+@pytest.mark.parametrize("B,G,large", SHAPES)
+def test_infinities_cost_the_others_no_precision(B, G, large):
+    """An infinite value that most sequences see, a NaN value, and a sequence whose query is NaN: the other dims and rows are
+    rounded as ever. Scores as in test_equal_scores, where a coarser rounding would not be averaged out."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B * G)
+    P = 1500
+    k, v = torch.zeros(1, 1, P, D, dtype=torch.bfloat16, device="cuda"), _normal(gen, 1, 1, 1, D).repeat(1, 1, P, 1)
+    k[:, :, ::32, 0] = 1
+    v[:, :, ::32] = 0
+    q = torch.zeros(B, G, D, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = torch.linspace(0.3, 6, B * G).view(B, G).bfloat16()
+    cache, lens = random_cache(gen, B, 1, 64, 16), [0] * B
+    prefix_lens = [P if b % 3 else 700 for b in range(B)]
+    ref = attention(q, [(*values((k, v)), prefix_lens), (*values(cache), lens)], 1.0)
+    special = [(5, 3, math.inf), (333, 127, -math.inf), (400, 64, math.nan), (900, 30, math.inf), (1499, 31, math.nan)]
+    finite = torch.ones(B, G, D, dtype=torch.bool)
+    for t, d, x in special:
+        v[0, 0, t, d] = x
+        finite[torch.tensor(prefix_lens) > t, :, d] = False
+    q[B - 1, G - 1, 7] = math.nan
+    finite[B - 1, G - 1] = False
+    prefix = _padded((k, v), _large(B * G, 1, P) if large else _cap(P))
+    print(f"case infinities B={B} G={G} large={large}", flush=True)
+    out, _ = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), softmax_scale=1.0)
+    assert torch.equal(out.isfinite().cpu(), finite)
+    check_rounded(out, ref, P, P_SPLIT, finite)
