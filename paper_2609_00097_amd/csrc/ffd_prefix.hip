@@ -90,6 +90,7 @@ struct PrefixLds {
     alignas(16) float km[4][Sh::kTokens];                               // 8 bits: M / 127 of keys and values
     alignas(16) float vm[4][Sh::kTokens];
     int nonfinite[4];                          // last tile with this index mod 4 that has an infinity or NaN as value
+    int longest[8];                            // each wave's; apart from m, which a run without tiles writes next, no barrier between
     float m[8][32], l[8][32];
 };
 
@@ -358,11 +359,11 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     }
     longest = __builtin_amdgcn_readfirstlane(longest);
     shortest = __builtin_amdgcn_readfirstlane(shortest);
-    if (lane == 0) reinterpret_cast<int*>(lds.m[wave])[0] = longest;
+    if (lane == 0) lds.longest[wave] = longest;
     __syncthreads();
     int all = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) all = max(all, reinterpret_cast<const int*>(lds.m[w])[0]);
+    for (int w = 0; w < 8; ++w) all = max(all, lds.longest[w]);
     all = __builtin_amdgcn_readfirstlane(all);
     int count;
     const int first = run_begin(all, run, S, count), last = first + count;

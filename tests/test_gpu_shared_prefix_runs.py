@@ -1,0 +1,31 @@
+"""Runs of a shared prefix that hold no tokens, beside those that do."""
+import pytest
+import torch
+
+from tests.kv8_reference import P_SPLIT, check_attention, random_cache
+from tests.test_gpu_shared_prefix import _gen, _int32, _normal, _reference
+from tests.test_gpu_shared_prefix_rounding import _large, _padded
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("B,G", [(8, 8), (16, 8), (32, 8), (70, 8)])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_empty_runs(B, G, bits):
+    """More runs than the prefix has tiles, rows whose lengths differ from wave to wave and only a few of which use the
+    prefix at all: all workgroups of a tile have to agree on the longest. The same bits in every call."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(B + bits)
+    P = 200
+    prefix_lens = [P if b == B - 1 else (b % 5) * 7 for b in range(B)]
+    lens = [b % 2 for b in range(B)]
+    q, prefix, cache = _normal(gen, B, G, 128), random_cache(gen, 1, 1, P, bits), random_cache(gen, B, 1, 64, 16)
+    ref = _reference(q, prefix, prefix_lens, cache, lens)
+    prefix = _padded(prefix, _large(B * G, 1, P))
+    for splits in (40, 200):
+        ws = ffd.new_shared_prefix_workspace(B, G, 1, prefix[0].shape[2], 64, splits).fill_(255)
+        first = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), num_splits=splits, workspace=ws)
+        check_attention(first, ref, P + 1, P_SPLIT)
+        for _ in range(10):
+            again = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), num_splits=splits, workspace=ws)
+            assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
