@@ -336,9 +336,9 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
                                        void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Workspace bytes of ffd_shared_prefix_decode_attention: (D + 2) * 4 bytes for each query row (their number per KV head
- * rounded up to the kernel's row tiles) and run of the prefix, and for each row of ffd_dense_decode_attention's partials
- * (automatically one per sequence and head where Lcap <= 1024 and there are eight groups or more per compute unit);
- * then, each on a 256-byte boundary, for up to 256 sequences 16 bytes each where there are several tiles of 256 rows,
+ * rounded up to the kernel's row tiles) and run of the prefix, the larger number where these differ between a bf16 and an
+ * 8-bit prefix, and for each row of ffd_dense_decode_attention's partials (automatically one per sequence and head where
+ * Lcap <= 1024 and there are eight groups or more per compute unit); then, each on a 256-byte boundary, for up to 256 sequences 16 bytes each where there are several tiles of 256 rows,
  * and a table of B * Hkv * 8 bytes. 0 on invalid or unsupported input. */
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits);
 

@@ -466,14 +466,21 @@ OwnPartials own_partials(void* workspace, int B, int Hq, int Hkv, int S) {      
     return own_partials(carve(workspace, rows), static_cast<uint8_t*>(workspace) + round_up(partials_bytes(rows), kAlign), B, Hkv, S);
 }
 
-// Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head (a prefix is then
-// read once), at most 256, and as many runs as give each CU one workgroup (64K, eight KV heads, whole calls: 16 rows 52
-// us, with two per CU 56, 32 rows 54 and 58; 128 rows 71, with two waves of workgroups 97).
-// More than 32 rows over little work are several tiles of 32, whose workgroups start sooner and take the own caches along,
-// though each reads the prefix (out of its XCD's L2): up to 64K query rows times tokens per CU. Whole calls with up to 512
-// own tokens, eight KV heads, tiles of 32 / one tile of them all, bf16: 64 rows on 4K 17 / 27 us, on 16K 26.7 / 33.2, on
-// 32K 40.5 / 44.4 (8 bits 37.6 / 35.5); 128 rows on 4K 23 / 32, on 16K 36.9 / 40.9 (37.5 / 36.0), on 20K 44.1 / 43.7 (42.9 /
-// 38.4); 256 rows on 4K 28.6 / 40.3, on 8K 38.3 / 44.0, on 12K 50.8 / 51.5.
+// Row tiles and runs of the prefix attention: the smallest tile that holds all query rows of a KV head, at most 256, and as
+// many runs as give each CU one workgroup (64K, eight KV heads, whole calls: 16 rows 52 us, with two per CU 56, 32 rows 54
+// and 58). More than 32 rows over little work are several tiles of 32, whose workgroups start sooner and take the own
+// caches along, though each reads the prefix (out of its XCD's L2). Little is, in rows of those tiles times tokens per CU, up
+// to 120K; 128K for up to 64 rows in bf16, where the staged kernel has the least to save; 64K for up to 128 rows in 8 bits, where
+// each tile converts the codes anew. Whole calls with up to 512 own tokens, eight KV heads, tiles of 32 / one tile of them
+// all (beyond 256 rows, several of 256), at the work named:
+//   bf16    64 rows 64K 42.6 / 47.6, 96K 55.2 / 59.3, 128K 67.0 / 69.9, 192K 88.4 / 88.8; 128 rows 64K 40.9 / 44.6, 96K
+//           51.3 / 52.9, 120K 57.8 / 57.3, 192K 83.1 / 76.3; 72 rows (three tiles, which leave 16 CUs idle) 96K 52.7 / 50.3,
+//           144K 69.4 / 62.5; 256 rows 96K 56.0 / 61.7, 160K 76.7 / 72.7; 320 rows 120K 66.9 / 71.4; 512 rows 64K 49.4 / 57.5, 192K 86.1 / 79.3
+//   8 bits  64 rows 64K 36.3 / 38.1, 96K 49.2 / 47.9; 128 rows 64K 36.5 / 37.4, 80K 42.3 / 42.0, 96K 47.8 / 44.6; 160 rows
+//           100K 52.2 / 54.8; 256 rows 96K 50.1 / 54.0, 128K 61.4 / 60.7; 320 rows 120K 62.4 / 69.3; 512 rows 64K 47.4 /
+//           51.4, 128K 64.9 / 63.2
+// Around the limits it is the own caches' size that decides, beside which tiles of 32 gain: 256 rows, 128K in bf16, with 64 own
+// tokens 56.2 / 53.0, up to 512 66.4 / 67.6, up to 2K 101 / 108; in 8 bits 58.6 / 51.9, 61.4 / 60.7, 74.9 / 83.7.
 struct PrefixPlan {
     int tile_rows, tiles, S;
     long long wgs;
@@ -483,13 +490,13 @@ struct PrefixPlan {
     size_t rows, all_rows;            // partial rows of the prefix, and with those of the own caches behind them
     size_t places_off, own_table_off, total;                    // in the workspace, behind the partial rows
 };
-constexpr long long kSmallTileWork = 64 << 10;       // query rows times prefix tokens, per CU
-PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int Lcap, int num_splits, int S_own) {
+PrefixPlan prefix_plan(int B, int Hq, int Hkv, int Pcap, int Lcap, int num_splits, int S_own, bool i8) {
     const long long rows = (long long)B * (Hq / Hkv);
+    const long long little = !i8 && rows <= 64 ? 128 << 10 : i8 && rows <= 128 ? 64 << 10 : 120 << 10;
     PrefixPlan p;
     p.tile_rows = 16;
     while (p.tile_rows < rows && p.tile_rows < 256) p.tile_rows *= 2;
-    if (rows > 32 && rows * Hkv * Pcap <= kSmallTileWork * device_cus()) p.tile_rows = 32;
+    if (rows > 32 && (rows + 31) / 32 * 32 * Hkv * Pcap <= little * device_cus()) p.tile_rows = 32;
     p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
     long long s = num_splits;
     if (s == 0) {
@@ -894,8 +901,12 @@ size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int L
     if (check_shapes(B, Hq, Hkv, Lcap, D) != FFD_OK || B == 0 || check_pcap(Pcap) != FFD_OK) return 0;
     const int S = resolve_splits(B, Hkv, Lcap, num_splits, true);
     if (S <= 0 || !own_fits(B, Hkv, S)) return 0;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S);
-    return prefix_fits(plan) ? plan.total : 0;
+    size_t bytes = 0;
+    for (const bool i8 : {false, true}) {
+        const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S, i8);
+        if (prefix_fits(plan)) bytes = std::max(bytes, plan.total);
+    }
+    return bytes;
 }
 
 int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, const int32_t* prefix_lens, int Pcap,
@@ -909,9 +920,9 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
     if (st != FFD_OK) return st;
     if ((st = check_pcap(Pcap)) != FFD_OK || B == 0) return st;
     if (!own_fits(B, Hkv, S)) return FFD_ERR_UNSUPPORTED;
-    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S);
-    if (!prefix_fits(plan)) return FFD_ERR_UNSUPPORTED;
     if ((st = check_kv(prefix, false, &prefix_bits)) != FFD_OK || (st = check_kv(own, false, &own_bits)) != FFD_OK) return st;
+    const PrefixPlan plan = prefix_plan(B, Hq, Hkv, Pcap, Lcap, num_splits, S, prefix_bits == 8);
+    if (!prefix_fits(plan)) return FFD_ERR_UNSUPPORTED;
     if (!prefix_lens || (reinterpret_cast<uintptr_t>(prefix_lens) & 3u)) return FFD_ERR_INVALID_ARGUMENT;
     if (workspace_bytes < ffd_shared_prefix_workspace_bytes(B, Hq, Hkv, Pcap, Lcap, D, num_splits))
         return FFD_ERR_WORKSPACE_TOO_SMALL;

@@ -29,7 +29,7 @@ def _cap(n):
 def _large(rows, Hkv, tokens):
     """A capacity of at least `tokens` for which `rows` query rows are no little work: they are taken by the kernel that
     stages tokens, in tiles of 64, 128 or 256."""
-    work = (1 << 17) * torch.cuda.get_device_properties(0).multi_processor_count
+    work = 129 * 1024 * torch.cuda.get_device_properties(0).multi_processor_count
     return _cap(max(tokens, -(-work // (rows * Hkv))))
 
 

@@ -29,3 +29,27 @@ def test_empty_runs(B, G, bits):
         for _ in range(10):
             again = ffd.shared_prefix_decode_attention(q, prefix, _int32(prefix_lens), cache, _int32(lens), num_splits=splits, workspace=ws)
             assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
+@pytest.mark.parametrize("rows,B,G", [(64, 10, 4), (128, 26, 4), (224, 25, 8), (320, 40, 8)])
+@pytest.mark.parametrize("thousands", [64, 120, 128])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_on_both_sides_of_little_work(rows, B, G, thousands, bits):
+    """Capacities around those up to which the rows are cut into tiles of 32 (64K, 120K and 128K rows of these tiles times
+    tokens per compute unit, by the prefix's form and the number of rows): a workspace of just the size asked for, which does not
+    depend on the form, holds either plan."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(rows + thousands)
+    Hkv, P = 2, 777
+    work = thousands * 1024 * torch.cuda.get_device_properties(0).multi_processor_count
+    cap = work // (64 * rows * Hkv) * 64
+    prefix_lens, lens = [P - 9 * b for b in range(B)], [b % 3 for b in range(B)]
+    q, prefix, cache = _normal(gen, B, Hkv * G, 128), random_cache(gen, 1, Hkv, P, bits), random_cache(gen, B, Hkv, 64, 16)
+    ref = _reference(q, prefix, prefix_lens, cache, lens)
+    for Pcap in (cap, cap + 64):
+        ws = ffd.new_shared_prefix_workspace(B, Hkv * G, Hkv, Pcap, 64)
+        assert ws.numel() == ffd.shared_prefix_workspace_bytes(B, Hkv * G, Hkv, Pcap, 64)
+        got = ffd.shared_prefix_decode_attention(q, _padded(prefix, Pcap), _int32(prefix_lens), cache, _int32(lens), workspace=ws.fill_(255))
+        check_attention(got, ref, P + 2, P_SPLIT)
+        with pytest.raises(ffd.FfdError, match="WORKSPACE"):
+            ffd.shared_prefix_decode_attention(q, _padded(prefix, Pcap), _int32(prefix_lens), cache, _int32(lens), workspace=ws[:-16])
