@@ -25,8 +25,8 @@
  *                               device-side positions, and read back in bf16.
  *   ffd_kv8_decode_attention    exact dense decode attention over the 8-bit cache.
  *   ffd_shared_prefix_decode_attention  exact dense decode attention of a batch whose sequences begin
- *                               with the same tokens: that prefix, kept once, is read once for all of
- *                               them, then each sequence's own cache; bf16 or 8-bit.
+ *                               with the same tokens: that prefix, kept once, is attended to for many
+ *                               sequences at a time, then each one's own cache; bf16 or 8-bit.
  *
  * Conventions for every entry point
  *  - Tensor arguments are DEVICE pointers to contiguous row-major buffers owned by the caller.
@@ -316,13 +316,14 @@ size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_
 /*
  * Exact dense decode attention of a batch over a shared prefix and each sequence's own tokens: sequence b attends
  * over the first prefix_lens[b] tokens of the prefix and then tokens [0, seq_lens[b]) of its own cache, with one
- * softmax over both. The prefix is read once for the batch, up to its longest use. Rounding is that of
- * ffd_kv8_decode_attention, whatever else the batch holds.
+ * softmax over both. The query rows of a KV head are taken in tiles of up to 256, and each tile reads the prefix once, up
+ * to its longest use; rows of the prefix behind that, and behind all lengths, may be loaded too (any up to Pcap), but
+ * count for nothing. Rounding is that of ffd_kv8_decode_attention, whatever else the batch holds.
  *   prefix        cache of one sequence, [Hkv, Pcap, ..], bf16 or 8 bits; Pcap a multiple of 64
  *   prefix_lens   int32 [B] (device), clamped to [0, Pcap]; 0 for a sequence that does not begin with the prefix
  *   own           cache of B sequences, [B, Hkv, Lcap, ..], bf16 or 8 bits (apart from the prefix's form)
  *   seq_lens      int32 [B] (device): each sequence's own tokens, clamped to [0, Lcap]
- *   num_splits    runs of the prefix per tile of query rows, and runs of blocks of the own caches as for
+ *   num_splits    runs of the prefix per tile of query rows (on average, where 256-row tiles follow the lengths), and runs of blocks of the own caches as for
  *                 ffd_dense_decode_attention (1..FFD_MAX_SPLITS), or 0 for automatic
  *   out, lse      as ffd_dense_decode_attention; a sequence with no token at all gets out = 0, lse = -inf
  *   workspace     ffd_shared_prefix_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that

@@ -291,7 +291,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
     const int n = lane & 31, h = lane >> 5;
     const int rg = wave % RW, tg = wave % Sh::kMathWaves / RW;
     // Workgroups of one run but different tiles read the same tokens: they are eight apart, on one XCD (consecutive
-    // workgroups go to the eight XCDs in turn).
+    // workgroups go to the eight XCDs in turn). Where sequences are sorted by length the tiles have runs of their own, and
+    // each XCD reads what its workgroups need (two tiles, of which the second ends at half of 268 MB: 404 MB).
     const int slot = (int)(blockIdx.x >> 3) % a.tiles;
     const int pair = (int)(blockIdx.x >> 3) / a.tiles * 8 + (int)(blockIdx.x & 7);
     if (pair >= a.Hkv * a.S) return;

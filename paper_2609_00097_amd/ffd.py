@@ -564,8 +564,8 @@ def shared_prefix_decode_attention(q, prefix, prefix_lens, cache, seq_lens, *, n
                                    lse=None):
     """Exact dense decode attention of a batch whose sequences begin with the same tokens: sequence b attends over the
     first ``prefix_lens[b]`` tokens of ``prefix`` and the ``seq_lens[b]`` tokens of its own ``cache``. The prefix is a
-    cache of one sequence (B = 1) and is read once for the whole batch. ``prefix`` and ``cache`` are each ``(k, v)``
-    in bf16 or an 8-bit cache; the lengths int32 ``[B]``. Returns ``(out, lse)``."""
+    cache of one sequence (B = 1) and is read once for up to 256 query rows of a KV head. ``prefix`` and ``cache`` are
+    each ``(k, v)`` in bf16 or an 8-bit cache; the lengths int32 ``[B]``. Returns ``(out, lse)``."""
     device, B, Hq, Hkv, Lcap, own, out, lse = _dense_arguments(q, cache, "cache", seq_lens, return_lse, out, lse, True)
     Pcap = _cache_dims(prefix, "prefix", True)[2]
     shared = _kv_cache(prefix, "prefix", device, (1, Hkv, Pcap, HEAD_DIM))
