@@ -42,10 +42,7 @@
 // values in 2 u + 2 and 2 u + 3. Each team stages half of the rows in its vector phases: team 1 the keys of tile u + 1
 // and the values of u in phase 2 u, team 0 the same in 2 u + 1, which is after the last read of tiles u - 1 and u - 2,
 // whose places they take, and before their first use. The loads for them are issued one vector phase earlier.
-#include <cfloat>
-
-#include "ffd_device.h"
-#include "ffd_kernels.h"
+#include "ffd_attend.h"
 
 namespace ffd {
 
@@ -57,7 +54,6 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 
 constexpr int kPThreads = kPrefixTileThreads;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;                  // growth of the maximum, in powers of two, that rescales
 
 template <int RW, bool I8>
@@ -99,7 +95,6 @@ __device__ __forceinline__ int key_chunk(int row, int c) { return c ^ (row & 15)
 template <bool I8>                             // 8 bits: a store takes every second chunk of two rows, which then complement
 __device__ __forceinline__ int value_chunk(int row, int c) { return c ^ (((row & 3) << 2) | ((row >> 2) & 3)) ^ (I8 ? row & 1 : 0); }
 
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float halves_max(float x) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -107,13 +102,6 @@ __device__ __forceinline__ float halves_max(float x) {
 __device__ __forceinline__ float halves_sum(float x) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-template <int BYTE>
-__device__ __forceinline__ float byte_value(uint32_t w) { return (float)(int8_t)(w >> (8 * BYTE)); }
-__device__ __forceinline__ uint2 expand4(uint32_t w) {          // four codes as bf16 (exact: their floats end in zeros)
-    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(byte_value<1>(w)), __float_as_uint(byte_value<0>(w)), 0x07060302u),
-                      __builtin_amdgcn_perm(__float_as_uint(byte_value<3>(w)), __float_as_uint(byte_value<2>(w)), 0x07060302u));
 }
 
 // A team's part of a tile on its way from memory to LDS, in registers: rows [part kPartTokens, ..) of the tile. `last` is
@@ -173,9 +161,8 @@ template <int RW> struct Staged<RW, true> {
     static __device__ __forceinline__ void expand(uint8_t* tile, int row, int c, bool keys, const v4u& w) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const uint2 a = expand4(w[2 * x]), b = expand4(w[2 * x + 1]);
             const int at = keys ? key_chunk(row, c + x) : value_chunk<true>(row, c + x);
-            *reinterpret_cast<v4u*>(tile + row * (2 * kD) + 16 * at) = v4u{a.x, a.y, b.x, b.y};
+            *reinterpret_cast<v8bf*>(tile + row * (2 * kD) + 16 * at) = expand8(w[2 * x], w[2 * x + 1]);
         }
     }
     __device__ __forceinline__ void load_keys(const KvSource& kv, int t0, int last, int part, int id) {
