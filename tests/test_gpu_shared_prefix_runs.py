@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from tests.kv8_reference import P_SPLIT, check_attention, random_cache
-from tests.test_gpu_shared_prefix import _gen, _int32, _normal, _reference
+from tests.test_gpu_shared_prefix import _capture, _gen, _int32, _normal, _reference
 from tests.test_gpu_shared_prefix_rounding import _large, _padded
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +53,33 @@ def test_on_both_sides_of_little_work(rows, B, G, thousands, bits):
         check_attention(got, ref, P + 2, P_SPLIT)
         with pytest.raises(ffd.FfdError, match="WORKSPACE"):
             ffd.shared_prefix_decode_attention(q, _padded(prefix, Pcap), _int32(prefix_lens), cache, _int32(lens), workspace=ws[:-16])
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_captured_call_follows_the_lengths(bits):
+    """One capture over several tiles of 256 rows, replayed with lengths that are sorted differently, all equal or all zero, on
+    a workspace that eager calls use in between: the eager call's bits and the 64-bit form each time."""
+    from paper_2609_00097_amd import ffd
+    gen = _gen(bits)
+    B, G, P = 70, 8, 900
+    q, prefix, cache = _normal(gen, B, G, 128), random_cache(gen, 1, 1, P, bits), random_cache(gen, B, 1, 64, 8)
+    whole = _padded(prefix, _large(B * G, 1, P))
+    prefix_lens, lens = _int32([P] * B), _int32([b % 3 for b in range(B)])
+    ws = ffd.new_shared_prefix_workspace(B, G, 1, whole[0].shape[2], 64)
+    out, lse = torch.empty_like(q), torch.empty(B, G, device="cuda")
+
+    def call():
+        ffd.shared_prefix_decode_attention(q, whole, prefix_lens, cache, lens, workspace=ws, out=out, lse=lse)
+
+    graph = _capture(call)
+    for i, step in enumerate((397, 0, 53, None, 701)):
+        now = [0] * B if step is None else [(step * b) % (P + 1) for b in range(B)] if step else [P] * B
+        prefix_lens.copy_(_int32(now))
+        q.copy_(_normal(gen, B, G, 128))
+        out.fill_(float("nan"))
+        graph.replay()
+        eager = ffd.shared_prefix_decode_attention(q, whole, prefix_lens, cache, lens)
+        ffd.shared_prefix_decode_attention(q.flip(0), whole, prefix_lens.flip(0).contiguous(), cache, lens, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1]), f"replay {i}"
+        check_attention((out, lse), _reference(q, prefix, now, cache, lens.tolist()), P + 2, P_SPLIT)
