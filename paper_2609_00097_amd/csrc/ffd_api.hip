@@ -527,7 +527,8 @@ void launch_own(bool i8, unsigned wgs, hipStream_t stream, const OwnArgs& o) {
 // Few rows: one launch for both, the prefix's workgroups first (whole calls: four sequences on 2K tokens 16.7 us with two
 // launches, 14.6 with one; eight on 64K with 1K of their own 70.6 and 65.0, with 16K 157 and 150). A large tile's
 // workgroup has its CU to itself, so the own caches wait for it in either form, with twelve waves per CU in a launch of
-// their own and eight in that kernel's registers: 64.2 us against 67.5 for 32 sequences on 32K.
+// their own and eight in that kernel's registers: 64.2 us against 67.5 for 32 sequences on 32K (then with one part of the
+// probabilities).
 template <bool I8>
 void launch_prefix(int tile_rows, hipStream_t stream, const PrefixArgs& a, bool own8, unsigned own_wgs, const OwnArgs& o) {
     const dim3 wgs((unsigned)a.wgs), both(a.wgs + own_wgs), small(kThreads), large(kPrefixTileThreads);

@@ -19,9 +19,10 @@
 // state per query row and workgroup.
 //
 // Bound: HBM (260 bytes a token and KV head in 8 bits, 512 in bf16), for short caches the chain of lengths, queries, first
-// tile and join, 5 us. Measured: 4 x 128K tokens in 8 bits, 32 and 8 heads, 186 us (5.85 TB/s); 16 sequences of 1 to 64K,
-// eight heads per KV head, 217 (5.6); 32 sequences of 8K 67 (4.7); 1 x 32K 16 (4.2). Staging the tokens in LDS for all waves
-// of a workgroup, as for many rows, has nothing to share here: a token is used by one wave.
+// tile and join, 5 us. Measured, by the card: 4 x 128K tokens in 8 bits, 32 and 8 heads, 186 to 196 us (5.85 to 5.55 TB/s); 16
+// sequences of 1 to 64K, eight heads per KV head, 217 to 225 (5.5); 32 sequences of 500 to 8K 68 (4.7); 1 x 32K 16 (4.2).
+// Staging the tokens in LDS for all waves of a workgroup, as for many rows, has nothing to share here: a token is used by
+// one wave.
 #pragma once
 
 #include <cfloat>

@@ -11,8 +11,8 @@ __global__ __launch_bounds__(kThreads, 2) void own_decode_kernel(OwnArgs a) {
 
 // The batch over its shared prefix, and in the workgroups behind those over the sequences' own caches: one launch. Without
 // LDS in the loop every wave loads, converts and sorts its tokens for at most 32 rows: 64K tokens in bf16, eight KV heads,
-// 16 rows 48 us (5.6 TB/s), 32 rows 52 (5.2); 128K in 8 bits 48 (5.7) and 62 (4.4, the vector instructions). Three waves
-// per SIMD for 16 rows: with two, four sequences on 64K tokens with 16K of their own take 106 us, not 98.
+// 16 rows 48 to 50 us (5.5 TB/s), 32 rows 52 (5.2), 64 rows in two tiles 62; 128K in 8 bits, 16 rows 48 to 50 (5.6), 32
+// rows 62 (4.4, the vector instructions). Three waves per SIMD for 16 rows: with two, four sequences on 64K tokens with 16K of their own take 106 us, not 98.
 template <int CT, bool I8, bool OWN8>
 __global__ __launch_bounds__(kThreads, CT == 1 ? 3 : 2) void prefix_kernel(PrefixArgs a, OwnArgs own) {
     __shared__ union {

@@ -5,10 +5,10 @@
 // Bound. A prefix token costs 512 bytes (8 bits: 260) and 768 operations per query row, 256 of them for the second part
 // of its probability: up to about 128 rows HBM's, beyond them the matrix cores'. Next to these, a score costs about ten
 // VALU slots (scale and subtract, exponential, maximum, sum, two conversions), as much time as its matrix instructions.
-// Measured, eight KV heads, of which about 13 us are the start, the join of the token groups and the partial rows: 64K
-// tokens in bf16, 64 rows 57 us (4.7 TB/s), 128 66 (4.1 TB/s), 256 105 (985 TFLOP/s, the second part's included), 512 204
-// to 228 as the clock allows (1010 to 900); 128K in 8 bits, 64 rows 76 us (3.6 TB/s), 128 122 to 130 (840 to 800 TFLOP/s); 64K, 256
-// rows 116 (890).
+// Measured, by the card, eight KV heads, of which about 13 us are the start, the join of the token groups and the partial
+// rows: in bf16, 64 rows on 80K tokens 67 to 69 us (4.9 TB/s), on 64K 128 rows 66 to 71 (4.0 TB/s), 256 105 to 110 (960
+// TFLOP/s, the second part's included), 512 201 to 239 as the clock allows (1020 to 860); in 8 bits, on 128K 64 rows 76 to
+// 81 us (3.5 TB/s), 128 122 to 130 (840 to 790 TFLOP/s), on 64K 256 rows 116 to 124 (890 to 830).
 //
 // Mapping. Eight waves: RW row groups of 32 query rows by 8 / RW token groups. Scores are computed transposed by
 // v_mfma_f32_32x32x16_bf16, S^T = K Q^T: lane (n, h) = (lane & 31, lane >> 5) holds, of query row n, tokens
@@ -318,8 +318,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefix_tile_kernel(PrefixArgs a)
             len = a.prefix_lens[b];
         }
     }
-    // The first tile is asked for before the lengths are there, as it is if they are the capacity (32 sequences on 32K
-    // tokens: 60.4 us with two dependent loads at the start, 59.4 so).
+    // The first tile is asked for before the lengths are there, as it is if they are the capacity (whole calls in turn
+    // on one card, four times: 32 sequences on 32K tokens 67.8 us with two dependent loads at the start, 66.4 so; 64 rows on
+    // 96K 90.9 and 88.6).
     Staged<RW, I8> st, head;
     int guess = -1;
     if constexpr (kGuess) {
