@@ -298,9 +298,9 @@ int ffd_read_kv8(const ffd_kv* cache, const int32_t* seq_lens, void* k, void* v,
 
 /*
  * Exact dense decode attention over an 8-bit cache: ffd_dense_decode_attention with k = n M / 127 and v likewise,
- * neither rounded to bf16. Scores and sums are fp32, a probability is rounded to 2^-16 of itself. Arguments are those of that call; the cache holds B sequences, the workspace takes
- * ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20 and B * Hkv * (S + 1) < 2^23 (S as there), else
- * FFD_ERR_UNSUPPORTED.
+ * neither rounded to bf16. Scores and sums are fp32, a probability is rounded to 2^-16 of itself. Arguments are those of
+ * that call; the cache holds B sequences, the workspace takes ffd_kv8_workspace_bytes(...) bytes. B * Hkv <= 2^20 and
+ * B * Hkv * (S + 1) < 2^23 (S as there), else FFD_ERR_UNSUPPORTED.
  */
 int ffd_kv8_decode_attention(const void* q, const ffd_kv* cache, const int32_t* seq_lens, int B, int Hq, int Hkv,
                              int Lcap, int D, int num_splits, float softmax_scale, void* out, float* lse,
@@ -323,8 +323,8 @@ size_t ffd_kv8_workspace_bytes(int B, int Hq, int Hkv, int Lcap, int D, int num_
  *   prefix_lens   int32 [B] (device), clamped to [0, Pcap]; 0 for a sequence that does not begin with the prefix
  *   own           cache of B sequences, [B, Hkv, Lcap, ..], bf16 or 8 bits (apart from the prefix's form)
  *   seq_lens      int32 [B] (device): each sequence's own tokens, clamped to [0, Lcap]
- *   num_splits    runs of the prefix per tile of query rows (on average, where 256-row tiles follow the lengths), and runs of blocks of the own caches as for
- *                 ffd_dense_decode_attention (1..FFD_MAX_SPLITS), or 0 for automatic
+ *   num_splits    runs of the prefix per tile of query rows (on average, where 256-row tiles follow the lengths), and runs of
+ *                 blocks of the own caches as for ffd_dense_decode_attention (1..FFD_MAX_SPLITS), or 0 for automatic
  *   out, lse      as ffd_dense_decode_attention; a sequence with no token at all gets out = 0, lse = -inf
  *   workspace     ffd_shared_prefix_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that
  *                 overlap in time need separate workspaces.
@@ -339,8 +339,9 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
 /* Workspace bytes of ffd_shared_prefix_decode_attention: (D + 2) * 4 bytes for each query row (their number per KV head
  * rounded up to the kernel's row tiles) and run of the prefix, the larger number where these differ between a bf16 and an
  * 8-bit prefix, and for each row of ffd_dense_decode_attention's partials (automatically one per sequence and head where
- * Lcap <= 1024 and there are eight groups or more per compute unit); then, each on a 256-byte boundary, for up to 256 sequences 16 bytes each where there are several tiles of 256 rows,
- * and a table of B * Hkv * 8 bytes. 0 on invalid or unsupported input. */
+ * Lcap <= 1024 and there are eight groups or more per compute unit); then, each on a 256-byte boundary, for up to 256
+ * sequences 16 bytes each where there are several tiles of 256 rows, and a table of B * Hkv * 8 bytes. 0 on invalid or
+ * unsupported input. */
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits);
 
 /* The split count S for this num_splits (0 = automatic), which sizes the workspace: num_splits itself, or
