@@ -27,6 +27,11 @@
  *   ffd_shared_prefix_decode_attention  exact dense decode attention of a batch whose sequences begin
  *                               with the same tokens: that prefix, kept once, is attended to for many
  *                               sequences at a time, then each one's own cache; bf16 or 8-bit.
+ *   ffd_write_paged             new queries, keys and values of a ragged batch: norms per head, rotation, keys and
+ *                               values into a paged cache (bf16 or 8 bits).
+ *   ffd_paged_attention         attention of each sequence's new tokens, one or a chunk, over a paged cache.
+ *   ffd_paged_attention_weights the attention weight that each cached token gets from them.
+ *   ffd_evict_paged             the heaviest and the latest tokens of a paged cache, moved into pages of their own.
  *
  * Conventions for every entry point
  *  - Tensor arguments are DEVICE pointers to contiguous row-major buffers owned by the caller.
@@ -343,6 +348,131 @@ int ffd_shared_prefix_decode_attention(const void* q, const ffd_kv* prefix, cons
  * sequences 16 bytes each where there are several tiles of 256 rows, and a table of B * Hkv * 8 bytes. 0 on invalid or
  * unsupported input. */
 size_t ffd_shared_prefix_workspace_bytes(int B, int Hq, int Hkv, int Pcap, int Lcap, int D, int num_splits);
+
+/*
+ * A paged cache and a ragged batch of new tokens, for the entry points below.
+ *
+ * pages holds num_pages pages of `page` tokens (16, 32, 64, 128 or 256) of every KV head: k, v bf16 or int8
+ * [num_pages, Hkv, page, D], and for 8 bits the absmaxes bf16 [num_pages, Hkv, page], in the formats of ffd_kv. page_table
+ * is int32 [B, max_pages] (device): token j of sequence b lies in page page_table[b][j / page], place j % page. An entry
+ * outside [0, num_pages) is a page that is not there: tokens are not written to it, and nothing sees them. The capacity
+ * Lcap = max_pages * page is at most 2^28.
+ *
+ * The batch has T rows of new tokens, head by head. Sequence b's are rows [q_start[b], q_start[b + 1]) (int32 [B + 1],
+ * device, not decreasing, clamped to [0, T]), n of them, none, one or many; they are the last n of its seq_lens[b] tokens
+ * (int32 [B], device; below 0 counts as 0, above 2^30 as 2^30), so that row t of them has the place seq_lens[b] - n + t. Rows before q_start[0] and
+ * from q_start[B] on belong to no sequence: they are not read, and outputs there are left as they were. The lengths are the
+ * caller's to advance, before ffd_write_paged of the tokens.
+ */
+typedef struct ffd_paged {
+    ffd_kv pages;
+    const int32_t* page_table;
+    int num_pages;
+    int page;
+    int max_pages;
+} ffd_paged;
+
+/*
+ * New tokens into a paged cache. y = x / sqrt(mean(x^2) + eps) * weight over each query's and key's D dims, then the
+ * rotation of its first rope_dims dims, both in fp32 with one rounding to bf16; values go as they are. In 8 bits a key's
+ * codes are those of the bf16 key, as ffd_write_kv8 writes it. Tokens whose place lies outside [0, Lcap) or in a page that
+ * is not there are not written; their queries are still given out.
+ *   q, k, v       bf16 [T, Hq, D], [T, Hkv, D], [T, Hkv, D], the dims of a vector contiguous. q may be NULL (with q_out).
+ *                 *_strides: HOST arrays of two strides in elements (token, head), each >= 0 and a multiple of 8, or NULL
+ *                 for a contiguous tensor.
+ *   q_out         bf16 [T, Hq, D], contiguous
+ *   rotation      NULL: neither norms nor a rotation
+ * ffd_rotation:
+ *   q_weight, k_weight   bf16 [D], or NULL: no norm;  eps >= 0
+ *   table         fp32 [rows, dims] (device), row p: the dims / 2 cosines of position p, then its sines; NULL: no rotation.
+ *   dims          32, 64, 96 or 128: pair i is dims (i, i + dims / 2), or (2 i, 2 i + 1) where interleaved; (x, y)
+ *                 becomes (x cos - y sin, y cos + x sin)
+ *   positions     int32 [T] (device), or NULL: a token's place. A position outside [0, rows) gives NaN in the rotated dims.
+ * T <= 2^24 and T * (Hq + 2 Hkv) < 2^28, else FFD_ERR_UNSUPPORTED.
+ */
+typedef struct ffd_rotation {
+    const void* q_weight;
+    const void* k_weight;
+    float eps;
+    const float* table;
+    int rows;
+    int dims;
+    int interleaved;
+    const int32_t* positions;
+} ffd_rotation;
+
+int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* q_strides, const int64_t* k_strides,
+                    const int64_t* v_strides, void* q_out, const ffd_rotation* rotation, const ffd_paged* cache,
+                    const int32_t* q_start, const int32_t* seq_lens, int B, int T, int Hq, int Hkv, int D,
+                    hipStream_t stream);
+
+/*
+ * What a score is, and which tokens a query sees; NULL for plain causal attention. The query at place i has with token j
+ *   z = softmax_scale q.k;  with softcap > 0  z = softcap tanh(z / softcap);  with slopes  z = z - slopes[head] |i - j|
+ * and sees it if j < min(seq_lens[b], Lcap), its page is there, and
+ *   (j <= i and (window == 0 or i - j < window))  or  j < prefix_lens[b].
+ * Distances are those of places in the cache. After an eviction, which closes gaps, they are no longer those of the text.
+ *   softcap       >= 0, 0: none;  window  >= 0, 0: none
+ *   slopes        fp32 [Hq] (device), or NULL;  prefix_lens  int32 [B] (device), or NULL
+ */
+typedef struct ffd_score_rules {
+    float softcap;
+    int window;
+    const float* slopes;
+    const int32_t* prefix_lens;
+} ffd_score_rules;
+
+/*
+ * Attention of a batch's new tokens over a paged cache that already holds their keys and values (causal unless the rules
+ * say otherwise). A sequence with few new tokens is cut along its cache, and a short batch altogether, so that single tokens
+ * (decoding), chunks of prompts and both together are served by one call. A score is fp32; a probability is rounded to
+ * bf16, for sequences of at most 32 query rows (new tokens times heads per KV head) to 2^-16.
+ *   q             bf16 [T, Hq, D];  out  bf16 [T, Hq, D];  lse  float [T, Hq] or NULL. A row that sees no token gets out
+ *                 = 0, lse = -inf.
+ *   softmax_scale > 0, or 0 for 1/sqrt(D)
+ *   workspace     ffd_paged_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that overlap in
+ *                 time need separate workspaces.
+ * T <= 2^24, T * Hq < 2^28, B * Hkv <= 2^20 and fewer than 2^23 workgroups, else FFD_ERR_UNSUPPORTED.
+ */
+int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
+                        const ffd_score_rules* rules, int B, int T, int Hq, int Hkv, int D, float softmax_scale, void* out,
+                        float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of ffd_paged_attention on the current device: fp32 partials, (D + 2) * 4 bytes a row, of as many row
+ * tiles as its workgroups can be cut into. 0 on invalid or unsupported input, and for B = 0 or T = 0, which needs none. */
+size_t ffd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int D);
+
+/*
+ * The attention weight that each cached token gets, for eviction: for token j < min(seq_lens[b], Lcap) of sequence b and
+ * KV head h
+ *   weights[b][h][j] = old + sum of exp(z_ij - lse_i) over the queries i of the group's heads that see j,
+ * old = previous[b][h][j] for tokens that were there before the new ones, 0 for the new tokens and without `previous`. Entries
+ * behind are left as they were. The sum has one order: results do not change from call to call.
+ *   q, cache, q_start, seq_lens, rules, softmax_scale   as of the attention that gave lse, float [T, Hq]
+ *   last          > 0: only the last `last` new tokens of a sequence count; 0: all
+ *   previous      float [B, Hkv, Lcap], or NULL; may be `weights` itself
+ *   weights       float [B, Hkv, Lcap]
+ */
+int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
+                                const ffd_score_rules* rules, const float* lse, int B, int T, int Hq, int Hkv, int D,
+                                float softmax_scale, int last, const float* previous, float* weights, hipStream_t stream);
+
+/*
+ * Eviction: of the tokens [0, min(seq_lens[b], Lcap)) whose pages are there, each KV head keeps `budget` (all, where there
+ * are no more): those among the last `recent` places, and of the others the ones with the largest weights, equal weights
+ * from the lowest place on (a NaN counts as larger than infinity). They keep their order and move to places 0, 1, .. of the
+ * pages of new_table (int32 [B, new_max_pages], in the same cache). Those pages must be others than the ones that
+ * cache->page_table has below the lengths, and each in one place only; the old pages are the caller's to reuse after it. A
+ * row whose new page is not there is not copied.
+ *   weights       float [B, Hkv, Lcap]
+ *   budget        1 .. new_max_pages * page;  recent  0 .. budget
+ *   new_lens      int32 [B]: tokens kept (the same for all KV heads)
+ *   kept          int32 [B, Hkv, budget]: the old place of the token now at place r, -1 from new_lens[b] on
+ *   new_weights   float [B, Hkv, new_max_pages * page] or NULL: the kept tokens' weights (entries behind them as they were)
+ */
+int ffd_evict_paged(const ffd_paged* cache, const int32_t* new_table, int new_max_pages, const int32_t* seq_lens,
+                    const float* weights, int B, int Hkv, int D, int budget, int recent, int32_t* new_lens, int32_t* kept,
+                    float* new_weights, hipStream_t stream);
 
 /* The split count S for this num_splits (0 = automatic), which sizes the workspace: num_splits itself, or
  * automatically the largest with (S + 1) * B * Hkv at most one per compute unit of the current device

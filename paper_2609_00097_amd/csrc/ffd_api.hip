@@ -5,41 +5,11 @@
 #include <cstdint>
 #include <mutex>
 
-#include "ffd.h"
-#include "ffd_device.h"
-#include "ffd_kernels.h"
+#include "ffd_host.h"
 
 using namespace ffd;
 
 namespace {
-
-// Compute units of the current device, queried once per device and cached (with the no-alloc
-// entry point's per-device scratch address below, the only state the library keeps). kFallbackCus
-// (an MI355X's count) is used if the query fails.
-constexpr int kFallbackCus = 256;
-constexpr int kMaxDevices = 64;
-std::atomic<int> g_cus[kMaxDevices];
-
-int lookup_cus() {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return kFallbackCus;
-    int n = g_cus[dev].load(std::memory_order_relaxed);
-    if (n > 0) return n;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
-        n = kFallbackCus;
-    g_cus[dev].store(n, std::memory_order_relaxed);
-    return n;
-}
-
-// The count, looked up once per call of an entry point (a call's sizes ask for it a dozen times, and the
-// current device can change between calls only).
-thread_local int t_call_cus = 0;
-struct CallScope {
-    const int outer = t_call_cus;
-    CallScope() { if (outer == 0) t_call_cus = lookup_cus(); }
-    ~CallScope() { t_call_cus = outer; }
-};
-int device_cus() { return t_call_cus != 0 ? t_call_cus : lookup_cus(); }
 
 // Device scratch of ffd_decode_attention_noalloc: one array per device, held until the process ends.
 // In host code `scratch` names a host-side stand-in, not device memory: the array is only ever
@@ -75,8 +45,6 @@ int ffd_target_workgroups() { return device_cus(); }
 int dense_target_workgroups(long long pairs) { return (pairs >= 64 ? 3 : 2) * device_cus(); }
 constexpr int kMinBlocksPerSplit = 8;
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int resolve_splits(int B, int Hkv, int Lcap, int num_splits, bool dense = false) {
     if (B <= 0 || Hkv <= 0 || Lcap <= 0 || num_splits < 0 || num_splits > FFD_MAX_SPLITS) return 0;
     if (num_splits > 0) return num_splits;
@@ -106,31 +74,6 @@ int check_shapes(int B, int Hq, int Hkv, int Lcap, int D) {
 int check_bits(int bits) {
     if (bits == 2 || bits == 4 || bits == 8) return FFD_OK;
     return bits > 0 ? FFD_ERR_UNSUPPORTED : FFD_ERR_INVALID_ARGUMENT;
-}
-
-int launch_status() {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? FFD_OK : FFD_ERR_HIP;
-}
-
-// Partial states of `rows` heads, at the start of a workspace: acc [rows, D], then m [rows], l [rows] (fp32). acc
-// comes first because the merge reads it four floats at a time: after an odd number of m and l (one query head
-// per KV head, odd counts) its rows would lie on 8 bytes only.
-struct Partials {
-    float* m;
-    float* l;
-    float* acc;
-};
-
-constexpr size_t kAlign = 256;
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-size_t partials_bytes(size_t rows) { return rows * (kD + 2) * sizeof(float); }
-
-Partials carve(void* ws, size_t rows) {
-    static_assert(kD * sizeof(float) % 16 == 0, "rows of acc on 16 bytes, like the workspace");
-    float* acc = static_cast<float*>(ws);
-    return Partials{acc + rows * kD, acc + rows * (kD + 1), acc};
 }
 
 // Workgroups of the scan kernel per (sequence, KV head): about one per CU in all (one 8-wave
@@ -431,20 +374,6 @@ bool own_whole(int B, int Hkv, int Lcap, int num_splits) {
 // What a launch takes: fewer than 2^32 threads (both attentions may share it), and pairs as the int indices of the kernels and the merge take them.
 bool own_fits(int B, int Hkv, int S) {
     return (long long)B * Hkv <= (1LL << 20) && (S + 1LL) * B * Hkv * kThreads < (1LL << 31);
-}
-
-// Pointers of a cache argument: all there and aligned; *bits is 8 or 16. An 8-bit one is required where only8.
-int check_kv(const ffd_kv* c, bool only8, int* bits) {
-    if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return FFD_ERR_INVALID_ARGUMENT;
-    if (!c->k_absmax != !c->v_absmax || (only8 && !c->k_absmax)) return FFD_ERR_INVALID_ARGUMENT;
-    if (c->k_absmax && (!aligned16(c->k_absmax) || !aligned16(c->v_absmax))) return FFD_ERR_INVALID_ARGUMENT;
-    *bits = c->k_absmax ? 8 : 16;
-    return FFD_OK;
-}
-
-KvSource source_of(const ffd_kv& c) {
-    return KvSource{static_cast<const uint8_t*>(c.k), static_cast<const uint8_t*>(c.v),
-                    static_cast<const uint16_t*>(c.k_absmax), static_cast<const uint16_t*>(c.v_absmax)};
 }
 
 // Partial states of a dense attention over whole caches: its rows, its table (null: S rows per head) and workgroups.

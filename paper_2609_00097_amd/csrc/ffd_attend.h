@@ -84,6 +84,15 @@ template <> struct KeyTile<false> {
             for (int s = 0; s < 4; ++s) k[t][s] = *reinterpret_cast<const uint4*>(base + off + 64 * s);
         }
     }
+    // Half t's rows from row[t] on.
+    __device__ __forceinline__ void load_halves(const KvSource& kv, const size_t (&row)[2], int n, int g) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint8_t* base = kv.k + row[t] * (2 * kD);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) k[t][s] = *reinterpret_cast<const uint4*>(base + (uint32_t)(n * (2 * kD) + 16 * g + 64 * s));
+        }
+    }
     __device__ __forceinline__ v8bf operand(int t, int s) const { return __builtin_bit_cast(v8bf, k[t][s]); }
 };
 template <> struct KeyTile<true> {
@@ -97,6 +106,16 @@ template <> struct KeyTile<true> {
             k[t][0] = *reinterpret_cast<const uint4*>(base + off);
             k[t][1] = *reinterpret_cast<const uint4*>(base + off + 16);
             m[t] = *reinterpret_cast<const uint2*>(kv.k_absmax + tok0 + 16 * t + 4 * g);
+        }
+    }
+    __device__ __forceinline__ void load_halves(const KvSource& kv, const size_t (&row)[2], int n, int g) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint8_t* base = kv.k + row[t] * kD;
+            const uint32_t off = (uint32_t)(n * kD + 32 * g);
+            k[t][0] = *reinterpret_cast<const uint4*>(base + off);
+            k[t][1] = *reinterpret_cast<const uint4*>(base + off + 16);
+            m[t] = *reinterpret_cast<const uint2*>(kv.k_absmax + row[t] + 4 * g);
         }
     }
     __device__ __forceinline__ v8bf operand(int t, int s) const {
@@ -121,6 +140,11 @@ template <> struct ValueTile<false> {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             v[e] = *reinterpret_cast<const uint4*>(base + (uint32_t)min(value_token(e, g), last) * (2 * kD) + 16 * n);
+    }
+    __device__ __forceinline__ void load_halves(const KvSource& kv, const size_t (&row)[2], int n, int g) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = *reinterpret_cast<const uint4*>(kv.v + row[e >> 2] * (2 * kD) + (uint32_t)((4 * g + (e & 3)) * (2 * kD) + 16 * n));
     }
     __device__ __forceinline__ void operands(v8bf (&f)[8]) const {
         uint32_t w[8][4];                       // [dim][token pair]
@@ -152,6 +176,12 @@ template <> struct ValueTile<false> {
         for (int e = 0; e < 8; ++e)
             if (value_token(e, g) >= end) v[e] = make_uint4(0u, 0u, 0u, 0u);
     }
+    // Rows that are not `alive` (bit e: row e of this lane) to zero.
+    __device__ __forceinline__ void keep(uint32_t alive) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!(alive >> e & 1)) v[e] = make_uint4(0u, 0u, 0u, 0u);
+    }
     // Infinities and NaN to zero.
     __device__ __forceinline__ void make_finite() {
         auto fix = [](uint32_t w) {
@@ -172,6 +202,13 @@ template <> struct ValueTile<true> {
             v[e] = *reinterpret_cast<const uint2*>(base + (uint32_t)value_token(e, g) * kD + 8 * n);
 #pragma unroll
         for (int t = 0; t < 2; ++t) m[t] = *reinterpret_cast<const uint2*>(kv.v_absmax + tok0 + 16 * t + 4 * g);
+    }
+    __device__ __forceinline__ void load_halves(const KvSource& kv, const size_t (&row)[2], int n, int g) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = *reinterpret_cast<const uint2*>(kv.v + row[e >> 2] * kD + (uint32_t)((4 * g + (e & 3)) * kD + 8 * n));
+#pragma unroll
+        for (int t = 0; t < 2; ++t) m[t] = *reinterpret_cast<const uint2*>(kv.v_absmax + row[t] + 4 * g);
     }
     template <int BYTE>
     __device__ __forceinline__ v8bf column(bool second) const {

@@ -228,6 +228,76 @@ struct SharedMergeArgs {
     int Hq, Hkv, G, tiles, tile_rows, S_prefix, S_own;
 };
 
+// A paged cache: pages [num_pages, Hkv, 2^page_shift, ..] and each sequence's row of the page table. Entries outside
+// [0, num_pages) are pages that are not there.
+struct PagedKv {
+    KvSource kv;
+    const int32_t* table;       // [B, max_pages]
+    int num_pages, page_shift, max_pages;
+};
+
+// A ragged batch of new tokens: those of sequence b are rows [q_start[b], q_start[b + 1]), the last of its seq_lens[b]
+// tokens.
+struct ChunkArgs {
+    const uint16_t* q;          // bf16 [T, Hq, 128]
+    PagedKv pages;
+    const int32_t* q_start;     // [B + 1]
+    const int32_t* seq_lens;    // [B]
+    const int32_t* prefix_lens; // [B] or null
+    const float* slopes;        // [Hq] or null
+    int B, T, Hq, Hkv, G, Lcap;
+    int window;                 // 0: none
+    float cap;                  // 0: none
+    float scale;
+};
+
+// Their attention. A kernel takes the sequences with rows_above < n G <= rows_upto query rows per KV head; `slots` is the
+// number of workgroups that its work is cut for (0: every row tile whole). Partial states of row tiles that are cut: part p
+// has the rows from part0 + p * (rows of a tile) on.
+struct ChunkAttendArgs : ChunkArgs {
+    float* part_m;
+    float* part_l;
+    float* part_acc;
+    uint16_t* out;              // bf16 [T, Hq, 128]
+    float* lse;                 // [T, Hq] or null
+    int rows_above, rows_upto, slots, max_parts;
+};
+
+struct ChunkWeightsArgs : ChunkArgs {
+    const float* lse;           // [T, Hq]
+    const float* previous;      // [B, Hkv, Lcap] or null
+    float* weights;             // [B, Hkv, Lcap]
+    int last;                   // new tokens that count, 0: all
+};
+
+struct WritePagedArgs {
+    const uint16_t* q;          // bf16 [T, Hq, 128] or null, element strides of token and head
+    const uint16_t* k;
+    const uint16_t* v;
+    uint16_t* q_out;            // bf16 [T, Hq, 128]
+    const uint16_t* q_weight;   // bf16 [128] or null
+    const uint16_t* k_weight;
+    const float* rope;          // [rope_rows, rope_dims], cosines then sines, or null
+    const int32_t* positions;   // [T] or null: the places in the cache
+    PagedKv pages;
+    const int32_t* q_start;
+    const int32_t* seq_lens;
+    int64_t qs[2], ks[2], vs[2];
+    int B, T, Hq, Hkv, rope_rows, rope_dims, parts;
+    float eps;
+};
+
+struct EvictArgs {
+    PagedKv from;
+    const int32_t* to_table;    // [B, to_pages]
+    const int32_t* seq_lens;
+    const float* weights;       // [B, Hkv, from.max_pages << page_shift]
+    int32_t* new_lens;          // [B]
+    int32_t* kept;              // [B, Hkv, budget]
+    float* new_weights;         // [B, Hkv, to_pages << page_shift] or null
+    int Hkv, to_pages, budget, recent;
+};
+
 struct QuantArgs {
     const uint16_t* k;          // bf16 [B, Hkv, Lcap, 128]
     uint32_t* codes;
@@ -279,6 +349,17 @@ constexpr int kPrefixTileThreads = 512;
 // RW (2, 4, 8): groups of 32 query rows per workgroup.
 template <int RW, bool I8> __global__ void prefix_tile_kernel(PrefixArgs a);
 template <int NW> __global__ void shared_merge_kernel(SharedMergeArgs a);
+// I8: 8-bit pages; INTERLEAVED: pairs of neighbouring dims are rotated.
+template <bool I8, bool INTERLEAVED> __global__ void write_paged_kernel(WritePagedArgs a);
+// CT (1, 2): tiles of 16 query rows per workgroup; RULED: a cap of the scores or slopes.
+template <int CT, bool I8, bool RULED> __global__ void chunk_rows_kernel(ChunkAttendArgs a);
+// Merges what chunk_rows_kernel<1> or <2> (ROWS 16, 32) cut.
+template <int ROWS, int SHIFT> __global__ void chunk_merge_kernel(ChunkAttendArgs a);
+template <bool I8, bool RULED> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
+constexpr int kEvictThreads = 1024;
+__global__ void evict_select_kernel(EvictArgs a);
+constexpr int kEvictMoveRows = 64;             // rows per workgroup of the move
+template <bool I8> __global__ void evict_move_kernel(EvictArgs a);
 constexpr int kMergeSlices = 4;                // workgroups per head of the merge, 32 dims each
 // NW waves per workgroup: 4, or 1 from kMergeOneWaveHeads heads on (their waves fill the chip alone).
 constexpr int kMergeOneWaveHeads = 256;

@@ -16,47 +16,10 @@
 // Bound: HBM (a written vector: 256 bytes read, 130 written; a read one the other way round), or the launch. Measured: one
 // token of 2 KV heads written 2.2 us, of 32 x 8 4.8; 2 x 2K tokens of 8 KV heads 6.9 (3.5 TB/s; over with its first round
 // of loads); 2 x 11.8K tokens read back 27 us (5.4 TB/s), 1 x 128K 137 (5.9).
-#include "ffd_device.h"
 #include "ffd_kernels.h"
+#include "ffd_kv8.h"
 
 namespace ffd {
-
-namespace {
-
-// Codes (16 bytes) and absmax bits of a vector from this lane's 16 dims; the vector's eight lanes call it together.
-__device__ __forceinline__ uint4 encode_slice(const uint4 (&raw)[2], uint32_t& absmax) {
-#pragma clang fp contract(off)          // the argument above names the fused product
-    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
-    uint32_t m2 = w[0] & 0x7fff7fffu;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) m2 = pk_max_u16(m2, w[i] & 0x7fff7fffu);
-    m2 = pk_max_u16(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, kDppXor1, 0xf, 0xf, false));
-    m2 = pk_max_u16(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, kDppXor2, 0xf, 0xf, false));
-    m2 = pk_max_u16(m2, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m2, kDppHalfMirror, 0xf, 0xf, false));
-    const uint32_t bits = max(m2 & 0xffffu, m2 >> 16);
-    const bool finite = bits < 0x7f80u;
-    absmax = finite ? bits : 0x7fc0u;
-    const uint32_t keep = finite && bits != 0 ? 0xffffffffu : 0u;
-    int E;
-    const float m = frexpf(bf16_to_f32((uint16_t)bits), &E);
-    const float hi = 127.f / m, lo = fmaf(-hi, m, 127.f) / m;
-    uint32_t out[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t n[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t word = w[2 * i + (e >> 1)];
-            const float x = ldexpf(e & 1 ? bf16_hi(word) : bf16_lo(word), -E);
-            n[e] = __float_as_uint(fmaf(x, hi, x * lo) + 12582912.f);
-        }
-        const uint32_t a = __builtin_amdgcn_perm(n[1], n[0], 0x0c0c0400u), b = __builtin_amdgcn_perm(n[3], n[2], 0x0c0c0400u);
-        out[i] = (a | b << 16) & keep;
-    }
-    return make_uint4(out[0], out[1], out[2], out[3]);
-}
-
-}  // namespace
 
 // A workgroup writes 32 vectors of one sequence: 2^tok_shift tokens of 32 / 2^tok_shift KV heads, eight lanes each,
 // key and value. With as many tokens as there are, up to 32, the absmaxes of a head leave side by side.

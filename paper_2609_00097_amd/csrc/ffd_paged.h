@@ -1,0 +1,171 @@
+// Paged caches and ragged batches of new tokens: what the kernels over them share.
+//
+// Sequence b has L = seq_lens[b] tokens, the last n = q_start[b + 1] - q_start[b] of them new: new token t has the place
+// i = L - n + t. Its query sees token j < min(L, Lcap) if j <= i and (no window, or i - j < window), or if j < prefix_lens[b],
+// and if j's page is there. All numbers come from the device and are clamped where they are read, so that no table, length
+// or start leads outside the buffers.
+#pragma once
+
+#include "ffd_attend.h"
+
+namespace ffd {
+
+constexpr int kMaxLen = 1 << 30;               // longer lengths count as this
+
+struct ChunkSeq {
+    int q0, n, L, pre;
+};
+
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs& a, int b) {
+    ChunkSeq s;
+    const int first = a.q_start[b], last = a.q_start[b + 1], len = a.seq_lens[b];
+    s.pre = a.prefix_lens ? a.prefix_lens[b] : 0;
+    s.q0 = min(max(first, 0), a.T);
+    s.n = min(max(last, s.q0), a.T) - s.q0;
+    s.L = min(max(len, 0), kMaxLen);
+    s.pre = min(max(s.pre, 0), min(s.L, a.Lcap));
+    return s;
+}
+
+// Blocks of 2^SHIFT tokens that hold what new tokens [first, last] of a sequence see: block(i), i < count.
+struct ChunkSpan {
+    int prefix, skip, count;
+    int end;                    // behind the last token that any of them sees
+    __device__ __forceinline__ int block(int i) const { return i < prefix ? i : i + skip; }
+};
+template <int SHIFT>
+__device__ __forceinline__ ChunkSpan chunk_span(const ChunkArgs& a, const ChunkSeq& s, int first, int last) {
+    const int cached = min(s.L, a.Lcap), place = s.L - s.n;
+    ChunkSpan p;
+    p.end = max(min(max(place + last + 1, s.pre), cached), 0);
+    const int from = a.window > 0 ? max(place + first - a.window + 1, 0) : 0;
+    const int high = (p.end + (1 << SHIFT) - 1) >> SHIFT;
+    p.prefix = min((s.pre + (1 << SHIFT) - 1) >> SHIFT, high);
+    const int low = min(max(from >> SHIFT, p.prefix), high);
+    p.skip = low - p.prefix;
+    p.count = high - p.skip;
+    return p;
+}
+
+// Whether a query at place i sees token j (of a page that is there, below min(L, Lcap)).
+__device__ __forceinline__ bool sees(int i, int j, int window, int pre) { return (j <= i && (window <= 0 || i - j < window)) || j < pre; }
+
+// Row of (token j, KV head kvh) in the pages: first row of the 16-token group that holds j, given its page's entry.
+__device__ __forceinline__ size_t page_row(const PagedKv& p, int Hkv, int kvh, int entry, int j) {
+    return (((size_t)entry * Hkv + kvh) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+}
+__device__ __forceinline__ bool page_there(const PagedKv& p, int entry) { return (unsigned)entry < (unsigned)p.num_pages; }
+// Entry of the page that holds token j; -1 behind the table's row.
+__device__ __forceinline__ int page_entry(const PagedKv& p, int b, int j) {
+    const int i = j >> p.page_shift;
+    const int e = p.table[(size_t)b * p.max_pages + min(i, p.max_pages - 1)];
+    return i < p.max_pages ? e : -1;
+}
+
+// The batch's work cut into items, computed by every wave alone, 64 sequences at a time. A sequence's n G query rows of a
+// KV head are row tiles of ROWS; a tile's blocks (of 2^SHIFT tokens) are cut into `cuts` runs. The cut is the same for all
+// tiles of a sequence: as few runs as keep the longest tile's at or below C blocks, where C gives each of the slots that
+// whole tiles leave an equal part of all blocks. So at most slots + 2 * (tiles * Hkv) items, at most 2 * slots of them parts.
+// Items of a sequence are in the order (tile from the last one, which sees most, on; run; KV head).
+struct ChunkItem {
+    ChunkSeq seq;
+    int b, kvh, tile, run, cuts;
+    int part;                   // number of the partial state, -1: the tile is whole
+};
+template <int ROWS, int SHIFT>
+struct ChunkPlan {
+    ChunkSeq seq;               // this lane's sequence of the 64 at hand
+    int tiles, blocks;
+    __device__ __forceinline__ void load(const ChunkAttendArgs& a, int b0, int lane) {
+        const int b = b0 + lane;
+        seq = chunk_seq(a, min(b, a.B - 1));
+        const long long rows = (long long)seq.n * a.G;
+        tiles = blocks = 0;
+        if (b < a.B && rows > a.rows_above && rows <= a.rows_upto) {
+            tiles = (int)((rows + ROWS - 1) / ROWS);
+            const int step = ROWS / a.G;
+            blocks = chunk_span<SHIFT>(a, seq, (tiles - 1) * step, seq.n - 1).count;
+        }
+    }
+    __device__ __forceinline__ int cuts_for(int C) const { return max((blocks + C - 1) / C, 1); }
+    // C, with the first 64 sequences loaded
+    __device__ __forceinline__ int run_blocks(const ChunkAttendArgs& a, int lane) {
+        if (a.slots <= 0) return INT32_MAX / 2;
+        long long all = 0, count = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            if (b0 > 0) load(a, b0, lane);
+            all += (long long)tiles * blocks;
+            count += tiles;
+        }
+        if (a.B > 64) load(a, 0, lane);
+#pragma unroll
+        for (int x = 32; x; x >>= 1) {
+            all += __shfl_xor(all, x);
+            count += __shfl_xor(count, x);
+        }
+        all *= a.Hkv;
+        count *= a.Hkv;
+        const long long spare = max(max((long long)a.slots - count, (long long)a.slots / 2), 1LL);
+        const long long c = (all + spare - 1) / spare;
+        return (int)min(max(c, 1LL), (long long)(INT32_MAX / 2));
+    }
+};
+
+// The item of workgroup wg; false: there is none. PARTS: only sequences that are cut count, and part is wg itself.
+template <int ROWS, int SHIFT>
+__device__ __forceinline__ bool chunk_item(const ChunkAttendArgs& a, int wg, int lane, ChunkItem& it) {
+    ChunkPlan<ROWS, SHIFT> plan;
+    plan.load(a, 0, lane);
+    const int C = plan.run_blocks(a, lane);
+    int before = 0, parts_before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        if (b0 > 0) plan.load(a, b0, lane);
+        const int cuts = plan.cuts_for(C), items = plan.tiles * cuts * a.Hkv, parts = cuts > 1 ? items : 0;
+        const int incl = wave_inclusive_scan(items), first = before + incl - items;
+        const int parts_incl = wave_inclusive_scan(parts);
+        const uint64_t hit = __ballot(wg >= first && wg < first + items);
+        if (hit != 0) {
+            const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
+            it.b = b0 + src;
+            it.seq.q0 = __builtin_amdgcn_readlane(plan.seq.q0, src);
+            it.seq.n = __builtin_amdgcn_readlane(plan.seq.n, src);
+            it.seq.L = __builtin_amdgcn_readlane(plan.seq.L, src);
+            it.seq.pre = __builtin_amdgcn_readlane(plan.seq.pre, src);
+            it.cuts = __builtin_amdgcn_readlane(cuts, src);
+            const int at = __builtin_amdgcn_readfirstlane(wg) - __builtin_amdgcn_readlane(first, src);
+            const int rest = at / a.Hkv;
+            it.kvh = at - rest * a.Hkv;
+            const int turn = rest / it.cuts;
+            it.run = rest - turn * it.cuts;
+            it.tile = __builtin_amdgcn_readlane(plan.tiles, src) - 1 - turn;
+            it.part = -1;
+            if (it.cuts > 1) it.part = parts_before + __builtin_amdgcn_readlane(parts_incl - parts, src) + at;
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+        parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
+    }
+    return false;
+}
+
+// What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). tanh(x) =
+// 1 - 2 / (1 + e^2x): no overflow, infinities and NaN as they are, 2^-23 of the cap off. An 8-bit key's product is
+// multiplied by its M before and by 1 / 127 within `scale`.
+struct ScoreRule {
+    float zscale;               // without a cap: scale log2(e); with one: 2 scale log2(e) / cap
+    float cap2;                 // cap log2(e), or 0
+    float slope2;               // this lane's row's slope log2(e)
+};
+__device__ __forceinline__ ScoreRule score_rule(const ChunkArgs& a, bool i8, int head) {
+    ScoreRule r;
+    const float scale = i8 ? a.scale / 127.f : a.scale;
+    r.zscale = a.cap > 0.f ? scale * 2.f * kLog2e / a.cap : scale * kLog2e;
+    r.cap2 = a.cap * kLog2e;
+    r.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    return r;
+}
+__device__ __forceinline__ float capped(float x, float cap2) {       // x = zscale s
+    return cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_hw(x)), 1.f);
+}
+
+}  // namespace ffd

@@ -1,0 +1,277 @@
+// C ABI of the paged cache: argument checks, the attention's cut into kernels and workgroups, launches.
+#include <algorithm>
+#include <cmath>
+
+#include "ffd_host.h"
+#include "ffd_paged.h"
+
+using namespace ffd;
+
+namespace {
+
+constexpr int kMaxCapacity = 1 << 28;
+constexpr int kMaxTokens = 1 << 24;
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int check_heads(int Hq, int Hkv, int D) {
+    if (Hq <= 0 || Hkv <= 0 || Hq % Hkv) return FFD_ERR_INVALID_ARGUMENT;
+    const int G = Hq / Hkv;
+    if (Hkv > 65535 || (G != 1 && G != 2 && G != 4 && G != 8) || D != FFD_HEAD_DIM) return FFD_ERR_UNSUPPORTED;
+    return FFD_OK;
+}
+
+int check_batch(int B, int T, int heads) {
+    if (B < 0 || T < 0) return FFD_ERR_INVALID_ARGUMENT;
+    if (B > 65535 || T > kMaxTokens || (long long)T * heads >= 1LL << 28) return FFD_ERR_UNSUPPORTED;
+    return FFD_OK;
+}
+bool pairs_fit(int B, int Hkv) { return (long long)B * Hkv <= 1LL << 20; }
+
+// The cache's shape and pointers; *i8: 8-bit pages.
+int check_paged(const ffd_paged* c, bool* i8) {
+    if (!c) return FFD_ERR_INVALID_ARGUMENT;
+    if (c->num_pages <= 0 || c->max_pages <= 0 || c->page <= 0 || (c->page & (c->page - 1))) return FFD_ERR_INVALID_ARGUMENT;
+    if (c->page < 16 || c->page > 256 || (long long)c->max_pages * c->page > kMaxCapacity) return FFD_ERR_UNSUPPORTED;
+    int bits;
+    const int st = check_kv(&c->pages, false, &bits);
+    if (st != FFD_OK) return st;
+    if (!c->page_table || !aligned4(c->page_table)) return FFD_ERR_INVALID_ARGUMENT;
+    *i8 = bits == 8;
+    return FFD_OK;
+}
+
+PagedKv paged_of(const ffd_paged& c) {
+    return PagedKv{source_of(c.pages), c.page_table, c.num_pages, __builtin_ctz(c.page), c.max_pages};
+}
+
+int check_rules(const ffd_score_rules* r) {
+    if (!r) return FFD_OK;
+    if (!(r->softcap >= 0.f) || std::isinf(r->softcap) || r->window < 0) return FFD_ERR_INVALID_ARGUMENT;
+    if (!aligned4(r->slopes) || !aligned4(r->prefix_lens)) return FFD_ERR_INVALID_ARGUMENT;
+    return FFD_OK;
+}
+
+ChunkArgs chunk_args(const void* q, const ffd_paged& c, const int32_t* q_start, const int32_t* seq_lens,
+                     const ffd_score_rules* rules, int B, int T, int Hq, int Hkv, float softmax_scale) {
+    ChunkArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.pages = paged_of(c);
+    a.q_start = q_start;
+    a.seq_lens = seq_lens;
+    a.B = B, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.G = Hq / Hkv, a.Lcap = c.max_pages * c.page;
+    a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)FFD_HEAD_DIM);
+    if (rules) {
+        a.prefix_lens = rules->prefix_lens;
+        a.slopes = rules->slopes;
+        a.window = std::min(rules->window, kMaxLen);
+        if (rules->window > kMaxLen) a.window = 0;              // as wide as no length is
+        a.cap = rules->softcap;
+    }
+    return a;
+}
+
+// One kernel's part of the attention: row tiles of `rows`, workgroups, and the partial states of tiles that are cut.
+struct ChunkKernel {
+    int rows, rows_above, rows_upto, slots;
+    long long grid;
+    int max_parts;
+};
+ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, int rows, int above, int upto, int per_cu) {
+    ChunkKernel k{rows, above, upto, per_cu * device_cus(), 0, 0};
+    const int G = Hq / Hkv;
+    // every sequence has at most one tile that is not full
+    const long long tiles = (long long)T * G / rows + std::min(B, T);
+    k.grid = std::max((long long)k.slots, k.slots / 2 + tiles * Hkv);
+    k.max_parts = 2 * k.slots;
+    return k;
+}
+struct ChunkLaunches {
+    ChunkKernel few;
+    size_t total;
+};
+ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv) {
+    ChunkLaunches p;
+    const long long rows = (long long)T * (Hq / Hkv);
+    const int tile = rows <= 16LL * B ? 16 : 32;
+    p.few = chunk_kernel(B, T, Hq, Hkv, tile, 0, INT32_MAX, tile == 16 ? 3 : 2);
+    p.total = partials_bytes((size_t)p.few.max_parts * tile);
+    return p;
+}
+
+bool chunk_fits(const ChunkLaunches& p) { return p.few.grid * kThreads < 1LL << 31; }
+
+template <int CT, bool I8>
+void launch_rows_ruled(bool ruled, dim3 grid, hipStream_t stream, const ChunkAttendArgs& a) {
+    if (ruled) hipLaunchKernelGGL((chunk_rows_kernel<CT, I8, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((chunk_rows_kernel<CT, I8, false>), grid, dim3(kThreads), 0, stream, a);
+}
+void launch_rows(int rows, bool i8, bool ruled, dim3 grid, hipStream_t stream, const ChunkAttendArgs& a) {
+    if (rows == 16 && i8) launch_rows_ruled<1, true>(ruled, grid, stream, a);
+    else if (rows == 16) launch_rows_ruled<1, false>(ruled, grid, stream, a);
+    else if (i8) launch_rows_ruled<2, true>(ruled, grid, stream, a);
+    else launch_rows_ruled<2, false>(ruled, grid, stream, a);
+}
+
+int check_strides(const int64_t* s) { return s && (s[0] < 0 || s[0] % 8 || s[1] < 0 || s[1] % 8) ? FFD_ERR_INVALID_ARGUMENT : FFD_OK; }
+
+}  // namespace
+
+extern "C" {
+
+int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* q_strides, const int64_t* k_strides,
+                    const int64_t* v_strides, void* q_out, const ffd_rotation* rotation, const ffd_paged* cache,
+                    const int32_t* q_start, const int32_t* seq_lens, int B, int T, int Hq, int Hkv, int D,
+                    hipStream_t stream) {
+    int st = check_heads(Hq, Hkv, D);
+    if (st == FFD_OK) st = check_batch(B, T, Hq + 2 * Hkv);
+    if (st != FFD_OK) return st;
+    if (check_strides(q_strides) || check_strides(k_strides) || check_strides(v_strides)) return FFD_ERR_INVALID_ARGUMENT;
+    static const ffd_rotation none{};
+    const ffd_rotation& r = rotation ? *rotation : none;
+    if (!(r.eps >= 0.f) || std::isinf(r.eps)) return FFD_ERR_INVALID_ARGUMENT;
+    if (r.table) {
+        if (r.rows <= 0 || r.dims <= 0 || r.dims % 2 || r.dims > D) return FFD_ERR_INVALID_ARGUMENT;
+        if (r.dims % 32) return FFD_ERR_UNSUPPORTED;
+    }
+    if (B == 0 || T == 0) return FFD_OK;
+    bool i8;
+    if ((st = check_paged(cache, &i8)) != FFD_OK) return st;
+    if (!k || !v || !q_start || !seq_lens || !q != !q_out) return FFD_ERR_INVALID_ARGUMENT;
+    for (const void* p : {q, k, v, (const void*)q_out, r.q_weight, r.k_weight, (const void*)r.table})
+        if (!aligned16(p)) return FFD_ERR_INVALID_ARGUMENT;
+    if (!aligned4(q_start) || !aligned4(seq_lens) || !aligned4(r.positions)) return FFD_ERR_INVALID_ARGUMENT;
+    WritePagedArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_weight = static_cast<const uint16_t*>(r.q_weight);
+    a.k_weight = static_cast<const uint16_t*>(r.k_weight);
+    a.rope = r.table;
+    a.positions = r.positions;
+    a.pages = paged_of(*cache);
+    a.q_start = q_start;
+    a.seq_lens = seq_lens;
+    const int64_t cq[2] = {(int64_t)Hq * D, D}, ckv[2] = {(int64_t)Hkv * D, D};
+    for (int i = 0; i < 2; ++i) {
+        a.qs[i] = (q_strides ? q_strides : cq)[i];
+        a.ks[i] = (k_strides ? k_strides : ckv)[i];
+        a.vs[i] = (v_strides ? v_strides : ckv)[i];
+    }
+    a.B = B, a.T = T, a.Hq = Hq, a.Hkv = Hkv;
+    a.rope_rows = r.rows, a.rope_dims = r.table ? r.dims : 0;
+    a.eps = r.eps;
+    // one vector a group of lanes while that leaves CUs idle, else up to six, so that the table's row is loaded less often
+    const int vectors = (q ? Hq : 0) + 2 * Hkv, groups = (vectors + 7) / 8;
+    const long long wanted = 16LL * device_cus();
+    const int waves = (int)std::min<long long>(groups, std::max<long long>((groups + 5) / 6, wanted / T));
+    a.parts = 8 * waves;
+    const dim3 grid((unsigned)(((long long)T * waves + kWaves - 1) / kWaves));
+    const bool inter = r.table && r.interleaved;
+    if (i8 && inter) hipLaunchKernelGGL((write_paged_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
+    else if (i8) hipLaunchKernelGGL((write_paged_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
+    else if (inter) hipLaunchKernelGGL((write_paged_kernel<false, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((write_paged_kernel<false, false>), grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+size_t ffd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
+    CallScope scope;
+    if (check_heads(Hq, Hkv, D) != FFD_OK || check_batch(B, T, Hq) != FFD_OK || B == 0 || T == 0) return 0;
+    const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv);
+    return pairs_fit(B, Hkv) && chunk_fits(plan) ? plan.total : 0;
+}
+
+int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
+                        const ffd_score_rules* rules, int B, int T, int Hq, int Hkv, int D, float softmax_scale, void* out,
+                        float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    CallScope scope;
+    int st = check_heads(Hq, Hkv, D);
+    if (st == FFD_OK) st = check_batch(B, T, Hq);
+    if (st != FFD_OK) return st;
+    if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return FFD_ERR_INVALID_ARGUMENT;
+    if ((st = check_rules(rules)) != FFD_OK || B == 0 || T == 0) return st;
+    bool i8;
+    if ((st = check_paged(cache, &i8)) != FFD_OK) return st;
+    if (!q || !q_start || !seq_lens || !out || !workspace) return FFD_ERR_INVALID_ARGUMENT;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(q_start) || !aligned4(seq_lens) || !aligned4(lse))
+        return FFD_ERR_INVALID_ARGUMENT;
+    const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv);
+    if (!pairs_fit(B, Hkv) || !chunk_fits(plan)) return FFD_ERR_UNSUPPORTED;
+    if (workspace_bytes < plan.total) return FFD_ERR_WORKSPACE_TOO_SMALL;
+    ChunkAttendArgs a{};
+    static_cast<ChunkArgs&>(a) = chunk_args(q, *cache, q_start, seq_lens, rules, B, T, Hq, Hkv, softmax_scale);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
+    const ChunkKernel& k = plan.few;
+    const Partials P = carve(workspace, (size_t)k.max_parts * k.rows);
+    a.part_m = P.m, a.part_l = P.l, a.part_acc = P.acc;
+    a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.max_parts = k.max_parts;
+    launch_rows(k.rows, i8, ruled, dim3((unsigned)k.grid), stream, a);
+    if ((st = launch_status()) != FFD_OK) return st;
+    const dim3 merge((unsigned)(k.max_parts / 2 * (k.rows / 8)));
+    if (k.rows == 16) hipLaunchKernelGGL((chunk_merge_kernel<16, 7>), merge, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((chunk_merge_kernel<32, 7>), merge, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
+                                const ffd_score_rules* rules, const float* lse, int B, int T, int Hq, int Hkv, int D,
+                                float softmax_scale, int last, const float* previous, float* weights, hipStream_t stream) {
+    CallScope scope;
+    int st = check_heads(Hq, Hkv, D);
+    if (st == FFD_OK) st = check_batch(B, T, Hq);
+    if (st != FFD_OK) return st;
+    if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale) || last < 0) return FFD_ERR_INVALID_ARGUMENT;
+    if ((st = check_rules(rules)) != FFD_OK || B == 0) return st;
+    bool i8;
+    if ((st = check_paged(cache, &i8)) != FFD_OK) return st;
+    if (!q_start || !seq_lens || !weights || (T > 0 && (!q || !lse))) return FFD_ERR_INVALID_ARGUMENT;
+    if (!pairs_fit(B, Hkv)) return FFD_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(weights) || !aligned16(previous) || !aligned4(lse) || !aligned4(q_start) || !aligned4(seq_lens))
+        return FFD_ERR_INVALID_ARGUMENT;
+    ChunkWeightsArgs a{};
+    static_cast<ChunkArgs&>(a) = chunk_args(q, *cache, q_start, seq_lens, rules, B, T, Hq, Hkv, softmax_scale);
+    a.lse = lse;
+    a.previous = previous;
+    a.weights = weights;
+    a.last = last;
+    const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
+    const long long items = (long long)B * Hkv * ((a.Lcap + kRound - 1) / kRound);
+    const dim3 grid((unsigned)std::min<long long>(items, 16LL * device_cus()));
+    if (i8 && ruled) hipLaunchKernelGGL((chunk_weights_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
+    else if (i8) hipLaunchKernelGGL((chunk_weights_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
+    else if (ruled) hipLaunchKernelGGL((chunk_weights_kernel<false, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((chunk_weights_kernel<false, false>), grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+int ffd_evict_paged(const ffd_paged* cache, const int32_t* new_table, int new_max_pages, const int32_t* seq_lens,
+                    const float* weights, int B, int Hkv, int D, int budget, int recent, int32_t* new_lens, int32_t* kept,
+                    float* new_weights, hipStream_t stream) {
+    int st = check_heads(Hkv, Hkv, D);
+    if (st == FFD_OK) st = check_batch(B, 0, 0);
+    if (st != FFD_OK) return st;
+    if (new_max_pages <= 0 || budget <= 0 || recent < 0 || recent > budget) return FFD_ERR_INVALID_ARGUMENT;
+    if (B == 0) return FFD_OK;
+    bool i8;
+    if ((st = check_paged(cache, &i8)) != FFD_OK) return st;
+    if ((long long)new_max_pages * cache->page > kMaxCapacity) return FFD_ERR_UNSUPPORTED;
+    if (budget > new_max_pages * cache->page) return FFD_ERR_INVALID_ARGUMENT;
+    if (!new_table || !seq_lens || !weights || !new_lens || !kept) return FFD_ERR_INVALID_ARGUMENT;
+    if (!aligned16(weights) || !aligned4(new_table) || !aligned4(seq_lens) || !aligned4(new_lens) || !aligned4(kept) || !aligned4(new_weights))
+        return FFD_ERR_INVALID_ARGUMENT;
+    const long long moves = (budget + kEvictMoveRows - 1) / kEvictMoveRows;
+    if (!pairs_fit(B, Hkv) || moves * B * Hkv * kThreads >= 1LL << 31) return FFD_ERR_UNSUPPORTED;
+    const EvictArgs a{paged_of(*cache), new_table, seq_lens, weights, new_lens, kept, new_weights, Hkv, new_max_pages, budget, recent};
+    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)Hkv, (unsigned)B), dim3(kEvictThreads), 0, stream, a);
+    if ((st = launch_status()) != FFD_OK) return st;
+    const dim3 grid((unsigned)moves, (unsigned)Hkv, (unsigned)B);
+    if (i8) hipLaunchKernelGGL(evict_move_kernel<true>, grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL(evict_move_kernel<false>, grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -26,7 +26,8 @@ NOALLOC_SCRATCH_BYTES = 16 << 20     # FFD_NOALLOC_SCRATCH_BYTES
 EXPORTS = ("ffd_quantize_keys", "ffd_append_kv", "ffd_decode_attention", "ffd_decode_attention_ex",
            "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_write_kv8", "ffd_read_kv8",
            "ffd_kv8_decode_attention", "ffd_kv8_workspace_bytes", "ffd_shared_prefix_decode_attention",
-           "ffd_shared_prefix_workspace_bytes", "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits",
+           "ffd_shared_prefix_workspace_bytes", "ffd_write_paged", "ffd_paged_attention", "ffd_paged_workspace_bytes",
+           "ffd_paged_attention_weights", "ffd_evict_paged", "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits",
            "ffd_workspace_bytes", "ffd_dense_workspace_bytes", "ffd_status_string")
 
 
@@ -61,6 +62,21 @@ class KvCache(ctypes.Structure):
     _fields_ = [("k", P), ("k_absmax", P), ("v", P), ("v_absmax", P)]
 
 
+class PagedCache(ctypes.Structure):
+    """``ffd_paged``: pages and the sequences' table of them."""
+    _fields_ = [("pages", KvCache), ("page_table", P), ("num_pages", I), ("page", I), ("max_pages", I)]
+
+
+class Rotation(ctypes.Structure):
+    """``ffd_rotation``: the norms' weights and the table of the rotation."""
+    _fields_ = [("q_weight", P), ("k_weight", P), ("eps", F), ("table", P), ("rows", I), ("dims", I), ("interleaved", I), ("positions", P)]
+
+
+class ScoreRules(ctypes.Structure):
+    """``ffd_score_rules``: what a score is, and which tokens a query sees."""
+    _fields_ = [("softcap", F), ("window", I), ("slopes", P), ("prefix_lens", P)]
+
+
 def lib() -> ctypes.CDLL:
     """Load libffd.so (once) and declare its signatures."""
     global _lib
@@ -87,6 +103,13 @@ def lib() -> ctypes.CDLL:
     so.ffd_shared_prefix_decode_attention.argtypes = [P, KV, P, I, KV, P, I, I, I, I, I, I, F, P, P, P, SZ, P]
     so.ffd_shared_prefix_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
     so.ffd_shared_prefix_workspace_bytes.restype = SZ
+    PAGED, RULES = ctypes.POINTER(PagedCache), ctypes.POINTER(ScoreRules)
+    so.ffd_write_paged.argtypes = [P, P, P, STRIDES, STRIDES, STRIDES, P, ctypes.POINTER(Rotation), PAGED, P, P, I, I, I, I, I, P]
+    so.ffd_paged_attention.argtypes = [P, PAGED, P, P, RULES, I, I, I, I, I, F, P, P, P, SZ, P]
+    so.ffd_paged_workspace_bytes.argtypes = [I, I, I, I, I]
+    so.ffd_paged_workspace_bytes.restype = SZ
+    so.ffd_paged_attention_weights.argtypes = [P, PAGED, P, P, RULES, P, I, I, I, I, I, F, I, P, P, P]
+    so.ffd_evict_paged.argtypes = [PAGED, P, I, P, P, I, I, I, I, I, P, P, P, P]
     so.ffd_resolve_splits.argtypes = [I, I, I, I]
     so.ffd_fused_splits.argtypes = [I, I, I, I]
     so.ffd_select_kernels.argtypes = [I, I, I, I]
@@ -98,8 +121,8 @@ def lib() -> ctypes.CDLL:
     so.ffd_status_string.restype = ctypes.c_char_p
     for name in ("ffd_quantize_keys", "ffd_append_kv", "ffd_decode_attention", "ffd_decode_attention_ex",
                  "ffd_decode_attention_noalloc", "ffd_dense_decode_attention", "ffd_write_kv8", "ffd_read_kv8",
-                 "ffd_kv8_decode_attention", "ffd_shared_prefix_decode_attention", "ffd_resolve_splits",
-                 "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits"):
+                 "ffd_kv8_decode_attention", "ffd_shared_prefix_decode_attention", "ffd_write_paged", "ffd_paged_attention",
+                 "ffd_paged_attention_weights", "ffd_evict_paged", "ffd_resolve_splits", "ffd_fused_splits", "ffd_select_kernels", "ffd_dense_resolve_splits"):
         getattr(so, name).restype = I
     _lib = so
     return so
@@ -577,6 +600,214 @@ def shared_prefix_decode_attention(q, prefix, prefix_lens, cache, seq_lens, *, n
             HEAD_DIM, num_splits, softmax_scale, out.data_ptr(), _ptr(lse), workspace.data_ptr(),
             _need_workspace(workspace, device))
     return out, lse
+
+
+# ---- paged caches -------------------------------------------------------------------------------------------
+# A paged cache is one of the tuples above whose first dimension counts pages and whose third the tokens of a page:
+# keys and values [num_pages, Hkv, page, 128] (bf16, or 8 bits with absmaxes [num_pages, Hkv, page]), as empty_kv8(num_pages,
+# Hkv, page) and empty_paged make them. page_table int32 [B, max_pages] says where a sequence's pages are; an entry outside
+# [0, num_pages) is a page that is not there. A batch's new tokens are rows q_start[b] .. q_start[b + 1] - 1 (int32 [B + 1]) for
+# sequence b, the last of its seq_lens[b] tokens (int32 [B]).
+
+def empty_paged(num_pages: int, Hkv: int, page: int, device="cuda"):
+    """A bf16 paged cache with uninitialised contents: ``(k, v)``. (For one in 8 bits: ``empty_kv8``.)"""
+    return tuple(torch.empty((num_pages, Hkv, page, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in range(2))
+
+
+def _paged(cache, page_table, device):
+    """(``ffd_paged``, B, Hkv, page, max_pages) of a cache whose tensors are as they have to be."""
+    num_pages, Hkv, page = _cache_dims(cache, "cache", True)
+    kv = _kv_cache(cache, "cache", device, (num_pages, Hkv, page, HEAD_DIM))
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be [B, max_pages]")
+    B, max_pages = page_table.shape
+    _need_on(device, page_table, "page_table", torch.int32, (B, max_pages))
+    return PagedCache(kv, page_table.data_ptr(), num_pages, page, max_pages), B, Hkv, page, max_pages
+
+
+def _ragged(q_start, seq_lens, device, B):
+    _need_on(device, q_start, "q_start", torch.int32, (B + 1,))
+    _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
+
+
+_Strides2 = ctypes.c_int64 * 2
+
+
+def _strided_rows(t, name, device, shape):
+    """The two strides, in elements, of ``t`` as [T, heads, 128]; None where it is contiguous."""
+    if (type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device >= 0
+            and t.is_contiguous()):
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != torch.bfloat16 or t.get_device() != device:
+        raise ValueError(f"{name} must be torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    strides = t.stride()
+    if strides[2] != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    # the stride of a dimension of one is never used, and may be anything
+    return _Strides2(strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0)
+
+
+def write_paged(q, k, v, cache, page_table, q_start, seq_lens, *, q_weight=None, k_weight=None, eps: float = 1e-6, rope=None,
+                interleaved: bool = False, positions=None, out=None):
+    """The new tokens' keys and values into a paged cache (bf16 or 8 bits), and their queries: each head of ``q`` and ``k``
+    is normalised (root mean square, where its weight ``[128]`` is given) and rotated (where ``rope`` is given), in fp32 with
+    one rounding. Returns the queries, bf16 ``[T, Hq, 128]`` (None without ``q``).
+
+    ``q`` bf16 ``[T, Hq, 128]`` or None, ``k``, ``v`` ``[T, Hkv, 128]``, with any strides that are multiples of 8 elements
+    (slices of a projection's output are taken as they are). ``seq_lens`` counts the new tokens already. ``rope``: fp32
+    ``[rows, dims]``, the ``dims / 2`` cosines of a position, then its sines (dims 32, 64, 96 or 128; the other dims are not
+    rotated); pairs are ``(i, i + dims / 2)``, or neighbours where ``interleaved``. ``positions``: int32 ``[T]``, the rows
+    of ``rope``; without it a token's place in the cache (after an eviction that is not its place in the text)."""
+    device = cache[0].get_device() if isinstance(cache, (tuple, list)) and cache and isinstance(cache[0], torch.Tensor) else -1
+    paged, B, Hkv, _, _ = _paged(cache, page_table, device)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError(f"k must be [T, Hkv, {HEAD_DIM}]")
+    T, Hq = k.shape[0], Hkv
+    k_strides, v_strides = _strided_rows(k, "k", device, (T, Hkv, HEAD_DIM)), _strided_rows(v, "v", device, (T, Hkv, HEAD_DIM))
+    q_strides = None
+    if q is not None:
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError(f"q must be [T, Hq, {HEAD_DIM}]")
+        Hq = q.shape[1]
+        q_strides = _strided_rows(q, "q", device, (T, Hq, HEAD_DIM))
+        if out is None:
+            out = q.new_empty((T, Hq, HEAD_DIM))
+        else:
+            _need_on(device, out, "out", torch.bfloat16, (T, Hq, HEAD_DIM))
+    elif out is not None or q_weight is not None:
+        raise ValueError("out and q_weight need q")
+    _ragged(q_start, seq_lens, device, B)
+    rows = dims = 0
+    if rope is not None:
+        if not isinstance(rope, torch.Tensor) or rope.dim() != 2:
+            raise ValueError("rope must be [rows, dims]")
+        rows, dims = rope.shape
+        _need_on(device, rope, "rope", torch.float32, (rows, dims))
+    if positions is not None:
+        _need_on(device, positions, "positions", torch.int32, (T,))
+    for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if weight is not None:
+            _need_on(device, weight, name, torch.bfloat16, (HEAD_DIM,))
+    rotation = Rotation(_ptr(q_weight), _ptr(k_weight), eps, _ptr(rope), rows, dims, bool(interleaved), _ptr(positions))
+    _launch("ffd_write_paged", lib().ffd_write_paged, device, _ptr(q), k.data_ptr(), v.data_ptr(), q_strides, k_strides, v_strides,
+            _ptr(out), ctypes.byref(rotation), ctypes.byref(paged), q_start.data_ptr(), seq_lens.data_ptr(), B, T, Hq, Hkv,
+            HEAD_DIM)
+    return out
+
+
+def paged_workspace_bytes(B: int, T: int, Hq: int, Hkv: int) -> int:
+    """Bytes for ``paged_attention`` of T new tokens of B sequences."""
+    return lib().ffd_paged_workspace_bytes(B, T, Hq, Hkv, HEAD_DIM)
+
+
+def new_paged_workspace(B: int, T: int, Hq: int, Hkv: int, device="cuda"):
+    """A workspace for ``paged_attention`` (one per stream)."""
+    return torch.empty(max(paged_workspace_bytes(B, T, Hq, Hkv), 16), dtype=torch.uint8, device=device)
+
+
+def _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, slopes, prefix_lens):
+    """Checks shared by the calls over new tokens' queries; (device, cache, rules, B, T, Hq, Hkv, Lcap)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError(f"q must be [T, Hq, {HEAD_DIM}]")
+    T, Hq, device = q.shape[0], q.shape[1], q.get_device()
+    _need_on(device, q, "q", torch.bfloat16, (T, Hq, HEAD_DIM))
+    paged, B, Hkv, page, max_pages = _paged(cache, page_table, device)
+    _ragged(q_start, seq_lens, device, B)
+    if slopes is not None:
+        _need_on(device, slopes, "slopes", torch.float32, (Hq,))
+    if prefix_lens is not None:
+        _need_on(device, prefix_lens, "prefix_lens", torch.int32, (B,))
+    rules = None
+    if softcap or window or slopes is not None or prefix_lens is not None:
+        rules = ctypes.byref(ScoreRules(softcap, window, _ptr(slopes), _ptr(prefix_lens)))
+    return device, paged, rules, B, T, Hq, Hkv, page * max_pages
+
+
+def paged_attention(q, cache, page_table, q_start, seq_lens, *, softmax_scale: float = 0.0, softcap: float = 0.0, window: int = 0,
+                    slopes=None, prefix_lens=None, return_lse: bool = True, workspace=None, out=None, lse=None):
+    """Attention of each sequence's new tokens, one or a chunk, over a paged cache that holds them already. ``q``: bf16
+    ``[T, Hq, 128]``. Returns ``(out [T, Hq, 128], lse [T, Hq])``.
+
+    The query at place i scores token j with ``softmax_scale`` q.k, then ``softcap tanh(. / softcap)``, then minus ``slopes[head]
+    |i - j|`` (fp32 ``[Hq]``), and sees it if ``j <= i`` and, with a ``window``, ``i - j < window``, or if ``j < prefix_lens[b]``
+    (int32 ``[B]``). A query that sees nothing gets zeros and ``lse = -inf``. ``workspace``: ``new_paged_workspace``'s."""
+    device, paged, rules, B, T, Hq, Hkv, _ = _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, slopes,
+                                                              prefix_lens)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need_on(device, out, "out", torch.bfloat16, (T, Hq, HEAD_DIM))
+    if lse is not None:
+        _need_on(device, lse, "lse", torch.float32, (T, Hq))
+    elif return_lse:
+        lse = q.new_empty((T, Hq), dtype=torch.float32)
+    if workspace is None:
+        workspace = new_paged_workspace(B, T, Hq, Hkv, q.device)
+    _launch("ffd_paged_attention", lib().ffd_paged_attention, device, q.data_ptr(), ctypes.byref(paged), q_start.data_ptr(),
+            seq_lens.data_ptr(), rules, B, T, Hq, Hkv, HEAD_DIM, softmax_scale, out.data_ptr(), _ptr(lse), workspace.data_ptr(),
+            _need_workspace(workspace, device))
+    return out, lse
+
+
+def paged_attention_weights(q, cache, page_table, q_start, seq_lens, lse, *, softmax_scale: float = 0.0, softcap: float = 0.0,
+                            window: int = 0, slopes=None, prefix_lens=None, last: int = 0, previous=None, out=None):
+    """The attention weight that each cached token gets from the new ones, summed over the query heads of its KV head: fp32
+    ``[B, Hkv, Lcap]``, Lcap the capacity of ``page_table``. ``q`` and the rules are those of the ``paged_attention`` call that
+    gave ``lse``; ``last > 0`` counts the last tokens of each sequence only. Tokens that were there before the new ones start from
+    ``previous`` (same shape; may be ``out``), the new ones from zero. Entries at and behind a length are left as they were
+    (zeros without ``out``)."""
+    device, paged, rules, B, T, Hq, Hkv, Lcap = _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, slopes,
+                                                                 prefix_lens)
+    _need_on(device, lse, "lse", torch.float32, (T, Hq))
+    if previous is not None:
+        _need_on(device, previous, "previous", torch.float32, (B, Hkv, Lcap))
+    if out is None:
+        out = q.new_zeros((B, Hkv, Lcap), dtype=torch.float32)
+    else:
+        _need_on(device, out, "out", torch.float32, (B, Hkv, Lcap))
+    _launch("ffd_paged_attention_weights", lib().ffd_paged_attention_weights, device, _ptr(q), ctypes.byref(paged),
+            q_start.data_ptr(), seq_lens.data_ptr(), rules, _ptr(lse), B, T, Hq, Hkv, HEAD_DIM, softmax_scale, last, _ptr(previous),
+            out.data_ptr())
+    return out
+
+
+def evict_paged(cache, page_table, new_table, seq_lens, weights, budget: int, *, recent: int = 0, new_lens=None, kept=None,
+                new_weights=None):
+    """Keep ``budget`` tokens of each sequence and KV head: the last ``recent`` and the heaviest of the others by ``weights``
+    (``[B, Hkv, Lcap]``; equal ones from the lowest place on), in their order, moved to the pages of ``new_table`` (int32
+    ``[B, new_max_pages]``, other pages of the same cache). Returns ``(kept, new_lens, new_weights)``: the old places int32
+    ``[B, Hkv, budget]`` (-1 behind the last), the lengths int32 ``[B]`` and the kept weights ``[B, Hkv, new_max_pages * page]``
+    (zeros behind the last, or what a given tensor holds)."""
+    device = cache[0].get_device() if isinstance(cache, (tuple, list)) and cache and isinstance(cache[0], torch.Tensor) else -1
+    paged, B, Hkv, page, max_pages = _paged(cache, page_table, device)
+    if not isinstance(new_table, torch.Tensor) or new_table.dim() != 2:
+        raise ValueError("new_table must be [B, new_max_pages]")
+    new_max_pages = new_table.shape[1]
+    _need_on(device, new_table, "new_table", torch.int32, (B, new_max_pages))
+    if new_table.data_ptr() == page_table.data_ptr() and B > 0:
+        raise ValueError("new_table must hold other pages than page_table")
+    _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
+    _need_on(device, weights, "weights", torch.float32, (B, Hkv, max_pages * page))
+    if kept is None:
+        kept = page_table.new_empty((B, Hkv, max(budget, 0)))
+    else:
+        _need_on(device, kept, "kept", torch.int32, (B, Hkv, budget))
+    if new_lens is None:
+        new_lens = page_table.new_empty((B,))
+    else:
+        _need_on(device, new_lens, "new_lens", torch.int32, (B,))
+    if new_weights is None:
+        new_weights = weights.new_zeros((B, Hkv, new_max_pages * page))
+    else:
+        _need_on(device, new_weights, "new_weights", torch.float32, (B, Hkv, new_max_pages * page))
+    _launch("ffd_evict_paged", lib().ffd_evict_paged, device, ctypes.byref(paged), new_table.data_ptr(), new_max_pages,
+            seq_lens.data_ptr(), weights.data_ptr(), B, Hkv, HEAD_DIM, budget, recent, new_lens.data_ptr(), kept.data_ptr(),
+            new_weights.data_ptr())
+    return kept, new_lens, new_weights
 
 
 def default_scale() -> float:
