@@ -353,7 +353,10 @@ template <int NW> __global__ void shared_merge_kernel(SharedMergeArgs a);
 template <bool I8, bool INTERLEAVED> __global__ void write_paged_kernel(WritePagedArgs a);
 // CT (1, 2): tiles of 16 query rows per workgroup; RULED: a cap of the scores or slopes.
 template <int CT, bool I8, bool RULED> __global__ void chunk_rows_kernel(ChunkAttendArgs a);
-// Merges what chunk_rows_kernel<1> or <2> (ROWS 16, 32) cut.
+constexpr int kChunkRowsShift = 7;             // blocks of 128 tokens
+constexpr int kChunkTileThreads = 512, kChunkTileRows = 256, kChunkTileShift = 6;
+template <bool I8, bool RULED> __global__ void chunk_tile_kernel(ChunkAttendArgs a);
+// Merges what a kernel of row tiles of ROWS and blocks of 2^SHIFT tokens cut.
 template <int ROWS, int SHIFT> __global__ void chunk_merge_kernel(ChunkAttendArgs a);
 template <bool I8, bool RULED> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
 constexpr int kEvictThreads = 1024;

@@ -65,7 +65,8 @@ __device__ __forceinline__ int page_entry(const PagedKv& p, int b, int j) {
 // The batch's work cut into items, computed by every wave alone, 64 sequences at a time. A sequence's n G query rows of a
 // KV head are row tiles of ROWS; a tile's blocks (of 2^SHIFT tokens) are cut into `cuts` runs. The cut is the same for all
 // tiles of a sequence: as few runs as keep the longest tile's at or below C blocks, where C gives each of the slots that
-// whole tiles leave an equal part of all blocks. So at most slots + 2 * (tiles * Hkv) items, at most 2 * slots of them parts.
+// whole tiles leave, or of half of all slots, an equal part of all blocks. So there are at most max(slots, slots / 2 + tiles *
+// Hkv) items and, each part being longer than C / 2, at most 2 * slots parts.
 // Items of a sequence are in the order (tile from the last one, which sees most, on; run; KV head).
 struct ChunkItem {
     ChunkSeq seq;
@@ -106,8 +107,18 @@ struct ChunkPlan {
         all *= a.Hkv;
         count *= a.Hkv;
         const long long spare = max(max((long long)a.slots - count, (long long)a.slots / 2), 1LL);
-        const long long c = (all + spare - 1) / spare;
-        return (int)min(max(c, 1LL), (long long)(INT32_MAX / 2));
+        const int C = (int)min(max((all + spare - 1) / spare, 1LL), (long long)(INT32_MAX / 2));
+        if (ROWS < kChunkTileRows || a.B > 64 || count >= a.slots) return C;
+        // Large tiles: a workgroup has its CU to itself, so the smallest C whose items fill the slots once; the lanes try 64.
+        const int least = (int)max(all / a.slots, 1LL), mine = least + (int)((long long)(C - least) * (lane + 1) / 64);
+        long long items = 0;
+        for (uint64_t left = __ballot(tiles > 0); left; left &= left - 1) {
+            const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(left));
+            const int n = __builtin_amdgcn_readlane(blocks, src);
+            items += (long long)__builtin_amdgcn_readlane(tiles, src) * max((n + mine - 1) / mine, 1);
+        }
+        const uint64_t fit = __ballot(items * a.Hkv <= a.slots);
+        return fit ? __builtin_amdgcn_readlane(mine, __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(fit))) : C;
     }
 };
 

@@ -86,20 +86,31 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, int rows, int above, int
     k.max_parts = 2 * k.slots;
     return k;
 }
+// Sequences with up to kFewRows query rows per KV head go to the kernel of few rows, the others to the one of large tiles; where
+// the batch cannot have one kind (few rows in all, or one sequence), or is likely to have none of the second (hardly more
+// new tokens than sequences), one kernel takes all.
+constexpr int kFewRows = 32;
 struct ChunkLaunches {
-    ChunkKernel few;
-    size_t total;
+    bool few, large;
+    ChunkKernel few_kernel, large_kernel;
+    size_t large_off, total;
 };
 ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv) {
     ChunkLaunches p;
     const long long rows = (long long)T * (Hq / Hkv);
-    const int tile = rows <= 16LL * B ? 16 : 32;
-    p.few = chunk_kernel(B, T, Hq, Hkv, tile, 0, INT32_MAX, tile == 16 ? 3 : 2);
-    p.total = partials_bytes((size_t)p.few.max_parts * tile);
+    p.few = B > 1 || rows <= kFewRows;
+    p.large = rows > kFewRows && T > 2LL * B;
+    if (!p.large) p.few = true;
+    const int tile = rows <= 16LL * B || p.large ? 16 : 32;
+    p.few_kernel = chunk_kernel(B, T, Hq, Hkv, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 ? 3 : 2);
+    p.large_kernel = chunk_kernel(B, T, Hq, Hkv, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);
+    p.large_off = p.few ? round_up(partials_bytes((size_t)p.few_kernel.max_parts * tile), kAlign) : 0;
+    p.total = p.large_off + (p.large ? partials_bytes((size_t)p.large_kernel.max_parts * kChunkTileRows) : 0);
     return p;
 }
-
-bool chunk_fits(const ChunkLaunches& p) { return p.few.grid * kThreads < 1LL << 31; }
+bool chunk_fits(const ChunkLaunches& p) {
+    return p.few_kernel.grid * kThreads < 1LL << 31 && p.large_kernel.grid * kChunkTileThreads < 1LL << 31;
+}
 
 template <int CT, bool I8>
 void launch_rows_ruled(bool ruled, dim3 grid, hipStream_t stream, const ChunkAttendArgs& a) {
@@ -205,16 +216,33 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
-    const ChunkKernel& k = plan.few;
-    const Partials P = carve(workspace, (size_t)k.max_parts * k.rows);
-    a.part_m = P.m, a.part_l = P.l, a.part_acc = P.acc;
-    a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.max_parts = k.max_parts;
-    launch_rows(k.rows, i8, ruled, dim3((unsigned)k.grid), stream, a);
-    if ((st = launch_status()) != FFD_OK) return st;
-    const dim3 merge((unsigned)(k.max_parts / 2 * (k.rows / 8)));
-    if (k.rows == 16) hipLaunchKernelGGL((chunk_merge_kernel<16, 7>), merge, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((chunk_merge_kernel<32, 7>), merge, dim3(kThreads), 0, stream, a);
-    return launch_status();
+    auto prepare = [&](const ChunkKernel& k, void* ws) {
+        const Partials P = carve(ws, (size_t)k.max_parts * k.rows);
+        a.part_m = P.m, a.part_l = P.l, a.part_acc = P.acc;
+        a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.max_parts = k.max_parts;
+        return dim3((unsigned)(k.max_parts / 2 * (k.rows / 8)));                // the merge's workgroups
+    };
+    if (plan.large) {
+        const ChunkKernel& k = plan.large_kernel;
+        const dim3 merge = prepare(k, static_cast<uint8_t*>(workspace) + plan.large_off), grid((unsigned)k.grid), block(kChunkTileThreads);
+        if (i8 && ruled) hipLaunchKernelGGL((chunk_tile_kernel<true, true>), grid, block, 0, stream, a);
+        else if (i8) hipLaunchKernelGGL((chunk_tile_kernel<true, false>), grid, block, 0, stream, a);
+        else if (ruled) hipLaunchKernelGGL((chunk_tile_kernel<false, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((chunk_tile_kernel<false, false>), grid, block, 0, stream, a);
+        if ((st = launch_status()) != FFD_OK) return st;
+        hipLaunchKernelGGL((chunk_merge_kernel<kChunkTileRows, kChunkTileShift>), merge, dim3(kThreads), 0, stream, a);
+        if ((st = launch_status()) != FFD_OK) return st;
+    }
+    if (plan.few) {
+        const ChunkKernel& k = plan.few_kernel;
+        const dim3 merge = prepare(k, workspace);
+        launch_rows(k.rows, i8, ruled, dim3((unsigned)k.grid), stream, a);
+        if ((st = launch_status()) != FFD_OK) return st;
+        if (k.rows == 16) hipLaunchKernelGGL((chunk_merge_kernel<16, kChunkRowsShift>), merge, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((chunk_merge_kernel<32, kChunkRowsShift>), merge, dim3(kThreads), 0, stream, a);
+        st = launch_status();
+    }
+    return st;
 }
 
 int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,

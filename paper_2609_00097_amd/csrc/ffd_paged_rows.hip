@@ -11,7 +11,7 @@ namespace ffd {
 
 namespace {
 
-constexpr int kRowsShift = 7;                   // blocks of kRound tokens
+constexpr int kRowsShift = kChunkRowsShift;     // blocks of kRound tokens
 static_assert(kRound == 1 << kRowsShift);
 
 // The pages of a wave's 32 tokens: first rows of both 16-token halves, whether they are there.
@@ -335,5 +335,6 @@ template __global__ void chunk_rows_kernel<2, true, false>(ChunkAttendArgs);
 template __global__ void chunk_rows_kernel<2, true, true>(ChunkAttendArgs);
 template __global__ void chunk_merge_kernel<16, kRowsShift>(ChunkAttendArgs);
 template __global__ void chunk_merge_kernel<32, kRowsShift>(ChunkAttendArgs);
+template __global__ void chunk_merge_kernel<kChunkTileRows, kChunkTileShift>(ChunkAttendArgs);
 
 }  // namespace ffd

@@ -42,19 +42,13 @@
 // values in 2 u + 2 and 2 u + 3. Each team stages half of the rows in its vector phases: team 1 the keys of tile u + 1
 // and the values of u in phase 2 u, team 0 the same in 2 u + 1, which is after the last read of tiles u - 1 and u - 2,
 // whose places they take, and before their first use. The loads for them are issued one vector phase earlier.
-#include "ffd_attend.h"
+#include "ffd_tile.h"
 
 namespace ffd {
 
 namespace {
 
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-
 constexpr int kPThreads = kPrefixTileThreads;
-constexpr float kSlack = 8.f;                  // growth of the maximum, in powers of two, that rescales
 
 template <int RW, bool I8>
 struct PrefixShape {
@@ -89,20 +83,6 @@ struct PrefixLds {
     int longest[8];                            // each wave's; apart from m, which a run without tiles writes next, no barrier between
     float m[8][32], l[8][32];
 };
-
-// Chunk order of the two kinds of rows.
-__device__ __forceinline__ int key_chunk(int row, int c) { return c ^ (row & 15); }
-template <bool I8>                             // 8 bits: a store takes every second chunk of two rows, which then complement
-__device__ __forceinline__ int value_chunk(int row, int c) { return c ^ (((row & 3) << 2) | ((row >> 2) & 3)) ^ (I8 ? row & 1 : 0); }
-
-__device__ __forceinline__ float halves_max(float x) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float halves_sum(float x) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
 
 // A team's part of a tile on its way from memory to LDS, in registers: rows [part kPartTokens, ..) of the tile. `last` is
 // the last row of the tile that any query sees; rows behind it repeat it.
