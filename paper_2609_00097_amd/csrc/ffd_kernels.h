@@ -251,16 +251,35 @@ struct ChunkArgs {
     float scale;
 };
 
-// Their attention. A kernel takes the sequences with rows_above < n G <= rows_upto query rows per KV head; `slots` is the
-// number of workgroups that its work is cut for (0: every row tile whole). Partial states of row tiles that are cut: part p
-// has the rows from part0 + p * (rows of a tile) on.
+// Partial states of the row tiles that are cut into runs: part p has `rows` rows from p * rows on. records tell the merge
+// what is there: (first token's row of the batch, KV head, rows in use, runs), no runs where there is none. Large tiles:
+// record p is of part p, for a tile's first run, the next one is part p + Hkv, and total[0] is the number of parts. Few rows
+// (total null): record w is of the tile that workgroup w begins but does not end; its runs are parts 2 w + 1, 2 (w + 1), 2 (w + 2), ..
+struct ChunkParts {
+    float* m;
+    float* l;
+    float* acc;
+    int4* records;
+    int* total;
+    int rows, count;            // rows of a tile, most parts
+};
+
+// Attention of a batch's new tokens. A kernel takes the sequences with rows_above < n G <= rows_upto query rows per KV head;
+// `slots` is the number of workgroups that its work is cut for.
 struct ChunkAttendArgs : ChunkArgs {
-    float* part_m;
-    float* part_l;
-    float* part_acc;
+    ChunkParts parts;
     uint16_t* out;              // bf16 [T, Hq, 128]
     float* lse;                 // [T, Hq] or null
-    int rows_above, rows_upto, slots, max_parts;
+    int rows_above, rows_upto, slots;
+    int min_share;              // few rows: fewest units of a workgroup
+    int unit_shift;             // few rows: work is counted in 2^unit_shift blocks, so that its sum fits 31 bits
+};
+struct ChunkMergeArgs {
+    ChunkParts parts[2];
+    int wgs;                    // workgroups of the first
+    uint16_t* out;
+    float* lse;
+    int Hq, Hkv, G;
 };
 
 struct ChunkWeightsArgs : ChunkArgs {
@@ -356,8 +375,9 @@ template <int CT, bool I8, bool RULED> __global__ void chunk_rows_kernel(ChunkAt
 constexpr int kChunkRowsShift = 7;             // blocks of 128 tokens
 constexpr int kChunkTileThreads = 512, kChunkTileRows = 256, kChunkTileShift = 6;
 template <bool I8, bool RULED> __global__ void chunk_tile_kernel(ChunkAttendArgs a);
-// Merges what a kernel of row tiles of ROWS and blocks of 2^SHIFT tokens cut.
-template <int ROWS, int SHIFT> __global__ void chunk_merge_kernel(ChunkAttendArgs a);
+// Rows of a tile of `rows` that a workgroup of the merge takes.
+__host__ __device__ constexpr int chunk_merge_rows(int rows) { return rows < kChunkTileRows ? 16 : 32; }
+__global__ void chunk_merge_kernel(ChunkMergeArgs a);
 template <bool I8, bool RULED> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
 constexpr int kEvictThreads = 1024;
 __global__ void evict_select_kernel(EvictArgs a);

@@ -62,12 +62,17 @@ __device__ __forceinline__ int page_entry(const PagedKv& p, int b, int j) {
     return i < p.max_pages ? e : -1;
 }
 
-// The batch's work cut into items, computed by every wave alone, 64 sequences at a time. A sequence's n G query rows of a
-// KV head are row tiles of ROWS; a tile's blocks (of 2^SHIFT tokens) are cut into `cuts` runs. The cut is the same for all
-// tiles of a sequence: as few runs as keep the longest tile's at or below C blocks, where C gives each of the slots that
-// whole tiles leave, or of half of all slots, an equal part of all blocks. So there are at most max(slots, slots / 2 + tiles *
-// Hkv) items and, each part being longer than C / 2, at most 2 * slots parts.
-// Items of a sequence are in the order (tile from the last one, which sees most, on; run; KV head).
+// The same for a token that all lanes agree on, through the scalar cache: the entry is waited for by itself and not, as a
+// vector load's result, behind all loads that are under way.
+__device__ __forceinline__ int uniform_page_entry(const PagedKv& p, int b, int j) {
+    const int i = __builtin_amdgcn_readfirstlane(j >> p.page_shift);
+    const auto* table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p.table));
+    const int e = table[(size_t)__builtin_amdgcn_readfirstlane(b) * p.max_pages + min(i, p.max_pages - 1)];
+    return i < p.max_pages ? e : -1;
+}
+
+// The batch's work, laid out by every wave alone, 64 sequences at a time. A sequence's n G query rows of a KV head are row
+// tiles of ROWS rows.
 struct ChunkItem {
     ChunkSeq seq;
     int b, kvh, tile, run, cuts;
@@ -76,7 +81,7 @@ struct ChunkItem {
 template <int ROWS, int SHIFT>
 struct ChunkPlan {
     ChunkSeq seq;               // this lane's sequence of the 64 at hand
-    int tiles, blocks;
+    int tiles, blocks;          // of a tile at most
     __device__ __forceinline__ void load(const ChunkAttendArgs& a, int b0, int lane) {
         const int b = b0 + lane;
         seq = chunk_seq(a, min(b, a.B - 1));
@@ -85,13 +90,21 @@ struct ChunkPlan {
         if (b < a.B && rows > a.rows_above && rows <= a.rows_upto) {
             tiles = (int)((rows + ROWS - 1) / ROWS);
             const int step = ROWS / a.G;
-            blocks = chunk_span<SHIFT>(a, seq, (tiles - 1) * step, seq.n - 1).count;
+            // of the last tile, as if it saw all before it, but within a window no more than a tile's first and last place span
+            const ChunkSpan all = chunk_span<SHIFT>(a, seq, (tiles - 1) * step, seq.n - 1);
+            blocks = all.count + all.skip;
+            if (a.window > 0) blocks = min(blocks, all.prefix + ((a.window + step - 2) >> SHIFT) + 2);
         }
+    }
+    __device__ __forceinline__ void give(ChunkSeq& s, int src) const {
+        s.q0 = __builtin_amdgcn_readlane(seq.q0, src);
+        s.n = __builtin_amdgcn_readlane(seq.n, src);
+        s.L = __builtin_amdgcn_readlane(seq.L, src);
+        s.pre = __builtin_amdgcn_readlane(seq.pre, src);
     }
     __device__ __forceinline__ int cuts_for(int C) const { return max((blocks + C - 1) / C, 1); }
     // C, with the first 64 sequences loaded
     __device__ __forceinline__ int run_blocks(const ChunkAttendArgs& a, int lane) {
-        if (a.slots <= 0) return INT32_MAX / 2;
         long long all = 0, count = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             if (b0 > 0) load(a, b0, lane);
@@ -122,13 +135,18 @@ struct ChunkPlan {
     }
 };
 
-// The item of workgroup wg; false: there is none. PARTS: only sequences that are cut count, and part is wg itself.
+// Large tiles: each tile's blocks (of 2^SHIFT tokens) are cut into `cuts` runs, the same number for all tiles of a sequence: as few
+// runs as keep the longest tile's at or below C blocks, where C gives each of the slots that whole tiles leave, or of half of all
+// slots, an equal part of all blocks. So there are at most max(slots, slots / 2 + tiles * Hkv) items and, a tile that is cut
+// being longer than C, at most `slots` parts. Items of a sequence are in the order (tile from the last one, which sees most, on;
+// run; KV head). The item of workgroup wg; false: there is none. Workgroup 0 leaves the number of parts for the merge.
 template <int ROWS, int SHIFT>
 __device__ __forceinline__ bool chunk_item(const ChunkAttendArgs& a, int wg, int lane, ChunkItem& it) {
     ChunkPlan<ROWS, SHIFT> plan;
     plan.load(a, 0, lane);
     const int C = plan.run_blocks(a, lane);
     int before = 0, parts_before = 0;
+    bool found = false;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         if (b0 > 0) plan.load(a, b0, lane);
         const int cuts = plan.cuts_for(C), items = plan.tiles * cuts * a.Hkv, parts = cuts > 1 ? items : 0;
@@ -138,10 +156,7 @@ __device__ __forceinline__ bool chunk_item(const ChunkAttendArgs& a, int wg, int
         if (hit != 0) {
             const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
             it.b = b0 + src;
-            it.seq.q0 = __builtin_amdgcn_readlane(plan.seq.q0, src);
-            it.seq.n = __builtin_amdgcn_readlane(plan.seq.n, src);
-            it.seq.L = __builtin_amdgcn_readlane(plan.seq.L, src);
-            it.seq.pre = __builtin_amdgcn_readlane(plan.seq.pre, src);
+            plan.give(it.seq, src);
             it.cuts = __builtin_amdgcn_readlane(cuts, src);
             const int at = __builtin_amdgcn_readfirstlane(wg) - __builtin_amdgcn_readlane(first, src);
             const int rest = at / a.Hkv;
@@ -151,12 +166,17 @@ __device__ __forceinline__ bool chunk_item(const ChunkAttendArgs& a, int wg, int
             it.tile = __builtin_amdgcn_readlane(plan.tiles, src) - 1 - turn;
             it.part = -1;
             if (it.cuts > 1) it.part = parts_before + __builtin_amdgcn_readlane(parts_incl - parts, src) + at;
-            return true;
+            found = it.part < a.parts.count;
+            if (wg != 0) return found;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
         parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
     }
-    return false;
+    if (wg == 0 && threadIdx.x == 0) a.parts.total[0] = min(parts_before, a.parts.count);
+    return found;
+}
+__device__ __forceinline__ void write_record(const ChunkAttendArgs& a, const ChunkItem& it, int tok0, int live) {
+    if (it.part >= 0 && threadIdx.x == 0) a.parts.records[it.part] = make_int4(it.seq.q0 + tok0, it.kvh, live, it.run == 0 ? it.cuts : 0);
 }
 
 // What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). tanh(x) =

@@ -71,46 +71,64 @@ ChunkArgs chunk_args(const void* q, const ffd_paged& c, const int32_t* q_start, 
     return a;
 }
 
-// One kernel's part of the attention: row tiles of `rows`, workgroups, and the partial states of tiles that are cut.
+// One kernel's part of the attention: row tiles of `rows`, workgroups, and its part of the workspace.
 struct ChunkKernel {
-    int rows, rows_above, rows_upto, slots;
+    int rows, rows_above, rows_upto, slots, unit_shift;
     long long grid;
-    int max_parts;
+    bool large() const { return rows == kChunkTileRows; }
+    int parts_count() const { return large() ? slots : 2 * slots; }
+    size_t records_off() const { return round_up(partials_bytes((size_t)parts_count() * rows), kAlign); }
+    size_t total_off() const { return records_off() + round_up(slots * sizeof(int4), kAlign); }
+    size_t bytes() const { return total_off() + kAlign; }
+    ChunkParts parts(uint8_t* ws) const {
+        const Partials P = carve(ws, (size_t)parts_count() * rows);
+        return ChunkParts{P.m, P.l, P.acc, reinterpret_cast<int4*>(ws + records_off()),
+                          large() ? reinterpret_cast<int*>(ws + total_off()) : nullptr, rows, parts_count()};
+    }
+    int merge_wgs() const { return slots * 4 * (rows / chunk_merge_rows(rows)); }
 };
-ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, int rows, int above, int upto, int per_cu) {
+ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows, int above, int upto, int per_cu) {
     ChunkKernel k{rows, above, upto, per_cu * device_cus(), 0, 0};
     const int G = Hq / Hkv;
     // every sequence has at most one tile that is not full
-    const long long tiles = (long long)T * G / rows + std::min(B, T);
-    k.grid = std::max((long long)k.slots, k.slots / 2 + tiles * Hkv);
-    k.max_parts = 2 * k.slots;
+    const long long tiles = ((long long)T * G / rows + std::min(B, T)) * Hkv;
+    k.grid = k.large() ? std::max((long long)k.slots, k.slots / 2 + tiles) : k.slots;
+    while (tiles * (((Lcap + kRound - 1) / kRound >> k.unit_shift) + 1) >= 1LL << 31) ++k.unit_shift;
     return k;
 }
-// Sequences with up to kFewRows query rows per KV head go to the kernel of few rows, the others to the one of large tiles; where
-// the batch cannot have one kind (few rows in all, or one sequence), or is likely to have none of the second (hardly more
-// new tokens than sequences), one kernel takes all.
+// Sequences with up to kFewRows query rows per KV head go to the kernel of few rows, the others to the one of large tiles. One
+// kernel takes all where the batch cannot have both kinds (few rows in all, or one sequence), is likely to have none of the second
+// (hardly more new tokens than sequences), or has little work: rows times tokens of the capacity per CU.
 constexpr int kFewRows = 32;
+constexpr long long kLittleWork = 24 << 10;
+// Blocks of a workgroup of the few-row kernel at least: 1 / 2 / 4, whole calls, eight heads, bf16: one token on 4K 12.7 / 12.6 / 14.2 us,
+// on 8K 18.4 / 14.6 / 15.5, 16 on 4K 28.4 / 20.6 / 19.9, 4 on 2K in eight sequences 23.3 / 23.0 / 20.6.
+constexpr int kMinShare = 2;
 struct ChunkLaunches {
     bool few, large;
     ChunkKernel few_kernel, large_kernel;
     size_t large_off, total;
 };
-ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv) {
+ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv, long long Lcap, bool i8) {
     ChunkLaunches p;
     const long long rows = (long long)T * (Hq / Hkv);
-    p.few = B > 1 || rows <= kFewRows;
-    p.large = rows > kFewRows && T > 2LL * B;
-    if (!p.large) p.few = true;
+    p.large = rows > kFewRows && T > 2LL * B && rows * Lcap * Hkv > kLittleWork * device_cus();
+    p.few = B > 1 || !p.large;
     const int tile = rows <= 16LL * B || p.large ? 16 : 32;
-    p.few_kernel = chunk_kernel(B, T, Hq, Hkv, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 ? 3 : 2);
-    p.large_kernel = chunk_kernel(B, T, Hq, Hkv, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);
-    p.large_off = p.few ? round_up(partials_bytes((size_t)p.few_kernel.max_parts * tile), kAlign) : 0;
-    p.total = p.large_off + (p.large ? partials_bytes((size_t)p.large_kernel.max_parts * kChunkTileRows) : 0);
+    p.few_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 && i8 ? 3 : 2);
+    p.large_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);
+    p.large_off = p.few ? p.few_kernel.bytes() : 0;
+    p.total = p.large_off + (p.large ? p.large_kernel.bytes() : 0);
     return p;
 }
-bool chunk_fits(const ChunkLaunches& p) {
-    return p.few_kernel.grid * kThreads < 1LL << 31 && p.large_kernel.grid * kChunkTileThreads < 1LL << 31;
+// Enough for any capacity and form of the cache.
+size_t chunk_workspace(int B, int T, int Hq, int Hkv) {
+    size_t bytes = 0;
+    for (const long long Lcap : {0, kMaxCapacity})
+        for (const bool i8 : {false, true}) bytes = std::max(bytes, chunk_launches(B, T, Hq, Hkv, Lcap, i8).total);
+    return bytes;
 }
+bool chunk_fits(const ChunkLaunches& p) { return p.large_kernel.grid * kChunkTileThreads < 1LL << 31; }
 
 template <int CT, bool I8>
 void launch_rows_ruled(bool ruled, dim3 grid, hipStream_t stream, const ChunkAttendArgs& a) {
@@ -190,8 +208,7 @@ int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* 
 size_t ffd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
     CallScope scope;
     if (check_heads(Hq, Hkv, D) != FFD_OK || check_batch(B, T, Hq) != FFD_OK || B == 0 || T == 0) return 0;
-    const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv);
-    return pairs_fit(B, Hkv) && chunk_fits(plan) ? plan.total : 0;
+    return pairs_fit(B, Hkv) && chunk_fits(chunk_launches(B, T, Hq, Hkv, 0, false)) ? chunk_workspace(B, T, Hq, Hkv) : 0;
 }
 
 int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
@@ -208,41 +225,41 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
     if (!q || !q_start || !seq_lens || !out || !workspace) return FFD_ERR_INVALID_ARGUMENT;
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(q_start) || !aligned4(seq_lens) || !aligned4(lse))
         return FFD_ERR_INVALID_ARGUMENT;
-    const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv);
+    const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv, (long long)cache->max_pages * cache->page, i8);
     if (!pairs_fit(B, Hkv) || !chunk_fits(plan)) return FFD_ERR_UNSUPPORTED;
-    if (workspace_bytes < plan.total) return FFD_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < chunk_workspace(B, T, Hq, Hkv)) return FFD_ERR_WORKSPACE_TOO_SMALL;
     ChunkAttendArgs a{};
     static_cast<ChunkArgs&>(a) = chunk_args(q, *cache, q_start, seq_lens, rules, B, T, Hq, Hkv, softmax_scale);
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
     const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
-    auto prepare = [&](const ChunkKernel& k, void* ws) {
-        const Partials P = carve(ws, (size_t)k.max_parts * k.rows);
-        a.part_m = P.m, a.part_l = P.l, a.part_acc = P.acc;
-        a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.max_parts = k.max_parts;
-        return dim3((unsigned)(k.max_parts / 2 * (k.rows / 8)));                // the merge's workgroups
+    ChunkMergeArgs m{{}, 0, a.out, lse, Hq, Hkv, Hq / Hkv};
+    int sets = 0, wgs = 0;
+    auto prepare = [&](const ChunkKernel& k, uint8_t* ws) {
+        a.parts = k.parts(ws);
+        a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.unit_shift = k.unit_shift, a.min_share = kMinShare;
+        m.parts[sets++] = a.parts;
+        if (sets == 1) m.wgs = k.merge_wgs();
+        wgs += k.merge_wgs();
     };
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (plan.large) {
         const ChunkKernel& k = plan.large_kernel;
-        const dim3 merge = prepare(k, static_cast<uint8_t*>(workspace) + plan.large_off), grid((unsigned)k.grid), block(kChunkTileThreads);
+        prepare(k, ws + plan.large_off);
+        const dim3 grid((unsigned)k.grid), block(kChunkTileThreads);
         if (i8 && ruled) hipLaunchKernelGGL((chunk_tile_kernel<true, true>), grid, block, 0, stream, a);
         else if (i8) hipLaunchKernelGGL((chunk_tile_kernel<true, false>), grid, block, 0, stream, a);
         else if (ruled) hipLaunchKernelGGL((chunk_tile_kernel<false, true>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((chunk_tile_kernel<false, false>), grid, block, 0, stream, a);
         if ((st = launch_status()) != FFD_OK) return st;
-        hipLaunchKernelGGL((chunk_merge_kernel<kChunkTileRows, kChunkTileShift>), merge, dim3(kThreads), 0, stream, a);
-        if ((st = launch_status()) != FFD_OK) return st;
     }
     if (plan.few) {
-        const ChunkKernel& k = plan.few_kernel;
-        const dim3 merge = prepare(k, workspace);
-        launch_rows(k.rows, i8, ruled, dim3((unsigned)k.grid), stream, a);
+        prepare(plan.few_kernel, ws);
+        launch_rows(plan.few_kernel.rows, i8, ruled, dim3((unsigned)plan.few_kernel.grid), stream, a);
         if ((st = launch_status()) != FFD_OK) return st;
-        if (k.rows == 16) hipLaunchKernelGGL((chunk_merge_kernel<16, kChunkRowsShift>), merge, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((chunk_merge_kernel<32, kChunkRowsShift>), merge, dim3(kThreads), 0, stream, a);
-        st = launch_status();
     }
-    return st;
+    hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)wgs), dim3(kThreads), 0, stream, m);
+    return launch_status();
 }
 
 int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,

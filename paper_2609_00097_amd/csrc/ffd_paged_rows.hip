@@ -18,13 +18,15 @@ static_assert(kRound == 1 << kRowsShift);
 struct TilePages {
     int entry[2];
     __device__ __forceinline__ void load(const PagedKv& p, int b, int t0) {
-        entry[0] = page_entry(p, b, t0);
-        entry[1] = page_entry(p, b, t0 + 16);
+        entry[0] = uniform_page_entry(p, b, t0);
+        entry[1] = uniform_page_entry(p, b, t0 + 16);
     }
-    __device__ __forceinline__ bool there(const PagedKv& p, int t) const { return page_there(p, entry[t]); }
-    __device__ __forceinline__ void rows(const PagedKv& p, int Hkv, int kvh, int t0, size_t (&row)[2]) const {
+    __device__ __forceinline__ void rows(const PagedKv& p, int Hkv, int kvh, int t0, size_t (&row)[2], bool (&there)[2]) const {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) row[t] = page_row(p, Hkv, kvh, there(p, t) ? entry[t] : 0, t0 + 16 * t);
+        for (int t = 0; t < 2; ++t) {
+            there[t] = page_there(p, entry[t]);
+            row[t] = page_row(p, Hkv, kvh, there[t] ? entry[t] : 0, t0 + 16 * t);
+        }
     }
 };
 
@@ -58,31 +60,32 @@ struct Rows {
     int low, high;              // the first and the last place, of all rows
 };
 
-// Blocks [first, last) of the span. FINITE: infinities and NaN are taken out of every tile, see attend().
-template <int CT, bool I8, bool RULED, bool FINITE>
+// Blocks [first, last) of the span. finite: infinities and NaN are taken out of every tile, see attend().
+template <int CT, bool I8, bool RULED>
 __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<CT>& st, const v8bf (&q)[CT][4], const Rows<CT>& rows,
                                              const ScoreRule& rule, const ChunkItem& it, const ChunkSpan& span, int first, int last,
-                                             int wave, int n, int g) {
+                                             bool finite, int wave, int n, int g) {
     if (first >= last) return;
     const int cached = min(it.seq.L, a.Lcap), pre = it.seq.pre, window = a.window;
     auto token = [&](int u) { return span.block(u) * kRound + kTile * wave; };
     // A wave's tile behind what any query sees is loaded all the same, from page 0 if its own is not there.
     TilePages pages, next_pages;
     size_t row[2];
+    bool there[2];
     int t0 = token(first);
     pages.load(a.pages, it.b, t0);
     next_pages.load(a.pages, it.b, token(min(first + 1, last - 1)));
     KeyTile<I8> kt;
     ValueTile<I8> vt;
     __builtin_amdgcn_s_waitcnt(0x0f70);         // vmcnt(0): see attend()
-    pages.rows(a.pages, a.Hkv, it.kvh, t0, row);
+    pages.rows(a.pages, a.Hkv, it.kvh, t0, row, there);
     kt.load_halves(a.pages.kv, row, n, g);
     vt.load_halves(a.pages.kv, row, n, g);
     for (int u = first; u < last; ++u) {
-        const bool there[2] = {pages.there(a.pages, 0), pages.there(a.pages, 1)};
         const int t1 = token(min(u + 1, last - 1));
         size_t next[2];
-        next_pages.rows(a.pages, a.Hkv, it.kvh, t1, next);
+        bool next_there[2];
+        next_pages.rows(a.pages, a.Hkv, it.kvh, t1, next, next_there);
         v4f s[CT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -102,7 +105,6 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
             else zs[e] = rule.zscale;
         }
         kt.load_halves(a.pages.kv, next, n, g);
-        pages = next_pages;
         next_pages.load(a.pages, it.b, token(min(u + 2, last - 1)));
 
         // every row sees the whole tile, or not
@@ -171,7 +173,7 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
         }
         if constexpr (!I8) {
             if (masked) vt.keep(alive);
-            if ((masked || FINITE) && __ballot(!vt.all_finite()) != 0) {
+            if ((masked || finite) && __ballot(!vt.all_finite()) != 0) {
                 vt.make_finite();
                 add_seen_nonfinite<CT>(st, a.pages.kv, row, there, t0, span.end, rows.at, window, pre, g);
             }
@@ -180,8 +182,13 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
         vt.operands(f);
         row[0] = next[0];
         row[1] = next[1];
+        there[0] = next_there[0];
+        there[1] = next_there[1];
         t0 = t1;
         vt.load_halves(a.pages.kv, row, n, g);
+        // The compiler would move these loads to their use in the next turn (none after the last one): 72 us for 32 sequences of
+        // 500 to 8K tokens in 8 bits, 58 so.
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -195,131 +202,164 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
 
 }  // namespace
 
+// Work in the order (sequence, tile, KV head, block), a tile of a sequence counted as its longest one, in equal shares of
+// consecutive blocks, one for each workgroup: a share is the end of one tile, whole tiles, and the beginning of another. A tile
+// that is whole in a share goes to the outputs, else the workgroup leaves at most two partial states: 2 w + 1 of the tile
+// that it begins, 2 w of one that another began.
 template <int CT, bool I8, bool RULED>
-__global__ __launch_bounds__(kThreads, CT == 1 ? 3 : 2) void chunk_rows_kernel(ChunkAttendArgs a) {
+__global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_kernel(ChunkAttendArgs a) {
     __shared__ JoinLds<CT> lds;
+    constexpr int kRows = 16 * CT;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int g = lane >> 4, n = lane & 15;
-    ChunkItem it;
-    if (!chunk_item<16 * CT, kRowsShift>(a, blockIdx.x, lane, it) || it.part >= a.max_parts) return;
-    const int gs = __builtin_ctz(a.G), step = (16 * CT) >> gs, tok0 = it.tile * step;
-    const int live = min(16 * CT, (it.seq.n - tok0) << gs);
-    const int hq0 = it.kvh * a.G, place = it.seq.L - it.seq.n;
-    v8bf q[CT][4];
-    Rows<CT> rows;
-    ScoreRule rule = score_rule(a, I8, hq0);
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int r = min(16 * c + n, live - 1), tok = tok0 + (r >> gs), head = hq0 + (r & (a.G - 1));
-        load_query<I8>(q[c], a.q + ((size_t)(it.seq.q0 + tok) * a.Hq + head) * kD, g);
-        rows.at[c] = place + tok;
-        rows.slope2[c] = RULED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    const int g = lane >> 4, n = lane & 15, wg = blockIdx.x;
+    const int gs = __builtin_ctz(a.G), step = kRows >> gs;
+    ChunkPlan<kRows, kRowsShift> plan;
+    auto units = [&]() { return (plan.blocks + (1 << a.unit_shift) - 1) >> a.unit_shift; };      // of a tile
+    // a tile without blocks is one unit, for its empty rows to be written
+    auto work = [&]() { return plan.tiles * max(units(), 1) * a.Hkv; };
+    int all = 0;
+    for (int b0 = (a.B - 1) & ~63; b0 >= 0; b0 -= 64) {         // backwards, to end at the first ones
+        plan.load(a, b0, lane);
+        all += __builtin_amdgcn_readlane(wave_inclusive_scan(work()), 63);
     }
-    const int tok1 = min(tok0 + step, it.seq.n) - 1;
-    rows.low = place + tok0;
-    rows.high = place + tok1;
-    const ChunkSpan span = chunk_span<kRowsShift>(a, it.seq, tok0, tok1);
-    const int first = (int)((long long)span.count * it.run / it.cuts), last = (int)((long long)span.count * (it.run + 1) / it.cuts);
-    RowState<CT> st;
-    st.clear();
-    attend_pages<CT, I8, RULED, false>(a, st, q, rows, rule, it, span, first, last, wave, n, g);
-    if (!I8 && __ballot(!st.all_finite()) != 0) {
-        st.clear();
-        attend_pages<CT, I8, RULED, true>(a, st, q, rows, rule, it, span, first, last, wave, n, g);
-    }
-    join_waves(lds, st, wave, n, g);
-    for (int i = tid; i < live * (kD / 4); i += kThreads) {
-        const int r = i >> 5, d4 = i & 31;
-        const float4 x = *reinterpret_cast<const float4*>(&lds.acc[0][r][4 * d4]);
-        const float4 y = *reinterpret_cast<const float4*>(&lds.acc[1][r][4 * d4]);
-        const float4 o = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-        if (it.part >= 0) {
-            const size_t to = (size_t)it.part * (16 * CT) + r;
-            *reinterpret_cast<float4*>(a.part_acc + to * kD + 4 * d4) = o;
-            if (d4 == 0) joined_ml(lds, r, a.part_m[to], a.part_l[to]);
-        } else {
-            const size_t to = (size_t)(it.seq.q0 + tok0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1));
-            float m, l;
-            joined_ml(lds, r, m, l);
-            const bool any = m != -INFINITY;
-            const float inv = any ? 1.f / l : 0.f;
-            const uint2 w = any ? make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
-            *reinterpret_cast<uint2*>(a.out + to * kD + 4 * d4) = w;
-            if (d4 == 0 && a.lse) a.lse[to] = any ? m + logf(l) : -INFINITY;
+    const int share = max((all + a.slots - 1) / a.slots, a.min_share);
+    int u = wg * share;
+    const int end = min(u + share, all);
+    bool begun = false;                         // a tile that another workgroup ends
+    while (u < end) {                           // uniform
+        ChunkItem it{};
+        int tile_units = 1, at = 0, before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            if (b0 > 0 || u != wg * share) plan.load(a, b0, lane);          // (kept, it would cost the loop registers)
+            const int mine = work(), incl = wave_inclusive_scan(mine), first = before + incl - mine;
+            const uint64_t hit = __ballot(u >= first && u < first + mine);
+            if (hit != 0) {
+                const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
+                it.b = b0 + src;
+                plan.give(it.seq, src);
+                tile_units = max(__builtin_amdgcn_readlane(units(), src), 1);
+                at = __builtin_amdgcn_readfirstlane(u) - __builtin_amdgcn_readlane(first, src);
+                break;
+            }
+            before += __builtin_amdgcn_readlane(incl, 63);
         }
+        const int pair = at / tile_units, from = at - pair * tile_units, to = min(tile_units, from + end - u);
+        it.tile = pair / a.Hkv;
+        it.kvh = pair - it.tile * a.Hkv;
+        it.part = from == 0 && to == tile_units ? -1 : 2 * wg + (from == 0 ? 1 : 0);
+        u += to - from;
+        const int tok0 = it.tile * step, live = min(kRows, (it.seq.n - tok0) << gs);
+        const int hq0 = it.kvh * a.G, place = it.seq.L - it.seq.n;
+        if (it.part >= 0 && from == 0) {
+            begun = true;
+            if (tid == 0) a.parts.records[wg] = make_int4(it.seq.q0 + tok0, it.kvh, live, 1 + (tile_units - to + share - 1) / share);
+        }
+        v8bf q[CT][4];
+        Rows<CT> rows;
+        const ScoreRule rule = score_rule(a, I8, hq0);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const int r = min(16 * c + n, live - 1), tok = tok0 + (r >> gs), head = hq0 + (r & (a.G - 1));
+            load_query<I8>(q[c], a.q + ((size_t)(it.seq.q0 + tok) * a.Hq + head) * kD, g);
+            rows.at[c] = place + tok;
+            rows.slope2[c] = RULED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+        }
+        const int tok1 = min(tok0 + step, it.seq.n) - 1;
+        rows.low = place + tok0;
+        rows.high = place + tok1;
+        const ChunkSpan span = chunk_span<kRowsShift>(a, it.seq, tok0, tok1);
+        const int first = (int)min((long long)span.count, (long long)from << a.unit_shift), last = (int)min((long long)span.count, (long long)to << a.unit_shift);
+        RowState<CT> st;
+        for (bool finite = false;; finite = true) {
+            st.clear();
+            attend_pages<CT, I8, RULED>(a, st, q, rows, rule, it, span, first, last, finite, wave, n, g);
+            if (I8 || finite || __ballot(!st.all_finite()) == 0) break;
+        }
+        join_waves(lds, st, wave, n, g);
+        for (int i = tid; i < live * (kD / 4); i += kThreads) {
+            const int r = i >> 5, d4 = i & 31;
+            const float4 x = *reinterpret_cast<const float4*>(&lds.acc[0][r][4 * d4]);
+            const float4 y = *reinterpret_cast<const float4*>(&lds.acc[1][r][4 * d4]);
+            const float4 o = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+            if (it.part >= 0) {
+                const size_t to = (size_t)it.part * kRows + r;
+                *reinterpret_cast<float4*>(a.parts.acc + to * kD + 4 * d4) = o;
+                if (d4 == 0) joined_ml(lds, r, a.parts.m[to], a.parts.l[to]);
+            } else {
+                const size_t to = (size_t)(it.seq.q0 + tok0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1));
+                float m, l;
+                joined_ml(lds, r, m, l);
+                const bool any = m != -INFINITY;
+                const float inv = any ? 1.f / l : 0.f;
+                const uint2 w = any ? make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
+                *reinterpret_cast<uint2*>(a.out + to * kD + 4 * d4) = w;
+                if (d4 == 0 && a.lse) a.lse[to] = any ? m + logf(l) : -INFINITY;
+            }
+        }
+        if (u < end) __syncthreads();           // the next tile takes the join's place
     }
+    if (!begun && tid == 0) a.parts.records[wg] = make_int4(0, 0, 0, 0);
 }
 
-// Joins the runs of the row tiles that were cut: a workgroup takes eight rows of one tile, 32 lanes a row.
-template <int ROWS, int SHIFT>
-__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkAttendArgs a) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    constexpr int kSlices = ROWS / 8;
-    const int pair = blockIdx.x / kSlices, slice = blockIdx.x % kSlices;
-    // the pair-th (sequence, tile, KV head) of those that are cut
-    ChunkPlan<ROWS, SHIFT> plan;
-    plan.load(a, 0, lane);
-    const int C = plan.run_blocks(a, lane);
-    int before = 0, parts_before = 0, b = -1, q0, n, tiles, cuts, first_part, at;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (b0 > 0) plan.load(a, b0, lane);
-        const int mine = plan.cuts_for(C), pairs = mine > 1 ? plan.tiles * a.Hkv : 0, parts = pairs * mine;
-        const int incl = wave_inclusive_scan(pairs), parts_incl = wave_inclusive_scan(parts), first = before + incl - pairs;
-        const uint64_t hit = __ballot(pair >= first && pair < first + pairs);
-        if (hit != 0) {
-            const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
-            b = b0 + src;
-            q0 = __builtin_amdgcn_readlane(plan.seq.q0, src);
-            n = __builtin_amdgcn_readlane(plan.seq.n, src);
-            tiles = __builtin_amdgcn_readlane(plan.tiles, src);
-            cuts = __builtin_amdgcn_readlane(mine, src);
-            first_part = parts_before + __builtin_amdgcn_readlane(parts_incl - parts, src);
-            at = pair - __builtin_amdgcn_readlane(first, src);
-            break;
-        }
-        before += __builtin_amdgcn_readlane(incl, 63);
-        parts_before += __builtin_amdgcn_readlane(parts_incl, 63);
-    }
-    if (b < 0) return;
-    const int turn = at / a.Hkv, kvh = at - turn * a.Hkv, tile = tiles - 1 - turn;
-    const int gs = __builtin_ctz(a.G), tok0 = tile * (ROWS >> gs), live = min(ROWS, (n - tok0) << gs);
-    const int r = 8 * slice + (tid >> 5), d4 = tid & 31;
-    if (r >= live) return;
-    const int part0 = first_part + turn * cuts * a.Hkv + kvh;
-    if (part0 + (cuts - 1) * a.Hkv >= a.max_parts) return;
-    auto row_of = [&](int s) { return (size_t)(part0 + s * a.Hkv) * ROWS + r; };
+// Joins the runs of the row tiles that were cut: a workgroup takes 16 or 32 rows of one tile and 32 dims, eight lanes a row;
+// where there are fewer rows several groups of lanes share a row's runs.
+__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkMergeArgs a) {
+    struct State {
+        float m, l;
+    };
+    __shared__ State states[32];
+    __shared__ float4 sums[32][8];
+    const bool second = (int)blockIdx.x >= a.wgs;
+    const ChunkParts& x = second ? a.parts[1] : a.parts[0];
+    const int slice_rows = chunk_merge_rows(x.rows), slices = 4 * (x.rows / slice_rows);
+    const int wg = second ? blockIdx.x - a.wgs : blockIdx.x, part = wg / slices, slice = wg % slices;
+    const int4 record = x.records[part];
+    if (record.w == 0 || (x.total && part >= x.total[0])) return;           // not the first run of a tile, or not used
+    const int live = min(record.z - slice_rows * (slice >> 2), slice_rows), cuts = record.w;
+    // part of run s
+    const int first = x.total ? part : 2 * part + 1, second_run = x.total ? part + a.Hkv : 2 * part + 2, step = x.total ? a.Hkv : 2;
+    if (live <= 0 || second_run + (cuts - 2) * step >= x.count) return;
+    int shift = 5;                              // 2^shift rows
+    while (shift > 0 && live <= 1 << (shift - 1)) --shift;
+    const int d4 = 8 * (slice & 3) + (threadIdx.x & 7), group = threadIdx.x >> 3;
+    const int r = group & ((1 << shift) - 1), k = group >> shift, groups = 32 >> shift;
+    const int row0 = slice_rows * (slice >> 2) + min(r, live - 1);
     float M = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int U = 4;
-    for (int s0 = 0; s0 < cuts; s0 += U) {
-        float m[U], pl[U];
-        float4 x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const size_t row = row_of(min(s0 + u, cuts - 1));
-            m[u] = s0 + u < cuts ? a.part_m[row] : -INFINITY;
-            pl[u] = a.part_l[row];
-            x[u] = *reinterpret_cast<const float4*>(a.part_acc + row * kD + 4 * d4);
-        }
-        float Mn = M;
-#pragma unroll
-        for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, m[u]);
-        if (Mn == -INFINITY) continue;
-        const float c = M == -INFINITY ? 0.f : __expf(M - Mn);
+    auto fold = [&](float m, float pl, const float4& y) {
+        if (m == -INFINITY) return;                             // a run that saw nothing
+        const float Mn = fmaxf(M, m), c = M == -INFINITY ? 0.f : __expf(M - Mn), w = __expf(m - Mn);
         M = Mn;
-        l *= c;
-        o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
+        l = fmaf(w, pl, l * c);
+        o = make_float4(fmaf(w, y.x, o.x * c), fmaf(w, y.y, o.y * c), fmaf(w, y.z, o.z * c), fmaf(w, y.w, o.w * c));
+    };
+    constexpr int U = 8;                        // rows asked for together
+    for (int s0 = k; s0 < cuts; s0 += U * groups) {
+        float m[U], pl[U];
+        float4 y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (m[u] == -INFINITY) continue;            // a run that saw nothing
-            const float w = __expf(m[u] - M);
-            l = fmaf(w, pl[u], l);
-            o = make_float4(fmaf(w, x[u].x, o.x), fmaf(w, x[u].y, o.y), fmaf(w, x[u].z, o.z), fmaf(w, x[u].w, o.w));
+            const int s = min(s0 + u * groups, cuts - 1);
+            const size_t row = (size_t)(s == 0 ? first : second_run + (s - 1) * step) * x.rows + row0;
+            m[u] = x.m[row];
+            pl[u] = x.l[row];
+            y[u] = *reinterpret_cast<const float4*>(x.acc + row * kD + 4 * d4);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) fold(s0 + u * groups < cuts ? m[u] : -INFINITY, pl[u], y[u]);
     }
+    if (groups > 1) {                           // uniform
+        if ((threadIdx.x & 7) == 0) states[group] = State{M, l};
+        sums[group][threadIdx.x & 7] = o;
+        __syncthreads();
+        if (k > 0) return;
+        for (int i = 1; i < groups; ++i) fold(states[group + (i << shift)].m, states[group + (i << shift)].l, sums[group + (i << shift)][threadIdx.x & 7]);
+    }
+    if (r >= live) return;
     const bool any = M != -INFINITY;
     const float inv = any ? 1.f / l : 0.f;
-    const size_t to = (size_t)(q0 + tok0 + (r >> gs)) * a.Hq + kvh * a.G + (r & (a.G - 1));
+    const int gs = __builtin_ctz(a.G);
+    const size_t to = (size_t)(record.x + (row0 >> gs)) * a.Hq + record.y * a.G + (row0 & (a.G - 1));
     *reinterpret_cast<uint2*>(a.out + to * kD + 4 * d4) =
         any ? make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
     if (d4 == 0 && a.lse) a.lse[to] = any ? M + logf(l) : -INFINITY;
@@ -333,8 +373,5 @@ template __global__ void chunk_rows_kernel<2, false, false>(ChunkAttendArgs);
 template __global__ void chunk_rows_kernel<2, false, true>(ChunkAttendArgs);
 template __global__ void chunk_rows_kernel<2, true, false>(ChunkAttendArgs);
 template __global__ void chunk_rows_kernel<2, true, true>(ChunkAttendArgs);
-template __global__ void chunk_merge_kernel<16, kRowsShift>(ChunkAttendArgs);
-template __global__ void chunk_merge_kernel<32, kRowsShift>(ChunkAttendArgs);
-template __global__ void chunk_merge_kernel<kChunkTileRows, kChunkTileShift>(ChunkAttendArgs);
 
 }  // namespace ffd

@@ -160,11 +160,12 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, h = lane >> 5;
     ChunkItem it;
-    if (!chunk_item<kChunkTileRows, kShift>(a, blockIdx.x, lane, it) || it.part >= a.max_parts) return;
+    if (!chunk_item<kChunkTileRows, kShift>(a, blockIdx.x, lane, it)) return;
     const int team = wave >> 2, part = team, id = tid & (kTeam - 1);
     const int gs = __builtin_ctz(a.G), step = kChunkTileRows >> gs, tok0 = it.tile * step;
     const int tok1 = min(tok0 + step, it.seq.n) - 1, live_rows = (tok1 - tok0 + 1) << gs;
     const int hq0 = it.kvh * a.G, place = it.seq.L - it.seq.n, cached = min(it.seq.L, a.Lcap);
+    write_record(a, it, tok0, live_rows);
     const ChunkSpan span = chunk_span<kShift>(a, it.seq, tok0, tok1);
     const int first = (int)((long long)span.count * it.run / it.cuts), last = (int)((long long)span.count * (it.run + 1) / it.cuts);
 
@@ -450,11 +451,11 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                *reinterpret_cast<float4*>(a.part_acc + to * kD + 32 * d + 8 * b + 4 * h) =
+                *reinterpret_cast<float4*>(a.parts.acc + to * kD + 32 * d + 8 * b + 4 * h) =
                     make_float4(o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]);
         if (h == 0) {
-            a.part_m[to] = ln;
-            a.part_l[to] = l;
+            a.parts.m[to] = ln;
+            a.parts.l[to] = l;
         }
         return;
     }
