@@ -3,7 +3,8 @@
 //
 // evict_select_kernel, one workgroup per (sequence, KV head): the order-preserving integer image of the weights, kept tokens
 // being those above a threshold and, of those equal to it, the first ones. The threshold is found by counting digits from
-// the highest on (11, 11 and 10 bits), each digit's counts in LDS, then a last pass in the tokens' order writes the list.
+// the highest on (11, 11 and 10 bits), each digit's counts in LDS; a last pass counts the kept tokens of each wave's part of the
+// sequence and then writes the list in the tokens' order. Up to 32K keys lie in LDS, those behind are made anew in each pass.
 // evict_move_kernel copies rows by the list. New pages are others than the old ones, so that rows can be copied in any order.
 //
 // Bound: the selection by its chain of passes over 4 bytes a token (out of L2 after the first), the move by HBM.
@@ -16,7 +17,9 @@ namespace {
 constexpr int kEvictWaves = kEvictThreads / 64;
 constexpr int kPerThread = 4;
 constexpr int kEvictStep = kEvictThreads * kPerThread;          // tokens a round
+constexpr int kHeld = 32768;                    // keys in LDS
 constexpr int kDigits = 2048;
+static_assert(kHeld % kEvictStep == 0);
 
 // Larger weight, larger key; +0 and -0 alike, NaN above infinity. 0 is no weight's key, and ~0 neither.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -27,6 +30,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 constexpr uint32_t kLatest = 0xffffffffu;
 
 struct EvictLds {
+    alignas(16) uint32_t keys[kHeld];
     int hist[kDigits];
     int sums[2][kEvictWaves];
     int digit, above;
@@ -53,16 +57,39 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
     const size_t pair = (size_t)b * gridDim.x + kvh;
     const float* weights = a.weights + pair * cap;
     const int latest = L - min(a.recent, L);
-    // keys of tokens 4 i .. 4 i + 3; 0: no token, or none of its page
-    auto keys_at = [&](int j, uint32_t (&key)[kPerThread], float (&w)[kPerThread]) {
+    // Keys of tokens j .. j + 3; 0: no token, or none of its page. 16 tokens of a page, of 16 or more, belong together.
+    const int last4 = max(L - 1, 0) & ~(kPerThread - 1);
+    auto keys_of = [&](int j, const float4& w, int entry) {
+        const float x[kPerThread] = {w.x, w.y, w.z, w.w};
+        const bool there = page_there(a.from, entry);
+        uint32_t key[kPerThread];
 #pragma unroll
-        for (int e = 0; e < kPerThread; ++e) key[e] = 0, w[e] = 0.f;
-        if (j >= L || !page_there(a.from, page_entry(a.from, b, j))) return;
-        const float4 x = *reinterpret_cast<const float4*>(weights + j);         // 16 tokens of a page, of 16 or more, belong together
-        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-#pragma unroll
-        for (int e = 0; e < kPerThread; ++e) key[e] = j + e >= L ? 0u : j + e >= latest ? kLatest : weight_key(w[e]);
+        for (int e = 0; e < kPerThread; ++e) {
+            const uint32_t k = j + e >= latest ? kLatest : weight_key(x[e]);
+            key[e] = there & (j + e < L) ? k : 0u;
+        }
+        return make_uint4(key[0], key[1], key[2], key[3]);
     };
+    auto weights_at = [&](int j) { return *reinterpret_cast<const float4*>(weights + min(j, last4)); };
+    auto keys_at = [&](int j) {
+        return j < kHeld ? *reinterpret_cast<const uint4*>(&lds.keys[j]) : keys_of(j, weights_at(j), page_entry(a.from, b, min(j, last4)));
+    };
+    const int rounds = (L + kEvictStep - 1) / kEvictStep;
+    for (int i0 = 0; i0 < min(rounds, kHeld / kEvictStep); i0 += 4) {
+        float4 w[4];
+        int entry[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {           // asked for together
+            const int j = (i0 + i) * kEvictStep + kPerThread * tid;
+            w[i] = weights_at(j);
+            entry[i] = page_entry(a.from, b, min(j, last4));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = (i0 + i) * kEvictStep + kPerThread * tid;
+            if (j < kHeld) *reinterpret_cast<uint4*>(&lds.keys[j]) = keys_of(j, w[i], entry[i]);
+        }
+    }
     // tokens above the threshold and equal to it: what is still to be found is the wanted-th largest of the keys with this prefix
     uint32_t prefix = 0;
     int wanted = a.budget, there = 0;
@@ -71,10 +98,9 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
         __syncthreads();
-        for (int j0 = 0; j0 < L; j0 += kEvictStep) {
-            uint32_t key[kPerThread];
-            float w[kPerThread];
-            keys_at(j0 + kPerThread * tid, key, w);
+        for (int i = 0; i < rounds; ++i) {
+            const uint4 k4 = keys_at(i * kEvictStep + kPerThread * tid);
+            const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
 #pragma unroll
             for (int e = 0; e < kPerThread; ++e) {
                 const bool active = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
@@ -106,80 +132,103 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
     int32_t* kept = a.kept + pair * a.budget;
     const int new_cap = a.to_pages << a.from.page_shift;
     float* new_weights = a.new_weights ? a.new_weights + pair * new_cap : nullptr;
+    // Each wave takes a part of the sequence: first its tokens above the threshold and equal to it are counted, then they are written.
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = (L + kEvictWaves * 256 - 1) / (kEvictWaves * 256) * 256, begin = min(wave * part, L), end = min(begin + part, L);
+    int above = 0, equal = 0;
+    auto of_thread = [&](const uint4& k, int& above, int& equal) {
+        above = (k.x > threshold) + (k.y > threshold) + (k.z > threshold) + (k.w > threshold);
+        equal = threshold == 0 ? 0 : (k.x == threshold) + (k.y == threshold) + (k.z == threshold) + (k.w == threshold);
+    };
+    for (int j = begin + kPerThread * lane; j < end; j += 64 * kPerThread) {
+        int x, y;
+        of_thread(keys_at(j), x, y);
+        above += x;
+        equal += y;
+    }
+    above = wave_sum_dpp(above);
+    equal = wave_sum_dpp(equal);
     __syncthreads();
-    int at = 0, equal = 0;
-    int turn = 0;
-    for (int j0 = 0; j0 < L; j0 += kEvictStep, turn ^= 1) {
-        uint32_t key[kPerThread];
-        float w[kPerThread];
-        const int j = j0 + kPerThread * tid;
-        keys_at(j, key, w);
-        int mine = 0;                           // above in the low half, equal in the high one
+    if (lane == 0) {
+        lds.sums[0][wave] = above;
+        lds.sums[1][wave] = equal;
+    }
+    __syncthreads();
+    int equals = 0, to_wave = 0;                // before this wave's part: equal ones, kept ones
+    for (int w = 0; w < wave; ++w) {
+        to_wave += lds.sums[0][w];
+        equals += lds.sums[1][w];
+    }
+    to_wave += min(equals, ties);
+    for (int j0 = begin; j0 < end; j0 += 64 * kPerThread) {
+        const int j = j0 + kPerThread * lane;
+        const uint4 k4 = keys_at(min(j, last4));
+        const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
+        const float4 w4 = weights_at(j);
+        const float w[kPerThread] = {w4.x, w4.y, w4.z, w4.w};
+        int x = 0, y = 0;
+        if (j < end) of_thread(k4, x, y);
+        const int both = x | y << 16, incl = wave_inclusive_scan(both), before = incl - both, all = __builtin_amdgcn_readlane(incl, 63);
+        int equal_here = equals + (before >> 16);
+        int to = to_wave + (before & 0xffff) + min(equal_here, ties) - min(equals, ties);
+        if (j < end) {
 #pragma unroll
-        for (int e = 0; e < kPerThread; ++e) mine += (key[e] > threshold ? 1 : 0) + (key[e] != 0 && key[e] == threshold ? 1 << 16 : 0);
-        int total;
-        const int before = wg_exclusive_scan<kEvictWaves>(mine, lds.sums[turn], &total);
-        int above_here = before & 0xffff, equal_here = equal + (before >> 16);
-        // kept before this thread: those above, and the equal ones up to `ties`
-        int to = at + above_here + min(equal_here, ties) - min(equal, ties);
-#pragma unroll
-        for (int e = 0; e < kPerThread; ++e) {
-            const bool is_equal = key[e] != 0 && key[e] == threshold;
-            if (key[e] > threshold || (is_equal && equal_here < ties)) {
-                kept[to] = j + e;
-                if (new_weights) new_weights[to] = w[e];
-                ++to;
+            for (int e = 0; e < kPerThread; ++e) {
+                const bool is_equal = threshold != 0 && key[e] == threshold;
+                if (key[e] > threshold || (is_equal && equal_here < ties)) {
+                    kept[to] = j + e;
+                    if (new_weights) new_weights[to] = w[e];
+                    ++to;
+                }
+                equal_here += is_equal;
             }
-            equal_here += is_equal;
         }
-        at += (total & 0xffff) + min(equal + (total >> 16), ties) - min(equal, ties);
-        equal += total >> 16;
+        to_wave += (all & 0xffff) + min(equals + (all >> 16), ties) - min(equals, ties);
+        equals += all >> 16;
     }
     for (int r = count + tid; r < a.budget; r += kEvictThreads) kept[r] = -1;
     if (kvh == 0 && tid == 0) a.new_lens[b] = count;
 }
 
-// 64 places of a (sequence, KV head), keys and values: 16 lanes a bf16 row, eight an 8-bit one.
+// 128 places of a (sequence, KV head), keys or values: 16 lanes a bf16 row, eight an 8-bit one. Everything passes once.
 template <bool I8>
 __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
     constexpr int kLanes = I8 ? 8 : 16, kRows = kThreads / kLanes, kSteps = kEvictMoveRows / kRows;
-    const int kvh = blockIdx.y, b = blockIdx.z, c = threadIdx.x % kLanes;
+    const bool values = blockIdx.x & 1;
+    const int kvh = blockIdx.y, b = blockIdx.z, c = threadIdx.x % kLanes, r0 = (int)(blockIdx.x >> 1) * kEvictMoveRows + (int)threadIdx.x / kLanes;
     const int32_t* kept = a.kept + ((size_t)b * a.Hkv + kvh) * a.budget;
     const PagedKv to{a.from.kv, a.to_table, a.from.num_pages, a.from.page_shift, a.to_pages};
+    int j[kSteps], to_entry[kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+        const int r = min(r0 + u * kRows, a.budget - 1);
+        j[u] = kept[r];
+        to_entry[u] = page_entry(to, b, r);
+    }
     size_t src[kSteps], dst[kSteps];
     bool move[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
-        const int r = (int)blockIdx.x * kEvictMoveRows + u * kRows + (int)threadIdx.x / kLanes;
-        const int j = r < a.budget ? kept[r] : -1;
-        const int from_entry = page_entry(a.from, b, max(j, 0)), to_entry = page_entry(to, b, min(r, a.budget - 1));
-        move[u] = j >= 0 && page_there(a.from, from_entry) && page_there(to, to_entry);
-        src[u] = move[u] ? page_row(a.from, a.Hkv, kvh, from_entry, j) : 0;
-        dst[u] = move[u] ? page_row(to, a.Hkv, kvh, to_entry, r) : 0;
+        const int from_entry = page_entry(a.from, b, max(j[u], 0));
+        move[u] = r0 + u * kRows < a.budget && j[u] >= 0 && page_there(a.from, from_entry) && page_there(to, to_entry[u]);
+        src[u] = move[u] ? page_row(a.from, a.Hkv, kvh, from_entry, j[u]) : 0;
+        dst[u] = move[u] ? page_row(to, a.Hkv, kvh, to_entry[u], r0 + u * kRows) : 0;
     }
-    uint4* k = reinterpret_cast<uint4*>(const_cast<uint8_t*>(a.from.kv.k));
-    uint4* v = reinterpret_cast<uint4*>(const_cast<uint8_t*>(a.from.kv.v));
-    uint4 x[2][kSteps];
-    uint16_t m[2][kSteps];
+    v4i* tokens = reinterpret_cast<v4i*>(const_cast<uint8_t*>(values ? a.from.kv.v : a.from.kv.k));
+    uint16_t* absmax = const_cast<uint16_t*>(values ? a.from.kv.v_absmax : a.from.kv.k_absmax);
+    v4i x[kSteps];
+    uint16_t m[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
-        x[0][u] = k[src[u] * kLanes + c];
-        x[1][u] = v[src[u] * kLanes + c];
-        if constexpr (I8) {
-            m[0][u] = a.from.kv.k_absmax[src[u]];
-            m[1][u] = a.from.kv.v_absmax[src[u]];
-        }
+        x[u] = __builtin_nontemporal_load(tokens + src[u] * kLanes + c);
+        if constexpr (I8) m[u] = absmax[src[u]];
     }
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
         if (!move[u]) continue;
-        k[dst[u] * kLanes + c] = x[0][u];
-        v[dst[u] * kLanes + c] = x[1][u];
+        __builtin_nontemporal_store(x[u], tokens + dst[u] * kLanes + c);
         if constexpr (I8) {
-            if (c == 0) {
-                const_cast<uint16_t*>(a.from.kv.k_absmax)[dst[u]] = m[0][u];
-                const_cast<uint16_t*>(a.from.kv.v_absmax)[dst[u]] = m[1][u];
-            }
+            if (c == 0) absmax[dst[u]] = m[u];
         }
     }
 }

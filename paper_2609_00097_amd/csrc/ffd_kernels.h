@@ -287,6 +287,7 @@ struct ChunkWeightsArgs : ChunkArgs {
     const float* previous;      // [B, Hkv, Lcap] or null
     float* weights;             // [B, Hkv, Lcap]
     int last;                   // new tokens that count, 0: all
+    int slots, unit_shift;      // workgroups, and units of 128 << unit_shift tokens that they share
 };
 
 struct WritePagedArgs {
@@ -381,7 +382,7 @@ __global__ void chunk_merge_kernel(ChunkMergeArgs a);
 template <bool I8, bool RULED> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
 constexpr int kEvictThreads = 1024;
 __global__ void evict_select_kernel(EvictArgs a);
-constexpr int kEvictMoveRows = 64;             // rows per workgroup of the move
+constexpr int kEvictMoveRows = 128;            // rows per workgroup of the move, which takes keys or values
 template <bool I8> __global__ void evict_move_kernel(EvictArgs a);
 constexpr int kMergeSlices = 4;                // workgroups per head of the merge, 32 dims each
 // NW waves per workgroup: 4, or 1 from kMergeOneWaveHeads heads on (their waves fill the chip alone).

@@ -47,8 +47,11 @@ __device__ __forceinline__ ChunkSpan chunk_span(const ChunkArgs& a, const ChunkS
     return p;
 }
 
-// Whether a query at place i sees token j (of a page that is there, below min(L, Lcap)).
-__device__ __forceinline__ bool sees(int i, int j, int window, int pre) { return (j <= i && (window <= 0 || i - j < window)) || j < pre; }
+// Whether a query at place i sees token j (of a page that is there, below min(L, Lcap)). Without branches: eight or 32 of these in
+// a row would become as many jumps.
+__device__ __forceinline__ bool sees(int i, int j, int window, int pre) {
+    return (((j <= i) & ((window <= 0) | (i - j < window))) | (j < pre)) != 0;
+}
 
 // Row of (token j, KV head kvh) in the pages: first row of the 16-token group that holds j, given its page's entry.
 __device__ __forceinline__ size_t page_row(const PagedKv& p, int Hkv, int kvh, int entry, int j) {
@@ -178,6 +181,22 @@ __device__ __forceinline__ bool chunk_item(const ChunkAttendArgs& a, int wg, int
 __device__ __forceinline__ void write_record(const ChunkAttendArgs& a, const ChunkItem& it, int tok0, int live) {
     if (it.part >= 0 && threadIdx.x == 0) a.parts.records[it.part] = make_int4(it.seq.q0 + tok0, it.kvh, live, it.run == 0 ? it.cuts : 0);
 }
+
+// Units 0 .. all - 1 of work in equal shares (they differ by one unit at most) of consecutive units, as many as there are
+// workgroups, or fewer, so that each has `least` units. Products below 2^52.
+struct Shares {
+    int all, count;
+    double r_all, r_count;
+    __device__ __forceinline__ Shares(int units, int slots, int least)
+        : all(units), count(min(slots, max(units / least, 1))), r_all(reciprocal((double)max(units, 1))), r_count(reciprocal((double)count)) {}
+    __device__ __forceinline__ int begin(int w) const {
+        return __builtin_amdgcn_readfirstlane(w >= count ? all : (int)floor_div((long long)w * all, count, r_count));
+    }
+    // the share that unit u belongs to
+    __device__ __forceinline__ int of(int u) const {
+        return __builtin_amdgcn_readfirstlane((int)floor_div((long long)(u + 1) * count - 1, all, r_all));
+    }
+};
 
 // What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). tanh(x) =
 // 1 - 2 / (1 + e^2x): no overflow, infinities and NaN as they are, 2^-23 of the cap off. An 8-bit key's product is

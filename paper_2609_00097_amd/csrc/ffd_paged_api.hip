@@ -142,6 +142,8 @@ void launch_rows(int rows, bool i8, bool ruled, dim3 grid, hipStream_t stream, c
     else launch_rows_ruled<2, false>(ruled, grid, stream, a);
 }
 
+constexpr int kFewWeightRows = 128;
+
 int check_strides(const int64_t* s) { return s && (s[0] < 0 || s[0] % 8 || s[1] < 0 || s[1] % 8) ? FFD_ERR_INVALID_ARGUMENT : FFD_OK; }
 
 }  // namespace
@@ -191,11 +193,11 @@ int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* 
     a.B = B, a.T = T, a.Hq = Hq, a.Hkv = Hkv;
     a.rope_rows = r.rows, a.rope_dims = r.table ? r.dims : 0;
     a.eps = r.eps;
-    // one vector a group of lanes while that leaves CUs idle, else up to six, so that the table's row is loaded less often
-    const int vectors = (q ? Hq : 0) + 2 * Hkv, groups = (vectors + 7) / 8;
+    // one vector a group of lanes while that leaves CUs idle, else up to twelve, so that the table's row is loaded less often
+    const int vectors = (q ? Hq : 0) + 2 * Hkv, groups = (vectors + 3) / 4;
     const long long wanted = 16LL * device_cus();
-    const int waves = (int)std::min<long long>(groups, std::max<long long>((groups + 5) / 6, wanted / T));
-    a.parts = 8 * waves;
+    const int waves = (int)std::min<long long>(groups, std::max<long long>((groups + 11) / 12, wanted / T));
+    a.parts = 4 * waves;
     const dim3 grid((unsigned)(((long long)T * waves + kWaves - 1) / kWaves));
     const bool inter = r.table && r.interleaved;
     if (i8 && inter) hipLaunchKernelGGL((write_paged_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
@@ -284,8 +286,14 @@ int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int
     a.weights = weights;
     a.last = last;
     const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
-    const long long items = (long long)B * Hkv * ((a.Lcap + kRound - 1) / kRound);
-    const dim3 grid((unsigned)std::min<long long>(items, 16LL * device_cus()));
+    // One share for each workgroup that fits the device at a time where a sequence's rows are few, so that all units take the
+    // same time; else one unit each, in which the rows that may see it differ.
+    long long units = 0;
+    while (units == 0 || units >= 1LL << 23) units = (long long)B * Hkv * ((a.Lcap + (kRound << a.unit_shift) - 1) / (kRound << a.unit_shift)), ++a.unit_shift;
+    --a.unit_shift;
+    const long long rows = std::min<long long>(T, last > 0 ? (long long)last * B : T) * a.G;
+    a.slots = (int)(rows <= kFewWeightRows * (long long)B ? std::min<long long>(units, 3LL * device_cus()) : units);
+    const dim3 grid((unsigned)a.slots);
     if (i8 && ruled) hipLaunchKernelGGL((chunk_weights_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
     else if (i8) hipLaunchKernelGGL((chunk_weights_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
     else if (ruled) hipLaunchKernelGGL((chunk_weights_kernel<false, true>), grid, dim3(kThreads), 0, stream, a);
@@ -308,7 +316,7 @@ int ffd_evict_paged(const ffd_paged* cache, const int32_t* new_table, int new_ma
     if (!new_table || !seq_lens || !weights || !new_lens || !kept) return FFD_ERR_INVALID_ARGUMENT;
     if (!aligned16(weights) || !aligned4(new_table) || !aligned4(seq_lens) || !aligned4(new_lens) || !aligned4(kept) || !aligned4(new_weights))
         return FFD_ERR_INVALID_ARGUMENT;
-    const long long moves = (budget + kEvictMoveRows - 1) / kEvictMoveRows;
+    const long long moves = 2LL * ((budget + kEvictMoveRows - 1) / kEvictMoveRows);
     if (!pairs_fit(B, Hkv) || moves * B * Hkv * kThreads >= 1LL << 31) return FFD_ERR_UNSUPPORTED;
     const EvictArgs a{paged_of(*cache), new_table, seq_lens, weights, new_lens, kept, new_weights, Hkv, new_max_pages, budget, recent};
     hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)Hkv, (unsigned)B), dim3(kEvictThreads), 0, stream, a);

@@ -115,7 +115,7 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
             alive = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (there[e >> 2] && t0 + value_token(e, g) < span.end) alive |= 1u << e;
+                alive |= (uint32_t)(there[e >> 2] & (t0 + value_token(e, g) < span.end)) << e;
         }
         float vs[8];
         if constexpr (I8) {
@@ -139,9 +139,9 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
                 seen = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const bool x = (alive >> e & 1) && sees(rows.at[c], t0 + value_token(e, g), window, pre);
+                    const uint32_t x = (alive >> e) & (uint32_t)sees(rows.at[c], t0 + value_token(e, g), window, pre);
                     z[e] = x ? z[e] : -INFINITY;
-                    seen |= x ? 1u << e : 0u;
+                    seen |= x << e;
                 }
             }
             float mn = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
@@ -222,15 +222,15 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
         plan.load(a, b0, lane);
         all += __builtin_amdgcn_readlane(wave_inclusive_scan(work()), 63);
     }
-    const int share = max((all + a.slots - 1) / a.slots, a.min_share);
-    int u = wg * share;
-    const int end = min(u + share, all);
+    const Shares shares(all, a.slots, a.min_share);
+    const int begin = shares.begin(wg), end = shares.begin(wg + 1);
+    int u = begin;
     bool begun = false;                         // a tile that another workgroup ends
     while (u < end) {                           // uniform
         ChunkItem it{};
         int tile_units = 1, at = 0, before = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
-            if (b0 > 0 || u != wg * share) plan.load(a, b0, lane);          // (kept, it would cost the loop registers)
+            if (b0 > 0 || u != begin) plan.load(a, b0, lane);          // (kept, it would cost the loop registers)
             const int mine = work(), incl = wave_inclusive_scan(mine), first = before + incl - mine;
             const uint64_t hit = __ballot(u >= first && u < first + mine);
             if (hit != 0) {
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
         const int hq0 = it.kvh * a.G, place = it.seq.L - it.seq.n;
         if (it.part >= 0 && from == 0) {
             begun = true;
-            if (tid == 0) a.parts.records[wg] = make_int4(it.seq.q0 + tok0, it.kvh, live, 1 + (tile_units - to + share - 1) / share);
+            if (tid == 0) a.parts.records[wg] = make_int4(it.seq.q0 + tok0, it.kvh, live, shares.of(u - to + tile_units - 1) - wg + 1);
         }
         v8bf q[CT][4];
         Rows<CT> rows;

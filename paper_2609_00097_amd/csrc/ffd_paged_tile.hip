@@ -306,17 +306,17 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         bool any = true;
         if (!((behind || t0 + kTokens <= it.seq.pre) && t0 + kTokens <= cached && there == 15u)) {
             const Limits see = limits(t0);
-            any = false;
+            uint32_t some = 0;
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int c = 32 * x + 8 * (i >> 2) + (i & 3);
-                    const bool seen = ((c <= see.high && c > see.low) || c < see.prefix) && (there >> (2 * x + (i >> 3)) & 1);
-                    s[x][i] = seen ? s[x][i] : -INFINITY;
-                    any |= seen;
+                    const uint32_t seen = (uint32_t)(((c <= see.high) & (c > see.low)) | (c < see.prefix)) & (there >> (2 * x + (i >> 3)));
+                    s[x][i] = seen & 1 ? s[x][i] : -INFINITY;
+                    some |= seen;
                 }
-            any = halves_max(any ? 1.f : 0.f) > 0.f;
+            any = halves_max(some & 1 ? 1.f : 0.f) > 0.f;
         }
         float mx[4];                                    // four chains, as for the sum below
 #pragma unroll

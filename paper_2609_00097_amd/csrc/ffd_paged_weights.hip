@@ -2,127 +2,268 @@
 // token j of e^(z_ij - lse_i), z and lse as of the attention (ffd_paged.h has the scores and what is seen). A sum has one
 // order and one place, so that results do not change from call to call.
 //
-// Mapping. A workgroup keeps the keys of 128 tokens of a (sequence, KV head) in registers, 32 a wave, and goes through the
-// query rows that may see them, 16 at a time, with S^T = K Q^T as in ffd_attend.h: lane (n, g) adds up its eight tokens' weights
-// from row n, and the 16 lanes of a group are joined at the end.
+// Mapping. Work in the order (sequence, KV head, token), in units of 128 tokens, is given out in equal shares of consecutive
+// units. For a (sequence, KV head) of its share a workgroup takes 128 tokens at a time, 32 a wave, and puts the query rows that
+// count into LDS, 128 of them at a time. With the keys of its 32 tokens in registers a wave goes through the rows, 16 by 16,
+// with S^T = K Q^T as in ffd_attend.h: lane (n, g) adds up its eight tokens' weights from row n, and the 16 lanes of a group are
+// joined at the end. Where 128 rows are all, they stay, the waves need no barrier, and the next keys are asked for early.
 //
 // Bound: HBM where few queries count (256 bytes a token and KV head), else the exponentials and the matrix cores.
+#include <type_traits>
+
 #include "ffd_paged.h"
+#include "ffd_tile.h"
 
 namespace ffd {
 
 namespace {
 
+constexpr int kRowsAtOnce = 128;
+struct WeightsLds {
+    alignas(16) uint8_t q[kRowsAtOnce * 2 * kD];
+    float lse2[kRowsAtOnce];
+};
+
+// Units [first, last) of a (sequence, KV head).
 struct WeightsItem {
     ChunkSeq seq;
-    int b, kvh, block;
+    int b, kvh, first, last;
 };
-// Item number `wanted` of the batch: blocks of kRound tokens by (sequence, KV head).
-__device__ __forceinline__ bool weights_item(const ChunkWeightsArgs& a, long long wanted, int lane, WeightsItem& it) {
-    long long before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const ChunkSeq s = chunk_seq(a, min(b0 + lane, a.B - 1));
-        const int blocks = b0 + lane < a.B ? (min(s.L, a.Lcap) + kRound - 1) / kRound : 0;
-        const int incl = wave_inclusive_scan(blocks);
-        const long long first = before + (long long)(incl - blocks) * a.Hkv;
-        const uint64_t hit = __ballot(wanted >= first && wanted < first + (long long)blocks * a.Hkv);
-        if (hit != 0) {
-            const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
-            it.b = b0 + src;
-            it.seq.q0 = __builtin_amdgcn_readlane(s.q0, src);
-            it.seq.n = __builtin_amdgcn_readlane(s.n, src);
-            it.seq.L = __builtin_amdgcn_readlane(s.L, src);
-            it.seq.pre = __builtin_amdgcn_readlane(s.pre, src);
-            const int count = __builtin_amdgcn_readlane(blocks, src);
-            const int at = (int)(wanted - before - (long long)__builtin_amdgcn_readlane(incl - blocks, src) * a.Hkv);
-            it.kvh = __builtin_amdgcn_readfirstlane(at / count);
-            it.block = __builtin_amdgcn_readfirstlane(at) - it.kvh * count;
-            return true;
-        }
-        before += (long long)__builtin_amdgcn_readlane(incl, 63) * a.Hkv;
-    }
-    return false;
-}
+
+// A wave's 32 tokens: their pages' rows, which of this lane's eight tokens there are, and what the four that it writes had.
+struct WeightsTile {
+    int t0;
+    uint32_t alive;
+    size_t row[2];
+    float4 old;
+};
 
 }  // namespace
 
 template <bool I8, bool RULED>
 __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeightsArgs a) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    __shared__ WeightsLds lds;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15, gs = __builtin_ctz(a.G);
-    const ScoreRule rule = score_rule(a, I8, 0);
-    WeightsItem it;
-    for (long long wanted = blockIdx.x; weights_item(a, wanted, lane, it); wanted += gridDim.x) {
-        const int cached = min(it.seq.L, a.Lcap), place = it.seq.L - it.seq.n, pre = it.seq.pre;
-        const int t0 = it.block * kRound + kTile * wave;
-        if (t0 >= cached) continue;
-        const int entry[2] = {page_entry(a.pages, it.b, t0), page_entry(a.pages, it.b, t0 + 16)};
-        size_t row[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) row[t] = page_row(a.pages, a.Hkv, it.kvh, page_there(a.pages, entry[t]) ? entry[t] : 0, t0 + 16 * t);
-        KeyTile<I8> kt;
-        kt.load_halves(a.pages.kv, row, n, g);
-        uint32_t alive = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (page_there(a.pages, entry[e >> 2]) && t0 + value_token(e, g) < cached) alive |= 1u << e;
-        const bool whole = __ballot(alive != 0xffu) == 0;
-        // new tokens [from, to) count and may see something of this tile
-        int from = a.last > 0 ? max(it.seq.n - a.last, 0) : 0, to = it.seq.n;
-        if (t0 >= pre) {
-            from = max(from, t0 - place);
-            if (a.window > 0) to = (int)min((long long)to, (long long)t0 + kTile - 1 + a.window - place);
+    const int unit = kRound << a.unit_shift;
+    auto load = [&](int b0, ChunkSeq& s) {      // units of this lane's sequence
+        s = chunk_seq(a, min(b0 + lane, a.B - 1));
+        return b0 + lane < a.B ? (min(s.L, a.Lcap) + unit - 1) / unit * a.Hkv : 0;
+    };
+    int all = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        ChunkSeq s;
+        all += __builtin_amdgcn_readlane(wave_inclusive_scan(load(b0, s)), 63);
+    }
+    const Shares shares(all, a.slots, 1);
+    const int begin = shares.begin(blockIdx.x), stop = shares.begin(blockIdx.x + 1);
+    for (int u = begin; u < stop;) {            // uniform
+        if (u != begin) __syncthreads();            // the rows in LDS are done with
+        WeightsItem it{};
+        for (int b0 = 0, before = 0; b0 < a.B; b0 += 64) {
+            ChunkSeq s;
+            const int mine = load(b0, s), incl = wave_inclusive_scan(mine), at = before + incl - mine;
+            const uint64_t hit = __ballot(u >= at && u < at + mine);
+            if (hit != 0) {
+                const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
+                it.b = b0 + src;
+                it.seq.q0 = __builtin_amdgcn_readlane(s.q0, src);
+                it.seq.n = __builtin_amdgcn_readlane(s.n, src);
+                it.seq.L = __builtin_amdgcn_readlane(s.L, src);
+                it.seq.pre = __builtin_amdgcn_readlane(s.pre, src);
+                const int count = __builtin_amdgcn_readlane(mine, src) / a.Hkv, in = __builtin_amdgcn_readfirstlane(u) - __builtin_amdgcn_readlane(at, src);
+                it.kvh = in / count;
+                it.first = in - it.kvh * count;
+                it.last = min(count, it.first + stop - u);
+                break;
+            }
+            before += __builtin_amdgcn_readlane(incl, 63);
         }
-        const int r1 = to << gs, hq0 = it.kvh * a.G;
-        v8bf q[4];
-        float lse2, slope2;
-        int at;
-        auto load_row = [&](int r) {
-            const int x = min(r + n, r1 - 1), tok = x >> gs, head = hq0 + (x & (a.G - 1));
-            const size_t i = (size_t)(it.seq.q0 + tok) * a.Hq + head;
-            load_query<I8>(q, a.q + i * kD, g);
-            lse2 = a.lse[i] * kLog2e;
-            at = place + tok;
-            slope2 = RULED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+        u += it.last - it.first;
+        const ScoreRule rule = score_rule(a, I8, it.kvh * a.G + (n & (a.G - 1)));
+        const int cached = min(it.seq.L, a.Lcap), place = it.seq.L - it.seq.n, pre = it.seq.pre;
+        const int first = it.first * unit, end = min(it.last * unit, cached), hq0 = it.kvh * a.G;
+        struct Entries {
+            int e[2];
         };
-        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (from < to) load_row(from << gs);
-        for (int r = from << gs; r < r1; r += 16) {
-            v4f s[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
+        auto entries_at = [&](int t0) {
+            return Entries{{uniform_page_entry(a.pages, it.b, t0), uniform_page_entry(a.pages, it.b, t0 + 16)}};
+        };
+        auto tile_of = [&](int t0, const Entries& entries) {
+            WeightsTile x;
+            x.t0 = t0;
+            x.alive = 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const bool there = page_there(a.pages, entries.e[t]);
+                x.row[t] = page_row(a.pages, a.Hkv, it.kvh, there ? entries.e[t] : 0, t0 + 16 * t);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x.alive |= (uint32_t)(there & (t0 + value_token(4 * t + i, g) < cached)) << (4 * t + i);
+            }
+            return x;
+        };
+        // new tokens [from, to) count and may see something of tokens [t0, t1)
+        auto rows_for = [&](int t0, int t1, int& from, int& to) {
+            from = a.last > 0 ? max(it.seq.n - a.last, 0) : 0;
+            to = it.seq.n;
+            if (t0 >= pre) {
+                from = max(from, t0 - place);
+                if (a.window > 0) to = (int)min((long long)to, (long long)t1 - 1 + a.window - place);
+            }
+        };
+        // What lanes n < 2 will add to: asked for with the keys, since a load waits for all loads before it.
+        auto load_old = [&](WeightsTile& x) {
+            x.old = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int j = x.t0 + 16 * n + 4 * g;
+            if (a.previous && n < 2 && j < cached) x.old = *reinterpret_cast<const float4*>(a.previous + ((size_t)it.b * a.Hkv + it.kvh) * a.Lcap + j);
+        };
+        int from, to;
+        rows_for(first, end, from, to);
+        const int r0 = from << gs, rows = from < to ? (to - from) << gs : 0;
+        // rows r0 + at .. into LDS; those behind the last one repeat it
+        auto stage = [&](int at) {
+#pragma unroll
+            for (int i = 0; i < kRowsAtOnce * 16 / kThreads; ++i) {
+                const int row = (tid >> 4) + 16 * i;
+                if (at + row >= rows + 15) break;
+                const int r = r0 + min(at + row, rows - 1);
+                const size_t from_row = (size_t)(it.seq.q0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1));
+                *reinterpret_cast<v4u*>(&lds.q[row * (2 * kD) + 16 * key_chunk(row, tid & 15)]) =
+                    *reinterpret_cast<const v4u*>(a.q + from_row * kD + 8 * (tid & 15));
+                if ((tid & 15) == 0) lds.lse2[row] = a.lse[from_row] * kLog2e;
+            }
+        };
+        float sum[8];
+        // the weights that rows [at, at + kRowsAtOnce) give this wave's tile
+        auto add_rows = [&](const KeyTile<I8>& kt, const WeightsTile& tile, int at) {
+            v8bf keys[2][4];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kt.operand(t, k), q[k], s[t], 0, 0, 0);
-            const float lse_now = lse2, slope_now = slope2;
-            const int at_now = at;
-            if (r + 16 < r1) load_row(r + 16);
-            const int low = place + (r >> gs), high = place + (min(r + 15, r1 - 1) >> gs);
-            const bool masked = !whole || r + 16 > r1 ||
-                                !((t0 + kTile <= low + 1 && (a.window <= 0 || t0 > high - a.window)) || t0 + kTile <= pre);
+                for (int k = 0; k < 4; ++k) keys[t][k] = kt.operand(t, k);
+            float km[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float z = s[e >> 2][e & 3] * rule.zscale;
-                if constexpr (I8) z *= absmax_of(kt.m[e >> 2], e & 3);
-                if constexpr (RULED) {
-                    if (rule.cap2 != 0.f) z = capped(z, rule.cap2);
-                    z = fmaf(-slope_now, fabsf((float)(at_now - t0 - value_token(e, g))), z);
+                if constexpr (I8) km[e] = absmax_of(kt.m[e >> 2], e & 3) * rule.zscale;
+                else km[e] = rule.zscale;
+            }
+            const bool whole = __ballot(tile.alive != 0xffu) == 0;
+            int lowest, highest;
+            rows_for(tile.t0, tile.t0 + kTile, lowest, highest);
+            lowest = max(((lowest - from) << gs) - at, 0) & ~15;
+            highest = min(((highest - from) << gs) - at, kRowsAtOnce);
+            auto tiles = [&](int r, auto count) {       // row tiles r, r + 16: two are each other's latency
+                constexpr int N = decltype(count)::value;
+                v4f s[N][2];
+                float lse2[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    lse2[i] = lds.lse2[r + 16 * i + n];
+                    s[i][0] = s[i][1] = v4f{0.f, 0.f, 0.f, 0.f};
                 }
-                float p = exp2_hw(z - lse_now);
-                if (masked) p = r + n < r1 && (alive >> e & 1) && sees(at_now, t0 + value_token(e, g), a.window, pre) ? p : 0.f;
-                sum[e] += p;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const v8bf q = *reinterpret_cast<const v8bf*>(&lds.q[(r + 16 * i + n) * (2 * kD) + 16 * key_chunk(n, key_dim<I8>(k, g) / 8)]);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys[t][k], q, s[i][t], 0, 0, 0);
+                    }
+                const int tok = from + ((at + r) >> gs), low = place + tok, high = place + min(tok + ((16 * N - 1) >> gs), to - 1), t0 = tile.t0;
+                const bool masked = !whole || at + r + 16 * N > rows ||
+                                    !((t0 + kTile <= low + 1 && (a.window <= 0 || t0 > high - a.window)) || t0 + kTile <= pre);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int row = at + r + 16 * i + n, mine = place + from + (row >> gs);
+                    float p[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float z = s[i][e >> 2][e & 3];
+                        if constexpr (RULED) {
+                            z *= km[e];
+                            if (rule.cap2 != 0.f) z = capped(z, rule.cap2);
+                            z = fmaf(-rule.slope2, fabsf((float)(mine - t0 - value_token(e, g))), z);
+                            p[e] = exp2_hw(z - lse2[i]);
+                        } else {
+                            p[e] = exp2_hw(fmaf(z, km[e], -lse2[i]));
+                        }
+                    }
+                    if (masked) {
+                        const uint32_t row_there = row < rows;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            p[e] = row_there & (tile.alive >> e) & (uint32_t)sees(mine, t0 + value_token(e, g), a.window, pre) ? p[e] : 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += p[e];
+                }
+            };
+            int r = lowest;
+            for (; r + 16 < highest; r += 32) tiles(r, std::integral_constant<int, 2>());
+            if (r < highest) tiles(r, std::integral_constant<int, 1>());
+        };
+        auto finish = [&](const WeightsTile& tile) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = row16_sum(sum[e]);
+            const int j = tile.t0 + 16 * n + 4 * g;
+            if (n >= 2 || j >= cached) return;      // half n of the tile
+            const float old[4] = {tile.old.x, tile.old.y, tile.old.z, tile.old.w};
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (j + e < place ? old[e] : 0.f) + (n == 0 ? sum[e] : sum[e + 4]);
+            float* to_weights = a.weights + ((size_t)it.b * a.Hkv + it.kvh) * a.Lcap + j;
+            if (j + 4 <= cached) {
+                *reinterpret_cast<float4*>(to_weights) = make_float4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (j + e < cached) to_weights[e] = w[e];
             }
+        };
+
+        KeyTile<I8> kt;
+        if (rows <= kRowsAtOnce) {
+            int t0 = first + kTile * wave;
+            // behind the end: a tile that is there, unused
+            auto within = [&](int t) { return min(t, end - 1) & ~(kTile - 1); };
+            WeightsTile tile = tile_of(within(t0), entries_at(within(t0)));
+            Entries entries = entries_at(within(t0 + kRound));
+            kt.load_halves(a.pages.kv, tile.row, n, g);
+            load_old(tile);
+            if (rows > 0) stage(0);
+            __syncthreads();
+            while (t0 < end) {
+                const int next = t0 + kRound;
+                KeyTile<I8> kn;
+                WeightsTile next_tile = tile_of(within(next), entries);
+                entries = entries_at(within(next + kRound));
+                kn.load_halves(a.pages.kv, next_tile.row, n, g);
+                load_old(next_tile);
+                asm volatile("" ::: "memory");      // here, not where they are used
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+                if (rows > 0) add_rows(kt, tile, 0);
+                finish(tile);
+                kt = kn;
+                tile = next_tile;
+                t0 = next;
+            }
+            continue;
         }
+        for (int t0 = first + kTile * wave; t0 - kTile * wave < end; t0 += kRound) {            // all waves alike, for the barriers
+            WeightsTile tile = tile_of(t0, entries_at(t0));
+            if (t0 < end) kt.load_halves(a.pages.kv, tile.row, n, g);
+            load_old(tile);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = row16_sum(sum[e]);
-        if (n < 2) {                            // half n of the tile
-            const int j = t0 + 16 * n + 4 * g;
-            const size_t to0 = ((size_t)it.b * a.Hkv + it.kvh) * a.Lcap + j;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (j + e >= cached) continue;
-                const float x = n == 0 ? sum[e] : sum[e + 4];
-                a.weights[to0 + e] = a.previous && j + e < place ? a.previous[to0 + e] + x : x;
+            for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+            for (int at = 0; at < rows; at += kRowsAtOnce) {
+                stage(at);
+                __syncthreads();
+                if (t0 < end) add_rows(kt, tile, at);
+                __syncthreads();
             }
+            if (t0 < end) finish(tile);
         }
     }
 }
