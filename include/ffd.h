@@ -412,7 +412,7 @@ int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* 
  * and sees it if j < min(seq_lens[b], Lcap), its page is there, and
  *   (j <= i and (window == 0 or i - j < window))  or  j < prefix_lens[b].
  * Distances are those of places in the cache. After an eviction, which closes gaps, they are no longer those of the text.
- *   softcap       >= 0, 0: none;  window  >= 0, 0: none
+ *   softcap       0 .. 1024 (above: FFD_ERR_UNSUPPORTED), 0: none;  window  >= 0, 0: none
  *   slopes        fp32 [Hq] (device), or NULL;  prefix_lens  int32 [B] (device), or NULL
  */
 typedef struct ffd_score_rules {
@@ -432,7 +432,7 @@ typedef struct ffd_score_rules {
  *   softmax_scale > 0, or 0 for 1/sqrt(D)
  *   workspace     ffd_paged_workspace_bytes(...) bytes; needs no initialisation and is clobbered. Calls that overlap in
  *                 time need separate workspaces.
- * T <= 2^24, T * Hq < 2^28, B * Hkv <= 2^20 and fewer than 2^23 workgroups, else FFD_ERR_UNSUPPORTED.
+ * T <= 2^24, T * Hq < 2^28 and B * Hkv <= 2^20, else FFD_ERR_UNSUPPORTED.
  */
 int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
                         const ffd_score_rules* rules, int B, int T, int Hq, int Hkv, int D, float softmax_scale, void* out,
@@ -468,7 +468,9 @@ int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int
  *   budget        1 .. new_max_pages * page;  recent  0 .. budget
  *   new_lens      int32 [B]: tokens kept (the same for all KV heads)
  *   kept          int32 [B, Hkv, budget]: the old place of the token now at place r, -1 from new_lens[b] on
- *   new_weights   float [B, Hkv, new_max_pages * page] or NULL: the kept tokens' weights (entries behind them as they were)
+ *   new_weights   float [B, Hkv, new_max_pages * page] or NULL: the kept tokens' weights (entries behind them as they were);
+ *                 not overlapping `weights`, nor new_table page_table: FFD_ERR_INVALID_ARGUMENT
+ * B * Hkv <= 2^20 and 2 * B * Hkv * ceil(budget / 128) < 2^23, else FFD_ERR_UNSUPPORTED.
  */
 int ffd_evict_paged(const ffd_paged* cache, const int32_t* new_table, int new_max_pages, const int32_t* seq_lens,
                     const float* weights, int B, int Hkv, int D, int budget, int recent, int32_t* new_lens, int32_t* kept,

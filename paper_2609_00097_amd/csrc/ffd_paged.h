@@ -199,7 +199,7 @@ struct Shares {
 };
 
 // What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). tanh(x) =
-// 1 - 2 / (1 + e^2x): no overflow, infinities and NaN as they are, 2^-23 of the cap off. An 8-bit key's product is
+// 1 - 2 / (1 + e^2x): no overflow, infinities and NaN as they are, at most 2^-20 of the cap off. An 8-bit key's product is
 // multiplied by its M before and by 1 / 127 within `scale`.
 struct ScoreRule {
     float zscale;               // without a cap: scale log2(e); with one: 2 scale log2(e) / cap
@@ -209,7 +209,7 @@ struct ScoreRule {
 __device__ __forceinline__ ScoreRule score_rule(const ChunkArgs& a, bool i8, int head) {
     ScoreRule r;
     const float scale = i8 ? a.scale / 127.f : a.scale;
-    r.zscale = a.cap > 0.f ? scale * 2.f * kLog2e / a.cap : scale * kLog2e;
+    r.zscale = a.cap > 0.f ? fminf(scale * 2.f * kLog2e / a.cap, FLT_MAX) : scale * kLog2e;
     r.cap2 = a.cap * kLog2e;
     r.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     return r;

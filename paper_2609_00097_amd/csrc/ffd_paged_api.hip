@@ -11,6 +11,7 @@ namespace {
 
 constexpr int kMaxCapacity = 1 << 28;
 constexpr int kMaxTokens = 1 << 24;
+constexpr float kMaxCap = 1024.f;               // a capped score is off by at most 2^-20 of the cap: 2^-10 here, half as much as a bf16 probability
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -49,7 +50,7 @@ int check_rules(const ffd_score_rules* r) {
     if (!r) return FFD_OK;
     if (!(r->softcap >= 0.f) || std::isinf(r->softcap) || r->window < 0) return FFD_ERR_INVALID_ARGUMENT;
     if (!aligned4(r->slopes) || !aligned4(r->prefix_lens)) return FFD_ERR_INVALID_ARGUMENT;
-    return FFD_OK;
+    return r->softcap > kMaxCap ? FFD_ERR_UNSUPPORTED : FFD_OK;
 }
 
 ChunkArgs chunk_args(const void* q, const ffd_paged& c, const int32_t* q_start, const int32_t* seq_lens,
@@ -92,6 +93,7 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows
     const int G = Hq / Hkv;
     // every sequence has at most one tile that is not full
     const long long tiles = ((long long)T * G / rows + std::min(B, T)) * Hkv;
+    // (T Hq < 2^28 and B Hkv <= 2^20: below 2^22 workgroups)
     k.grid = k.large() ? std::max((long long)k.slots, k.slots / 2 + tiles) : k.slots;
     while (tiles * (((Lcap + kRound - 1) / kRound >> k.unit_shift) + 1) >= 1LL << 31) ++k.unit_shift;
     return k;
@@ -128,7 +130,6 @@ size_t chunk_workspace(int B, int T, int Hq, int Hkv) {
         for (const bool i8 : {false, true}) bytes = std::max(bytes, chunk_launches(B, T, Hq, Hkv, Lcap, i8).total);
     return bytes;
 }
-bool chunk_fits(const ChunkLaunches& p) { return p.large_kernel.grid * kChunkTileThreads < 1LL << 31; }
 
 template <int CT, bool I8>
 void launch_rows_ruled(bool ruled, dim3 grid, hipStream_t stream, const ChunkAttendArgs& a) {
@@ -210,7 +211,7 @@ int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* 
 size_t ffd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
     CallScope scope;
     if (check_heads(Hq, Hkv, D) != FFD_OK || check_batch(B, T, Hq) != FFD_OK || B == 0 || T == 0) return 0;
-    return pairs_fit(B, Hkv) && chunk_fits(chunk_launches(B, T, Hq, Hkv, 0, false)) ? chunk_workspace(B, T, Hq, Hkv) : 0;
+    return pairs_fit(B, Hkv) ? chunk_workspace(B, T, Hq, Hkv) : 0;
 }
 
 int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_start, const int32_t* seq_lens,
@@ -227,8 +228,8 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
     if (!q || !q_start || !seq_lens || !out || !workspace) return FFD_ERR_INVALID_ARGUMENT;
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(q_start) || !aligned4(seq_lens) || !aligned4(lse))
         return FFD_ERR_INVALID_ARGUMENT;
+    if (!pairs_fit(B, Hkv)) return FFD_ERR_UNSUPPORTED;
     const ChunkLaunches plan = chunk_launches(B, T, Hq, Hkv, (long long)cache->max_pages * cache->page, i8);
-    if (!pairs_fit(B, Hkv) || !chunk_fits(plan)) return FFD_ERR_UNSUPPORTED;
     if (workspace_bytes < chunk_workspace(B, T, Hq, Hkv)) return FFD_ERR_WORKSPACE_TOO_SMALL;
     ChunkAttendArgs a{};
     static_cast<ChunkArgs&>(a) = chunk_args(q, *cache, q_start, seq_lens, rules, B, T, Hq, Hkv, softmax_scale);
@@ -318,6 +319,9 @@ int ffd_evict_paged(const ffd_paged* cache, const int32_t* new_table, int new_ma
         return FFD_ERR_INVALID_ARGUMENT;
     const long long moves = 2LL * ((budget + kEvictMoveRows - 1) / kEvictMoveRows);
     if (!pairs_fit(B, Hkv) || moves * B * Hkv * kThreads >= 1LL << 31) return FFD_ERR_UNSUPPORTED;
+    const size_t pairs = (size_t)B * Hkv * cache->page, at = reinterpret_cast<uintptr_t>(weights), new_at = reinterpret_cast<uintptr_t>(new_weights);
+    if (new_table == cache->page_table) return FFD_ERR_INVALID_ARGUMENT;
+    if (new_weights && new_at < at + pairs * cache->max_pages * sizeof(float) && at < new_at + pairs * new_max_pages * sizeof(float)) return FFD_ERR_INVALID_ARGUMENT;
     const EvictArgs a{paged_of(*cache), new_table, seq_lens, weights, new_lens, kept, new_weights, Hkv, new_max_pages, budget, recent};
     hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)Hkv, (unsigned)B), dim3(kEvictThreads), 0, stream, a);
     if ((st = launch_status()) != FFD_OK) return st;

@@ -625,6 +625,11 @@ def _paged(cache, page_table, device):
     return PagedCache(kv, page_table.data_ptr(), num_pages, page, max_pages), B, Hkv, page, max_pages
 
 
+def _need_int(x, name):
+    if not -1 << 31 <= x < 1 << 31:                      # ctypes would take its low bits
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+
+
 def _ragged(q_start, seq_lens, device, B):
     _need_on(device, q_start, "q_start", torch.int32, (B + 1,))
     _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
@@ -721,6 +726,7 @@ def _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, s
         _need_on(device, slopes, "slopes", torch.float32, (Hq,))
     if prefix_lens is not None:
         _need_on(device, prefix_lens, "prefix_lens", torch.int32, (B,))
+    _need_int(window, "window")
     rules = None
     if softcap or window or slopes is not None or prefix_lens is not None:
         rules = ctypes.byref(ScoreRules(softcap, window, _ptr(slopes), _ptr(prefix_lens)))
@@ -763,6 +769,7 @@ def paged_attention_weights(q, cache, page_table, q_start, seq_lens, lse, *, sof
     device, paged, rules, B, T, Hq, Hkv, Lcap = _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, slopes,
                                                                  prefix_lens)
     _need_on(device, lse, "lse", torch.float32, (T, Hq))
+    _need_int(last, "last")
     if previous is not None:
         _need_on(device, previous, "previous", torch.float32, (B, Hkv, Lcap))
     if out is None:
@@ -787,6 +794,8 @@ def evict_paged(cache, page_table, new_table, seq_lens, weights, budget: int, *,
     if not isinstance(new_table, torch.Tensor) or new_table.dim() != 2:
         raise ValueError("new_table must be [B, new_max_pages]")
     new_max_pages = new_table.shape[1]
+    _need_int(budget, "budget")
+    _need_int(recent, "recent")
     _need_on(device, new_table, "new_table", torch.int32, (B, new_max_pages))
     if new_table.data_ptr() == page_table.data_ptr() and B > 0:
         raise ValueError("new_table must hold other pages than page_table")

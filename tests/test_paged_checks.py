@@ -160,3 +160,25 @@ def test_binding_checks():
         ffd.evict_paged(cache, table, table, lens, torch.zeros(1, 2, 32), 8)
     with pytest.raises(ValueError, match="q must be \\[T"):
         ffd.paged_attention_weights(None, cache, table, q_start, lens, torch.zeros(3, 4))
+
+
+@pytest.mark.parametrize("call", ["attend", "weights"])
+def test_caps_too_large(so, call):
+    assert CALLS[call](so, rules=_rules(softcap=1025.0)) == 2
+    assert CALLS[call](so, B=0, rules=_rules(softcap=1024.0)) == 0
+
+
+def test_evict_overlaps(so):
+    """new_weights on the weights, and one table for both sides."""
+    weights, new = 4 * 2 * 8 * 64, 4 * 2 * 8 * 32               # bytes
+    for at in (FAKE, FAKE + weights - 4, FAKE - new + 4):
+        assert _evict(so, new_table=FAKE + 64, new_weights=at) == 1
+    assert _evict(so, new_table=FAKE) == 1
+
+
+def test_integers_of_more_than_32_bits():
+    from paper_2609_00097_amd import ffd
+    for x in (1 << 31, (1 << 32) + 5, -(1 << 31) - 1):
+        with pytest.raises(ValueError, match="window must fit 32 bits"):
+            ffd._need_int(x, "window")
+    ffd._need_int((1 << 31) - 1, "window")
