@@ -12,9 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libffd.so")
 SOURCES = ["ffd_api.hip", "ffd_attend.hip", "ffd_decode.hip", "ffd_dense.hip", "ffd_evict.hip", "ffd_kv8.hip",
-           "ffd_merge.hip", "ffd_paged_api.hip", "ffd_paged_rows.hip", "ffd_paged_tile.hip", "ffd_paged_weights.hip",
-           "ffd_paged_write.hip",
-           "ffd_prefix.hip", "ffd_quantize.hip", "ffd_topk.hip"]
+           "ffd_merge.hip", "ffd_paged_api.hip", "ffd_paged_rows.hip", "ffd_paged_tile.hip", "ffd_paged_tile8.hip", "ffd_paged_weights.hip",
+           "ffd_paged_write.hip", "ffd_prefix.hip", "ffd_quantize.hip", "ffd_topk.hip"]
 ARCH = os.environ.get("FFD_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [

@@ -375,7 +375,8 @@ template <bool I8, bool INTERLEAVED> __global__ void write_paged_kernel(WritePag
 template <int CT, bool I8, bool RULED> __global__ void chunk_rows_kernel(ChunkAttendArgs a);
 constexpr int kChunkRowsShift = 7;             // blocks of 128 tokens
 constexpr int kChunkTileThreads = 512, kChunkTileRows = 256, kChunkTileShift = 6;
-template <bool I8, bool RULED> __global__ void chunk_tile_kernel(ChunkAttendArgs a);
+template <bool RULED> __global__ void chunk_tile_kernel(ChunkAttendArgs a);       // bf16
+template <bool RULED> __global__ void chunk_tile8_kernel(ChunkAttendArgs a);      // 8 bits
 // Rows of a tile of `rows` that a workgroup of the merge takes.
 __host__ __device__ constexpr int chunk_merge_rows(int rows) { return rows < kChunkTileRows ? 16 : 32; }
 __global__ void chunk_merge_kernel(ChunkMergeArgs a);

@@ -250,10 +250,10 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
         const ChunkKernel& k = plan.large_kernel;
         prepare(k, ws + plan.large_off);
         const dim3 grid((unsigned)k.grid), block(kChunkTileThreads);
-        if (i8 && ruled) hipLaunchKernelGGL((chunk_tile_kernel<true, true>), grid, block, 0, stream, a);
-        else if (i8) hipLaunchKernelGGL((chunk_tile_kernel<true, false>), grid, block, 0, stream, a);
-        else if (ruled) hipLaunchKernelGGL((chunk_tile_kernel<false, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((chunk_tile_kernel<false, false>), grid, block, 0, stream, a);
+        if (i8 && ruled) hipLaunchKernelGGL((chunk_tile8_kernel<true>), grid, block, 0, stream, a);
+        else if (i8) hipLaunchKernelGGL((chunk_tile8_kernel<false>), grid, block, 0, stream, a);
+        else if (ruled) hipLaunchKernelGGL((chunk_tile_kernel<true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((chunk_tile_kernel<false>), grid, block, 0, stream, a);
         if ((st = launch_status()) != FFD_OK) return st;
     }
     if (plan.few) {

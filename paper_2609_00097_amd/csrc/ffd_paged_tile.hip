@@ -1,21 +1,35 @@
-// Attention of chunks of new tokens over a paged cache for gfx950 (ffd_attend.h has the mathematics, ffd_paged.h which tokens a
-// query sees and how the work is cut; ffd_paged_rows.hip takes the sequences with few query rows): tiles of 256 query rows of
-// a KV head, new tokens by query heads, for which the cache's tokens are staged in LDS, 64 at a time.
+// Attention of chunks of new tokens over a paged bf16 cache for gfx950 (ffd_attend.h has the mathematics, ffd_paged.h which tokens a
+// query sees and how the work is cut; ffd_paged_rows.hip takes the sequences with few query rows, ffd_paged_tile8.hip 8-bit
+// caches): tiles of 256 query rows of a KV head, new tokens by query heads, in eight waves of 32 rows, and the cache's tokens from
+// memory straight to LDS, 64 at a time.
 //
-// Mapping, phases and LDS layout are those of ffd_prefix.hip with eight row groups: wave w holds rows 32 w .. 32 w + 31; S^T = K Q^T
-// by v_mfma_f32_32x32x16_bf16, lane (n, h) = (lane & 31, lane >> 5) with row n and tokens 8 a + 4 h + i (a, i = 0 .. 3) of each 32,
-// which are its contraction indices in O^T = V^T P^T; two teams of four waves, one wave of each on every SIMD, are one phase
-// apart, so that one's matrix instructions run beside the other's softmax and staging.
+// Mapping: S^T = K Q^T by v_mfma_f32_32x32x16_bf16; lane (n, h) = (lane & 31, lane >> 5) has row n and tokens 8 a + 4 h + i (a, i =
+// 0 .. 3) of a sub-tile of 32, which are its contraction indices in O^T = V^T P^T, so probabilities stay where they are made.
+// LDS holds rows of 256 bytes with their chunks in the orders of ffd_tile.h; V is read by transposing reads.
+//
+// A wave takes a step for each sub-tile t, in two halves, so that the matrix cores always have products that wait for nothing:
+// first the scores of t + 1 beside the exponentials of t, then the products of t - 1 beside the largest score of t + 1. The
+// maximum is settled between two steps; where it grows (by more than 2^8, or at first) the sum is scaled at once and o after the
+// products that are still to come. Operands are read two products ahead; a step's first ones at the end of the step before. A
+// workgroup meets once a tile, in the middle of its first step (`turn`), with two places for keys and three for values.
 //
 // Probabilities enter the second product rounded to bf16, in one part: a second part would cost half as much again of a product
 // that the matrix cores bound (the few-row kernel, which memory bounds, has two). So that the roundings cancel where they are
 // alike (equal scores, one token with most of the weight), a row is divided by the sum of the rounded probabilities; the exact
-// sum is kept beside it for the lse. 8-bit values multiply their probability by M / 127 before the rounding and have no such sum.
+// sum is kept beside it for the lse.
 //
-// Pages: 16 tokens lie together, so a thread's load is one page's, whose entry is read a tile ahead; rows of pages that are not
-// there, and behind what any query sees, become zeros on their way into LDS.
+// Pages: 16 tokens lie together, so a wave's load is one page's, whose entry is read a tile ahead. Values of pages that are not
+// there, and behind what any query sees, become zeros in LDS, in the tiles that have such. An infinity or NaN among the values of
+// tokens that some rows see and others do not turns results into NaN; a workgroup that finds a result not finite repeats
+// its run with all of them taken out of the tiles, and adds them at the end to the rows that see them.
 //
-// Bound: the matrix cores, 512 operations a query row and token.
+// Bound: the issue of instructions by two waves a SIMD (without any matrix instruction two thirds of the time are left, without
+// the loads, or the barrier, all of it) beside the matrix cores, which 512 operations a query row and token keep busy for less than half of it.
+// Against two teams of waves with matrix and softmax phases in turn and tokens staged in registers, eight KV heads of four:
+// 8K tokens 620 -> 585 us (0.94 PFLOP/s), 512 on 32K 309 -> 291, 3800 in a window of 1024 with a cap, twice, 252 -> 229.
+// Not kept: the waves of a SIMD half a step apart (297), operands three products ahead (293), four waves of 64 rows (365).
+#include <type_traits>
+
 #include "ffd_paged.h"
 #include "ffd_tile.h"
 
@@ -24,144 +38,37 @@ namespace ffd {
 namespace {
 
 constexpr int kTThreads = kChunkTileThreads;
-constexpr int kTeam = kTThreads / 2;
 constexpr int kTokens = 64;                     // tokens of a tile
 constexpr int kShift = kChunkTileShift;
-constexpr int kPart = kTokens / 2;              // tokens that a team stages
+constexpr int kTileBytes = kTokens * 2 * kD;
+constexpr int kMarks = 1024;
 static_assert(kTokens == 1 << kShift);
 
-struct TileLds {
-    alignas(16) uint8_t keys[2][kTokens * 2 * kD];
-    alignas(16) uint8_t values[2][kTokens * 2 * kD];
-    alignas(16) float km[4][kTokens];           // 8 bits: M / 127 of keys and values
-    alignas(16) float vm[4][kTokens];
-    int nonfinite[4];                           // last tile with this index mod 4 that has an infinity or NaN as value
+struct alignas(2 * kTileBytes) TileLds {
+    uint8_t keys[2][kTileBytes];                // places that differ in one bit of the address
+    uint8_t values[3][kTileBytes];
+    uint32_t nonfinite[kMarks / 32];            // bits: runs of tiles that have an infinity or NaN among their values
 };
 
-// A tile's place and pages: the rows of this team's two 16-token groups, and which of the tile's four are there.
-struct TileAt {
-    int t0;
-    uint32_t there;
-    size_t row[2];
-};
-
-// A team's half of a tile on its way from memory to LDS, in registers.
-template <bool I8> struct Staged;
-template <> struct Staged<false> {
-    v4u k[2], v[2];
-    __device__ __forceinline__ void load(v4u (&x)[2], const uint8_t* from, const TileAt& at, int id) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            x[j] = *reinterpret_cast<const v4u*>(from + at.row[j] * (2 * kD) + (uint32_t)((id >> 4) * (2 * kD) + 16 * (id & 15)));
-    }
-    __device__ __forceinline__ void load_keys(const KvSource& kv, const TileAt& at, int id) { load(k, kv.k, at, id); }
-    __device__ __forceinline__ void load_values(const KvSource& kv, const TileAt& at, int id) { load(v, kv.v, at, id); }
-    __device__ __forceinline__ void store_keys(TileLds& lds, int u, const TileAt&, int, int part, int id) const {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int row = kPart * part + 16 * j + (id >> 4);
-            *reinterpret_cast<v4u*>(&lds.keys[u & 1][row * (2 * kD) + 16 * key_chunk(row, id & 15)]) = k[j];
-        }
-    }
-    __device__ __forceinline__ void store_values(TileLds& lds, int u, const TileAt& at, int end, int part, int id) const {
-        const bool alive = at.there == 15u && at.t0 + kTokens <= end;           // uniform
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int row = kPart * part + 16 * j + (id >> 4);
-            v4u x = v[j];
-            if (!alive && !((at.there >> (2 * part + j) & 1) && at.t0 + row < end)) x = v4u{0, 0, 0, 0};
-            const uint32_t big = pk_max_u16(pk_max_u16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max_u16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-            if (max(big & 0xffffu, big >> 16) >= 0x7f80u) {
-                lds.nonfinite[u & 3] = u;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t lo = (x[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu, hi = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
-                    x[i] &= lo | hi;
-                }
-            }
-            *reinterpret_cast<v4u*>(&lds.values[u & 1][row * (2 * kD) + 16 * value_chunk<false>(row, id & 15)]) = x;
-        }
-    }
-};
-template <> struct Staged<true> {
-    v4u k, v;
-    uint32_t m;                                 // absmax of a key (threads below kPart) or value (the next kPart)
-    __device__ __forceinline__ void load(v4u& x, const uint8_t* from, const TileAt& at, int id) {
-        const size_t row = (id >> 7 ? at.row[1] : at.row[0]) + ((id >> 3) & 15);
-        x = *reinterpret_cast<const v4u*>(from + row * kD + 16 * (id & 7));
-    }
-    __device__ __forceinline__ void load_keys(const KvSource& kv, const TileAt& at, int id) {
-        load(k, kv.k, at, id);
-        m = 0;                                  // the values' absmaxes come with the keys: they are needed with the scores
-        if (id < 2 * kPart) {
-            const int t = id & (kPart - 1);
-            m = (id < kPart ? kv.k_absmax : kv.v_absmax)[(t >> 4 ? at.row[1] : at.row[0]) + (t & 15)];
-        }
-    }
-    __device__ __forceinline__ void load_values(const KvSource& kv, const TileAt& at, int id) { load(v, kv.v, at, id); }
-    static __device__ __forceinline__ void expand(uint8_t* tile, int row, int c, bool keys, const v4u& w) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int at = keys ? key_chunk(row, c + x) : value_chunk<true>(row, c + x);
-            *reinterpret_cast<v8bf*>(tile + row * (2 * kD) + 16 * at) = expand8(w[2 * x], w[2 * x + 1]);
-        }
-    }
-    __device__ __forceinline__ void store_keys(TileLds& lds, int u, const TileAt& at, int end, int part, int id) const {
-        expand(lds.keys[u & 1], kPart * part + (id >> 3), 2 * (id & 7), true, k);
-        if (id < 2 * kPart) {
-            const int t = kPart * part + (id & (kPart - 1));
-            const bool alive = (at.there >> (t >> 4) & 1) && at.t0 + t < end;
-            const float x = alive ? bf16_to_f32((uint16_t)m) * (1.f / 127.f) : 0.f;
-            const bool finite = fabsf(x) < INFINITY;
-            if (id < kPart) {
-                lds.km[u & 3][t] = x;
-            } else {
-                lds.vm[u & 3][t] = finite ? x : 0.f;
-                if (!finite) lds.nonfinite[u & 3] = u;
-            }
-        }
-    }
-    __device__ __forceinline__ void store_values(TileLds& lds, int u, const TileAt&, int, int part, int id) const {
-        expand(lds.values[u & 1], kPart * part + (id >> 3), 2 * (id & 7), false, v);
-    }
-};
-
-// What a lane's row sees of a tile, token c of the tile counted from 4 h: c <= high and c > low, or c < prefix.
-struct Limits {
-    int high, low, prefix;
-};
-
-// Infinities and NaN among the values of tile [t0, t0 + kTokens), which are zeros in LDS: added to the rows that see them.
-template <bool I8>
-__device__ __forceinline__ void add_nonfinite(v16f (&o)[4], const ChunkAttendArgs& a, const ChunkItem& it, int t0, int end, const Limits& see, int h) {
-#pragma unroll 1
-    for (int t = 0; t < kTokens && t0 + t < end; ++t) {
-        const int entry = page_entry(a.pages, it.b, t0 + t);
-        if (!page_there(a.pages, entry)) continue;
-        const size_t at = page_row(a.pages, a.Hkv, it.kvh, entry, t0 + t);
-        const uint16_t* row = I8 ? a.pages.kv.v_absmax + at : reinterpret_cast<const uint16_t*>(a.pages.kv.v) + at * kD + 4 * h;
-        const int c = t - 4 * h;
-        const bool seen = (c <= see.high && c > see.low) || c < see.prefix;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float x = bf16_to_f32(row[I8 ? 0 : 32 * d + 8 * (i >> 2) + (i & 3)]);
-                o[d][i] += !(fabsf(x) < INFINITY) && seen ? x : 0.f;
-            }
-    }
+// 16 bytes a lane from memory straight to LDS, where a wave's 64 pieces lie one after the other; `lds_at` and `base` are the
+// same in all lanes. The compiler does not count this load: whoever needs it waits with wait_for_loads() and a barrier. (As a
+// builtin it would be taken to be in the way of every read of LDS, and waited for there.)
+__device__ __forceinline__ void load_to_lds(uint32_t lds_at, const uint8_t* base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_at), "v"(offset), "s"(base) : "memory", "m0");
 }
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+template <int N> using Int = std::integral_constant<int, N>;
 
 }  // namespace
 
-template <bool I8, bool RULED>
+template <bool RULED>
 __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArgs a) {
     __shared__ TileLds lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int n = lane & 31, h = lane >> 5;
     ChunkItem it;
     if (!chunk_item<kChunkTileRows, kShift>(a, blockIdx.x, lane, it)) return;
-    const int team = wave >> 2, part = team, id = tid & (kTeam - 1);
     const int gs = __builtin_ctz(a.G), step = kChunkTileRows >> gs, tok0 = it.tile * step;
     const int tok1 = min(tok0 + step, it.seq.n) - 1, live_rows = (tok1 - tok0 + 1) << gs;
     const int hq0 = it.kvh * a.G, place = it.seq.L - it.seq.n, cached = min(it.seq.L, a.Lcap);
@@ -170,310 +77,391 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     const int first = (int)((long long)span.count * it.run / it.cuts), last = (int)((long long)span.count * (it.run + 1) / it.cuts);
 
     // this lane's row
-    const int r = 32 * wave + n;
+    const int r = 32 * wave + n, tok = tok0 + (min(r, live_rows - 1) >> gs), head = hq0 + (r & (a.G - 1));
     const bool live = r < live_rows;
-    const int tok = tok0 + (min(r, live_rows - 1) >> gs), head = hq0 + (r & (a.G - 1));
     const size_t row_at = (size_t)(it.seq.q0 + tok) * a.Hq + head;
     const int at = place + tok;
+    const ScoreRule rule = score_rule(a, false, head);
     v8bf q[8];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        const v4u x = *reinterpret_cast<const v4u*>(a.q + row_at * kD + 16 * s + 8 * h);
-        q[s] = __builtin_bit_cast(v8bf, live ? x : v4u{0, 0, 0, 0});
+    for (int k = 0; k < 8; ++k) {
+        const v4u x = *reinterpret_cast<const v4u*>(a.q + row_at * kD + 16 * k + 8 * h);
+        q[k] = __builtin_bit_cast(v8bf, live ? x : v4u{0, 0, 0, 0});
     }
-    const ScoreRule rule = score_rule(a, I8, head);
-    const float zscale = RULED ? 1.f : I8 ? a.scale * kLog2e : rule.zscale;     // of what the maximum is taken of
     // the wave's first and last place, and the tile from which on none of its rows sees a token
-    const bool any_row = 32 * wave < live_rows;
     const int low = place + tok0 + ((32 * wave) >> gs), high = place + min(tok0 + ((32 * wave + 31) >> gs), tok1);
-    const int wave_end = any_row ? max(min(max(high + 1, it.seq.pre), cached), 0) : 0;
+    const int wave_end = 32 * wave < live_rows ? max(min(max(high + 1, it.seq.pre), cached), 0) : 0;
     const int high_block = (wave_end + kTokens - 1) >> kShift;
     const int mine_last = max(first, min(last, high_block <= span.prefix ? high_block : max(high_block - span.skip, span.prefix)));
+    // 32 tokens from t0 on are seen whole by every row of the wave if they are there, t0 <= whole_to and t0 > whole_from or
+    // t0 <= prefix_to
+    const int whole_to = min(max(low + 1, it.seq.pre), cached) - 32, whole_from = a.window > 0 ? high - a.window : INT32_MIN, prefix_to = it.seq.pre - 32;
 
-    if (tid < 4) lds.nonfinite[tid] = -1;
-    v16f o[4];
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, l = 0.f, rounded = 0.f;
-
-    // pages: the entries of a tile's four groups lie in the lanes, two tiles ahead of the loads by them
     auto token0 = [&](int u) { return span.block(min(u, last - 1)) << kShift; };
-    auto load_entries = [&](int u) { return page_entry(a.pages, it.b, token0(u) + 16 * (lane & 3)); };
-    uint32_t ring = 0;                          // four bits a tile, which groups are there, by its number mod 4
-    auto place_of = [&](int u, int entries) {
-        TileAt x;
-        x.t0 = token0(u);
-        x.there = (uint32_t)__ballot(page_there(a.pages, entries)) & 15u;
+    uint32_t ring = 0;                          // four bits a tile, which 16-token groups are there, by its number mod 4
+    // A wave brings eight rows of a tile, four a load. The entries of a tile's four groups lie in lanes 0 .. 3.
+    const int my_row = 8 * wave + (lane >> 4);
+    uint32_t key_from[2], value_from[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int r = my_row + 4 * j, in = (4 * j + (lane >> 4)) * (2 * kD);
+        key_from[j] = in + 16 * key_chunk(r, lane & 15);
+        value_from[j] = in + 16 * value_chunk<false>(r, lane & 15);
+    }
+    // (whether they are the table's is seen where they are used, so that the load is waited for there)
+    auto load_entries = [&](int u) {
+        return a.pages.table[(size_t)it.b * a.pages.max_pages + min((token0(u) + 16 * (lane & 3)) >> a.pages.page_shift, a.pages.max_pages - 1)];
+    };
+    auto load_rows = [&](const uint8_t* tile, const uint8_t* pages, size_t row, const uint32_t (&from)[2]) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            load_to_lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)(tile + (8 * wave + 4 * j) * (2 * kD)), pages + row * (2 * kD), from[j]);
+    };
+    int entries = 0;                            // of the tile whose keys are asked for next
+    size_t row = 0;                             // this wave's, of the tile whose keys were asked for last
+    auto bring_keys = [&](int u) {
+        const int shift = 4 * (u & 3), known = (token0(u) + 16 * (lane & 3)) >> a.pages.page_shift < a.pages.max_pages ? entries : -1;
+        const int e = __builtin_amdgcn_readlane(known, wave >> 1);
+        ring = (ring & ~(15u << shift)) | ((uint32_t)__ballot(page_there(a.pages, known)) & 15u) << shift;
+        row = page_row(a.pages, a.Hkv, it.kvh, page_there(a.pages, e) ? e : 0, token0(u) + 8 * wave);
+        entries = load_entries(u + 1);
+        load_rows(lds.keys[u & 1], a.pages.kv.k, row, key_from);
+    };
+    // Rows that nobody sees to zero (zero times infinity); `careful`: infinities and NaN of the others too.
+    int mark_shift = 0;                         // tiles of a mark
+    while ((last - first) >> mark_shift >= kMarks) ++mark_shift;
+    auto fix_rows = [&](int u, uint8_t* values, bool careful) {
+        const int t0 = token0(u);
+        const uint32_t there = ring >> (4 * (u & 3)) & 15u;
+        if (!careful && there == 15u && t0 + kTokens <= span.end) return;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int e = __builtin_amdgcn_readlane(entries, 2 * part + j);
-            x.row[j] = page_row(a.pages, a.Hkv, it.kvh, page_there(a.pages, e) ? e : 0, x.t0 + 16 * (2 * part + j));
+            const int r = my_row + 4 * j;
+            v4u* p = reinterpret_cast<v4u*>(values + r * (2 * kD) + 16 * (lane & 15));
+            v4u x = *p;
+            if (!((there >> (wave >> 1)) & (uint32_t)(t0 + r < span.end) & 1u)) x = v4u{0, 0, 0, 0};
+            const uint32_t big = pk_max_u16(pk_max_u16(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max_u16(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+            if (careful && max(big & 0xffffu, big >> 16) >= 0x7f80u) {
+                atomicOr(&lds.nonfinite[(u - first) >> mark_shift >> 5], 1u << ((u - first) >> mark_shift & 31));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t lo = (x[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu, hi = (x[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u;
+                    x[i] &= lo | hi;
+                }
+            }
+            *p = x;
         }
-        const int s = 4 * (u & 3);
-        ring = (ring & ~(15u << s)) | x.there << s;
-        return x;
     };
 
-    // this lane's places in a tile: its key row's chunk for step 0, and its piece of a transposing read of dims 0 .. 31
-    const uint32_t k_at = n * (2 * kD) + 16 * key_chunk(n, h);
+    v16f o[4], s[2];                            // 32 dims each; scores by sub-tile of 32 tokens mod 2
+    v8bf p[2][2];                               // [sub-tile mod 2][16 tokens]
+    float m, l, rounded;
+
     const int i16 = lane & 15;
     const int v_row = 4 * h + (i16 >> 2), v_c = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-    const uint32_t v_at = v_row * (2 * kD) + 16 * value_chunk<I8>(v_row, v_c) + 8 * (i16 & 1);
-
-    v16f s[2];
-    v8bf p[4];
-    auto value_operand = [&](const uint8_t* values, int y, int d) {
+    // Places of the operands in LDS, kept for the tiles at hand: of the keys that the next scores take, of the values that the
+    // next products take. Operand j of a sub-tile: keys' dims 16 j .., or 32 dims 32 (j & 3) .. of values' tokens 16 (j >> 2) ..
+    using Lds = __attribute__((address_space(3))) const uint8_t*;
+    uint32_t key_at[8], value_at[4][2];
+    auto keys_at = [&](int u) {
+        const uint32_t keys = (uint32_t)(uintptr_t)(Lds)lds.keys[u & 1] + n * (2 * kD) + 16 * key_chunk(n, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) key_at[j] = keys ^ (j << 5);
+    };
+    auto key_operand = [&](int half, int j) { return *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((Lds)(uintptr_t)key_at[j] + half * 32 * 2 * kD); };
+    auto value_operand = [&](int half, int j) {
         v4s v[2];
 #pragma unroll
         for (int z = 0; z < 2; ++z)
             v[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
-                values + (v_at ^ (d << 6) ^ (z << 5)) + (16 * y + 8 * z) * 2 * kD));
-        return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                (uintptr_t)(value_at[j & 3][z] + (16 * (j >> 2) + 8 * z + 32 * half) * 2 * kD)));
+        return __builtin_bit_cast(v8bf, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    // s = K Q^T of tile u; the next four key operands are on their way from LDS while four are used
-    v8bf kf[2][4];
-    auto read_key_operands = [&](int u, int j) {
-        const uint8_t* keys = lds.keys[u & 1];
+    auto values_at = [&](const uint8_t* values) {
+        const uint32_t x = (uint32_t)(uintptr_t)(Lds)values + v_row * (2 * kD) + 16 * value_chunk<false>(v_row, v_c) + 8 * (i16 & 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            kf[j & 1][e] = *reinterpret_cast<const v8bf*>(keys + ((k_at ^ (((j & 1) * 4 + e) << 5)) + (j >> 1) * 32 * 2 * kD));
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) value_at[d][z] = x ^ (d << 6) ^ (z << 5);
     };
-    auto scores = [&](int u) {
-#pragma unroll
-        for (int j = 1; j < 5; ++j) {
-            if (j < 4) read_key_operands(u, j);
-            __builtin_amdgcn_sched_barrier(0);
-            const int x = (j - 1) >> 1, k = (j - 1) & 1;
-            if (k == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][e], q[4 * k + e], s[x], 0, 0, 0);
-        }
-    };
-    auto read_scales = [&](v4f (&x)[2][4], const float* from) {
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) x[y][b] = *reinterpret_cast<const v4f*>(from + 32 * y + 8 * b + 4 * h);
-    };
-    auto limits = [&](int t0) {
-        Limits see;
-        const int rel = at - t0 - 4 * h, behind = cached - t0 - 4 * h;
-        see.high = min(rel, behind - 1);
-        see.low = a.window > 0 ? rel - a.window : INT32_MIN;
-        see.prefix = min(it.seq.pre - t0 - 4 * h, behind);
-        return see;
+    auto add_product = [&](int j, const v8bf& operand, const v8bf (&prob)[2]) {
+        o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, prob[j >> 2], o[j & 3], 0, 0, 0);
     };
 
-    // p = the probabilities of tile u against the maximum m, which follows the running one; their sum into l.
-    auto softmax = [&](int u) {
-        const int t0 = token0(u);
-        const uint32_t there = ring >> (4 * (u & 3)) & 15u;
-        v4f scales[2][4];
-        if constexpr (I8) {
-            read_scales(scales, lds.km[u & 3]);
+    // Sub-tile t's products x on their way to scores: the largest of the row (in powers of two), whether any is seen; rules and
+    // masks are applied where there are any, else x stays the product (`raw`), to be scaled, and capped, with the exponential.
+    float top = -INFINITY;
+    bool raw = true;
+    auto rules_and_masks = [&](int t, v16f& x) {
+        asm volatile("");                       // a branch around all this, not selections after it
+        const int t0 = token0(t >> 1) + 32 * (t & 1);
+        const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
+        const int rel = at - t0 - 4 * h, end = cached - t0 - 4 * h;
+        const int high = min(rel, end - 1), low = a.window > 0 ? rel - a.window : INT32_MIN, prefix = min(it.seq.pre - t0 - 4 * h, end);
+        uint32_t some = 0;
+        float mx = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+        for (int i = 0; i < 16; ++i) {
+            const int k = 8 * (i >> 2) + (i & 3);
+            float z = x[i];
+            if constexpr (RULED) {
+                z *= rule.zscale;
+                if (rule.cap2 != 0.f) z = capped(z, rule.cap2);
+                z = fmaf(-rule.slope2, fabsf((float)rel - (float)k), z);
+            }
+            const uint32_t seen = (uint32_t)(((k <= high) & (k > low)) | (k < prefix)) & (there >> (i >> 3));
+            x[i] = seen & 1 ? z : -INFINITY;
+            mx = fmaxf(mx, x[i]);
+            some |= seen;
+        }
+        const bool any = halves_max(some & 1 ? 1.f : 0.f) > 0.f;
+        top = any ? fmaxf(halves_max(mx) * (RULED ? 1.f : rule.zscale), -FLT_MAX) : -INFINITY;
+        raw = false;
+    };
+    // The reference m up to the largest score of sub-tile t. The products of t - 1 are still to come with the old one: o follows
+    // after them.
+    float corr = 1.f;
+    uint64_t grown = 0;                         // lanes whose reference has grown
+    auto settle = [&]() {
+        grown = __ballot(top > m + kSlack);
+        if (grown == 0) return;
+        const float mn = top > m + kSlack ? top : m;
+        corr = mn == m ? 1.f : exp2_hw(m - mn);
+        m = mn;
+        l *= corr;
+        rounded *= corr;
+    };
+
+    v8bf kf[3], vf[3];                          // operands on their way: two products ahead
+    // First half of a step: the probabilities of a sub-tile, beside them the scores of the next one, which is half `half` of its tile.
+    auto exponentials = [&](v16f& now, v16f& next, v8bf (&probs)[2], auto half, auto capping) {
+        constexpr int H = decltype(half)::value;
+        constexpr bool CAP = decltype(capping)::value;
+        const float scale = RULED && !CAP && !raw ? 1.f : rule.zscale;
+        const float ref = m == -INFINITY ? 0.f : m, shift = rule.cap2 - ref;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[x][i] *= scales[x][i >> 2][i & 3];
+        for (int i = 0; i < 16; ++i) next[i] = 0.f;
+        // With each product the arguments of pair j + 2, the exponentials of pair j, sum and rounding of pair j - 1, so that none
+        // waits for the one before it.
+        float sum[2] = {0.f, 0.f}, x[3][2], e[2][2];
+        auto arguments = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (CAP) x[j % 3][i] = fmaf(-2.f * rule.cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(now[2 * j + i] * rule.zscale)), shift);
+                else x[j % 3][i] = fmaf(now[2 * j + i], scale, -ref);
+            }
+        };
+        auto round_pair = [&](int j) {
+            uint32_t w0 = pack_bf16(e[j & 1][0], e[j & 1][1]);
+            asm volatile("" : "+v"(w0));
+            sum[0] += e[j & 1][0];
+            sum[1] += e[j & 1][1];
+            rounded = pair_sum(w0, rounded);
+            v4u w = __builtin_bit_cast(v4u, probs[j >> 2]);
+            w[j & 3] = w0;
+            probs[j >> 2] = __builtin_bit_cast(v8bf, w);
+        };
+        arguments(0);
+        arguments(1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j < 6) kf[(j + 2) % 3] = key_operand(H, j + 2);
+            else vf[j - 6] = value_operand(H, j - 6);           // of the sub-tile before this one: the other half of its tile
+            next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % 3], q[j], next, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) e[j & 1][i] = exp2_hw(x[j % 3][i]);
+            if (j < 6) arguments(j + 2);
+            if (j > 0) round_pair(j - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        round_pair(7);
+        l += sum[0] + sum[1];
+        asm volatile("" : "+v"(l), "+v"(rounded));        // here, not where they are needed
+    };
+    // Second half: the products of the sub-tile before, beside them the largest of the next one, t; then the first operands
+    // of the step to come, from half `half` of its keys' tile.
+    auto second = [&](int t, v16f& next, v8bf (&before)[2], auto half, auto products) {
+        constexpr bool P = decltype(products)::value;
+        constexpr int H = decltype(half)::value;
+        const int t0 = token0(t >> 1) + 32 * (t & 1);
+        const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
+        const bool plain = (there == 3u) & (t0 <= whole_to) & ((t0 > whole_from) | (t0 <= prefix_to)) & !(RULED && a.slopes);
+        float mx[4], up_to = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (P) {
+                if (j < 6) vf[(j + 2) % 3] = value_operand(1 - H, j + 2);
+                else kf[j - 6] = key_operand(H, j - 6);
+                add_product(j, vf[j % 3], before);
+            } else if (j >= 6) {
+                kf[j - 6] = key_operand(H, j - 6);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (j == 2) mx[i] = fmaxf(next[4 * i], next[4 * i + 1]);
+                if (j == 3) mx[i] = fmaxf(fmaxf(mx[i], next[4 * i + 2]), next[4 * i + 3]);
+            }
+            if (j == 4) mx[0] = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
+            if (j == 5) mx[0] = fmaxf(mx[0], mx[3]);
+            if (j == 6) up_to = halves_max(mx[0]);
+            if (j == 7) up_to *= rule.zscale;
+            __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (RULED) {
-            const float scale = I8 ? rule.zscale * 127.f : rule.zscale;         // 1 / 127 is in the scales here
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[x][i] *= scale;
-            if (rule.cap2 != 0.f) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[x][i] = capped(s[x][i], rule.cap2);
-            }
-            if (a.slopes) {
-                const float rel = (float)(at - t0 - 4 * h);
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[x][i] = fmaf(-rule.slope2, fabsf(rel - (float)(32 * x + 8 * (i >> 2) + (i & 3))), s[x][i]);
-            }
+            if (rule.cap2 != 0.f) up_to = capped(up_to, rule.cap2);
         }
-        const bool behind = t0 + kTokens <= low + 1 && (a.window <= 0 || t0 > high - a.window);
-        bool any = true;
-        if (!((behind || t0 + kTokens <= it.seq.pre) && t0 + kTokens <= cached && there == 15u)) {
-            const Limits see = limits(t0);
-            uint32_t some = 0;
+        top = fmaxf(up_to, -FLT_MAX);           // NaN: of no weight for the reference
+        raw = true;
+        if ((grown != 0) | !plain) {            // uniform
+            asm volatile("");
+            if (grown != 0) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = 32 * x + 8 * (i >> 2) + (i & 3);
-                    const uint32_t seen = (uint32_t)(((c <= see.high) & (c > see.low)) | (c < see.prefix)) & (there >> (2 * x + (i >> 3)));
-                    s[x][i] = seen & 1 ? s[x][i] : -INFINITY;
-                    some |= seen;
-                }
-            any = halves_max(some & 1 ? 1.f : 0.f) > 0.f;
-        }
-        float mx[4];                                    // four chains, as for the sum below
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = s[0][i];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[x][i]);
-        const float top = halves_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * zscale;
-        const bool up = any && (m == -INFINITY || !(top <= m + kSlack));                // NaN: up
-        if (__ballot(up) != 0) {
-            const float mn = up ? fmaxf(fmaxf(m, top), -FLT_MAX) : m;                   // finite once a token is seen
-            const float corr = mn == m ? 1.f : exp2_hw(m - mn);
-            m = mn;
-            l *= corr;
-            rounded *= corr;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) o[d] *= corr;
-        }
-        const float m0 = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (I8) read_scales(scales, lds.vm[u & 3]);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float e[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                e[i] = exp2_hw(fmaf(s[x][i], zscale, -m0));
-                sum[i & 3] += e[i];
+                for (int d = 0; d < 4; ++d) o[d] *= corr;
             }
-            if constexpr (I8) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) e[i] *= scales[x][i >> 2][i & 3];
-            }
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    w[k] = pack_bf16(e[8 * y + 2 * k], e[8 * y + 2 * k + 1]);
-                    if constexpr (!I8) rounded = pair_sum(w[k], rounded);
-                }
-                p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
-            }
+            if (!plain) rules_and_masks(t, next);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
-    // o += V^T P^T of tile u, and the infinities and NaN among its values
-    auto products = [&](int u) {
-        const uint8_t* values = lds.values[u & 1];
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_operand(values, y, d)), p[y], o[d], 0, 0, 0);
-    };
-    auto nonfinite = [&](int u) {
-        if (__builtin_amdgcn_readfirstlane(lds.nonfinite[u & 3]) == u) {
+    // They reach the rows that see them at the end, when o is scaled no more.
+    auto add_nonfinite = [&]() {
+#pragma unroll 1
+        for (int u = first; u < last; ++u) {
+            const int mark = (u - first) >> mark_shift;
+            if (!(__builtin_amdgcn_readfirstlane(lds.nonfinite[mark >> 5]) >> (mark & 31) & 1)) continue;
             const int t0 = token0(u);
-            add_nonfinite<I8>(o, a, it, t0, span.end, limits(t0), h);
+#pragma unroll 1
+            for (int t = t0; t < min(t0 + kTokens, span.end); ++t) {
+                const int entry = page_entry(a.pages, it.b, t);
+                if (!page_there(a.pages, entry)) continue;
+                const uint16_t* row = reinterpret_cast<const uint16_t*>(a.pages.kv.v) + page_row(a.pages, a.Hkv, it.kvh, entry, t) * kD + 4 * h;
+                const bool seen = sees(at, t, a.window, it.seq.pre);
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = bf16_to_f32(row[32 * d + 8 * (i >> 2) + (i & 3)]);
+                        o[d][i] += !(fabsf(x) < INFINITY) & seen ? x : 0.f;
+                    }
+            }
         }
     };
 
-    __syncthreads();
-    if (first < last) {
-        Staged<I8> st, head_keys;
-        const int e0 = load_entries(first), e1 = load_entries(first + 1);
-        int entries = load_entries(first + 2);
-        TileAt before = place_of(first, e0), now = before;
-        head_keys.load_keys(a.pages.kv, now, id);
-        st.load_values(a.pages.kv, now, id);
-        now = place_of(first + 1, e1);
-        st.load_keys(a.pages.kv, now, id);
-        head_keys.store_keys(lds, first, before, span.end, part, id);
-        // this team's half of the keys of tile u and the values of u - 1 to LDS; those after them are asked for. Behind the
-        // run's end its last tile is staged again.
-        auto stage = [&](int u) {
-            st.store_keys(lds, u, now, span.end, part, id);
-            st.store_values(lds, u - 1, before, span.end, part, id);
-            before = now;
-            now = place_of(u + 1, entries);
-            entries = load_entries(u + 2);
-            st.load_keys(a.pages.kv, now, id);
-            st.load_values(a.pages.kv, before, id);
-        };
-        __syncthreads();
-        if (team == 1) {
-            stage(first + 1);
+    for (bool careful = false;; careful = true) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) p[1][y] = __builtin_bit_cast(v8bf, v4u{0, 0, 0, 0});
+        m = -INFINITY;
+        l = rounded = 0.f;
+        grown = 0;
+        if (tid < kMarks / 32) lds.nonfinite[tid] = 0;
+        if (first < last) {
+            entries = load_entries(first);
+            __syncthreads();                    // a careful run: the first one's reads are done
+            uint8_t *before = lds.values[0], *now = lds.values[1], *after = lds.values[2];      // values of tiles u - 1, u, u + 1
+            for (int i = tid; i < kTileBytes / 16; i += kTThreads) reinterpret_cast<v4u*>(before)[i] = v4u{0, 0, 0, 0};
+            bring_keys(first);
+            wait_for_loads();
+            asm volatile("" : "+v"(entries));
             __syncthreads();
-        }
-        // a tile's two phases: scores after the products of the tile before, then softmax
-        auto vector_phase = [&](int u) {
-            __syncthreads();
-            softmax(u);
-            stage(u + 1 + team);
-            __syncthreads();
-        };
-        if (first < mine_last) {
-            read_key_operands(first, 0);
-            scores(first);
-            vector_phase(first);
-            for (int u = first + 1; u < mine_last; ++u) {
-                read_key_operands(u, 0);
-                products(u - 1);
-                scores(u);
-                nonfinite(u - 1);
-                vector_phase(u);
+            load_rows(now, a.pages.kv.v, row, value_from);
+            if (first + 1 < last) bring_keys(first + 1);
+            // In the middle of the first step of tile u: its values and the next one's keys are there; those after them are asked for,
+            // to the places of the values of u - 2 and the keys of u, which are done with.
+            auto turn = [&](int u) {
+                wait_for_loads();
+                asm volatile("" : "+v"(entries));       // counted as there from here on, not after the next loads
+                fix_rows(u, now, careful);
+                __syncthreads();
+                if (u + 1 < last) load_rows(after, a.pages.kv.v, row, value_from);
+                if (u + 2 < last) bring_keys(u + 2);
+            };
+            auto rotate = [&]() {
+                uint8_t* x = before;
+                before = now, now = after, after = x;
+            };
+            constexpr Int<0> kFirst{};
+            constexpr Int<1> kSecond{};
+            int u = first;
+            if (first < mine_last) {
+                keys_at(first);
+                values_at(before);
+                kf[0] = key_operand(0, 0), kf[1] = key_operand(0, 1);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j < 6) kf[(j + 2) % 3] = key_operand(0, j + 2);
+                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % 3], q[j], s[0], 0, 0, 0);
+                }
+                second(2 * u, s[0], p[1], kSecond, std::false_type());
+                for (; u < mine_last; ++u) {
+                    settle();
+                    if (RULED && raw && rule.cap2 != 0.f) exponentials(s[0], s[1], p[0], kSecond, std::true_type());
+                    else exponentials(s[0], s[1], p[0], kSecond, std::false_type());
+                    turn(u);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) key_at[j] ^= kTileBytes;
+                    second(2 * u + 1, s[1], p[1], kFirst, std::true_type());
+                    values_at(now);
+                    settle();
+                    if (RULED && raw && rule.cap2 != 0.f) exponentials(s[1], s[0], p[1], kFirst, std::true_type());
+                    else exponentials(s[1], s[0], p[1], kFirst, std::false_type());
+                    second(2 * u + 2, s[0], p[0], kSecond, std::true_type());
+                    rotate();
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) add_product(j, value_operand(1, j), p[1]);
             }
-            products(mine_last - 1);
-            nonfinite(mine_last - 1);
+            for (; u < last; ++u) {
+                turn(u);
+                rotate();
+            }
         }
-        for (int u = mine_last; u <= last; ++u) {
-            __syncthreads();
-            if (u < last) stage(u + 1 + team);
-            __syncthreads();
+        if (careful) {
+            add_nonfinite();                    // the last turn's barrier is behind all marks
+            break;
         }
-        if (team == 0) __syncthreads();
+        float x = 0.f;                          // stays zero where every o is finite
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = fmaf(o[d][i], 0.f, x);
+        if (!__syncthreads_or(x != 0.f)) break;
     }
 
-    l = halves_sum(l);
-    if constexpr (!I8) {
-        rounded = halves_sum(rounded);
-        const float f = m == -INFINITY ? 1.f : l / rounded;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[d] *= f;
-    }
+    const float sum = halves_sum(l), near = halves_sum(rounded);
+    const bool any_seen = m != -INFINITY;
     if (!live) return;
     const float ln = m * 0.69314718055994531f;
     if (it.part >= 0) {
+        const float f = any_seen ? sum / near : 1.f;
         const size_t to = (size_t)it.part * kChunkTileRows + r;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
                 *reinterpret_cast<float4*>(a.parts.acc + to * kD + 32 * d + 8 * b + 4 * h) =
-                    make_float4(o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]);
+                    make_float4(o[d][4 * b] * f, o[d][4 * b + 1] * f, o[d][4 * b + 2] * f, o[d][4 * b + 3] * f);
         if (h == 0) {
             a.parts.m[to] = ln;
-            a.parts.l[to] = l;
+            a.parts.l[to] = sum;
         }
         return;
     }
-    const bool any = m != -INFINITY;
-    const float inv = any ? 1.f / l : 0.f;
+    const float inv = any_seen ? 1.f / near : 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const uint2 w = make_uint2(pack_bf16(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), pack_bf16(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv));
-            *reinterpret_cast<uint2*>(a.out + row_at * kD + 32 * d + 8 * b + 4 * h) = any ? w : make_uint2(0u, 0u);
+            *reinterpret_cast<uint2*>(a.out + row_at * kD + 32 * d + 8 * b + 4 * h) = any_seen ? w : make_uint2(0u, 0u);
         }
-    if (h == 0 && a.lse) a.lse[row_at] = any ? ln + logf(l) : -INFINITY;
+    if (h == 0 && a.lse) a.lse[row_at] = any_seen ? ln + logf(sum) : -INFINITY;
 }
 
-template __global__ void chunk_tile_kernel<false, false>(ChunkAttendArgs);
-template __global__ void chunk_tile_kernel<false, true>(ChunkAttendArgs);
-template __global__ void chunk_tile_kernel<true, false>(ChunkAttendArgs);
-template __global__ void chunk_tile_kernel<true, true>(ChunkAttendArgs);
+template __global__ void chunk_tile_kernel<false>(ChunkAttendArgs);
+template __global__ void chunk_tile_kernel<true>(ChunkAttendArgs);
 
 }  // namespace ffd
