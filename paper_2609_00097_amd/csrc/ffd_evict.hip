@@ -75,6 +75,17 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         return j < kHeld ? *reinterpret_cast<const uint4*>(&lds.keys[j]) : keys_of(j, weights_at(j), page_entry(a.from, b, min(j, last4)));
     };
     const int rounds = (L + kEvictStep - 1) / kEvictStep;
+    // The digits of the first pass are counted as the keys are made.
+    for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
+    __syncthreads();
+    auto count_keys = [&](const uint4& k4, int pass, int shift, int bits, uint32_t prefix) {
+        const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int e = 0; e < kPerThread; ++e) {
+            const bool active = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
+            count_digit(lds.hist, (int)(key[e] >> shift) & ((1 << bits) - 1), active, lane);
+        }
+    };
     for (int i0 = 0; i0 < min(rounds, kHeld / kEvictStep); i0 += 4) {
         float4 w[4];
         int entry[4];
@@ -87,7 +98,11 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = (i0 + i) * kEvictStep + kPerThread * tid;
-            if (j < kHeld) *reinterpret_cast<uint4*>(&lds.keys[j]) = keys_of(j, w[i], entry[i]);
+            if (j < kHeld) {                    // uniform
+                const uint4 k4 = keys_of(j, w[i], entry[i]);
+                *reinterpret_cast<uint4*>(&lds.keys[j]) = k4;
+                count_keys(k4, 0, 21, 11, 0);
+            }
         }
     }
     // tokens above the threshold and equal to it: what is still to be found is the wanted-th largest of the keys with this prefix
@@ -96,17 +111,11 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
-        __syncthreads();
-        for (int i = 0; i < rounds; ++i) {
-            const uint4 k4 = keys_at(i * kEvictStep + kPerThread * tid);
-            const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-            for (int e = 0; e < kPerThread; ++e) {
-                const bool active = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
-                count_digit(lds.hist, (int)(key[e] >> shift) & ((1 << bits) - 1), active, lane);
-            }
+        if (pass > 0) {
+            for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
+            __syncthreads();
         }
+        for (int i = pass == 0 ? kHeld / kEvictStep : 0; i < rounds; ++i) count_keys(keys_at(i * kEvictStep + kPerThread * tid), pass, shift, bits, prefix);
         __syncthreads();
         // counts from the highest digit down: thread t has digits 2047 - 2 t and 2046 - 2 t
         const int high = lds.hist[kDigits - 1 - 2 * tid], low = lds.hist[kDigits - 2 - 2 * tid];
@@ -160,11 +169,14 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         equals += lds.sums[1][w];
     }
     to_wave += min(equals, ties);
+    float4 next = weights_at(begin + kPerThread * lane);        // a round early
     for (int j0 = begin; j0 < end; j0 += 64 * kPerThread) {
         const int j = j0 + kPerThread * lane;
         const uint4 k4 = keys_at(min(j, last4));
         const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
-        const float4 w4 = weights_at(j);
+        const float4 w4 = next;
+        next = weights_at(j + 64 * kPerThread);
+        asm volatile("" ::: "memory");          // here, not where it is used
         const float w[kPerThread] = {w4.x, w4.y, w4.z, w4.w};
         int x = 0, y = 0;
         if (j < end) of_thread(k4, x, y);
