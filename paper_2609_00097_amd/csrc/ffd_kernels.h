@@ -271,7 +271,6 @@ struct ChunkAttendArgs : ChunkArgs {
     uint16_t* out;              // bf16 [T, Hq, 128]
     float* lse;                 // [T, Hq] or null
     int rows_above, rows_upto, slots;
-    int min_share;              // few rows: fewest units of a workgroup
     int unit_shift;             // few rows: work is counted in 2^unit_shift blocks, so that its sum fits 31 bits
 };
 struct ChunkMergeArgs {

@@ -183,12 +183,12 @@ __device__ __forceinline__ void write_record(const ChunkAttendArgs& a, const Chu
 }
 
 // Units 0 .. all - 1 of work in equal shares (they differ by one unit at most) of consecutive units, as many as there are
-// workgroups, or fewer, so that each has `least` units. Products below 2^52.
+// workgroups. Products below 2^52.
 struct Shares {
     int all, count;
     double r_all, r_count;
-    __device__ __forceinline__ Shares(int units, int slots, int least)
-        : all(units), count(min(slots, max(units / least, 1))), r_all(reciprocal((double)max(units, 1))), r_count(reciprocal((double)count)) {}
+    __device__ __forceinline__ Shares(int units, int slots)
+        : all(units), count(min(slots, max(units, 1))), r_all(reciprocal((double)max(units, 1))), r_count(reciprocal((double)count)) {}
     __device__ __forceinline__ int begin(int w) const {
         return __builtin_amdgcn_readfirstlane(w >= count ? all : (int)floor_div((long long)w * all, count, r_count));
     }

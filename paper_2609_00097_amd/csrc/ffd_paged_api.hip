@@ -103,9 +103,11 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows
 // (hardly more new tokens than sequences), or has little work: rows times tokens of the capacity per CU.
 constexpr int kFewRows = 32;
 constexpr long long kLittleWork = 24 << 10;
-// Blocks of a workgroup of the few-row kernel at least: 1 / 2 / 4, whole calls, eight heads, bf16: one token on 4K 12.7 / 12.6 / 14.2 us,
-// on 8K 18.4 / 14.6 / 15.5, 16 on 4K 28.4 / 20.6 / 19.9, 4 on 2K in eight sequences 23.3 / 23.0 / 20.6.
-constexpr int kMinShare = 2;
+// Tiles of the kernel of few rows: 32 rows, so that a tile's tokens are read once for them; 16 where the batch has hardly more in a
+// sequence, and where that leaves no more than one workgroup of two blocks for each CU. 16 / 32, whole calls, four heads per KV head:
+// 8 tokens on 300 11.9 / 15.8 us, 16 on 1K 13.0 / 16.8, 8 on 4K 15.0 / 18.0 (256 such pairs), 16 on 4K 21.9 / 19.2 (512), 8 on 32K
+// 53 / 39.
+bool may_be_large(int B, int T, int Hq, int Hkv) { return (long long)T * (Hq / Hkv) > kFewRows && T > 2LL * B; }
 struct ChunkLaunches {
     bool few, large;
     ChunkKernel few_kernel, large_kernel;
@@ -114,9 +116,10 @@ struct ChunkLaunches {
 ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv, long long Lcap, bool i8) {
     ChunkLaunches p;
     const long long rows = (long long)T * (Hq / Hkv);
-    p.large = rows > kFewRows && T > 2LL * B && rows * Lcap * Hkv > kLittleWork * device_cus();
+    p.large = may_be_large(B, T, Hq, Hkv) && rows * Lcap * Hkv > kLittleWork * device_cus();
     p.few = B > 1 || !p.large;
-    const int tile = rows <= 16LL * B || p.large ? 16 : 32;
+    const long long pairs = (rows + 15LL * std::min(B, T)) / 16 * Hkv * ((Lcap + 2 * kRound - 1) / (2 * kRound));
+    const int tile = rows <= 16LL * B || p.large || pairs <= device_cus() ? 16 : 32;
     p.few_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 && i8 ? 3 : 2);
     p.large_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);
     p.large_off = p.few ? p.few_kernel.bytes() : 0;
@@ -125,10 +128,8 @@ ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv, long long Lcap, bool
 }
 // Enough for any capacity and form of the cache.
 size_t chunk_workspace(int B, int T, int Hq, int Hkv) {
-    size_t bytes = 0;
-    for (const long long Lcap : {0, kMaxCapacity})
-        for (const bool i8 : {false, true}) bytes = std::max(bytes, chunk_launches(B, T, Hq, Hkv, Lcap, i8).total);
-    return bytes;
+    const size_t few = std::max(chunk_kernel(B, T, Hq, Hkv, 0, 16, 0, 0, 3).bytes(), chunk_kernel(B, T, Hq, Hkv, 0, 32, 0, 0, 2).bytes());
+    return few + (may_be_large(B, T, Hq, Hkv) ? chunk_kernel(B, T, Hq, Hkv, 0, kChunkTileRows, 0, 0, 1).bytes() : 0);
 }
 
 template <int CT, bool I8>
@@ -240,7 +241,7 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
     int sets = 0, wgs = 0;
     auto prepare = [&](const ChunkKernel& k, uint8_t* ws) {
         a.parts = k.parts(ws);
-        a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.unit_shift = k.unit_shift, a.min_share = kMinShare;
+        a.rows_above = k.rows_above, a.rows_upto = k.rows_upto, a.slots = k.slots, a.unit_shift = k.unit_shift;
         m.parts[sets++] = a.parts;
         if (sets == 1) m.wgs = k.merge_wgs();
         wgs += k.merge_wgs();

@@ -185,10 +185,14 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
         there[0] = next_there[0];
         there[1] = next_there[1];
         t0 = t1;
-        vt.load_halves(a.pages.kv, row, n, g);
-        // The compiler would move these loads to their use in the next turn (none after the last one): 72 us for 32 sequences of
-        // 500 to 8K tokens in 8 bits, 58 so.
-        asm volatile("" ::: "memory");
+        // The next values are asked for here, or behind the products where that would spill (8 tokens on 32K 45 us with spills, 39
+        // so; 32 sequences of 8K in 8 bits 114 and 109), and not, where the compiler would have them, at their use in the next turn
+        // (of which there is none after the last one).
+        constexpr bool kEarly = CT == 1 && !I8;
+        if constexpr (kEarly) {
+            vt.load_halves(a.pages.kv, row, n, g);
+            asm volatile("" ::: "memory");
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -197,6 +201,10 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int c = 0; c < CT; ++c) st.o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], lo[c], st.o[c][i], 0, 0, 0);
+        if constexpr (!kEarly) {
+            vt.load_halves(a.pages.kv, row, n, g);
+            asm volatile("" ::: "memory");
+        }
     }
 }
 
@@ -214,15 +222,19 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
     const int g = lane >> 4, n = lane & 15, wg = blockIdx.x;
     const int gs = __builtin_ctz(a.G), step = kRows >> gs;
     ChunkPlan<kRows, kRowsShift> plan;
-    auto units = [&]() { return (plan.blocks + (1 << a.unit_shift) - 1) >> a.unit_shift; };      // of a tile
+    auto units = [&](int shift) { return (plan.blocks + (1 << shift) - 1) >> shift; };           // of a tile
     // a tile without blocks is one unit, for its empty rows to be written
-    auto work = [&]() { return plan.tiles * max(units(), 1) * a.Hkv; };
-    int all = 0;
+    auto work = [&](int shift) { return plan.tiles * max(units(shift), 1) * a.Hkv; };
+    int all = 0, pairs = 0;
     for (int b0 = (a.B - 1) & ~63; b0 >= 0; b0 -= 64) {         // backwards, to end at the first ones
         plan.load(a, b0, lane);
-        all += __builtin_amdgcn_readlane(wave_inclusive_scan(work()), 63);
+        all += __builtin_amdgcn_readlane(wave_inclusive_scan(work(a.unit_shift)), 63);
+        pairs += __builtin_amdgcn_readlane(wave_inclusive_scan(work(a.unit_shift + 1)), 63);
     }
-    const Shares shares(all, a.slots, a.min_share);
+    // Where there is a workgroup for every two blocks of a tile, it takes just these.
+    const int shift = pairs <= a.slots ? a.unit_shift + 1 : a.unit_shift;
+    if (shift != a.unit_shift) all = pairs;
+    const Shares shares(all, a.slots);
     const int begin = shares.begin(wg), end = shares.begin(wg + 1);
     int u = begin;
     bool begun = false;                         // a tile that another workgroup ends
@@ -231,13 +243,13 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
         int tile_units = 1, at = 0, before = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             if (b0 > 0 || u != begin) plan.load(a, b0, lane);          // (kept, it would cost the loop registers)
-            const int mine = work(), incl = wave_inclusive_scan(mine), first = before + incl - mine;
+            const int mine = work(shift), incl = wave_inclusive_scan(mine), first = before + incl - mine;
             const uint64_t hit = __ballot(u >= first && u < first + mine);
             if (hit != 0) {
                 const int src = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(hit));
                 it.b = b0 + src;
                 plan.give(it.seq, src);
-                tile_units = max(__builtin_amdgcn_readlane(units(), src), 1);
+                tile_units = max(__builtin_amdgcn_readlane(units(shift), src), 1);
                 at = __builtin_amdgcn_readfirstlane(u) - __builtin_amdgcn_readlane(first, src);
                 break;
             }
@@ -268,7 +280,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
         rows.low = place + tok0;
         rows.high = place + tok1;
         const ChunkSpan span = chunk_span<kRowsShift>(a, it.seq, tok0, tok1);
-        const int first = (int)min((long long)span.count, (long long)from << a.unit_shift), last = (int)min((long long)span.count, (long long)to << a.unit_shift);
+        const int first = (int)min((long long)span.count, (long long)from << shift), last = (int)min((long long)span.count, (long long)to << shift);
         RowState<CT> st;
         for (bool finite = false;; finite = true) {
             st.clear();

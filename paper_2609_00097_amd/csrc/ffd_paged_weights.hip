@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
         ChunkSeq s;
         all += __builtin_amdgcn_readlane(wave_inclusive_scan(load(b0, s)), 63);
     }
-    const Shares shares(all, a.slots, 1);
+    const Shares shares(all, a.slots);
     const int begin = shares.begin(blockIdx.x), stop = shares.begin(blockIdx.x + 1);
     for (int u = begin; u < stop;) {            // uniform
         if (u != begin) __syncthreads();            // the rows in LDS are done with
