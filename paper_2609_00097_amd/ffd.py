@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 
 import torch
 
@@ -103,13 +104,13 @@ def lib() -> ctypes.CDLL:
     so.ffd_shared_prefix_decode_attention.argtypes = [P, KV, P, I, KV, P, I, I, I, I, I, I, F, P, P, P, SZ, P]
     so.ffd_shared_prefix_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
     so.ffd_shared_prefix_workspace_bytes.restype = SZ
-    PAGED, RULES = ctypes.POINTER(PagedCache), ctypes.POINTER(ScoreRules)
-    so.ffd_write_paged.argtypes = [P, P, P, STRIDES, STRIDES, STRIDES, P, ctypes.POINTER(Rotation), PAGED, P, P, I, I, I, I, I, P]
-    so.ffd_paged_attention.argtypes = [P, PAGED, P, P, RULES, I, I, I, I, I, F, P, P, P, SZ, P]
+    # (structures as addresses: the binding packs them, others pass them by ctypes.byref)
+    so.ffd_write_paged.argtypes = [P, P, P, P, P, P, P, P, P, P, P, I, I, I, I, I, P]
+    so.ffd_paged_attention.argtypes = [P, P, P, P, P, I, I, I, I, I, F, P, P, P, SZ, P]
     so.ffd_paged_workspace_bytes.argtypes = [I, I, I, I, I]
     so.ffd_paged_workspace_bytes.restype = SZ
-    so.ffd_paged_attention_weights.argtypes = [P, PAGED, P, P, RULES, P, I, I, I, I, I, F, I, P, P, P]
-    so.ffd_evict_paged.argtypes = [PAGED, P, I, P, P, I, I, I, I, I, P, P, P, P]
+    so.ffd_paged_attention_weights.argtypes = [P, P, P, P, P, P, I, I, I, I, I, F, I, P, P, P]
+    so.ffd_evict_paged.argtypes = [P, P, I, P, P, I, I, I, I, I, P, P, P, P]
     so.ffd_resolve_splits.argtypes = [I, I, I, I]
     so.ffd_fused_splits.argtypes = [I, I, I, I]
     so.ffd_select_kernels.argtypes = [I, I, I, I]
@@ -614,15 +615,39 @@ def empty_paged(num_pages: int, Hkv: int, page: int, device="cuda"):
     return tuple(torch.empty((num_pages, Hkv, page, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in range(2))
 
 
+# The structures of these calls, packed as C lays them out: cheaper than ctypes' own, like the single expressions that the
+# usual tensors pass (see _need).
+_pack_paged = struct.Struct("@5P3i0P").pack
+_pack_rotation = struct.Struct("@2Pf0PP3i0PP").pack
+_pack_rules = struct.Struct("@fi2P").pack
+_pack_strides = struct.Struct("@2q").pack
+
+
+def _address(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
 def _paged(cache, page_table, device):
     """(``ffd_paged``, B, Hkv, page, max_pages) of a cache whose tensors are as they have to be."""
+    try:
+        if len(cache) == 2:
+            k, v = cache
+            num_pages, Hkv, page, D = shape = k.shape
+            B, max_pages = page_table.shape
+            if (k.dtype is torch.bfloat16 and v.dtype is torch.bfloat16 and page_table.dtype is torch.int32 and v.shape == shape and D == HEAD_DIM
+                    and k.get_device() == v.get_device() == page_table.get_device() == device >= 0
+                    and k.is_contiguous() and v.is_contiguous() and page_table.is_contiguous()):
+                return _pack_paged(k.data_ptr(), 0, v.data_ptr(), 0, page_table.data_ptr(), num_pages, page, max_pages), B, Hkv, page, max_pages
+    except (AttributeError, TypeError, ValueError):
+        pass                                             # named below
     num_pages, Hkv, page = _cache_dims(cache, "cache", True)
     kv = _kv_cache(cache, "cache", device, (num_pages, Hkv, page, HEAD_DIM))
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be [B, max_pages]")
     B, max_pages = page_table.shape
     _need_on(device, page_table, "page_table", torch.int32, (B, max_pages))
-    return PagedCache(kv, page_table.data_ptr(), num_pages, page, max_pages), B, Hkv, page, max_pages
+    return (_pack_paged(kv.k or 0, kv.k_absmax or 0, kv.v or 0, kv.v_absmax or 0, page_table.data_ptr(), num_pages, page, max_pages),
+            B, Hkv, page, max_pages)
 
 
 def _need_int(x, name):
@@ -631,29 +656,36 @@ def _need_int(x, name):
 
 
 def _ragged(q_start, seq_lens, device, B):
+    try:
+        if (q_start.dtype is torch.int32 and seq_lens.dtype is torch.int32 and q_start.shape == (B + 1,) and seq_lens.shape == (B,)
+                and q_start.get_device() == seq_lens.get_device() == device and q_start.is_contiguous() and seq_lens.is_contiguous()):
+            return
+    except AttributeError:
+        pass
     _need_on(device, q_start, "q_start", torch.int32, (B + 1,))
     _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
 
 
-_Strides2 = ctypes.c_int64 * 2
-
-
 def _strided_rows(t, name, device, shape):
     """The two strides, in elements, of ``t`` as [T, heads, 128]; None where it is contiguous."""
-    if (type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device >= 0
-            and t.is_contiguous()):
+    try:
+        usual = t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device >= 0
+    except AttributeError:
+        usual = False
+    if not usual:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+        if t.dtype != torch.bfloat16 or t.get_device() != device:
+            raise ValueError(f"{name} must be torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.is_contiguous():
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype != torch.bfloat16 or t.get_device() != device:
-        raise ValueError(f"{name} must be torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
     strides = t.stride()
     if strides[2] != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
     # the stride of a dimension of one is never used, and may be anything
-    return _Strides2(strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0)
+    return _pack_strides(strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0)
 
 
 def write_paged(q, k, v, cache, page_table, q_start, seq_lens, *, q_weight=None, k_weight=None, eps: float = 1e-6, rope=None,
@@ -697,9 +729,9 @@ def write_paged(q, k, v, cache, page_table, q_start, seq_lens, *, q_weight=None,
     for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
         if weight is not None:
             _need_on(device, weight, name, torch.bfloat16, (HEAD_DIM,))
-    rotation = Rotation(_ptr(q_weight), _ptr(k_weight), eps, _ptr(rope), rows, dims, bool(interleaved), _ptr(positions))
+    rotation = _pack_rotation(_address(q_weight), _address(k_weight), eps, _address(rope), rows, dims, bool(interleaved), _address(positions))
     _launch("ffd_write_paged", lib().ffd_write_paged, device, _ptr(q), k.data_ptr(), v.data_ptr(), q_strides, k_strides, v_strides,
-            _ptr(out), ctypes.byref(rotation), ctypes.byref(paged), q_start.data_ptr(), seq_lens.data_ptr(), B, T, Hq, Hkv,
+            _ptr(out), rotation, paged, q_start.data_ptr(), seq_lens.data_ptr(), B, T, Hq, Hkv,
             HEAD_DIM)
     return out
 
@@ -729,7 +761,7 @@ def _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, s
     _need_int(window, "window")
     rules = None
     if softcap or window or slopes is not None or prefix_lens is not None:
-        rules = ctypes.byref(ScoreRules(softcap, window, _ptr(slopes), _ptr(prefix_lens)))
+        rules = _pack_rules(softcap, window, _address(slopes), _address(prefix_lens))
     return device, paged, rules, B, T, Hq, Hkv, page * max_pages
 
 
@@ -753,7 +785,7 @@ def paged_attention(q, cache, page_table, q_start, seq_lens, *, softmax_scale: f
         lse = q.new_empty((T, Hq), dtype=torch.float32)
     if workspace is None:
         workspace = new_paged_workspace(B, T, Hq, Hkv, q.device)
-    _launch("ffd_paged_attention", lib().ffd_paged_attention, device, q.data_ptr(), ctypes.byref(paged), q_start.data_ptr(),
+    _launch("ffd_paged_attention", lib().ffd_paged_attention, device, q.data_ptr(), paged, q_start.data_ptr(),
             seq_lens.data_ptr(), rules, B, T, Hq, Hkv, HEAD_DIM, softmax_scale, out.data_ptr(), _ptr(lse), workspace.data_ptr(),
             _need_workspace(workspace, device))
     return out, lse
@@ -776,7 +808,7 @@ def paged_attention_weights(q, cache, page_table, q_start, seq_lens, lse, *, sof
         out = q.new_zeros((B, Hkv, Lcap), dtype=torch.float32)
     else:
         _need_on(device, out, "out", torch.float32, (B, Hkv, Lcap))
-    _launch("ffd_paged_attention_weights", lib().ffd_paged_attention_weights, device, _ptr(q), ctypes.byref(paged),
+    _launch("ffd_paged_attention_weights", lib().ffd_paged_attention_weights, device, _ptr(q), paged,
             q_start.data_ptr(), seq_lens.data_ptr(), rules, _ptr(lse), B, T, Hq, Hkv, HEAD_DIM, softmax_scale, last, _ptr(previous),
             out.data_ptr())
     return out
@@ -813,7 +845,7 @@ def evict_paged(cache, page_table, new_table, seq_lens, weights, budget: int, *,
         new_weights = weights.new_zeros((B, Hkv, new_max_pages * page))
     else:
         _need_on(device, new_weights, "new_weights", torch.float32, (B, Hkv, new_max_pages * page))
-    _launch("ffd_evict_paged", lib().ffd_evict_paged, device, ctypes.byref(paged), new_table.data_ptr(), new_max_pages,
+    _launch("ffd_evict_paged", lib().ffd_evict_paged, device, paged, new_table.data_ptr(), new_max_pages,
             seq_lens.data_ptr(), weights.data_ptr(), B, Hkv, HEAD_DIM, budget, recent, new_lens.data_ptr(), kept.data_ptr(),
             new_weights.data_ptr())
     return kept, new_lens, new_weights

@@ -182,3 +182,12 @@ def test_integers_of_more_than_32_bits():
         with pytest.raises(ValueError, match="window must fit 32 bits"):
             ffd._need_int(x, "window")
     ffd._need_int((1 << 31) - 1, "window")
+
+
+def test_packed_structures():
+    """What the binding packs is what ctypes lays out."""
+    from paper_2609_00097_amd import ffd
+    assert ffd._pack_paged(1, 2, 3, 4, 5, 6, 7, 8) == bytes(ffd.PagedCache(ffd.KvCache(1, 2, 3, 4), 5, 6, 7, 8))
+    assert ffd._pack_rotation(1, 2, 0.5, 3, 4, 5, True, 6) == bytes(ffd.Rotation(1, 2, 0.5, 3, 4, 5, 1, 6))
+    assert ffd._pack_rules(20.0, 3, 4, 5) == bytes(ffd.ScoreRules(20.0, 3, 4, 5))
+    assert ffd._pack_strides(1 << 40, 8) == bytes((ctypes.c_int64 * 2)(1 << 40, 8))
