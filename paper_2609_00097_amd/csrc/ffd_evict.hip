@@ -31,9 +31,9 @@ constexpr uint32_t kLatest = 0xffffffffu;
 
 struct EvictLds {
     alignas(16) uint32_t keys[kHeld];
-    int hist[kDigits];
-    int sums[2][kEvictWaves];
-    int digit, above;
+    int hist[3][kDigits];                       // of each pass
+    int sums[3][kEvictWaves];
+    int digit[3], above[3];
 };
 
 // hist[digit] += 1 for the active lanes, those of one digit by one atomic where the first lane's digit is common.
@@ -76,33 +76,43 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
     };
     const int rounds = (L + kEvictStep - 1) / kEvictStep;
     // The digits of the first pass are counted as the keys are made.
-    for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
+    for (int i = tid; i < 3 * kDigits; i += kEvictThreads) lds.hist[0][i] = 0;
     __syncthreads();
     auto count_keys = [&](const uint4& k4, int pass, int shift, int bits, uint32_t prefix) {
         const uint32_t key[kPerThread] = {k4.x, k4.y, k4.z, k4.w};
 #pragma unroll
         for (int e = 0; e < kPerThread; ++e) {
             const bool active = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
-            count_digit(lds.hist, (int)(key[e] >> shift) & ((1 << bits) - 1), active, lane);
+            count_digit(lds.hist[pass], (int)(key[e] >> shift) & ((1 << bits) - 1), active, lane);
         }
     };
-    for (int i0 = 0; i0 < min(rounds, kHeld / kEvictStep); i0 += 4) {
-        float4 w[4];
-        int entry[4];
+    // rounds of tokens, four asked for together while the four before are counted
+    constexpr int U = 4;
+    float4 w[U];
+    int entry[U];
+    auto ask = [&](int i0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {           // asked for together
+        for (int i = 0; i < U; ++i) {
             const int j = (i0 + i) * kEvictStep + kPerThread * tid;
             w[i] = weights_at(j);
             entry[i] = page_entry(a.from, b, min(j, last4));
         }
+    };
+    const int held = min(rounds, kHeld / kEvictStep);
+    ask(0);
+    for (int i0 = 0; i0 < held; i0 += U) {
+        uint4 k4[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = (i0 + i) * kEvictStep + kPerThread * tid;
-            if (j < kHeld) {                    // uniform
-                const uint4 k4 = keys_of(j, w[i], entry[i]);
-                *reinterpret_cast<uint4*>(&lds.keys[j]) = k4;
-                count_keys(k4, 0, 21, 11, 0);
-            }
+        for (int i = 0; i < U; ++i) k4[i] = keys_of((i0 + i) * kEvictStep + kPerThread * tid, w[i], entry[i]);
+        if (i0 + U < held) {                    // uniform
+            ask(i0 + U);
+            asm volatile("" ::: "memory");      // here, not where they are used
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (i0 + i >= held) break;          // uniform
+            *reinterpret_cast<uint4*>(&lds.keys[(i0 + i) * kEvictStep + kPerThread * tid]) = k4[i];
+            count_keys(k4[i], 0, 21, 11, 0);
         }
     }
     // tokens above the threshold and equal to it: what is still to be found is the wanted-th largest of the keys with this prefix
@@ -111,29 +121,24 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        if (pass > 0) {
-            for (int i = tid; i < kDigits; i += kEvictThreads) lds.hist[i] = 0;
-            __syncthreads();
-        }
         for (int i = pass == 0 ? kHeld / kEvictStep : 0; i < rounds; ++i) count_keys(keys_at(i * kEvictStep + kPerThread * tid), pass, shift, bits, prefix);
         __syncthreads();
         // counts from the highest digit down: thread t has digits 2047 - 2 t and 2046 - 2 t
-        const int high = lds.hist[kDigits - 1 - 2 * tid], low = lds.hist[kDigits - 2 - 2 * tid];
+        const int high = lds.hist[pass][kDigits - 1 - 2 * tid], low = lds.hist[pass][kDigits - 2 - 2 * tid];
         int total;
-        const int before = wg_exclusive_scan<kEvictWaves>(high + low, lds.sums[pass & 1], &total);
+        const int before = wg_exclusive_scan<kEvictWaves>(high + low, lds.sums[pass], &total);
         if (pass == 0) there = total;
         if (there <= a.budget) break;           // uniform: all are kept
         if (before < wanted && wanted <= before + high) {
-            lds.digit = kDigits - 1 - 2 * tid;
-            lds.above = before;
+            lds.digit[pass] = kDigits - 1 - 2 * tid;
+            lds.above[pass] = before;
         } else if (before + high < wanted && wanted <= before + high + low) {
-            lds.digit = kDigits - 2 - 2 * tid;
-            lds.above = before + high;
+            lds.digit[pass] = kDigits - 2 - 2 * tid;
+            lds.above[pass] = before + high;
         }
         __syncthreads();
-        prefix = prefix << bits | (uint32_t)lds.digit;
-        wanted -= lds.above;
-        __syncthreads();
+        prefix = prefix << bits | (uint32_t)lds.digit[pass];
+        wanted -= lds.above[pass];
     }
     const int count = min(there, a.budget);
     const uint32_t threshold = there <= a.budget ? 0 : prefix;
