@@ -412,7 +412,7 @@ int ffd_write_paged(const void* q, const void* k, const void* v, const int64_t* 
  * and sees it if j < min(seq_lens[b], Lcap), its page is there, and
  *   (j <= i and (window == 0 or i - j < window))  or  j < prefix_lens[b].
  * Distances are those of places in the cache. After an eviction, which closes gaps, they are no longer those of the text.
- *   softcap       0 .. 1024 (above: FFD_ERR_UNSUPPORTED), 0: none;  window  >= 0, 0: none
+ *   softcap       >= 0, 0: none;  window  >= 0, 0: none
  *   slopes        fp32 [Hq] (device), or NULL;  prefix_lens  int32 [B] (device), or NULL
  */
 typedef struct ffd_score_rules {

@@ -248,6 +248,7 @@ struct ChunkArgs {
     int B, T, Hq, Hkv, G, Lcap;
     int window;                 // 0: none
     float cap;                  // 0: none
+    float cap_near[5];          // cap tanh(z / cap) of small scores, see ScoreRule
     float scale;
 };
 

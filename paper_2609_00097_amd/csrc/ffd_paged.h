@@ -198,24 +198,39 @@ struct Shares {
     }
 };
 
-// What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). tanh(x) =
-// 1 - 2 / (1 + e^2x): no overflow, infinities and NaN as they are, at most 2^-20 of the cap off. An 8-bit key's product is
+// What a product s = q.k becomes, in powers of two: z2 = log2(e) (cap tanh(scale s / cap) - slope |i - j|). An 8-bit key's product is
 // multiplied by its M before and by 1 / 127 within `scale`.
+//
+// With y = scale s / cap and x = 2 log2(e) y: tanh(y) = 1 - 2 / (1 + 2^x) has no overflow and keeps infinities and NaN, but is up to
+// 2^-22 off, of scores far below the cap as of others. So up to |y| = 1/2 it is y times a polynomial of degree four in y^2, the
+// interpolation of tanh(y) / y at the Chebyshev points of y^2 in [0, 1/4] (1.4e-8 off), whose coefficients come in terms of x and with
+// the cap multiplied in (near_caps).
 struct ScoreRule {
     float zscale;               // without a cap: scale log2(e); with one: 2 scale log2(e) / cap
     float cap2;                 // cap log2(e), or 0
     float slope2;               // this lane's row's slope log2(e)
+    float near[5];
 };
+constexpr float kNearCap = 1.4426950408889634f;                         // x of y = 1/2
+constexpr double kTanhNear[5] = {0.9999999867573891, -0.33333067944418876, 0.13324750504729285, -0.05298423882487847, 0.017131344424267444};
 __device__ __forceinline__ ScoreRule score_rule(const ChunkArgs& a, bool i8, int head) {
     ScoreRule r;
     const float scale = i8 ? a.scale / 127.f : a.scale;
     r.zscale = a.cap > 0.f ? fminf(scale * 2.f * kLog2e / a.cap, FLT_MAX) : scale * kLog2e;
     r.cap2 = a.cap * kLog2e;
     r.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) r.near[i] = a.cap_near[i];
     return r;
 }
-__device__ __forceinline__ float capped(float x, float cap2) {       // x = zscale s
-    return cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_hw(x)), 1.f);
+// x = zscale s; of scores up to half of the cap, factor of x
+__device__ __forceinline__ float near_cap(float x, const ScoreRule& r) {
+    const float u = x * x;
+    return fmaf(u, fmaf(u, fmaf(u, fmaf(u, r.near[4], r.near[3]), r.near[2]), r.near[1]), r.near[0]);
+}
+__device__ __forceinline__ float capped(float x, const ScoreRule& r) {
+    const float far = r.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_hw(x)), 1.f);
+    return fabsf(x) <= kNearCap ? x * near_cap(x, r) : far;
 }
 
 }  // namespace ffd

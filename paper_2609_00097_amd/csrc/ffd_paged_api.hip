@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kMaxCapacity = 1 << 28;
 constexpr int kMaxTokens = 1 << 24;
-constexpr float kMaxCap = 1024.f;               // a capped score is off by at most 2^-20 of the cap: 2^-10 here, half as much as a bf16 probability
+constexpr float kNoCapFrom = 0x1p100f;          // a cap that no score comes near: none, and nothing under- or overflows
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -50,7 +50,7 @@ int check_rules(const ffd_score_rules* r) {
     if (!r) return FFD_OK;
     if (!(r->softcap >= 0.f) || std::isinf(r->softcap) || r->window < 0) return FFD_ERR_INVALID_ARGUMENT;
     if (!aligned4(r->slopes) || !aligned4(r->prefix_lens)) return FFD_ERR_INVALID_ARGUMENT;
-    return r->softcap > kMaxCap ? FFD_ERR_UNSUPPORTED : FFD_OK;
+    return FFD_OK;
 }
 
 ChunkArgs chunk_args(const void* q, const ffd_paged& c, const int32_t* q_start, const int32_t* seq_lens,
@@ -67,7 +67,9 @@ ChunkArgs chunk_args(const void* q, const ffd_paged& c, const int32_t* q_start, 
         a.slopes = rules->slopes;
         a.window = std::min(rules->window, kMaxLen);
         if (rules->window > kMaxLen) a.window = 0;              // as wide as no length is
-        a.cap = rules->softcap;
+        a.cap = rules->softcap < kNoCapFrom ? rules->softcap : 0.f;
+        double x = 1.0;                         // tanh(y) = y P(y^2) with y = x ln(2) / 2, times cap log2(e)
+        for (int i = 0; i < 5; ++i, x *= M_LN2 * M_LN2 / 4) a.cap_near[i] = (float)(a.cap / 2.0 * x * kTanhNear[i]);
     }
     return a;
 }

@@ -59,6 +59,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds_at, const uint8_t* base
 __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 template <int N> using Int = std::integral_constant<int, N>;
+enum : int { kNoCap, kNearOnly, kAnyCap };       // scores that are capped with the exponential: none, all of them small ones, any
 
 }  // namespace
 
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     // Sub-tile t's products x on their way to scores: the largest of the row (in powers of two), whether any is seen; rules and
     // masks are applied where there are any, else x stays the product (`raw`), to be scaled, and capped, with the exponential.
     float top = -INFINITY;
-    bool raw = true;
+    bool raw = true, near = false;              // near: all of the wave's products are of scores up to half of the cap
     auto rules_and_masks = [&](int t, v16f& x) {
         asm volatile("");                       // a branch around all this, not selections after it
         const int t0 = token0(t >> 1) + 32 * (t & 1);
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
             float z = x[i];
             if constexpr (RULED) {
                 z *= rule.zscale;
-                if (rule.cap2 != 0.f) z = capped(z, rule.cap2);
+                if (rule.cap2 != 0.f) z = capped(z, rule);
                 z = fmaf(-rule.slope2, fabsf((float)rel - (float)k), z);
             }
             const uint32_t seen = (uint32_t)(((k <= high) & (k > low)) | (k < prefix)) & (there >> (i >> 3));
@@ -236,9 +237,9 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     // First half of a step: the probabilities of a sub-tile, beside them the scores of the next one, which is half `half` of its tile.
     auto exponentials = [&](v16f& now, v16f& next, v8bf (&probs)[2], auto half, auto capping) {
         constexpr int H = decltype(half)::value;
-        constexpr bool CAP = decltype(capping)::value;
-        const float scale = RULED && !CAP && !raw ? 1.f : rule.zscale;
-        const float ref = m == -INFINITY ? 0.f : m, shift = rule.cap2 - ref;
+        constexpr int CAP = decltype(capping)::value;
+        const float scale = RULED && CAP == kNoCap && !raw ? 1.f : rule.zscale;
+        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < 16; ++i) next[i] = 0.f;
         // With each product the arguments of pair j + 2, the exponentials of pair j, sum and rounding of pair j - 1, so that none
@@ -247,8 +248,10 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         auto arguments = [&](int j) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if constexpr (CAP) x[j % 3][i] = fmaf(-2.f * rule.cap2, __builtin_amdgcn_rcpf(1.f + exp2_hw(now[2 * j + i] * rule.zscale)), shift);
-                else x[j % 3][i] = fmaf(now[2 * j + i], scale, -ref);
+                const float z = now[2 * j + i];
+                if constexpr (CAP == kNearOnly) x[j % 3][i] = fmaf(z * scale, near_cap(z * scale, rule), -ref);
+                else if constexpr (CAP == kAnyCap) x[j % 3][i] = capped(z * scale, rule) - ref;
+                else x[j % 3][i] = fmaf(z, scale, -ref);
             }
         };
         auto round_pair = [&](int j) {
@@ -278,6 +281,14 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         l += sum[0] + sum[1];
         asm volatile("" : "+v"(l), "+v"(rounded));        // here, not where they are needed
     };
+    auto probabilities = [&](v16f& now, v16f& next, v8bf (&probs)[2], auto half) {
+        if (RULED && raw && rule.cap2 != 0.f) {
+            if (near) exponentials(now, next, probs, half, Int<kNearOnly>());
+            else exponentials(now, next, probs, half, Int<kAnyCap>());
+        } else {
+            exponentials(now, next, probs, half, Int<kNoCap>());
+        }
+    };
     // Second half: the products of the sub-tile before, beside them the largest of the next one, t; then the first operands
     // of the step to come, from half `half` of its keys' tile.
     auto second = [&](int t, v16f& next, v8bf (&before)[2], auto half, auto products) {
@@ -286,7 +297,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         const int t0 = token0(t >> 1) + 32 * (t & 1);
         const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
         const bool plain = (there == 3u) & (t0 <= whole_to) & ((t0 > whole_from) | (t0 <= prefix_to)) & !(RULED && a.slopes);
-        float mx[4], up_to = 0.f;
+        float mx[4], abs_mx[4], up_to = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if constexpr (P) {
@@ -300,6 +311,10 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
             for (int i = 0; i < 4; ++i) {
                 if (j == 2) mx[i] = fmaxf(next[4 * i], next[4 * i + 1]);
                 if (j == 3) mx[i] = fmaxf(fmaxf(mx[i], next[4 * i + 2]), next[4 * i + 3]);
+                if constexpr (RULED) {
+                    if (j == 2) abs_mx[i] = fmaxf(fabsf(next[4 * i]), fabsf(next[4 * i + 1]));
+                    if (j == 3) abs_mx[i] = fmaxf(fmaxf(abs_mx[i], fabsf(next[4 * i + 2])), fabsf(next[4 * i + 3]));
+                }
             }
             if (j == 4) mx[0] = fmaxf(fmaxf(mx[0], mx[1]), mx[2]);
             if (j == 5) mx[0] = fmaxf(mx[0], mx[3]);
@@ -308,7 +323,10 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (RULED) {
-            if (rule.cap2 != 0.f) up_to = capped(up_to, rule.cap2);
+            if (rule.cap2 != 0.f) {
+                up_to = capped(up_to, rule);
+                near = __ballot(fmaxf(fmaxf(abs_mx[0], abs_mx[1]), fmaxf(abs_mx[2], abs_mx[3])) * rule.zscale > kNearCap) == 0;
+            }
         }
         top = fmaxf(up_to, -FLT_MAX);           // NaN: of no weight for the reference
         raw = true;
@@ -398,16 +416,14 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
                 second(2 * u, s[0], p[1], kSecond, std::false_type());
                 for (; u < mine_last; ++u) {
                     settle();
-                    if (RULED && raw && rule.cap2 != 0.f) exponentials(s[0], s[1], p[0], kSecond, std::true_type());
-                    else exponentials(s[0], s[1], p[0], kSecond, std::false_type());
+                    probabilities(s[0], s[1], p[0], kSecond);
                     turn(u);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) key_at[j] ^= kTileBytes;
                     second(2 * u + 1, s[1], p[1], kFirst, std::true_type());
                     values_at(now);
                     settle();
-                    if (RULED && raw && rule.cap2 != 0.f) exponentials(s[1], s[0], p[1], kFirst, std::true_type());
-                    else exponentials(s[1], s[0], p[1], kFirst, std::false_type());
+                    probabilities(s[1], s[0], p[1], kFirst);
                     second(2 * u + 2, s[0], p[0], kSecond, std::true_type());
                     rotate();
                 }
@@ -431,12 +447,12 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         if (!__syncthreads_or(x != 0.f)) break;
     }
 
-    const float sum = halves_sum(l), near = halves_sum(rounded);
+    const float sum = halves_sum(l), rounded_sum = halves_sum(rounded);
     const bool any_seen = m != -INFINITY;
     if (!live) return;
     const float ln = m * 0.69314718055994531f;
     if (it.part >= 0) {
-        const float f = any_seen ? sum / near : 1.f;
+        const float f = any_seen ? sum / rounded_sum : 1.f;
         const size_t to = (size_t)it.part * kChunkTileRows + r;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -450,7 +466,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         }
         return;
     }
-    const float inv = any_seen ? 1.f / near : 0.f;
+    const float inv = any_seen ? 1.f / rounded_sum : 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile8_kernel(ChunkAttendAr
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[x][i] = capped(s[x][i], rule.cap2);
+                    for (int i = 0; i < 16; ++i) s[x][i] = capped(s[x][i], rule);
             }
             if (a.slopes) {
                 const float rel = (float)(at - t0 - 4 * h);

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
                         float z = s[i][e >> 2][e & 3];
                         if constexpr (RULED) {
                             z *= km[e];
-                            if (rule.cap2 != 0.f) z = capped(z, rule.cap2);
+                            if (rule.cap2 != 0.f) z = capped(z, rule);
                             z = fmaf(-rule.slope2, fabsf((float)(mine - t0 - value_token(e, g))), z);
                             p[e] = exp2_hw(z - lse2[i]);
                         } else {

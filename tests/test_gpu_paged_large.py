@@ -33,7 +33,7 @@ def test_attention(ffd, lens, new, Hkv, G, page, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-@pytest.mark.parametrize("rule", RULES + [dict(softcap=1024.0), dict(softcap=0.01), dict(window=64, slopes=True), dict(window=257, softcap=30.0)],
+@pytest.mark.parametrize("rule", RULES + [dict(softcap=1024.0), dict(softcap=1e6), dict(softcap=1e36), dict(softcap=0.01), dict(softcap=1e-30), dict(window=64, slopes=True), dict(window=257, softcap=30.0)],
                          ids=lambda r: "_".join(f"{k}{v if v is not True else ''}" for k, v in r.items()))
 @pytest.mark.parametrize("lens,new", [([700], [700]), ([1500, 515, 90, 40], [200, 300, 90, 1])])
 def test_rules(ffd, lens, new, rule, bits):
@@ -142,6 +142,26 @@ def test_captured(ffd):
         run()
         rows = slice(0, sum(new))
         assert torch.equal(got[0][rows], out[rows]) and torch.equal(got[1][rows], lse[rows])
+
+
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("cap", [2.0, 50.0, 1e4])
+def test_small_scores_of_a_cap(ffd, cap, bits, large):
+    """Scores far below the cap keep their relative precision: of a row that sees one token the lse is the score, of which tanh takes
+    2^-24 (polynomial) and six roundings; before them its 128 products have 136, and from there it is made of powers of two and
+    back, two more. Also where the other row of the wave has a score near the cap."""
+    n = 300 if large else 1
+    batch = _batch([n] * 2, [n] * 2, 1, 4, 16, bits, 41) if large else R.Batch([n] * 2, [n] * 2, 1, 4, 16, bits, seed=41)
+    batch.q[0] *= 0.01
+    batch.q[batch.starts[1]] *= 40.0
+    _, lse = _attend(ffd, batch, softcap=cap)
+    for b in range(2):
+        z, worst, _ = batch.scores(b, 0, softcap=cap)
+        got, want = lse[batch.starts[b]].double(), z[0, :, 0]
+        # the first token of each sequence; far from zero of tanh's slope the roundings of the products count less
+        far = 2.0 ** -22 * cap * (want.abs() > 0.45 * cap)
+        assert bool(((got - want).abs() <= 136 * 2.0 ** -24 * worst[0] + 10 * 2.0 ** -24 * want.abs() + far).all()), (got, want)
 
 
 @pytest.mark.parametrize("lens,last", [([3000, 600], 0), ([3000, 600], 150)])

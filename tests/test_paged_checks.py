@@ -162,12 +162,6 @@ def test_binding_checks():
         ffd.paged_attention_weights(None, cache, table, q_start, lens, torch.zeros(3, 4))
 
 
-@pytest.mark.parametrize("call", ["attend", "weights"])
-def test_caps_too_large(so, call):
-    assert CALLS[call](so, rules=_rules(softcap=1025.0)) == 2
-    assert CALLS[call](so, B=0, rules=_rules(softcap=1024.0)) == 0
-
-
 def test_evict_overlaps(so):
     """new_weights on the weights, and one table for both sides."""
     weights, new = 4 * 2 * 8 * 64, 4 * 2 * 8 * 32               # bytes
