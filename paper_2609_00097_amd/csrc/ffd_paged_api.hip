@@ -112,6 +112,7 @@ constexpr long long kLittleWork = 24 << 10;
 bool may_be_large(int B, int T, int Hq, int Hkv) { return (long long)T * (Hq / Hkv) > kFewRows && T > 2LL * B; }
 struct ChunkLaunches {
     bool few, large;
+    bool cut;                   // tiles may be cut, and need the merge
     ChunkKernel few_kernel, large_kernel;
     size_t large_off, total;
 };
@@ -121,6 +122,7 @@ ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv, long long Lcap, bool
     p.large = may_be_large(B, T, Hq, Hkv) && rows * Lcap * Hkv > kLittleWork * device_cus();
     p.few = B > 1 || !p.large;
     const long long pairs = (rows + 15LL * std::min(B, T)) / 16 * Hkv * ((Lcap + 2 * kRound - 1) / (2 * kRound));
+    p.cut = p.large || Lcap > 2 * kRound || (Lcap > kRound && pairs > 2LL * device_cus());      // else a tile is one unit
     const int tile = rows <= 16LL * B || p.large || pairs <= device_cus() ? 16 : 32;
     p.few_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 && i8 ? 3 : 2);
     p.large_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);
@@ -264,6 +266,7 @@ int ffd_paged_attention(const void* q, const ffd_paged* cache, const int32_t* q_
         launch_rows(plan.few_kernel.rows, i8, ruled, dim3((unsigned)plan.few_kernel.grid), stream, a);
         if ((st = launch_status()) != FFD_OK) return st;
     }
+    if (!plan.cut) return FFD_OK;
     hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)wgs), dim3(kThreads), 0, stream, m);
     return launch_status();
 }

@@ -750,8 +750,10 @@ def _chunk_arguments(q, cache, page_table, q_start, seq_lens, softcap, window, s
     """Checks shared by the calls over new tokens' queries; (device, cache, rules, B, T, Hq, Hkv, Lcap)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError(f"q must be [T, Hq, {HEAD_DIM}]")
-    T, Hq, device = q.shape[0], q.shape[1], q.get_device()
-    _need_on(device, q, "q", torch.bfloat16, (T, Hq, HEAD_DIM))
+    T, Hq, D = q.shape
+    device = q.get_device()
+    if not (q.dtype is torch.bfloat16 and D == HEAD_DIM and device >= 0 and q.is_contiguous()):
+        _need_on(device, q, "q", torch.bfloat16, (T, Hq, HEAD_DIM))
     paged, B, Hkv, page, max_pages = _paged(cache, page_table, device)
     _ragged(q_start, seq_lens, device, B)
     if slopes is not None:
@@ -828,11 +830,19 @@ def evict_paged(cache, page_table, new_table, seq_lens, weights, budget: int, *,
     new_max_pages = new_table.shape[1]
     _need_int(budget, "budget")
     _need_int(recent, "recent")
-    _need_on(device, new_table, "new_table", torch.int32, (B, new_max_pages))
+    try:
+        usual = (new_table.dtype is torch.int32 and seq_lens.dtype is torch.int32 and weights.dtype is torch.float32
+                 and new_table.shape[0] == B and seq_lens.shape == (B,) and weights.shape == (B, Hkv, max_pages * page)
+                 and new_table.get_device() == seq_lens.get_device() == weights.get_device() == device
+                 and new_table.is_contiguous() and seq_lens.is_contiguous() and weights.is_contiguous())
+    except AttributeError:
+        usual = False
+    if not usual:
+        _need_on(device, new_table, "new_table", torch.int32, (B, new_max_pages))
+        _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
+        _need_on(device, weights, "weights", torch.float32, (B, Hkv, max_pages * page))
     if new_table.data_ptr() == page_table.data_ptr() and B > 0:
         raise ValueError("new_table must hold other pages than page_table")
-    _need_on(device, seq_lens, "seq_lens", torch.int32, (B,))
-    _need_on(device, weights, "weights", torch.float32, (B, Hkv, max_pages * page))
     if kept is None:
         kept = page_table.new_empty((B, Hkv, max(budget, 0)))
     else:
