@@ -380,7 +380,7 @@ template <bool RULED> __global__ void chunk_tile8_kernel(ChunkAttendArgs a);    
 // Rows of a tile of `rows` that a workgroup of the merge takes.
 __host__ __device__ constexpr int chunk_merge_rows(int rows) { return rows < kChunkTileRows ? 16 : 32; }
 __global__ void chunk_merge_kernel(ChunkMergeArgs a);
-template <bool I8, bool RULED> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
+template <bool I8, bool RULED, bool MANY> __global__ void chunk_weights_kernel(ChunkWeightsArgs a);
 constexpr int kEvictThreads = 1024;
 __global__ void evict_select_kernel(EvictArgs a);
 constexpr int kEvictMoveRows = 128;            // rows per workgroup of the move, which takes keys or values

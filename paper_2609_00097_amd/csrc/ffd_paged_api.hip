@@ -102,9 +102,11 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows
 }
 // Sequences with up to kFewRows query rows per KV head go to the kernel of few rows, the others to the one of large tiles. One
 // kernel takes all where the batch cannot have both kinds (few rows in all, or one sequence), is likely to have none of the second
-// (hardly more new tokens than sequences), or has little work: rows times tokens of the capacity per CU.
+// (hardly more new tokens than sequences), or has little work: rows times tokens of the capacity per CU. Large / few, whole
+// calls, eight KV heads of four in bf16: 32K (256 tokens on 1K) 34.2 / 33.4 us; 64K (512 on 1K) 36.8 / 33.9, (128 on 4K) 36.1 / 42.3;
+// 128K (256 on 4K) 41.5 / 58.1, (32 on 32K) 41.2 / 56.0, (512 on 2K) 42.3 / 48.7; in 8 bits alike.
 constexpr int kFewRows = 32;
-constexpr long long kLittleWork = 24 << 10;
+constexpr long long kLittleWork = 40 << 10;
 // Tiles of the kernel of few rows: 32 rows, so that a tile's tokens are read once for them; 16 where the batch has hardly more in a
 // sequence, and where that leaves no more than one workgroup of two blocks for each CU. 16 / 32, whole calls, four heads per KV head:
 // 8 tokens on 300 11.9 / 15.8 us, 16 on 1K 13.0 / 16.8, 8 on 4K 15.0 / 18.0 (256 such pairs), 16 on 4K 21.9 / 19.2 (512), 8 on 32K
@@ -148,7 +150,18 @@ void launch_rows(int rows, bool i8, bool ruled, dim3 grid, hipStream_t stream, c
     else launch_rows_ruled<2, false>(ruled, grid, stream, a);
 }
 
-constexpr int kFewWeightRows = 128;
+// Query rows of a sequence up to which the weights' workgroups take equal shares, three to a CU; above, a unit each, in which the
+// rows that may see it differ, with two places for rows in LDS. Shares / units, eight KV heads of four: 128 rows on 32K 26.1 / 40.4 us,
+// 256 45.3 / 51.5, on 4 x 8K 53.3 / 52.4, 512 on 32K 78.2 / 80.1, 2K on 8 x 2K 221 / 115.
+constexpr int kFewWeightRows = 256;
+template <bool MANY>
+void launch_weights(bool i8, bool ruled, hipStream_t stream, const ChunkWeightsArgs& a) {
+    const dim3 grid((unsigned)a.slots), block(kThreads);
+    if (i8 && ruled) hipLaunchKernelGGL((chunk_weights_kernel<true, true, MANY>), grid, block, 0, stream, a);
+    else if (i8) hipLaunchKernelGGL((chunk_weights_kernel<true, false, MANY>), grid, block, 0, stream, a);
+    else if (ruled) hipLaunchKernelGGL((chunk_weights_kernel<false, true, MANY>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((chunk_weights_kernel<false, false, MANY>), grid, block, 0, stream, a);
+}
 
 int check_strides(const int64_t* s) { return s && (s[0] < 0 || s[0] % 8 || s[1] < 0 || s[1] % 8) ? FFD_ERR_INVALID_ARGUMENT : FFD_OK; }
 
@@ -293,18 +306,14 @@ int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int
     a.weights = weights;
     a.last = last;
     const bool ruled = rules && (rules->softcap > 0.f || rules->slopes);
-    // One share for each workgroup that fits the device at a time where a sequence's rows are few, so that all units take the
-    // same time; else one unit each, in which the rows that may see it differ.
     long long units = 0;
     while (units == 0 || units >= 1LL << 23) units = (long long)B * Hkv * ((a.Lcap + (kRound << a.unit_shift) - 1) / (kRound << a.unit_shift)), ++a.unit_shift;
     --a.unit_shift;
     const long long rows = std::min<long long>(T, last > 0 ? (long long)last * B : T) * a.G;
-    a.slots = (int)(rows <= kFewWeightRows * (long long)B ? std::min<long long>(units, 3LL * device_cus()) : units);
-    const dim3 grid((unsigned)a.slots);
-    if (i8 && ruled) hipLaunchKernelGGL((chunk_weights_kernel<true, true>), grid, dim3(kThreads), 0, stream, a);
-    else if (i8) hipLaunchKernelGGL((chunk_weights_kernel<true, false>), grid, dim3(kThreads), 0, stream, a);
-    else if (ruled) hipLaunchKernelGGL((chunk_weights_kernel<false, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((chunk_weights_kernel<false, false>), grid, dim3(kThreads), 0, stream, a);
+    const bool many = rows > kFewWeightRows * (long long)B;
+    a.slots = (int)(many ? units : std::min<long long>(units, 3LL * device_cus()));
+    if (many) launch_weights<true>(i8, ruled, stream, a);
+    else launch_weights<false>(i8, ruled, stream, a);
     return launch_status();
 }
 

@@ -3,12 +3,15 @@
 // order and one place, so that results do not change from call to call.
 //
 // Mapping. Work in the order (sequence, KV head, token), in units of 128 tokens, is given out in equal shares of consecutive
-// units. For a (sequence, KV head) of its share a workgroup takes 128 tokens at a time, 32 a wave, and puts the query rows that
-// count into LDS, 128 of them at a time. With the keys of its 32 tokens in registers a wave goes through the rows, 16 by 16,
-// with S^T = K Q^T as in ffd_attend.h: lane (n, g) adds up its eight tokens' weights from row n, and the 16 lanes of a group are
-// joined at the end. Where 128 rows are all, they stay, the waves need no barrier, and the next keys are asked for early.
+// units (MANY: a unit each). For a (sequence, KV head) of its share a workgroup takes 128 tokens at a time, 32 a wave, and puts
+// the query rows that count into LDS, 128 of them at a time. With the keys of its 32 tokens in registers a wave goes through the
+// rows, 16 by 16, with S^T = K Q^T as in ffd_attend.h: lane (n, g) adds up its eight tokens' weights from row n, and the 16 lanes of
+// a group are joined at the end. Where 128 rows are all, they stay, the waves need no barrier, and the next keys are asked for
+// early. MANY: two places for rows, one filled from memory by loads straight to LDS while the other is used (8K new tokens of one
+// prompt 1712 -> 763 us, 5 x 1K on 8K 847 -> 498).
 //
-// Bound: HBM where few queries count (256 bytes a token and KV head), else the exponentials and the matrix cores.
+// Bound: HBM where few queries count (256 bytes a token and KV head: one token of 16 sequences on 8K 49 us, 5.5 TB/s), else the
+// instructions of the exponentials beside the matrix cores (8K new tokens: 0.36 PFLOP/s of products).
 #include <type_traits>
 
 #include "ffd_paged.h"
@@ -19,9 +22,10 @@ namespace ffd {
 namespace {
 
 constexpr int kRowsAtOnce = 128;
+template <int N>
 struct WeightsLds {
-    alignas(16) uint8_t q[kRowsAtOnce * 2 * kD];
-    float lse2[kRowsAtOnce];
+    alignas(16) uint8_t q[N][kRowsAtOnce * 2 * kD];
+    float lse2[N][kRowsAtOnce];
 };
 
 // Units [first, last) of a (sequence, KV head).
@@ -38,11 +42,18 @@ struct WeightsTile {
     float4 old;
 };
 
+// 16 bytes a lane from memory straight to LDS, where a wave's 64 pieces lie one after the other from lds_at on (the same in all
+// lanes). The compiler does not count this load.
+__device__ __forceinline__ void rows_to_lds(uint32_t lds_at, const uint8_t* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_at), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
 }  // namespace
 
-template <bool I8, bool RULED>
-__global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeightsArgs a) {
-    __shared__ WeightsLds lds;
+template <bool I8, bool RULED, bool MANY>
+__global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void chunk_weights_kernel(ChunkWeightsArgs a) {
+    __shared__ WeightsLds<MANY ? 2 : 1> lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int g = lane >> 4, n = lane & 15, gs = __builtin_ctz(a.G);
     const int unit = kRound << a.unit_shift;
@@ -129,14 +140,27 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
                 if (at + row >= rows + 15) break;
                 const int r = r0 + min(at + row, rows - 1);
                 const size_t from_row = (size_t)(it.seq.q0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1));
-                *reinterpret_cast<v4u*>(&lds.q[row * (2 * kD) + 16 * key_chunk(row, tid & 15)]) =
+                *reinterpret_cast<v4u*>(&lds.q[0][row * (2 * kD) + 16 * key_chunk(row, tid & 15)]) =
                     *reinterpret_cast<const v4u*>(a.q + from_row * kD + 8 * (tid & 15));
-                if ((tid & 15) == 0) lds.lse2[row] = a.lse[from_row] * kLog2e;
+                if ((tid & 15) == 0) lds.lse2[0][row] = a.lse[from_row] * kLog2e;
             }
+        };
+        // The same without a register between, asked for here and there after a wait and a barrier: a wave brings 32 rows, four a
+        // load, each piece from the chunk that belongs to its place. This thread's row's lse comes with them.
+        auto bring = [&](int at, int buffer) {
+#pragma unroll
+            for (int i = 0; i < kRowsAtOnce / kWaves / 4; ++i) {
+                const int row = (kRowsAtOnce / kWaves) * wave + 4 * i, mine = row + (lane >> 4), r = r0 + min(at + mine, rows - 1);
+                const size_t from_row = (size_t)(it.seq.q0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1));
+                rows_to_lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds.q[buffer][row * (2 * kD)],
+                            reinterpret_cast<const uint8_t*>(a.q + from_row * kD + 8 * key_chunk(mine, lane & 15)));
+            }
+            const int r = r0 + min(at + (tid & (kRowsAtOnce - 1)), rows - 1);
+            return a.lse[(size_t)(it.seq.q0 + (r >> gs)) * a.Hq + hq0 + (r & (a.G - 1))];
         };
         float sum[8];
         // the weights that rows [at, at + kRowsAtOnce) give this wave's tile
-        auto add_rows = [&](const KeyTile<I8>& kt, const WeightsTile& tile, int at) {
+        auto add_rows = [&](const KeyTile<I8>& kt, const WeightsTile& tile, int at, int buffer) {
             v8bf keys[2][4];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -159,14 +183,14 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
                 float lse2[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    lse2[i] = lds.lse2[r + 16 * i + n];
+                    lse2[i] = lds.lse2[buffer][r + 16 * i + n];
                     s[i][0] = s[i][1] = v4f{0.f, 0.f, 0.f, 0.f};
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
-                        const v8bf q = *reinterpret_cast<const v8bf*>(&lds.q[(r + 16 * i + n) * (2 * kD) + 16 * key_chunk(n, key_dim<I8>(k, g) / 8)]);
+                        const v8bf q = *reinterpret_cast<const v8bf*>(&lds.q[buffer][(r + 16 * i + n) * (2 * kD) + 16 * key_chunk(n, key_dim<I8>(k, g) / 8)]);
 #pragma unroll
                         for (int t = 0; t < 2; ++t) s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys[t][k], q, s[i][t], 0, 0, 0);
                     }
@@ -243,7 +267,7 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
                 asm volatile("" ::: "memory");      // here, not where they are used
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-                if (rows > 0) add_rows(kt, tile, 0);
+                if (rows > 0) add_rows(kt, tile, 0, 0);
                 finish(tile);
                 kt = kn;
                 tile = next_tile;
@@ -257,20 +281,41 @@ __global__ __launch_bounds__(kThreads, 3) void chunk_weights_kernel(ChunkWeights
             load_old(tile);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-            for (int at = 0; at < rows; at += kRowsAtOnce) {
-                stage(at);
+            if constexpr (MANY) {
+                // rows that some of the 128 tokens may count for
+                int lowest, highest;
+                rows_for(t0 - kTile * wave, min(t0 - kTile * wave + kRound, end), lowest, highest);
+                const int begin_row = max((lowest - from) << gs, 0) / kRowsAtOnce * kRowsAtOnce, end_row = min((highest - from) << gs, rows);
+                float lse = 0.f;
+                if (begin_row < end_row) lse = bring(begin_row, 0);
+                for (int at = begin_row, buffer = 0; at < end_row; at += kRowsAtOnce, buffer ^= 1) {       // uniform
+                    wait_for_loads();
+                    if (tid < kRowsAtOnce) lds.lse2[buffer][tid] = lse * kLog2e;
+                    __syncthreads();
+                    if (at + kRowsAtOnce < end_row) lse = bring(at + kRowsAtOnce, buffer ^ 1);
+                    if (t0 < end) add_rows(kt, tile, at, buffer);
+                }
                 __syncthreads();
-                if (t0 < end) add_rows(kt, tile, at);
-                __syncthreads();
+            } else {
+                for (int at = 0; at < rows; at += kRowsAtOnce) {
+                    stage(at);
+                    __syncthreads();
+                    if (t0 < end) add_rows(kt, tile, at, 0);
+                    __syncthreads();
+                }
             }
             if (t0 < end) finish(tile);
         }
     }
 }
 
-template __global__ void chunk_weights_kernel<false, false>(ChunkWeightsArgs);
-template __global__ void chunk_weights_kernel<false, true>(ChunkWeightsArgs);
-template __global__ void chunk_weights_kernel<true, false>(ChunkWeightsArgs);
-template __global__ void chunk_weights_kernel<true, true>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<false, false, false>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<false, false, true>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<false, true, false>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<false, true, true>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<true, false, false>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<true, false, true>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<true, true, false>(ChunkWeightsArgs);
+template __global__ void chunk_weights_kernel<true, true, true>(ChunkWeightsArgs);
 
 }  // namespace ffd

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 def _batch(lens, new, Hkv, G, page, bits, seed, **kw):
     """With a capacity that makes rows times tokens twice what the small tiles take on 256 CUs."""
-    cap = 2 * 256 * (24 << 10) // (sum(new) * G * Hkv) + max(lens)
+    cap = 2 * 256 * (40 << 10) // (sum(new) * G * Hkv) + max(lens)
     return R.Batch(lens, new, Hkv, G, page, bits, seed=seed, width=-(-cap // page), **kw)
 
 
