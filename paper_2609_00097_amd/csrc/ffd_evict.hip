@@ -7,7 +7,9 @@
 // sequence and then writes the list in the tokens' order. Up to 32K keys lie in LDS, those behind are made anew in each pass.
 // evict_move_kernel copies rows by the list. New pages are others than the old ones, so that rows can be copied in any order.
 //
-// Bound: the selection by its chain of passes over 4 bytes a token (out of L2 after the first), the move by HBM.
+// Bound: the selection by its chain of passes, keys in LDS (four sequences of 32K, eight heads: 31 us, of which 11 bring the keys
+// and count the first digit, 10 the two others, 10 count and write the list; 1K tokens 8 us), the move by HBM (8K of each of them: 57 us,
+// 4.7 TB/s). Workgroups of 256 threads are no faster for 1K tokens (11.9 and 12.2 us both kernels) and slower from 2K on.
 #include "ffd_paged.h"
 
 namespace ffd {

@@ -5,6 +5,10 @@
 // Probabilities enter the second product in two bf16 parts (2^-16), which costs nothing where memory bounds.
 //
 // Bound: HBM, 512 bytes a token and KV head (8 bits: 260), for short caches the chain of lengths, pages, first tile and join.
+// One token of 32 sequences, eight KV heads, with the merge: on 4K 101 us (5.3 TB/s; 8 bits 50, 5.4), on 32K 703 us (6.1 TB/s; 388, 5.6),
+// of one sequence on 4K 12.8 us. Equal shares instead of runs of one length for all tiles: one chunk beside 15 decoding sequences 197
+// -> 172 us, 37 tokens of three prompts 39 -> 16 (with tiles of 16 rows 13.5). Pages through the scalar cache: their wait does not
+// drain the loads that are under way.
 #include "ffd_paged.h"
 
 namespace ffd {
@@ -314,7 +318,8 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
 }
 
 // Joins the runs of the row tiles that were cut: a workgroup takes 16 or 32 rows of one tile and 32 dims, eight lanes a row;
-// where there are fewer rows several groups of lanes share a row's runs.
+// where there are fewer rows several groups of lanes share a row's runs, eight of which are asked for together. Bound: latency (4 us
+// for a few tiles, 10 for 64 tiles of 256 rows in four runs each).
 __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkMergeArgs a) {
     struct State {
         float m, l;

@@ -13,7 +13,8 @@
 // Pages: 16 tokens lie together, so a thread's load is one page's, whose entry is read a tile ahead; codes of pages that are not
 // there, and behind what any query sees, have M = 0.
 //
-// Bound: the matrix cores, 512 operations a query row and token.
+// Bound: the phases' instructions, matrix and softmax ones in turn on each SIMD: a prompt of 8K, eight KV heads of four, 720 us (0.76
+// PFLOP/s), 512 tokens on 32K 352 us.
 #include "ffd_paged.h"
 #include "ffd_tile.h"
 

@@ -8,7 +8,9 @@
 // Pairs are (d, d + rope_dims / 2), or neighbours (2 d, 2 d + 1). A key is rounded to bf16 before its 8-bit codes are taken
 // (ffd_kv8.hip), so that they are those of the same key written by ffd_write_kv8.
 //
-// Bound: HBM (256 bytes read and written per vector), for few tokens the chain of starts, length, page and vector.
+// Bound: HBM (256 bytes read and written per vector): 7K tokens of 32 + 2 x 8 heads with norms and rotation 41 us, 4.0 TB/s. For few
+// tokens the chain of starts, length, page and vector, 4.5 us; the vectors are asked for before it. 16 lanes a vector: with eight, and
+// the vectors asked for behind the chain, the 7K tokens took 47 us where this took 45. A wave's loads are whole rows, and the other half of a pair is eight lanes away, which is a DPP rotation.
 #include "ffd_kv8.h"
 #include "ffd_paged.h"
 #include "ffd_tile.h"
