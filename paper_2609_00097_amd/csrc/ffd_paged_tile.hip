@@ -77,18 +77,12 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     const ChunkSpan span = chunk_span<kShift>(a, it.seq, tok0, tok1);
     const int first = (int)((long long)span.count * it.run / it.cuts), last = (int)((long long)span.count * (it.run + 1) / it.cuts);
 
-    // this lane's row
+    // this lane's row; behind the last one it is that one again, whose results are not written
     const int r = 32 * wave + n, tok = tok0 + (min(r, live_rows - 1) >> gs), head = hq0 + (r & (a.G - 1));
     const bool live = r < live_rows;
     const size_t row_at = (size_t)(it.seq.q0 + tok) * a.Hq + head;
     const int at = place + tok;
     const ScoreRule rule = score_rule(a, false, head);
-    v8bf q[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const v4u x = *reinterpret_cast<const v4u*>(a.q + row_at * kD + 16 * k + 8 * h);
-        q[k] = __builtin_bit_cast(v8bf, live ? x : v4u{0, 0, 0, 0});
-    }
     // the wave's first and last place, and the tile from which on none of its rows sees a token
     const int low = place + tok0 + ((32 * wave) >> gs), high = place + min(tok0 + ((32 * wave + 31) >> gs), tok1);
     const int wave_end = 32 * wave < live_rows ? max(min(max(high + 1, it.seq.pre), cached), 0) : 0;
@@ -113,6 +107,11 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     auto load_entries = [&](int u) {
         return a.pages.table[(size_t)it.b * a.pages.max_pages + min((token0(u) + 16 * (lane & 3)) >> a.pages.page_shift, a.pages.max_pages - 1)];
     };
+    const int first_entries = load_entries(first);
+    v8bf q[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) q[k] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4u*>(a.q + row_at * kD + 16 * k + 8 * h));
+    asm volatile("" ::: "memory");              // on their way while the first tile's page is awaited
     auto load_rows = [&](const uint8_t* tile, const uint8_t* pages, size_t row, const uint32_t (&from)[2]) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -375,7 +374,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         grown = 0;
         if (tid < kMarks / 32) lds.nonfinite[tid] = 0;
         if (first < last) {
-            entries = load_entries(first);
+            entries = first_entries;
             __syncthreads();                    // a careful run: the first one's reads are done
             uint8_t *before = lds.values[0], *now = lds.values[1], *after = lds.values[2];      // values of tiles u - 1, u, u + 1
             for (int i = tid; i < kTileBytes / 16; i += kTThreads) reinterpret_cast<v4u*>(before)[i] = v4u{0, 0, 0, 0};
@@ -437,6 +436,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         }
         if (careful) {
             add_nonfinite();                    // the last turn's barrier is behind all marks
+            __syncthreads();
             break;
         }
         float x = 0.f;                          // stays zero where every o is finite
@@ -447,34 +447,57 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         if (!__syncthreads_or(x != 0.f)) break;
     }
 
+    // Out through LDS, which nobody reads any more, 8 KB a wave, so that rows go out whole: rows of 256 bytes, their 16-byte chunks
+    // XORed with the row against bank conflicts.
     const float sum = halves_sum(l), rounded_sum = halves_sum(rounded);
-    const bool any_seen = m != -INFINITY;
-    if (!live) return;
+    const bool any = m != -INFINITY;
     const float ln = m * 0.69314718055994531f;
+    uint8_t* mine = lds.keys[0] + wave * (32 * 256);
+    const int row4 = lane >> 4, chunk = lane & 15;
+    auto place_of = [&](int row, int chunk) { return row * 256 + 16 * (chunk ^ (row & 15)); };
     if (it.part >= 0) {
-        const float f = any_seen ? sum / rounded_sum : 1.f;
-        const size_t to = (size_t)it.part * kChunkTileRows + r;
+        const float f = any ? sum / rounded_sum : 1.f;
+        const size_t to = (size_t)it.part * kChunkTileRows + 32 * wave;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                *reinterpret_cast<float4*>(a.parts.acc + to * kD + 32 * d + 8 * b + 4 * h) =
-                    make_float4(o[d][4 * b] * f, o[d][4 * b + 1] * f, o[d][4 * b + 2] * f, o[d][4 * b + 3] * f);
-        if (h == 0) {
-            a.parts.m[to] = ln;
-            a.parts.l[to] = sum;
+            for (int d = 0; d < 2; ++d)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const v16f& x = o[2 * half + d];
+                    *reinterpret_cast<float4*>(mine + place_of(n, 8 * d + 2 * b + h)) = make_float4(x[4 * b] * f, x[4 * b + 1] * f, x[4 * b + 2] * f, x[4 * b + 3] * f);
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = 4 * i + row4;
+                const float4 x = *reinterpret_cast<const float4*>(mine + place_of(row, chunk));
+                if (32 * wave + row < live_rows) *reinterpret_cast<float4*>(a.parts.acc + (to + row) * kD + 64 * half + 4 * chunk) = x;
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (h == 0 && live) {
+            a.parts.m[to + n] = ln;
+            a.parts.l[to + n] = sum;
         }
         return;
     }
-    const float inv = any_seen ? 1.f / rounded_sum : 0.f;
+    const float inv = any ? 1.f / rounded_sum : 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const uint2 w = make_uint2(pack_bf16(o[d][4 * b] * inv, o[d][4 * b + 1] * inv), pack_bf16(o[d][4 * b + 2] * inv, o[d][4 * b + 3] * inv));
-            *reinterpret_cast<uint2*>(a.out + row_at * kD + 32 * d + 8 * b + 4 * h) = any_seen ? w : make_uint2(0u, 0u);
+            *reinterpret_cast<uint2*>(mine + place_of(n, 4 * d + b) + 8 * h) = any ? w : make_uint2(0u, 0u);
         }
-    if (h == 0 && a.lse) a.lse[row_at] = any_seen ? ln + logf(sum) : -INFINITY;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = 32 * wave + 4 * i + row4;
+        const uint4 x = *reinterpret_cast<const uint4*>(mine + place_of(4 * i + row4, chunk));
+        if (row < live_rows) *reinterpret_cast<uint4*>(a.out + ((size_t)(it.seq.q0 + tok0 + (row >> gs)) * a.Hq + hq0 + (row & (a.G - 1))) * kD + 8 * chunk) = x;
+    }
+    if (h == 0 && live && a.lse) a.lse[row_at] = any ? ln + logf(sum) : -INFINITY;
 }
 
 template __global__ void chunk_tile_kernel<false>(ChunkAttendArgs);
