@@ -105,7 +105,8 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     }
     // (whether they are the table's is seen where they are used, so that the load is waited for there)
     auto load_entries = [&](int u) {
-        return a.pages.table[(size_t)it.b * a.pages.max_pages + min((token0(u) + 16 * (lane & 3)) >> a.pages.page_shift, a.pages.max_pages - 1)];
+        const int page = (max(token0(u), 0) + 16 * (lane & 3)) >> a.pages.page_shift;            // (no tile: the first page's)
+        return a.pages.table[(size_t)it.b * a.pages.max_pages + min(page, a.pages.max_pages - 1)];
     };
     const int first_entries = load_entries(first);
     v8bf q[8];

@@ -98,6 +98,16 @@ def test_keys_that_are_not_finite(ffd):
     assert torch.equal(lse.isnan().any(-1), nan)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("rule", [dict(), dict(window=5, softcap=10.0)], ids=["plain", "ruled"])
+def test_rows_that_see_no_block(ffd, bits, rule):
+    """Tiles of rows before the first token, the table's first entry a hole, beside one that sees tokens."""
+    batch = _batch([0, 100, 10], [300, 300, 300], 1, 4, 16, bits, 43, holes=[(1, 0), (2, 0)])
+    out, lse = _attend(ffd, batch, **rule)
+    R.check_attention(batch, (out, lse), P_BF16, **rule)
+    assert bool((lse[:500 + 16] == -math.inf).all()) and bool((lse[600:] == -math.inf).all()) and bool((out[600:] == 0).all())
+
+
 @pytest.mark.parametrize("B", [3, 63, 64, 65, 130])
 def test_cuts_of_several_sequences(ffd, B):
     """Tiles of several sequences cut into runs, beside ones that decode; more sequences than a wave has lanes."""
