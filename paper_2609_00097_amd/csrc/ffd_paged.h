@@ -229,8 +229,25 @@ __device__ __forceinline__ float near_cap(float x, const ScoreRule& r) {
     return fmaf(u, fmaf(u, fmaf(u, fmaf(u, r.near[4], r.near[3]), r.near[2]), r.near[1]), r.near[0]);
 }
 __device__ __forceinline__ float capped(float x, const ScoreRule& r) {
-    const float far = r.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_hw(x)), 1.f);
-    return fabsf(x) <= kNearCap ? x * near_cap(x, r) : far;
+    float far = r.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + exp2_hw(x)), 1.f), near = x * near_cap(x, r);
+    asm volatile("" : "+v"(far), "+v"(near));   // a selection, not a branch for each score
+    return fabsf(x) <= kNearCap ? near : far;
 }
+// Several at once: the polynomial alone where the wave has no others.
+template <int N, typename X>
+__device__ __forceinline__ void cap_several(X& x, const ScoreRule& r) {
+    float largest = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) largest = fmaxf(largest, fabsf(x[i]));
+    if (__ballot(largest > kNearCap) == 0) {    // uniform
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= near_cap(x[i], r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = capped(x[i], r);
+    }
+}
+template <int N> __device__ __forceinline__ void cap_all(float (&x)[N], const ScoreRule& r) { cap_several<N>(x, r); }
+template <typename V> __device__ __forceinline__ void cap_scores(V& x, const ScoreRule& r) { cap_several<16>(x, r); }       // v16f
 
 }  // namespace ffd

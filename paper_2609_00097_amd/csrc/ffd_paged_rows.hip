@@ -132,12 +132,11 @@ __device__ __forceinline__ void attend_pages(const ChunkAttendArgs& a, RowState<
             float z[8];
             uint32_t seen = 0xffu;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[e] = s[c][e >> 2][e & 3] * zs[e];
-                if constexpr (RULED) {
-                    if (rule.cap2 != 0.f) z[e] = capped(z[e], rule);
-                    z[e] = fmaf(-rows.slope2[c], fabsf((float)(rows.at[c] - t0 - value_token(e, g))), z[e]);
-                }
+            for (int e = 0; e < 8; ++e) z[e] = s[c][e >> 2][e & 3] * zs[e];
+            if constexpr (RULED) {
+                if (rule.cap2 != 0.f) cap_all(z, rule);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = fmaf(-rows.slope2[c], fabsf((float)(rows.at[c] - t0 - value_token(e, g))), z[e]);
             }
             if (masked) {
                 seen = 0;

@@ -201,15 +201,15 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         const int high = min(rel, end - 1), low = a.window > 0 ? rel - a.window : INT32_MIN, prefix = min(it.seq.pre - t0 - 4 * h, end);
         uint32_t some = 0;
         float mx = -INFINITY;
+        if constexpr (RULED) {
+            x *= rule.zscale;
+            if (rule.cap2 != 0.f) cap_scores(x, rule);
+        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int k = 8 * (i >> 2) + (i & 3);
             float z = x[i];
-            if constexpr (RULED) {
-                z *= rule.zscale;
-                if (rule.cap2 != 0.f) z = capped(z, rule);
-                z = fmaf(-rule.slope2, fabsf((float)rel - (float)k), z);
-            }
+            if constexpr (RULED) z = fmaf(-rule.slope2, fabsf((float)rel - (float)k), z);
             const uint32_t seen = (uint32_t)(((k <= high) & (k > low)) | (k < prefix)) & (there >> (i >> 3));
             x[i] = seen & 1 ? z : -INFINITY;
             mx = fmaxf(mx, x[i]);

@@ -245,9 +245,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile8_kernel(ChunkAttendAr
                 for (int i = 0; i < 16; ++i) s[x][i] *= scale;
             if (rule.cap2 != 0.f) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[x][i] = capped(s[x][i], rule);
+                for (int x = 0; x < 2; ++x) cap_scores(s[x], rule);
             }
             if (a.slopes) {
                 const float rel = (float)(at - t0 - 4 * h);

@@ -201,17 +201,15 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void chunk_weights_kernel(C
                 for (int i = 0; i < N; ++i) {
                     const int row = at + r + 16 * i + n, mine = place + from + (row >> gs);
                     float p[8];
+                    if constexpr (RULED) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float z = s[i][e >> 2][e & 3];
-                        if constexpr (RULED) {
-                            z *= km[e];
-                            if (rule.cap2 != 0.f) z = capped(z, rule);
-                            z = fmaf(-rule.slope2, fabsf((float)(mine - t0 - value_token(e, g))), z);
-                            p[e] = exp2_hw(z - lse2[i]);
-                        } else {
-                            p[e] = exp2_hw(fmaf(z, km[e], -lse2[i]));
-                        }
+                        for (int e = 0; e < 8; ++e) p[e] = s[i][e >> 2][e & 3] * km[e];
+                        if (rule.cap2 != 0.f) cap_all(p, rule);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = exp2_hw(fmaf(-rule.slope2, fabsf((float)(mine - t0 - value_token(e, g))), p[e]) - lse2[i]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = exp2_hw(fmaf(s[i][e >> 2][e & 3], km[e], -lse2[i]));
                     }
                     if (masked) {
                         const uint32_t row_there = row < rows;
