@@ -193,29 +193,35 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     // masks are applied where there are any, else x stays the product (`raw`), to be scaled, and capped, with the exponential.
     float top = -INFINITY;
     bool raw = true, near = false;              // near: all of the wave's products are of scores up to half of the cap
-    auto rules_and_masks = [&](int t, v16f& x) {
+    auto rules_and_masks = [&](int t, v16f& x, bool whole) {
         asm volatile("");                       // a branch around all this, not selections after it
-        const int t0 = token0(t >> 1) + 32 * (t & 1);
-        const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
-        const int rel = at - t0 - 4 * h, end = cached - t0 - 4 * h;
-        const int high = min(rel, end - 1), low = a.window > 0 ? rel - a.window : INT32_MIN, prefix = min(it.seq.pre - t0 - 4 * h, end);
-        uint32_t some = 0;
-        float mx = -INFINITY;
+        const int t0 = token0(t >> 1) + 32 * (t & 1), rel = at - t0 - 4 * h;
         if constexpr (RULED) {
             x *= rule.zscale;
             if (rule.cap2 != 0.f) cap_scores(x, rule);
-        }
+            if (a.slopes) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int k = 8 * (i >> 2) + (i & 3);
-            float z = x[i];
-            if constexpr (RULED) z = fmaf(-rule.slope2, fabsf((float)rel - (float)k), z);
-            const uint32_t seen = (uint32_t)(((k <= high) & (k > low)) | (k < prefix)) & (there >> (i >> 3));
-            x[i] = seen & 1 ? z : -INFINITY;
-            mx = fmaxf(mx, x[i]);
-            some |= seen;
+                for (int i = 0; i < 16; ++i) x[i] = fmaf(-rule.slope2, fabsf((float)rel - (float)(8 * (i >> 2) + (i & 3))), x[i]);
+            }
         }
-        const bool any = halves_max(some & 1 ? 1.f : 0.f) > 0.f;
+        bool any = true;
+        if (!whole) {
+            const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
+            const int end = cached - t0 - 4 * h;
+            const int high = min(rel, end - 1), low = a.window > 0 ? rel - a.window : INT32_MIN, prefix = min(it.seq.pre - t0 - 4 * h, end);
+            uint32_t some = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int k = 8 * (i >> 2) + (i & 3);
+                const uint32_t seen = (uint32_t)(((k <= high) & (k > low)) | (k < prefix)) & (there >> (i >> 3));
+                x[i] = seen & 1 ? x[i] : -INFINITY;
+                some |= seen;
+            }
+            any = halves_max(some & 1 ? 1.f : 0.f) > 0.f;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[i]);
         top = any ? fmaxf(halves_max(mx) * (RULED ? 1.f : rule.zscale), -FLT_MAX) : -INFINITY;
         raw = false;
     };
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
         constexpr int H = decltype(half)::value;
         const int t0 = token0(t >> 1) + 32 * (t & 1);
         const uint32_t there = ring >> (4 * ((t >> 1) & 3) + 2 * (t & 1)) & 3u;
-        const bool plain = (there == 3u) & (t0 <= whole_to) & ((t0 > whole_from) | (t0 <= prefix_to)) & !(RULED && a.slopes);
+        const bool whole = (there == 3u) & (t0 <= whole_to) & ((t0 > whole_from) | (t0 <= prefix_to)), plain = whole & !(RULED && a.slopes);
         float mx[4], abs_mx[4], up_to = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
 #pragma unroll
                 for (int d = 0; d < 4; ++d) o[d] *= corr;
             }
-            if (!plain) rules_and_masks(t, next);
+            if (!plain) rules_and_masks(t, next, whole);
         }
     };
     // They reach the rows that see them at the end, when o is scaled no more.

@@ -580,3 +580,20 @@ def test_short_capacities(ffd, B, n, cap):
     """Capacities around those at which no tile is cut, with few and with more tiles than workgroups."""
     batch = R.Batch([cap - (7 * b) % 90 for b in range(B)], [n] * B, 4, 4, 16, seed=42, width=cap // 16)
     R.check_attention(batch, _attend(ffd, batch), _p_error(batch))
+
+
+@pytest.mark.parametrize("T", [5, 700])
+def test_batches_without_rows(ffd, T):
+    """Rows that belong to no sequence, and sequences without any: nothing is written."""
+    batch = R.Batch([40, 0, 300], [0, 0, 0], 2, 4, 16, seed=44, behind=T, width=2000)
+    _attend(ffd, batch)                         # looks at the rows around
+    q, k, v = (torch.randn(T, h, D, device="cuda", dtype=torch.bfloat16) for h in (8, 2, 2))
+    before, out = _snapshot(batch.cache), torch.full((T, 8, D), 3.0, device="cuda", dtype=torch.bfloat16)
+    ffd.write_paged(q, k, v, batch.cache, *batch.args[2:], out=out)
+    assert bool((out == 3).all())
+    for x, y in zip(batch.cache, before):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+    previous = torch.rand(3, 2, batch.cap, device="cuda")
+    got = ffd.paged_attention_weights(q, *batch.args[1:], torch.zeros(T, 8, device="cuda"), previous=previous)
+    for b, L in enumerate(batch.lens):
+        assert torch.equal(got[b, :, :L], previous[b, :, :L]) and bool((got[b, :, L:] == 0).all())
