@@ -27,7 +27,7 @@
 // the loads, or the barrier, all of it) beside the matrix cores, which 512 operations a query row and token keep busy for 47 to 49 % of it.
 // Against two teams of waves with matrix and softmax phases in turn and tokens staged in registers, eight KV heads of four:
 // 8K tokens 620 -> 585 us, 512 on 32K 309 -> 291, 3800 in a window of 1024 with a cap, twice, 252 -> 229; with the queries asked for
-// beside the first tile's page and results out in whole rows 562 us (0.97 PFLOP/s) and 287. A tile starts in 7 us and ends in 4.
+// beside the first tile's page and results out in whole rows 562 us (0.97 PFLOP/s) and 287.
 // Not kept: the waves of a SIMD half a step apart (8K 599), operands three products ahead (589), four waves of 64 rows (763).
 #include <type_traits>
 
