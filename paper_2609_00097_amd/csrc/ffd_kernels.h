@@ -372,6 +372,10 @@ template <int NW> __global__ void shared_merge_kernel(SharedMergeArgs a);
 // I8: 8-bit pages; INTERLEAVED: pairs of neighbouring dims are rotated.
 template <bool I8, bool INTERLEAVED> __global__ void write_paged_kernel(WritePagedArgs a);
 // CT (1, 2): tiles of 16 query rows per workgroup; RULED: a cap of the scores or slopes.
+// Tiles of up to this many blocks are not cut, and of twice as many where there are many tiles. Whole / cut, whole calls, one token of
+// sequences with eight heads in bf16: 4 sequences, 512 tokens 10.4 / 11.8 us, 1K 14.8 / 12.2; 16 sequences, 512 11.6 / 13.8, 1K 16.9 /
+// 22.3; 100 sequences, 512 39.7 / 44.4, 1K 83.5 / 87.1 (8 bits, 64 sequences: 16.8 / 25.5 and 25.8 / 33.7).
+constexpr int kWholeBlocks = 4;
 template <int CT, bool I8, bool RULED> __global__ void chunk_rows_kernel(ChunkAttendArgs a);
 constexpr int kChunkRowsShift = 7;             // blocks of 128 tokens
 constexpr int kChunkTileThreads = 512, kChunkTileRows = 256, kChunkTileShift = 6;

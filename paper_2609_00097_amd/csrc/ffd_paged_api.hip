@@ -124,7 +124,7 @@ ChunkLaunches chunk_launches(int B, int T, int Hq, int Hkv, long long Lcap, bool
     p.large = may_be_large(B, T, Hq, Hkv) && rows * Lcap * Hkv > kLittleWork * device_cus();
     p.few = B > 1 || !p.large;
     const long long pairs = (rows + 15LL * std::min(B, T)) / 16 * Hkv * ((Lcap + 2 * kRound - 1) / (2 * kRound));
-    p.cut = p.large || Lcap > 2 * kRound || (Lcap > kRound && pairs > 2LL * device_cus());      // else a tile is one unit
+    p.cut = p.large || Lcap > kWholeBlocks * kRound;
     const int tile = rows <= 16LL * B || p.large || pairs <= device_cus() ? 16 : 32;
     p.few_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, tile, 0, p.large ? kFewRows : INT32_MAX, tile == 16 && i8 ? 3 : 2);
     p.large_kernel = chunk_kernel(B, T, Hq, Hkv, Lcap, kChunkTileRows, p.few ? kFewRows : 0, INT32_MAX, 1);

@@ -17,6 +17,8 @@ namespace {
 
 constexpr int kRowsShift = kChunkRowsShift;     // blocks of kRound tokens
 static_assert(kRound == 1 << kRowsShift);
+constexpr int kWholeShift = 8;                  // a unit of more blocks than a tile that is not cut has
+static_assert(2 * kWholeBlocks < 1 << kWholeShift);
 
 // The pages of a wave's 32 tokens: first rows of both 16-token halves, whether they are there.
 struct TilePages {
@@ -228,15 +230,21 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
     auto units = [&](int shift) { return (plan.blocks + (1 << shift) - 1) >> shift; };           // of a tile
     // a tile without blocks is one unit, for its empty rows to be written
     auto work = [&](int shift) { return plan.tiles * max(units(shift), 1) * a.Hkv; };
-    int all = 0, pairs = 0;
+    int all = 0, pairs = 0, tiles = 0;
+    bool over[2] = {false, false};              // a tile of more than kWholeBlocks, of more than twice as many
     for (int b0 = (a.B - 1) & ~63; b0 >= 0; b0 -= 64) {         // backwards, to end at the first ones
         plan.load(a, b0, lane);
         all += __builtin_amdgcn_readlane(wave_inclusive_scan(work(a.unit_shift)), 63);
         pairs += __builtin_amdgcn_readlane(wave_inclusive_scan(work(a.unit_shift + 1)), 63);
+        tiles += __builtin_amdgcn_readlane(wave_inclusive_scan(plan.tiles * a.Hkv), 63);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) over[i] |= __ballot(plan.blocks > kWholeBlocks << i) != 0;
     }
-    // Where there is a workgroup for every two blocks of a tile, it takes just these.
-    const int shift = pairs <= a.slots ? a.unit_shift + 1 : a.unit_shift;
-    if (shift != a.unit_shift) all = pairs;
+    // Short tiles are not cut (longer ones where there are many), others, where there is a workgroup for every two blocks, into these.
+    const bool whole = !over[0] || (!over[1] && 4 * tiles >= a.slots);
+    const int shift = whole ? kWholeShift : pairs <= a.slots ? a.unit_shift + 1 : a.unit_shift;
+    if (whole) all = tiles;
+    else if (shift != a.unit_shift) all = pairs;
     const Shares shares(all, a.slots);
     const int begin = shares.begin(wg), end = shares.begin(wg + 1);
     int u = begin;

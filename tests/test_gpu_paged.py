@@ -575,7 +575,8 @@ def test_two_streams(ffd):
             assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
 
 
-@pytest.mark.parametrize("B,n,cap", [(1, 1, 128), (3, 5, 256), (40, 3, 256), (200, 3, 256), (200, 3, 128), (2, 100, 272)])
+@pytest.mark.parametrize("B,n,cap", [(1, 1, 128), (3, 5, 256), (40, 3, 256), (200, 3, 256), (200, 3, 128), (2, 100, 272), (3, 5, 512), (3, 5, 528),
+                                     (150, 1, 1024), (150, 2, 1040), (20, 1, 1024)])
 def test_short_capacities(ffd, B, n, cap):
     """Capacities around those at which no tile is cut, with few and with more tiles than workgroups."""
     batch = R.Batch([cap - (7 * b) % 90 for b in range(B)], [n] * B, 4, 4, 16, seed=42, width=cap // 16)
