@@ -466,7 +466,7 @@ int ffd_paged_attention_weights(const void* q, const ffd_paged* cache, const int
  * row whose new page is not there is not copied.
  *   weights       float [B, Hkv, Lcap]
  *   budget        1 .. new_max_pages * page;  recent  0 .. budget
- *   new_lens      int32 [B]: tokens kept (the same for all KV heads)
+ *   new_lens      int32 [B]: tokens kept (the same for all KV heads); may be seq_lens itself
  *   kept          int32 [B, Hkv, budget]: the old place of the token now at place r, -1 from new_lens[b] on
  *   new_weights   float [B, Hkv, new_max_pages * page] or NULL: the kept tokens' weights (entries behind them as they were);
  *                 not overlapping `weights`, nor new_table page_table: FFD_ERR_INVALID_ARGUMENT

@@ -5,7 +5,8 @@
 // being those above a threshold and, of those equal to it, the first ones. The threshold is found by counting digits from
 // the highest on (11, 11 and 10 bits), each digit's counts in LDS; a last pass counts the kept tokens of each wave's part of the
 // sequence and then writes the list in the tokens' order. Up to 32K keys lie in LDS, those behind are made anew in each pass.
-// evict_move_kernel copies rows by the list. New pages are others than the old ones, so that rows can be copied in any order.
+// evict_move_kernel copies rows by the list. New pages are others than the old ones, so that rows can be copied in any order. It
+// also leaves the new lengths, which may take the old ones' place: the selection's workgroups, which all read those, are done.
 //
 // Bound: the selection by its chain of passes, keys in LDS (four sequences of 32K, eight heads: 31 us, of which 11 bring the keys
 // and count the first digit, 10 the two others, 10 count and write the list; 1K tokens 8 us), the move by HBM (8K of each of them: 57 us,
@@ -206,7 +207,6 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
         equals += all >> 16;
     }
     for (int r = count + tid; r < a.budget; r += kEvictThreads) kept[r] = -1;
-    if (kvh == 0 && tid == 0) a.new_lens[b] = count;
 }
 
 // 128 places of a (sequence, KV head), keys or values: 16 lanes a bf16 row, eight an 8-bit one. Everything passes once.
@@ -217,12 +217,14 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
     const int kvh = blockIdx.y, b = blockIdx.z, c = threadIdx.x % kLanes, r0 = (int)(blockIdx.x >> 1) * kEvictMoveRows + (int)threadIdx.x / kLanes;
     const int32_t* kept = a.kept + ((size_t)b * a.Hkv + kvh) * a.budget;
     const PagedKv to{a.from.kv, a.to_table, a.from.num_pages, a.from.page_shift, a.to_pages};
-    int j[kSteps], to_entry[kSteps];
+    const bool counts = !values && kvh == 0;    // uniform: these workgroups leave the new length
+    int j[kSteps], to_entry[kSteps], after[kSteps];
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
         const int r = min(r0 + u * kRows, a.budget - 1);
         j[u] = kept[r];
         to_entry[u] = page_entry(to, b, r);
+        after[u] = counts && r + 1 < a.budget ? kept[r + 1] : -1;
     }
     size_t src[kSteps], dst[kSteps];
     bool move[kSteps];
@@ -241,6 +243,13 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
     for (int u = 0; u < kSteps; ++u) {
         x[u] = __builtin_nontemporal_load(tokens + src[u] * kLanes + c);
         if constexpr (I8) m[u] = absmax[src[u]];
+    }
+    if (counts && c == 0) {                     // of the list's last place in use, or of its first where there is none
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int r = r0 + u * kRows;
+            if (r < a.budget && (j[u] >= 0 ? after[u] < 0 : r == 0)) a.new_lens[b] = j[u] >= 0 ? r + 1 : 0;
+        }
     }
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {

@@ -312,7 +312,7 @@ struct EvictArgs {
     const int32_t* to_table;    // [B, to_pages]
     const int32_t* seq_lens;
     const float* weights;       // [B, Hkv, from.max_pages << page_shift]
-    int32_t* new_lens;          // [B]
+    int32_t* new_lens;          // [B], may be seq_lens
     int32_t* kept;              // [B, Hkv, budget]
     float* new_weights;         // [B, Hkv, to_pages << page_shift] or null
     int Hkv, to_pages, budget, recent;

@@ -821,8 +821,8 @@ def evict_paged(cache, page_table, new_table, seq_lens, weights, budget: int, *,
     """Keep ``budget`` tokens of each sequence and KV head: the last ``recent`` and the heaviest of the others by ``weights``
     (``[B, Hkv, Lcap]``; equal ones from the lowest place on), in their order, moved to the pages of ``new_table`` (int32
     ``[B, new_max_pages]``, other pages of the same cache). Returns ``(kept, new_lens, new_weights)``: the old places int32
-    ``[B, Hkv, budget]`` (-1 behind the last), the lengths int32 ``[B]`` and the kept weights ``[B, Hkv, new_max_pages * page]``
-    (zeros behind the last, or what a given tensor holds)."""
+    ``[B, Hkv, budget]`` (-1 behind the last), the lengths int32 ``[B]`` (``new_lens`` may be ``seq_lens``) and the kept weights
+    ``[B, Hkv, new_max_pages * page]`` (zeros behind the last, or what a given tensor holds)."""
     device = cache[0].get_device() if isinstance(cache, (tuple, list)) and cache and isinstance(cache[0], torch.Tensor) else -1
     paged, B, Hkv, page, max_pages = _paged(cache, page_table, device)
     if not isinstance(new_table, torch.Tensor) or new_table.dim() != 2:
