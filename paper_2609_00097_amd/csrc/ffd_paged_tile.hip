@@ -464,7 +464,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile_kernel(ChunkAttendArg
     const int row4 = lane >> 4, chunk = lane & 15;
     auto place_of = [&](int row, int chunk) { return row * 256 + 16 * (chunk ^ (row & 15)); };
     if (it.part >= 0) {
-        const float f = any ? sum / rounded_sum : 1.f;
+        const float f = rounded_sum > 0.f ? sum / rounded_sum : 1.f;            // (0 of 0: all scores are minus infinity)
         const size_t to = (size_t)it.part * kChunkTileRows + 32 * wave;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
