@@ -425,8 +425,10 @@ typedef struct ffd_score_rules {
 /*
  * Attention of a batch's new tokens over a paged cache that already holds their keys and values (causal unless the rules
  * say otherwise). A sequence with few new tokens is cut along its cache, and a short batch altogether, so that single tokens
- * (decoding), chunks of prompts and both together are served by one call. A score is fp32; a probability is rounded to
- * bf16, for sequences of at most 32 query rows (new tokens times heads per KV head) to 2^-16.
+ * (decoding), chunks of prompts and both together are served by one call. A score is fp32. A probability is rounded to
+ * 2^-16 over 8-bit caches and for sequences of at most 32 query rows (new tokens times heads per KV head). For sequences of
+ * more over bf16 it may be rounded to bf16, the row then being divided by the sum of the rounded ones: by the batch's
+ * sizes and the capacity, so that a sequence's result can differ by that rounding from batch to batch.
  *   q             bf16 [T, Hq, D];  out  bf16 [T, Hq, D];  lse  float [T, Hq] or NULL. A row that sees no token gets out
  *                 = 0, lse = -inf.
  *   softmax_scale > 0, or 0 for 1/sqrt(D)

@@ -7,14 +7,16 @@
 // apart, so that one's matrix instructions run beside the other's softmax and staging. Codes take registers on their way, which
 // the order of the bf16 kernel does not have.
 //
-// Probabilities enter the second product rounded to bf16, in one part, as over bf16; they are multiplied by M / 127 of their value
-// before the rounding, and the row is divided by the sum of the unrounded ones.
+// Probabilities are multiplied by M / 127 of their value and enter the second product in two bf16 parts, hi + lo: rounded to 2^-16. One
+// part (2^-8) does not average out where one token has most of the weight or equal scores meet equal M, and the bf16 kernel's remedy, a
+// row divided by the sum of what the rounded ones stand for, takes 127 / M of every token here and as much time: a prompt of 8K, eight
+// KV heads of four, 724 us with one part, 866 with that divisor, 877 with two; two of 4K in a window of 1024 under a cap 315, 357 and 338.
 //
 // Pages: 16 tokens lie together, so a thread's load is one page's, whose entry is read a tile ahead; codes of pages that are not
 // there, and behind what any query sees, have M = 0.
 //
-// Bound: the phases' instructions, matrix and softmax ones in turn on each SIMD: a prompt of 8K, eight KV heads of four, 720 us (0.76
-// PFLOP/s), 512 tokens on 32K 352 us.
+// Bound: the phases' instructions, matrix and softmax ones in turn on each SIMD: a prompt of 8K 877 us (0.63 PFLOP/s of the operator's
+// products), 512 tokens on 32K 435 us.
 #include "ffd_paged.h"
 #include "ffd_tile.h"
 
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile8_kernel(ChunkAttendAr
     const uint32_t v_at = v_row * (2 * kD) + 16 * value_chunk<true>(v_row, v_c) + 8 * (i16 & 1);
 
     v16f s[2];
-    v8bf p[4];
+    v8bf p[4], p_low[4];
     auto value_operand = [&](const uint8_t* values, int y, int d) {
         v4s v[2];
 #pragma unroll
@@ -304,12 +306,14 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile8_kernel(ChunkAttendAr
             for (int i = 0; i < 16; ++i) e[i] *= scales[x][i >> 2][i & 3];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                uint32_t w[4];
+                uint32_t w[4], low[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     w[k] = pack_bf16(e[8 * y + 2 * k], e[8 * y + 2 * k + 1]);
+                    low[k] = pack_bf16(e[8 * y + 2 * k] - bf16_lo(w[k]), e[8 * y + 2 * k + 1] - bf16_hi(w[k]));
                 }
                 p[2 * x + y] = __builtin_bit_cast(v8bf, v4u{w[0], w[1], w[2], w[3]});
+                p_low[2 * x + y] = __builtin_bit_cast(v8bf, v4u{low[0], low[1], low[2], low[3]});
             }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -320,8 +324,11 @@ __global__ __launch_bounds__(kTThreads, 2) void chunk_tile8_kernel(ChunkAttendAr
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, value_operand(values, y, d)), p[y], o[d], 0, 0, 0);
+            for (int d = 0; d < 4; ++d) {
+                const v8bf v = __builtin_bit_cast(v8bf, value_operand(values, y, d));
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[y], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p_low[y], o[d], 0, 0, 0);
+            }
     };
     auto nonfinite = [&](int u) {
         if (__builtin_amdgcn_readfirstlane(lds.nonfinite[u & 3]) == u) {

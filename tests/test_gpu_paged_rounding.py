@@ -6,8 +6,9 @@ import pytest
 import torch
 
 from . import paged_reference as R
-from .kv8_reference import P_BF16
-from .test_gpu_paged import _attend, ffd  # noqa: F401
+from .kv8_reference import D, P_BF16, P_SPLIT, encode
+from .test_gpu_paged import _attend, _for_reference, _rules, ffd  # noqa: F401
+from .test_gpu_paged_large import SHAPES as LARGE
 from .test_gpu_paged_large import _batch
 
 pytestmark = pytest.mark.gpu
@@ -27,3 +28,53 @@ def test_runs_of_tokens_with_scores_of_minus_infinity(ffd, rule, large):  # noqa
     batch.cache[0][batch.page_table[0, at // 64].long(), 0, at % 64, 3] = -math.inf
     batch.q[..., 3] = batch.q[..., 3].abs() + 0.5
     R.check_attention(batch, _attend(ffd, batch, **rule), P_BF16, **rule)
+
+
+# Sequences of at most 32 query rows, and 8-bit caches: probabilities are rounded to 2^-16. Chunks over bf16: to 2^-8, but a row is
+# divided by the sum of the rounded ones, which cancels what is alike.
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("ahead", [False, True])
+def test_one_heavy_token(ffd, ahead, large, bits):  # noqa: F811
+    """A token with nearly all of a row's weight gives its value with the output's rounding alone: the others have e^-41 of it (key
+    and query in one direction: 4 * 128 / sqrt(128) = 45, against N(0, 1)). `ahead`: one before it comes 5 nats close, so that the
+    maximum that the exponents are taken against may stay behind; its rounding, of a weight of e^-5, moves the row by 2 * 2^-8 *
+    e^-5 = 2^-14.2 where it is to 2^-8."""
+    batch = _sized(large, [900, 640], [300, 40], 2, 4, 32, bits, 54)
+    u = torch.where(torch.rand(D, device="cuda") < 0.5, -1.0, 1.0)
+    keys = batch.cache[0]
+    for h in range(2):
+        for b, near, heavy in ((0, 70, 500), (1, 5, 300)):
+            for at, size in ((near, 4 - 5 * math.sqrt(D) / D), (heavy, 4.0))[0 if ahead else 1:]:
+                page, place = batch.table[b][at // 32], at % 32
+                key = (size * u).bfloat16()
+                if bits == 8:
+                    keys[page, h, place], batch.cache[1][page, h, place] = encode(key)
+                else:
+                    keys[page, h, place] = key
+    batch.q.copy_(u)
+    R.check_attention(batch, _attend(ffd, batch), P_SPLIT if not ahead else P_SPLIT + 2.0 ** -14)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("M", [1.0, 1.3, 0.011])
+def test_equal_scores(ffd, M, large, bits):  # noqa: F811
+    """Queries of zeros: every row is the mean of the values it sees, which all have the same largest size and mostly one sign."""
+    batch = _sized(large, [900, 640], [300, 40], 2, 4, 32, bits, 55)
+    v = (torch.rand(batch.num_pages, 2, 32, D, device="cuda", generator=torch.Generator("cuda").manual_seed(55)) * 0.5 + 0.45).bfloat16()
+    v[..., 0] = 1.0
+    v = (v * M).bfloat16()
+    for x, y in zip(batch.cache[len(batch.cache) // 2:], encode(v) if bits == 8 else (v,)):
+        x.copy_(y)
+    batch.q.zero_()
+    R.check_attention(batch, _attend(ffd, batch), P_SPLIT)
+
+
+@pytest.mark.parametrize("rule", [dict(), dict(softcap=20.0), dict(window=50, slopes=True), dict(window=33, prefix=True)], ids=lambda r: "_".join(r) or "plain")
+@pytest.mark.parametrize("lens,new,Hkv,G,page", LARGE)
+def test_chunks_over_8_bits(ffd, lens, new, Hkv, G, page, rule):  # noqa: F811
+    batch = _batch(lens, new, Hkv, G, page, 8, 56)
+    rules = _rules(batch, rule)
+    R.check_attention(batch, _attend(ffd, batch, **rules), P_SPLIT, **_for_reference(batch, rules))
