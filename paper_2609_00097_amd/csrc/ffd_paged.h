@@ -213,12 +213,14 @@ struct ScoreRule {
 };
 constexpr float kNearCap = 1.4426950408889634f;                         // x of y = 1/2
 constexpr double kTanhNear[5] = {0.9999999867573891, -0.33333067944418876, 0.13324750504729285, -0.05298423882487847, 0.017131344424267444};
+// finite, for the distance of zero
+__device__ __forceinline__ float slope_in_twos(float slope) { return fminf(fmaxf(slope * kLog2e, -FLT_MAX), FLT_MAX); }
 __device__ __forceinline__ ScoreRule score_rule(const ChunkArgs& a, bool i8, int head) {
     ScoreRule r;
     const float scale = i8 ? a.scale / 127.f : a.scale;
     r.zscale = a.cap > 0.f ? fminf(scale * 2.f * kLog2e / a.cap, FLT_MAX) : scale * kLog2e;
     r.cap2 = a.cap * kLog2e;
-    r.slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    r.slope2 = a.slopes ? slope_in_twos(a.slopes[head]) : 0.f;
 #pragma unroll
     for (int i = 0; i < 5; ++i) r.near[i] = a.cap_near[i];
     return r;

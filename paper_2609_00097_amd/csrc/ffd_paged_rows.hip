@@ -285,7 +285,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 && I8 ? 3 : 2) void chunk_rows_ke
             const int r = min(16 * c + n, live - 1), tok = tok0 + (r >> gs), head = hq0 + (r & (a.G - 1));
             load_query<I8>(q[c], a.q + ((size_t)(it.seq.q0 + tok) * a.Hq + head) * kD, g);
             rows.at[c] = place + tok;
-            rows.slope2[c] = RULED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+            rows.slope2[c] = RULED && a.slopes ? slope_in_twos(a.slopes[head]) : 0.f;
         }
         const int tok1 = min(tok0 + step, it.seq.n) - 1;
         rows.low = place + tok0;

@@ -78,3 +78,25 @@ def test_chunks_over_8_bits(ffd, lens, new, Hkv, G, page, rule):  # noqa: F811
     batch = _batch(lens, new, Hkv, G, page, 8, 56)
     rules = _rules(batch, rule)
     R.check_attention(batch, _attend(ffd, batch, **rules), P_SPLIT, **_for_reference(batch, rules))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("large", [False, True])
+def test_slopes_that_leave_the_nearest_token(ffd, large, bits):  # noqa: F811
+    """Distances that overflow, slopes up to the largest number: all tokens but the query's own have no weight."""
+    batch = _sized(large, [3000, 50], [300, 50], 1, 4, 64, bits, 53)
+    slopes = torch.tensor([1e37, torch.finfo(torch.float32).max, 1e30, 2e36], device="cuda")
+    out, lse = _attend(ffd, batch, slopes=slopes)
+    weights = ffd.paged_attention_weights(*batch.args, lse, slopes=slopes)
+    for b in range(2):
+        rows, first = slice(batch.starts[b], batch.starts[b + 1]), batch.lens[b] - batch.new[b]
+        own = slice(first, batch.lens[b])
+        k, v = batch.rows(0, b, 0)[own].unsqueeze(1), batch.rows(1, b, 0)[own].unsqueeze(1)
+        q = batch.q[rows].double()
+        z, reach = (q * k).sum(-1) / math.sqrt(D), (q * k).abs().sum(-1) / math.sqrt(D)
+        # of one token: the output's rounding, and its probability's
+        assert bool(((out[rows].double() - v).abs() <= (2.0 ** -8 + P_SPLIT) * v.abs()).all())
+        assert bool(((lse[rows].double() - z).abs() <= R.score_error(reach, 0) + 2.0 ** -21 * z.abs()).all())
+        # e^(z - lse) of the four heads, each off by its exponent's error and the exponential's
+        assert bool(((weights[b, 0, own] - 4).abs() <= (R.score_error(reach, 0) + 2.0 ** -20 * (z.abs() + 1)).sum(-1)).all())
+        assert bool((weights[b, 0, :first] == 0).all()) and bool((weights[b, 0, batch.lens[b]:] == 0).all())
