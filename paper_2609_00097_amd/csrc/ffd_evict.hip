@@ -224,7 +224,10 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
         const int r = min(r0 + u * kRows, a.budget - 1);
         j[u] = kept[r];
         to_entry[u] = page_entry(to, b, r);
-        after[u] = counts && r + 1 < a.budget ? kept[r + 1] : -1;
+    }
+    if (counts) {
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) after[u] = kept[min(r0 + u * kRows + 1, a.budget - 1)];
     }
     size_t src[kSteps], dst[kSteps];
     bool move[kSteps];
@@ -248,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
             const int r = r0 + u * kRows;
-            if (r < a.budget && (j[u] >= 0 ? after[u] < 0 : r == 0)) a.new_lens[b] = j[u] >= 0 ? r + 1 : 0;
+            if (r < a.budget && (j[u] >= 0 ? after[u] < 0 || r + 1 == a.budget : r == 0)) a.new_lens[b] = j[u] >= 0 ? r + 1 : 0;
         }
     }
 #pragma unroll
