@@ -426,9 +426,11 @@ typedef struct ffd_score_rules {
  * Attention of a batch's new tokens over a paged cache that already holds their keys and values (causal unless the rules
  * say otherwise). A sequence with few new tokens is cut along its cache, and a short batch altogether, so that single tokens
  * (decoding), chunks of prompts and both together are served by one call. A score is fp32. A probability is rounded to
- * 2^-16 over 8-bit caches and for sequences of at most 32 query rows (new tokens times heads per KV head). For sequences of
- * more over bf16 it may be rounded to bf16, the row then being divided by the sum of the rounded ones: by the batch's
- * sizes and the capacity, so that a sequence's result can differ by that rounding from batch to batch.
+ * 2^-16 over 8-bit caches and for sequences of at most 32 query rows (new tokens times heads per KV head; a batch of one
+ * sequence counts T, rows of no sequence too). For more rows over bf16 it may be rounded to bf16, the row then being
+ * divided by the sum of the rounded ones: by the batch's sizes and the capacity, so that a sequence's result can differ by
+ * that rounding from batch to batch. One below 2^-126 of the row's largest counts as zero; infinite values that it meets
+ * give an infinity or NaN.
  *   q             bf16 [T, Hq, D];  out  bf16 [T, Hq, D];  lse  float [T, Hq] or NULL. A row that sees no token gets out
  *                 = 0, lse = -inf.
  *   softmax_scale > 0, or 0 for 1/sqrt(D)
@@ -449,7 +451,8 @@ size_t ffd_paged_workspace_bytes(int B, int T, int Hq, int Hkv, int D);
  * KV head h
  *   weights[b][h][j] = old + sum of exp(z_ij - lse_i) over the queries i of the group's heads that see j,
  * old = previous[b][h][j] for tokens that were there before the new ones, 0 for the new tokens and without `previous`. Entries
- * behind are left as they were. The sum has one order: results do not change from call to call.
+ * behind are left as they were. The sum has one order: results do not change from call to call. A weight of one query below
+ * 2^-126 counts as zero.
  *   q, cache, q_start, seq_lens, rules, softmax_scale   as of the attention that gave lse, float [T, Hq]
  *   last          > 0: only the last `last` new tokens of a sequence count; 0: all
  *   previous      float [B, Hkv, Lcap], or NULL; may be `weights` itself

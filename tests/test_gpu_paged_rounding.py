@@ -100,3 +100,40 @@ def test_slopes_that_leave_the_nearest_token(ffd, large, bits):  # noqa: F811
         # e^(z - lse) of the four heads, each off by its exponent's error and the exponential's
         assert bool(((weights[b, 0, own] - 4).abs() <= (R.score_error(reach, 0) + 2.0 ** -20 * (z.abs() + 1)).sum(-1)).all())
         assert bool((weights[b, 0, :first] == 0).all()) and bool((weights[b, 0, batch.lens[b]:] == 0).all())
+
+
+@pytest.mark.parametrize("T", [4, 5, 64])
+def test_rows_of_no_sequence_count_for_one(ffd, T):  # noqa: F811
+    """One sequence with one new token, in a batch of T rows over a long table: by T it is one of few rows or of many."""
+    batch = R.Batch([700], [1], 2, 8, 32, 16, seed=57, behind=T - 1, width=50000)
+    R.check_attention(batch, _attend(ffd, batch), P_SPLIT if T * 8 <= 32 else P_BF16)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("large", [False, True])
+def test_tokens_of_almost_no_weight(ffd, large, bits):  # noqa: F811
+    """A heavy token whose value is zero in half of the dims: there the others' probabilities, of e^-45 to e^-115 of it, are all that
+    counts. Below 2^-126 = e^-87 they may be zeros, so that a result is off by up to 2^-126 times the sum of the values seen, beside
+    the usual bound; a weight by up to 2^-126 for each query."""
+    batch = _sized(large, [900], [300], 1, 4, 32, bits, 58)
+    u = torch.where(torch.rand(D, device="cuda", generator=torch.Generator("cuda").manual_seed(58)) < 0.5, -1.0, 1.0).bfloat16()
+    page, place = batch.table[0][7 // 32], 7 % 32
+    key, value = 4 * u, torch.where(torch.arange(D, device="cuda") < 64, 1.0, 0.0).bfloat16()
+    for x, y in zip(batch.cache, (*encode(key), *encode(value)) if bits == 8 else (key, value)):
+        x[page, 0, place] = y
+    for head, size in enumerate((1.0, 1.5, 2.0, 2.5)):
+        batch.q[:, head] = size * u
+    got, lse = _attend(ffd, batch)
+    weights = ffd.paged_attention_weights(*batch.args, lse)
+    z, worst, _ = batch.scores(0, 0)
+    v = batch.rows(1, 0, 0)
+    p, seen = torch.softmax(z, -1), (z > -math.inf).double()
+    true, mass, sizes = p @ v, p @ v.abs(), seen @ v.abs()
+    assert bool((p[seen > 0].log().min() < -100)) and bool((true[..., 64:].abs() < 2.0 ** -30).all())
+    e = R.score_error(worst, 0).unsqueeze(-1) + (900 + 4) * 2.0 ** -24 + 2.0 ** -22
+    p_error = P_BF16 if large and bits == 16 else P_SPLIT
+    bound = 2.0 ** -8 * true.abs() + (2 * e + p_error) * mass * (1 + 2.0 ** -8) + 2.0 ** -126 * (sizes + 1)
+    assert bool(((got.double() - true).abs() <= bound).all())
+    w = torch.exp(z - lse.double().unsqueeze(-1))
+    error = (w * (R.score_error(worst, 0) + 2.0 ** -22 * (lse.double().abs() + 2)).unsqueeze(-1)).sum((0, 1)) + 1202 * 2.0 ** -24 * w.sum((0, 1))
+    assert bool(((weights[0, 0, :900].double() - w.sum((0, 1))).abs() <= error + 1200 * 2.0 ** -126).all())
