@@ -106,7 +106,7 @@ struct ChunkPlan {
         s.pre = __builtin_amdgcn_readlane(seq.pre, src);
     }
     __device__ __forceinline__ int cuts_for(int C) const { return max((blocks + C - 1) / C, 1); }
-    // C, with the first 64 sequences loaded
+    // C of chunk_item, with the first 64 sequences loaded
     __device__ __forceinline__ int run_blocks(const ChunkAttendArgs& a, int lane) {
         long long all = 0, count = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -124,8 +124,8 @@ struct ChunkPlan {
         count *= a.Hkv;
         const long long spare = max(max((long long)a.slots - count, (long long)a.slots / 2), 1LL);
         const int C = (int)min(max((all + spare - 1) / spare, 1LL), (long long)(INT32_MAX / 2));
-        if (ROWS < kChunkTileRows || a.B > 64 || count >= a.slots) return C;
-        // Large tiles: a workgroup has its CU to itself, so the smallest C whose items fill the slots once; the lanes try 64.
+        if (a.B > 64 || count >= a.slots) return C;
+        // A workgroup has its CU to itself, so the smallest C whose items fill the slots once; the lanes try 64.
         const int least = (int)max(all / a.slots, 1LL), mine = least + (int)((long long)(C - least) * (lane + 1) / 64);
         long long items = 0;
         for (uint64_t left = __ballot(tiles > 0); left; left &= left - 1) {

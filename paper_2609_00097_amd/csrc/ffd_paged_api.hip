@@ -101,10 +101,14 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows
     return k;
 }
 // Sequences with up to kFewRows query rows per KV head go to the kernel of few rows, the others to the one of large tiles. One
-// kernel takes all where the batch cannot have both kinds (few rows in all, or one sequence), is likely to have none of the second
-// (hardly more new tokens than sequences), or has little work: rows times tokens of the capacity per CU. Large / few, whole
-// calls, eight KV heads of four in bf16: 32K (256 tokens on 1K) 34.2 / 33.4 us; 64K (512 on 1K) 36.8 / 33.9, (128 on 4K) 36.1 / 42.3;
-// 128K (256 on 4K) 41.5 / 58.1, (32 on 32K) 41.2 / 56.0, (512 on 2K) 42.3 / 48.7; in 8 bits alike.
+// kernel takes all where the batch cannot have both kinds (few rows in all, or one sequence, whose rows are taken to be all T), has at
+// most two new tokens a sequence, or has little work: rows times tokens of the capacity per CU.
+// Two tokens a sequence: a batch that decodes would pay for the second kernel (256 sequences of 2K 366 us, 399 with it), one that hides a
+// chunk would win by it (256 tokens on 32K in that batch 1420 us, 554 with it). Nothing but T tells them apart on the host.
+// Little work. Large / few, whole calls, tables as long as the sequences, eight KV heads of four in bf16: 32K (256 tokens on 1K) 34.2 /
+// 33.4 us; 64K (512 on 1K) 36.8 / 33.9, (128 on 4K) 36.1 / 42.3; 128K (256 on 4K) 41.5 / 58.1, (32 on 32K) 41.2 / 56.0, (512 on 2K) 42.3 / 48.7. In 8 bits 32K 35.8 / 24.7, 64K 40.1 / 32.9 and
+// 42.5 / 43.0, 128K 52.0 / 62.6, 58.0 / 58.9 and 52.2 / 52.7. Long tables count as long sequences: three prompts of up to 1K with 20 to
+// 37 new tokens 15 us, with a table for 128K tokens 24.
 constexpr int kFewRows = 32;
 constexpr long long kLittleWork = 40 << 10;
 // Tiles of the kernel of few rows: 32 rows, so that a tile's tokens are read once for them; 16 where the batch has hardly more in a
@@ -152,7 +156,9 @@ void launch_rows(int rows, bool i8, bool ruled, dim3 grid, hipStream_t stream, c
 
 // Query rows of a sequence up to which the weights' workgroups take equal shares, three to a CU; above, a unit each, in which the
 // rows that may see it differ, with two places for rows in LDS. Shares / units, eight KV heads of four: 128 rows on 32K 26.1 / 40.4 us,
-// 256 45.3 / 51.5, on 4 x 8K 53.3 / 52.4, 512 on 32K 78.2 / 80.1, 2K on 8 x 2K 221 / 115.
+// 256 45.3 / 51.5, on 4 x 8K 53.3 / 52.4, 512 on 32K 78.2 / 80.1, 2K on 8 x 2K 221 / 115 with tables as long as the sequences. By the mean
+// of the batch, so one chunk of 512 tokens beside 15 that decode, on 8K, takes shares (791 us, units 165); and units are of the
+// capacity: eight whole prompts of 2K 399 us, with a table for 128K tokens 445.
 constexpr int kFewWeightRows = 256;
 template <bool MANY>
 void launch_weights(bool i8, bool ruled, hipStream_t stream, const ChunkWeightsArgs& a) {

@@ -57,7 +57,6 @@ struct alignas(2 * kTileBytes) TileLds {
 __device__ __forceinline__ void load_to_lds(uint32_t lds_at, const uint8_t* base, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_at), "v"(offset), "s"(base) : "memory", "m0");
 }
-__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 template <int N> using Int = std::integral_constant<int, N>;
 enum : int { kNoCap, kNearOnly, kAnyCap };       // scores that are capped with the exponential: none, all of them small ones, any

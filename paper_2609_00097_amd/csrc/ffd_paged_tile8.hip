@@ -15,8 +15,8 @@
 // Pages: 16 tokens lie together, so a thread's load is one page's, whose entry is read a tile ahead; codes of pages that are not
 // there, and behind what any query sees, have M = 0.
 //
-// Bound: the phases' instructions, matrix and softmax ones in turn on each SIMD: a prompt of 8K 877 us (0.63 PFLOP/s of the operator's
-// products), 512 tokens on 32K 435 us.
+// Bound: the phases' instructions, matrix and softmax ones in turn on each SIMD: a prompt of 8K 859 to 877 us (0.64 PFLOP/s of the
+// operator's products), 512 tokens on 32K 421 to 435 us.
 #include "ffd_paged.h"
 #include "ffd_tile.h"
 

@@ -10,8 +10,10 @@
 // early. MANY: two places for rows, one filled from memory by loads straight to LDS while the other is used (8K new tokens of one
 // prompt 1712 -> 763 us, 5 x 1K on 8K 847 -> 498).
 //
-// Bound: HBM where few queries count (256 bytes a token and KV head: one token of 16 sequences on 8K 49 us, 5.5 TB/s), else the
-// instructions of the exponentials beside the matrix cores (8K new tokens: 0.36 PFLOP/s of products).
+// Bound: HBM where few queries count (256 bytes a token and KV head: one token of 16 sequences on 8K 49 us, 5.5 TB/s). 8K new tokens of
+// one prompt: the units of its first tokens, which all rows see, while those of its last ones are long done: all 512 begin at once,
+// two a CU, and the CUs are busy for 58 % of the time; in that time the matrix cores for 28 %, vector instructions for 53, LDS for 16
+// (0.36 PFLOP/s of products).
 #include <type_traits>
 
 #include "ffd_paged.h"
@@ -47,7 +49,6 @@ struct WeightsTile {
 __device__ __forceinline__ void rows_to_lds(uint32_t lds_at, const uint8_t* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_at), "v"(from) : "memory", "m0");
 }
-__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
 }  // namespace
 

@@ -26,6 +26,9 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// For loads straight to LDS written as assembly, which the compiler does not count.
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
 // x plus both bf16 values of a pair.
 __device__ __forceinline__ float pair_sum(uint32_t pair, float x) {
     typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
