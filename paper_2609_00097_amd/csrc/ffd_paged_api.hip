@@ -106,9 +106,9 @@ ChunkKernel chunk_kernel(int B, int T, int Hq, int Hkv, long long Lcap, int rows
 // Two tokens a sequence: a batch that decodes would pay for the second kernel (256 sequences of 2K 366 us, 399 with it), one that hides a
 // chunk would win by it (256 tokens on 32K in that batch 1420 us, 554 with it). Nothing but T tells them apart on the host.
 // Little work. Large / few, whole calls, tables as long as the sequences, eight KV heads of four in bf16: 32K (256 tokens on 1K) 34.2 /
-// 33.4 us; 64K (512 on 1K) 36.8 / 33.9, (128 on 4K) 36.1 / 42.3; 128K (256 on 4K) 41.5 / 58.1, (32 on 32K) 41.2 / 56.0, (512 on 2K) 42.3 / 48.7. In 8 bits 32K 35.8 / 24.7, 64K 40.1 / 32.9 and
-// 42.5 / 43.0, 128K 52.0 / 62.6, 58.0 / 58.9 and 52.2 / 52.7. Long tables count as long sequences: three prompts of up to 1K with 20 to
-// 37 new tokens 15 us, with a table for 128K tokens 24.
+// 33.4 us; 64K (512 on 1K) 36.8 / 33.9, (128 on 4K) 36.1 / 42.3; 128K (256 on 4K) 41.5 / 58.1, (32 on 32K) 41.2 / 56.0, (512 on 2K) 42.3 /
+// 48.7. In 8 bits 32K 35.8 / 24.7; 64K 40.1 / 32.9, 42.5 / 43.0; 128K 52.0 / 62.6, 58.0 / 58.9, 52.2 / 52.7. Long tables count as long
+// sequences: three prompts of up to 1K with 20 to 37 new tokens 15 us, with a table for 128K tokens 24.
 constexpr int kFewRows = 32;
 constexpr long long kLittleWork = 40 << 10;
 // Tiles of the kernel of few rows: 32 rows, so that a tile's tokens are read once for them; 16 where the batch has hardly more in a
